@@ -38,8 +38,8 @@
  *
  * Errors.  Every call returns a vfl_status; nothing else crosses the ABI.
  * vfl_last_error() gives a text for the last failure on a context; with a
- * NULL context, the text of the calling thread's last vfl_workspace_size or
- * vfl_create failure (empty after a success).
+ * NULL context, the text of the calling thread's last vfl_workspace_size,
+ * vfl_create or row operator failure (empty after a success of one of them).
  */
 #ifndef VFL_H
 #define VFL_H
@@ -406,6 +406,122 @@ vfl_status vfl_check(vfl_ctx* c, uint32_t* header_mismatches, uint32_t* bad_ids)
 vfl_status vfl_philox(uint64_t seed, uint32_t step, uint32_t tag, uint32_t row0, int32_t rows,
                       int32_t groups, uint32_t* out_dev, void* stream);
 
+/* Row operators of residual towers: dropout, layer norm and the residual
+ * join of the two, forward and backward.  They need no context: a program
+ * that trains its own tower in front of the exchange (residual blocks instead
+ * of the bottom model's plain layers) calls them on its own buffers.  Each
+ * call enqueues its work on `stream` (a hipStream_t, NULL: the null stream) of
+ * the current device and returns; nothing is allocated, and every result is
+ * the same from run to run.  Activations and their gradients have the
+ * elements of `dtype`; weights, statistics, sums and the weights' gradients
+ * are float32, and a value is rounded to bf16 once, where it is stored.
+ *
+ * A refused call enqueues nothing, returns VFL_E_INVALID (VFL_E_NOMEM for a
+ * workspace that is too small) and leaves its reason in vfl_last_error(NULL). */
+
+/* A row-major matrix: ld elements from row to row (0: as many as the
+ * operator's columns; never fewer).  Element-aligned data of any ld is taken.
+ * An output may be the same matrix as an input of its call (same data, same
+ * ld); otherwise its elements must be none of an input's or of another
+ * output's. */
+typedef struct {
+  void* data;
+  int64_t ld;
+} vfl_matrix;
+
+/* Dropout whose mask is never stored.  Element (r, c) is kept when its 16-bit
+ * number u is at least t = floor(65536 p + 1/2), 0 <= p <= 1, and kept
+ * elements are multiplied by 65536 / (65536 - t), so the expectation is exact
+ * for the probability t / 65536 that is applied.  The numbers of columns 8q ..
+ * 8q+7 are the halves (low half first) of the words of one Philox4x32-10
+ * block with key = (seed low word, seed high word) and counter = (step, low
+ * word of row0 + r, q, 2^31 + 2^16 * high word of (row0 + r) + tag).  The mask
+ * thus follows from the global sample id whichever batch or replica a row
+ * lands in, a backward pass makes the forward's mask again from the same
+ * spec, and counters never meet those of the message noise (whose last word
+ * is 0 or 1).  tag (below 65536) tells the dropouts of a model apart; step
+ * usually counts training steps.  step_dev (device uint32, may be NULL) is
+ * added to step when the kernel runs, so a replayed graph can advance it.
+ * row0 >= 0 and row0 + rows <= 2^47.  A dropped element is 0 whatever its
+ * value (infinities and NaN included). */
+typedef struct {
+  float p;
+  uint32_t tag;
+  uint64_t seed;
+  uint32_t step;
+  const uint32_t* step_dev;
+  int64_t row0;
+} vfl_dropout_spec;
+
+/* y = dropout(x).  Its own adjoint: the backward pass is the same call with
+ * the gradient of y as x and the gradient of x as y. */
+typedef struct {
+  vfl_dtype dtype;
+  int32_t cols;
+  int64_t rows;
+  vfl_dropout_spec drop;
+  vfl_matrix x, y;
+} vfl_dropout_args;
+vfl_status vfl_dropout(const vfl_dropout_args* a, void* stream);
+
+/* Device workspace (16-byte aligned) that a backward pass over rows x cols
+ * needs for its weights' gradients; its contents need no preparation and mean
+ * nothing between calls.  Calls that may run at the same time need one each.
+ * Host-only. */
+#define VFL_NORM_MAX_COLS 32768
+vfl_status vfl_norm_workspace_size(int64_t rows, int32_t cols, size_t* bytes);
+
+/* Layer norm over the columns of each row:
+ *   mean = sum_c x / cols, k = 1 / sqrt(sum_c (x - mean)^2 / cols + eps),
+ *   y = (x - mean) * k * gamma + beta,
+ * 1 <= cols <= VFL_NORM_MAX_COLS, eps > 0; gamma, beta float32 [cols] (NULL: 1
+ * and 0).  The forward reads x and writes y and stats (float32 [rows x 2] of
+ * mean and k, 8-byte aligned; NULL: not kept).  The backward reads x, dy and
+ * stats and writes, with h = (x - mean) * k and g = dy * gamma,
+ *   dx = k * (g - sum_c g / cols - h * sum_c (g h) / cols),
+ *   dgamma = sum_r dy * h, dbeta = sum_r dy      (float32 [cols]),
+ * each where it is not NULL (one at least); dgamma and dbeta need a workspace
+ * of vfl_norm_workspace_size() bytes.  Fields that a direction does not use
+ * are ignored, so one descriptor serves both. */
+typedef struct {
+  vfl_dtype dtype;
+  int32_t cols;
+  int64_t rows;
+  float eps;
+  const float *gamma, *beta;
+  vfl_matrix x, y, dy, dx;
+  float* stats;
+  float *dgamma, *dbeta;
+  void* workspace;
+  size_t workspace_bytes;
+} vfl_layernorm_args;
+vfl_status vfl_layernorm_forward(const vfl_layernorm_args* a, void* stream);
+vfl_status vfl_layernorm_backward(const vfl_layernorm_args* a, void* stream);
+
+/* The residual join of a block: s = r + dropout(x), y = layer norm of s (of
+ * its float32 value, before it is rounded for storage).  The forward reads x
+ * and r and writes y, s and stats (the last two where they are not NULL).  The
+ * backward reads s, stats, dy and ds (the gradient that reaches s past the
+ * norm; NULL data: none) and writes
+ *   dr = ds + (the layer norm's dx of dy), dx = dropout(dr),
+ *   dgamma, dbeta as above,
+ * each where it is not NULL (one at least).  drop is the forward's. */
+typedef struct {
+  vfl_dtype dtype;
+  int32_t cols;
+  int64_t rows;
+  float eps;
+  const float *gamma, *beta;
+  vfl_dropout_spec drop;
+  vfl_matrix x, r, s, y, dy, ds, dr, dx;
+  float* stats;
+  float *dgamma, *dbeta;
+  void* workspace;
+  size_t workspace_bytes;
+} vfl_residual_args;
+vfl_status vfl_residual_forward(const vfl_residual_args* a, void* stream);
+vfl_status vfl_residual_backward(const vfl_residual_args* a, void* stream);
+
 /* Kernel classes for vfl_timing_* (bit i of a mask selects class i). */
 typedef enum {
   VFL_K_FWD = 0,        /* party B: bottom forward + published embedding */
@@ -438,8 +554,9 @@ vfl_status vfl_timing_read(vfl_ctx* c, int32_t kernel_class, double* ms, int64_t
                            double* work);
 
 /* Text of the last failure on c (owned by the context, valid until its next
- * call); c == NULL: the calling thread's last vfl_workspace_size/vfl_create
- * failure (thread-local storage, valid until that thread's next such call). */
+ * call); c == NULL: the calling thread's last vfl_workspace_size, vfl_create
+ * or row operator failure (thread-local storage, valid until that thread's
+ * next such call). */
 const char* vfl_last_error(const vfl_ctx* c);
 
 /* Synchronise both streams and release the context's events and host state.

@@ -281,8 +281,9 @@ namespace {
 template <typename T>
 T* at(vfl_ctx* c, size_t off) { return (T*)(c->ws + off); }
 
-// Failures of calls that have no context yet (vfl_workspace_size, vfl_create)
-// keep their text per host thread; vfl_last_error(NULL) returns it.
+// Failures of calls that have no context (vfl_workspace_size, vfl_create, the
+// row operators) keep their text per host thread; vfl_last_error(NULL) returns
+// it.
 thread_local std::string t_create_err;
 
 vfl_status fail(vfl_ctx* c, vfl_status st, const std::string& msg) {
@@ -1976,6 +1977,16 @@ vfl_status finish_create(vfl_ctx* c, const vfl_opts* o, void* workspace, void* s
 }
 
 }  // namespace
+
+namespace vfl {
+void set_call_error(const char* why) noexcept {
+  try {
+    t_create_err = why;
+  } catch (...) {                      // no memory for the text: the status still tells
+    t_create_err.clear();
+  }
+}
+}  // namespace vfl
 
 extern "C" {
 

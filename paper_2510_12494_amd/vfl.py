@@ -22,6 +22,7 @@ VFL_FIFO_DISCARD, VFL_LOSS_MSE = 16, 32
 VFL_MAX_LAYERS = 16
 VFL_GRAPH_CYCLES = 4
 VFL_STATIC_WORKSPACE_BYTES = 64 << 20
+VFL_NORM_MAX_COLS = 32768
 VFL_TIMED_EVERY = 4       # vfl_run times the launches of every 4th tick of a captured cycle
 STATUS_NAMES = {0: "VFL_OK", 1: "VFL_E_INVALID", 2: "VFL_E_NOMEM", 3: "VFL_E_HIP",
                 4: "VFL_E_NOT_READY", 5: "VFL_E_STALE", 6: "VFL_E_STATE"}
@@ -31,7 +32,9 @@ EXPORTS = ("vfl_workspace_size", "vfl_create", "vfl_create_static", "vfl_set_par
            "vfl_step", "vfl_get_message", "vfl_get_trace", "vfl_schedule_tick", "vfl_check",
            "vfl_philox", "vfl_timing_enable", "vfl_timing_read", "vfl_bind_dataset", "vfl_run",
            "vfl_state_size", "vfl_get_state", "vfl_set_state", "vfl_discard", "vfl_plan", "vfl_fit_delay",
-           "vfl_sync_interval", "vfl_replica_average",
+           "vfl_sync_interval", "vfl_replica_average", "vfl_dropout", "vfl_norm_workspace_size",
+           "vfl_layernorm_forward", "vfl_layernorm_backward", "vfl_residual_forward",
+           "vfl_residual_backward",
            "vfl_last_error", "vfl_destroy")
 KERNEL_CLASSES = ("fwd", "active", "bwd", "dw", "reduce", "cast", "emb_sgd", "gemm", "dwt", "avg")
 
@@ -74,6 +77,36 @@ class vfl_batch(C.Structure):
 class vfl_dataset(C.Structure):
     _fields_ = [("dense", C.c_void_p), ("ld", C.c_int64), ("ids", C.c_void_p),
                 ("labels", C.c_void_p)]
+
+
+class vfl_matrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("ld", C.c_int64)]
+
+
+class vfl_dropout_spec(C.Structure):
+    _fields_ = [("p", C.c_float), ("tag", C.c_uint32), ("seed", C.c_uint64), ("step", C.c_uint32),
+                ("step_dev", C.c_void_p), ("row0", C.c_int64)]
+
+
+class vfl_dropout_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("cols", C.c_int32), ("rows", C.c_int64), ("drop", vfl_dropout_spec),
+                ("x", vfl_matrix), ("y", vfl_matrix)]
+
+
+class vfl_layernorm_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("cols", C.c_int32), ("rows", C.c_int64), ("eps", C.c_float),
+                ("gamma", C.c_void_p), ("beta", C.c_void_p), ("x", vfl_matrix), ("y", vfl_matrix),
+                ("dy", vfl_matrix), ("dx", vfl_matrix), ("stats", C.c_void_p), ("dgamma", C.c_void_p),
+                ("dbeta", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class vfl_residual_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("cols", C.c_int32), ("rows", C.c_int64), ("eps", C.c_float),
+                ("gamma", C.c_void_p), ("beta", C.c_void_p), ("drop", vfl_dropout_spec), ("x", vfl_matrix),
+                ("r", vfl_matrix), ("s", vfl_matrix), ("y", vfl_matrix), ("dy", vfl_matrix),
+                ("ds", vfl_matrix), ("dr", vfl_matrix), ("dx", vfl_matrix), ("stats", C.c_void_p),
+                ("dgamma", C.c_void_p), ("dbeta", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t)]
 
 
 class VflError(RuntimeError):
@@ -121,6 +154,12 @@ def _load():
         "vfl_get_state": [P, P, SZ],
         "vfl_set_state": [P, P, SZ],
         "vfl_destroy": [P],
+        "vfl_dropout": [C.POINTER(vfl_dropout_args), P],
+        "vfl_norm_workspace_size": [I64, I32, C.POINTER(SZ)],
+        "vfl_layernorm_forward": [C.POINTER(vfl_layernorm_args), P],
+        "vfl_layernorm_backward": [C.POINTER(vfl_layernorm_args), P],
+        "vfl_residual_forward": [C.POINTER(vfl_residual_args), P],
+        "vfl_residual_backward": [C.POINTER(vfl_residual_args), P],
     }
     for name, args in sig.items():
         f = getattr(lib, name)
@@ -137,7 +176,7 @@ _lib = _load()
 def _chk(st: int, where: str, ctx=None):
     if st != VFL_OK:
         # without a context the text is the calling thread's last
-        # vfl_workspace_size / vfl_create failure
+        # vfl_workspace_size / vfl_create / row operator failure
         raw = _lib.vfl_last_error(ctx)
         text = raw.decode() if raw else ""
         raise VflError(st, where, text)
@@ -251,6 +290,34 @@ def vfl_philox(seed: int, step: int, tag: int, row0: int, rows: int, groups: int
                stream: int = 0):
     _chk(_lib.vfl_philox(seed, step, tag, row0, rows, groups, C.c_void_p(out_ptr),
                          C.c_void_p(stream or None)), "vfl_philox")
+
+
+# row operators: `a` describes the call (fill it once per layer), stream is a
+# raw hipStream_t (0: the null stream)
+def vfl_dropout(a: vfl_dropout_args, stream: int = 0):
+    _chk(_lib.vfl_dropout(a, stream), "vfl_dropout")
+
+
+def vfl_norm_workspace_size(rows: int, cols: int) -> int:
+    n = C.c_size_t(0)
+    _chk(_lib.vfl_norm_workspace_size(rows, cols, C.byref(n)), "vfl_norm_workspace_size")
+    return n.value
+
+
+def vfl_layernorm_forward(a: vfl_layernorm_args, stream: int = 0):
+    _chk(_lib.vfl_layernorm_forward(a, stream), "vfl_layernorm_forward")
+
+
+def vfl_layernorm_backward(a: vfl_layernorm_args, stream: int = 0):
+    _chk(_lib.vfl_layernorm_backward(a, stream), "vfl_layernorm_backward")
+
+
+def vfl_residual_forward(a: vfl_residual_args, stream: int = 0):
+    _chk(_lib.vfl_residual_forward(a, stream), "vfl_residual_forward")
+
+
+def vfl_residual_backward(a: vfl_residual_args, stream: int = 0):
+    _chk(_lib.vfl_residual_backward(a, stream), "vfl_residual_backward")
 
 
 def vfl_timing_enable(ctx, mask: int):
