@@ -58,6 +58,7 @@ struct Checks {
   }
   DropKey drop(const vfl_dropout_spec& d) {
     DropKey k;
+    if (why) return k;                               // rows is in range below
     need(d.p >= 0.f && d.p <= 1.f, "p must be in [0, 1]");      // a NaN fails too
     need(d.tag < 65536u, "tag must be below 65536");
     need(d.row0 >= 0 && d.row0 <= kMaxSampleId - rows, "sample ids must be in [0, 2^47)");
