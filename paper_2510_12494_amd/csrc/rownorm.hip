@@ -1,9 +1,12 @@
 // Row operators of residual towers on gfx950: dropout, layer norm and the
 // residual join of the two, forward and backward.
 //
-// A workgroup of 256 threads takes a row at a time; a thread takes chunks of
-// eight columns, which share one Philox block of the dropout's numbers.  All
-// sums are float32.
+// The unit of work is a chunk: eight consecutive columns of a row, which share
+// one Philox block of the dropout's numbers and are 16 bytes of bf16 or 32 of
+// float32.  All of these operators move a few bytes per operation, so HBM
+// bounds them; every matrix is read once and written once, and a row stays in
+// registers between the passes over it.  All sums are float32; a value is
+// rounded to the storage type where it is stored.
 #include <algorithm>
 
 #include "device.h"
@@ -17,22 +20,150 @@ using namespace dev;
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kMaxParts = 256;
 
-// bit i: column 8q + i of the row is kept
-__device__ __forceinline__ uint32_t keep_bits(const DropKey& d, uint32_t step, int64_t row, uint32_t q) {
-  const uint64_t id = (uint64_t)row;
-  uint32_t c[4] = {step, (uint32_t)id, q, 0x80000000u | ((uint32_t)(id >> 32) << 16) | d.tag};
-  philox4x32_10(c, d.k0, d.k1);
-  uint32_t bits = 0;
+// ------------------------------------------------------------------- chunks
+// Vectors at element alignment: gfx950 loads and stores 16 bytes at any
+// address, so rows of an odd stride take the same path as aligned ones.
+typedef u32x4 __attribute__((aligned(2))) u32x4_a2;
+typedef u32x2 __attribute__((aligned(2))) u32x2_a2;
+typedef uint32_t __attribute__((aligned(2))) u32_a2;
+typedef f32x4 __attribute__((aligned(4))) f32x4_a4;
+typedef f32x2 __attribute__((aligned(4))) f32x2_a4;
+
+template <typename T> struct Raw;                 // a chunk as it is stored
+template <> struct Raw<uint16_t> { u32x4 a; };
+template <> struct Raw<float> { f32x4 a, b; };
+
+__device__ __forceinline__ Raw<uint16_t> load_at(const uint16_t* p) { return {*(const u32x4_a2*)p}; }
+__device__ __forceinline__ Raw<float> load_at(const float* p) {
+  return {*(const f32x4_a4*)p, *(const f32x4_a4*)(p + 4)};
+}
+__device__ __forceinline__ void unpack(const Raw<uint16_t>& r, float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    bits |= ((c[i] & 0xffffu) >= d.thr ? 1u : 0u) << (2 * i);
-    bits |= ((c[i] >> 16) >= d.thr ? 1u : 0u) << (2 * i + 1);
+    v[2 * i] = __uint_as_float(r.a[i] << 16);
+    v[2 * i + 1] = __uint_as_float(r.a[i] & 0xffff0000u);
   }
-  return bits;
+}
+__device__ __forceinline__ void unpack(const Raw<float>& r, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[i] = r.a[i];
+    v[4 + i] = r.b[i];
+  }
 }
 
+// The columns of a row (kernel-uniform): n of them in `per` chunks, the last
+// one `part` columns wide when that is not 0.
+struct Cols {
+  int n, per, part;
+  __device__ explicit Cols(int cols) : n(cols), per((cols + 7) >> 3), part(cols & 7) {}
+};
+
+// Chunk q of a row, loaded without a branch: the last chunk of a row that ends
+// inside it, and chunks past the row's end, are read from the row's last eight
+// columns, so that no access leaves the row (rows of fewer than eight columns
+// are gathered; kSmall marks the kernels that meet them).
+template <bool kSmall, typename T>
+__device__ __forceinline__ Raw<T> load_chunk(const T* row, int q, const Cols& k) {
+  if constexpr (kSmall) {
+    if (k.n < 8) {
+      T e[8] = {};
+#pragma unroll
+      for (int i = 0; i < 7; ++i)
+        if (i < k.n) e[i] = row[i];
+      return __builtin_bit_cast(Raw<T>, e);
+    }
+  }
+  return load_at(row + min(8 * q, k.n - 8));
+}
+
+// Its values: those of a partial chunk moved to their places, zero at and past
+// the row's end.
+template <bool kSmall, typename T>
+__device__ __forceinline__ void chunk_values(const Raw<T>& r, int q, const Cols& k, float (&v)[8]) {
+  unpack(r, v);
+  if (kSmall && k.n < 8) return;
+  if (k.part && q == k.per - 1) {
+    const int by = 8 - k.part;
+    if (by & 4) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = i + 4 < 8 ? v[(i + 4) & 7] : 0.f;
+    }
+    if (by & 2) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = i + 2 < 8 ? v[(i + 2) & 7] : 0.f;
+    }
+    if (by & 1) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = i + 1 < 8 ? v[(i + 1) & 7] : 0.f;
+    }
+  }
+  if (q >= k.per) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 0.f;
+  }
+}
+
+__device__ __forceinline__ void store4(uint16_t* p, const float* v) {
+  *(u32x2_a2*)p = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+}
+__device__ __forceinline__ void store4(float* p, const float* v) { *(f32x4_a4*)p = f32x4{v[0], v[1], v[2], v[3]}; }
+__device__ __forceinline__ void store2(uint16_t* p, const float* v) { *(u32_a2*)p = pack_bf16(v[0], v[1]); }
+__device__ __forceinline__ void store2(float* p, const float* v) { *(f32x2_a4*)p = f32x2{v[0], v[1]}; }
+__device__ __forceinline__ void store8(uint16_t* p, const float* v) {
+  *(u32x4_a2*)p = u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+}
+__device__ __forceinline__ void store8(float* p, const float* v) {
+  store4(p, v);
+  store4(p + 4, v + 4);
+}
+
+// Stores chunk q of a row: whole, or the columns that the row has of it, in
+// pieces of four, two and one.
+template <typename T>
+__device__ __forceinline__ void store_chunk(T* row, int q, const Cols& k, const float (&v)[8]) {
+  T* p = row + 8 * q;
+  if (8 * q + 8 <= k.n) {
+    store8(p, v);
+  } else if (q < k.per) {
+    const int m = k.part;                          // uniform
+    if (m & 4) {
+      store4(p, v);
+      if (m & 2) {
+        store2(p + 4, v + 4);
+        if (m & 1) st1<T>(p + 6, v[6]);
+      } else if (m & 1) {
+        st1<T>(p + 4, v[4]);
+      }
+    } else if (m & 2) {
+      store2(p, v);
+      if (m & 1) st1<T>(p + 2, v[2]);
+    } else {
+      st1<T>(p, v[0]);
+    }
+  }
+}
+
+// ------------------------------------------------------------------ dropout
 __device__ __forceinline__ uint32_t step_of(const DropKey& d) {
   return d.step + (d.step_dev ? *d.step_dev : 0u);
+}
+
+// v = dropout(v) of chunk q of global row id `row`.  One Philox block of
+// 16-bit numbers per chunk: with 32-bit numbers the two blocks' 40 wide
+// multiplications would take longer than the chunk's bytes.  A number u is at
+// least thr where u * 2^16 exceeds (thr - 1) * 2^16 + 65535, which compares a
+// word's high half without moving it.
+__device__ __forceinline__ void drop_chunk(const DropKey& d, uint32_t step, int64_t row, int q, float (&v)[8]) {
+  const uint64_t id = (uint64_t)row;
+  uint32_t c[4] = {step, (uint32_t)id, (uint32_t)q, 0x80000000u | ((uint32_t)(id >> 32) << 16) | d.tag};
+  philox4x32_10(c, d.k0, d.k1);
+  const uint32_t last = (d.thr << 16) - 1u;        // thr in 1 .. 65536
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = (c[i] << 16) > last ? v[2 * i] * d.scale : 0.f;
+    v[2 * i + 1] = c[i] > last ? v[2 * i + 1] * d.scale : 0.f;
+  }
 }
 
 template <typename T>
@@ -40,6 +171,169 @@ __device__ __forceinline__ const T* row_of(const Mat& m, int64_t r) { return (co
 template <typename T>
 __device__ __forceinline__ T* out_row(const Mat& m, int64_t r) { return (T*)m.p + r * m.ld; }
 
+// The matrix's chunks dealt to the threads in order, so that a wavefront's are
+// consecutive whatever the width; a thread steps its (row, chunk) pair by
+// (drow, dq), a whole grid, without a division.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_dropout(DropJob j, int64_t drow, int dq) {
+  const Cols k(j.cols);
+  const uint32_t step = step_of(j.d);
+  const uint32_t first = blockIdx.x * kThreads + threadIdx.x;
+  int64_t r = first / (uint32_t)k.per;
+  int q = (int)(first % (uint32_t)k.per);
+  while (r < j.rows) {
+    const Raw<T> raw = load_chunk<true>(row_of<T>(j.x, r), q, k);
+    float v[8];
+    chunk_values<true>(raw, q, k, v);
+    if (j.d.thr) drop_chunk(j.d, step, j.d.row0 + r, q, v);
+    store_chunk(out_row<T>(j.y, r), q, k, v);
+    r += drow;
+    q += dq;
+    if (q >= k.per) {
+      q -= k.per;
+      ++r;
+    }
+  }
+}
+
+// --------------------------------------------------------------------- sums
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xf, 0xf, true));
+}
+
+// The sum over each group of G lanes, in every lane of it (the same bits: each
+// step adds the same two values, in either order).
+template <int G>
+__device__ __forceinline__ float group_sum(float v) {
+  if constexpr (G >= 2) v += dpp<0xB1>(v);          // lane ^ 1
+  if constexpr (G >= 4) v += dpp<0x4E>(v);          // lane ^ 2
+  if constexpr (G >= 8) v += dpp<0x141>(v);         // mirrored in 8 lanes
+  if constexpr (G >= 16) v += dpp<0x140>(v);        // mirrored in 16 lanes
+  if constexpr (G >= 32) {
+    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+  }
+  if constexpr (G >= 64) {
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+  }
+  return v;
+}
+
+// ------------------------------------------------------------------ forward
+// G lanes hold a row, CH chunks each (chunk c * G + lane); a workgroup of
+// max(kThreads, G) threads holds kThreads / G rows, or one.  Mean and variance
+// in two sums over the registers.  Where a row spans W = G / 64 wavefronts,
+// each forms its own mean and sum of squares, and these meet in LDS: with
+// n_w, m_w, M_w of wavefront w, the row's sum of squares is the sum of
+// M_w + n_w (m_w - mean)^2, which takes one barrier a row (the slots alternate)
+// and loses nothing to cancellation.
+template <typename T, bool RES, int G, int CH>
+__global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(NormJob j) {
+  constexpr int W = G > 64 ? G / 64 : 1;
+  constexpr int RPB = G > 64 ? 1 : kThreads / G;
+  constexpr int GL = G < 64 ? G : 64;
+  constexpr bool HOIST = G <= 64;
+  static_assert(G <= 64 || G >= kThreads, "a workgroup holds whole rows");
+  __shared__ f32x2 slots[2][W];
+  const Cols k(j.cols);
+  const int lane = threadIdx.x % G, wave = threadIdx.x / 64;
+  const float inv = 1.f / (float)k.n;
+  const bool whole = k.n == 8 * G * CH;
+  uint32_t step = 0;
+  if constexpr (RES) step = step_of(j.d);
+
+  float g[HOIST ? CH : 1][8], b[HOIST ? CH : 1][8];
+  auto weights = [&](int c, int slot) {
+    const int q = c * G + lane;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) g[slot][i] = 1.f, b[slot][i] = 0.f;
+    if (j.gamma) chunk_values<G == 1>(load_chunk<G == 1>(j.gamma, q, k), q, k, g[slot]);
+    if (j.beta) chunk_values<G == 1>(load_chunk<G == 1>(j.beta, q, k), q, k, b[slot]);
+  };
+  if constexpr (HOIST)
+    for (int c = 0; c < CH; ++c) weights(c, c);
+  // this wavefront's columns (W > 1)
+  float nw = 0.f;
+  if constexpr (W > 1) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) nw += (float)min(max(k.n - 8 * (c * G + 64 * wave), 0), 512);
+  }
+
+  int flip = 0;
+  for (int64_t r = (int64_t)blockIdx.x * RPB + threadIdx.x / G; r < j.rows; r += (int64_t)gridDim.x * RPB) {
+    Raw<T> x[CH], res[CH];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      x[c] = load_chunk<G == 1>(row_of<T>(j.x, r), c * G + lane, k);
+      if constexpr (RES) res[c] = load_chunk<G == 1>(row_of<T>(j.r, r), c * G + lane, k);
+    }
+    float v[CH][8];
+    float sum = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int q = c * G + lane;
+      chunk_values<G == 1>(x[c], q, k, v[c]);
+      if constexpr (RES) {
+        if (j.d.thr) drop_chunk(j.d, step, j.d.row0 + r, q, v[c]);
+        float t[8];
+        chunk_values<G == 1>(res[c], q, k, t);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[c][i] += t[i];
+        if (j.s.p) store_chunk(out_row<T>(j.s, r), q, k, v[c]);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += v[c][i];
+    }
+    sum = group_sum<GL>(sum);
+    float mean = sum * inv;
+    if constexpr (W > 1) mean = nw > 0.f ? sum / nw : 0.f;
+    float sq = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int left = k.n - 8 * (c * G + lane);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float d = whole || i < left ? v[c][i] - mean : 0.f;
+        sq = fmaf(d, d, sq);
+      }
+    }
+    sq = group_sum<GL>(sq);
+    if constexpr (W > 1) {
+      if (threadIdx.x % 64 == 0) slots[flip][wave] = f32x2{sum, sq};
+      __syncthreads();
+      sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) sum += slots[flip][w][0];
+      mean = sum * inv;
+      sq = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        float n = 0.f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) n += (float)min(max(k.n - 8 * (c * G + 64 * w), 0), 512);
+        const f32x2 s = slots[flip][w];
+        const float d = n > 0.f ? s[0] / n - mean : 0.f;
+        sq += fmaf(n * d, d, s[1]);
+      }
+      flip ^= 1;
+    }
+    const float rs = 1.f / sqrtf(fmaf(sq, inv, j.eps));
+    if (j.stats && lane == 0) *(f32x2*)(j.stats + 2 * r) = f32x2{mean, rs};
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int at = HOIST ? c : 0;
+      if constexpr (!HOIST) weights(c, 0);
+      float y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = fmaf((v[c][i] - mean) * rs, g[at][i], b[at][i]);
+      store_chunk(out_row<T>(j.y, r), c * G + lane, k, y);
+    }
+  }
+}
+
+// ----------------------------------------------------------------- backward
 // the sum over the workgroup's threads, in every thread
 __device__ __forceinline__ float block_sum(float v, float* lds) {
 #pragma unroll
@@ -53,53 +347,18 @@ __device__ __forceinline__ float block_sum(float v, float* lds) {
   return s;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void k_dropout(DropJob j) {
-  const uint32_t step = step_of(j.d);
-  for (int64_t r = blockIdx.x; r < j.rows; r += gridDim.x)
-    for (int q = threadIdx.x; q * 8 < j.cols; q += kThreads) {
-      const uint32_t keep = j.d.thr ? keep_bits(j.d, step, j.d.row0 + r, q) : 0xffu;
-      for (int i = 0; i < 8 && q * 8 + i < j.cols; ++i) {
-        const float v = ld1<T>(row_of<T>(j.x, r) + q * 8 + i);
-        st1<T>(out_row<T>(j.y, r) + q * 8 + i, (keep >> i & 1u) ? v * j.d.scale : 0.f);
-      }
-    }
-}
-
-template <typename T>
-__global__ __launch_bounds__(kThreads) void k_norm_forward(NormJob j) {
-  __shared__ float lds[kWaves];
-  const uint32_t step = step_of(j.d);
-  const float inv = 1.f / (float)j.cols;
-  for (int64_t r = blockIdx.x; r < j.rows; r += gridDim.x) {
-    const T* x = row_of<T>(j.x, r);
-    const T* res = j.r.p ? row_of<T>(j.r, r) : nullptr;
-    auto visit = [&](auto&& f) {
-      for (int q = threadIdx.x; q * 8 < j.cols; q += kThreads) {
-        const uint32_t keep = j.d.thr ? keep_bits(j.d, step, j.d.row0 + r, q) : 0xffu;
-        for (int i = 0; i < 8 && q * 8 + i < j.cols; ++i) {
-          const int c = q * 8 + i;
-          float v = (keep >> i & 1u) ? ld1<T>(x + c) * j.d.scale : 0.f;
-          if (res) v += ld1<T>(res + c);
-          f(c, v);
-        }
-      }
-    };
-    float sum = 0.f, sq = 0.f;
-    visit([&](int, float v) { sum += v; });
-    const float mean = block_sum(sum, lds) * inv;
-    visit([&](int, float v) { sq += (v - mean) * (v - mean); });
-    const float k = 1.f / sqrtf(block_sum(sq, lds) * inv + j.eps);
-    visit([&](int c, float v) {
-      const float g = j.gamma ? j.gamma[c] : 1.f, b = j.beta ? j.beta[c] : 0.f;
-      if (j.s.p) st1<T>(out_row<T>(j.s, r) + c, v);
-      st1<T>(out_row<T>(j.y, r) + c, (v - mean) * k * g + b);
-    });
-    if (j.stats && threadIdx.x == 0) {
-      j.stats[2 * r] = mean;
-      j.stats[2 * r + 1] = k;
-    }
+// bit i: column 8q + i of the row is kept
+__device__ __forceinline__ uint32_t keep_bits(const DropKey& d, uint32_t step, int64_t row, uint32_t q) {
+  const uint64_t id = (uint64_t)row;
+  uint32_t c[4] = {step, (uint32_t)id, q, 0x80000000u | ((uint32_t)(id >> 32) << 16) | d.tag};
+  philox4x32_10(c, d.k0, d.k1);
+  uint32_t bits = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    bits |= ((c[i] & 0xffffu) >= d.thr ? 1u : 0u) << (2 * i);
+    bits |= ((c[i] >> 16) >= d.thr ? 1u : 0u) << (2 * i + 1);
   }
+  return bits;
 }
 
 // Partial weight gradients: block (x, y) sums the rows of part y in columns
@@ -161,22 +420,56 @@ __global__ __launch_bounds__(kThreads) void k_norm_dx(NormJob j) {
 
 int row_grid(int64_t rows) { return (int)std::min<int64_t>(rows, 1 << 16); }
 
+// one round of resident workgroups: 256 CUs, eight workgroups of 256 threads
+constexpr int kResident = 2048;
+
+template <typename T, bool RES, int G, int CH>
+hipError_t forward_with(const NormJob& j, hipStream_t st) {
+  constexpr int nt = G > kThreads ? G : kThreads;
+  constexpr int rpb = nt / G;
+  const int64_t blocks = (j.rows + rpb - 1) / rpb;
+  const int grid = (int)std::min<int64_t>(blocks, kResident * kThreads / nt);
+  hipLaunchKernelGGL((k_norm_forward<T, RES, G, CH>), dim3(grid), dim3(nt), 0, st, j);
+  return hipGetLastError();
+}
+
+template <typename T, bool RES>
+hipError_t forward(const NormJob& j, hipStream_t st) {
+  const int per = (j.cols + 7) / 8;
+  if (per <= 1) return forward_with<T, RES, 1, 1>(j, st);
+  if (per <= 2) return forward_with<T, RES, 2, 1>(j, st);
+  if (per <= 4) return forward_with<T, RES, 4, 1>(j, st);
+  if (per <= 8) return forward_with<T, RES, 8, 1>(j, st);
+  if (per <= 16) return forward_with<T, RES, 16, 1>(j, st);
+  if (per <= 32) return forward_with<T, RES, 32, 1>(j, st);
+  if (per <= 64) return forward_with<T, RES, 64, 1>(j, st);
+  if (per <= 128) return forward_with<T, RES, 64, 2>(j, st);
+  if (per <= 256) return forward_with<T, RES, 256, 1>(j, st);
+  if (per <= 512) return forward_with<T, RES, 256, 2>(j, st);
+  if (per <= 1024) return forward_with<T, RES, 512, 2>(j, st);
+  if (per <= 2048) return forward_with<T, RES, 1024, 2>(j, st);
+  return forward_with<T, RES, 1024, 4>(j, st);
+}
+
 }  // namespace
 
 int norm_parts(int64_t rows, int) { return (int)std::min<int64_t>(rows, kMaxParts); }
 
 hipError_t launch_dropout(Elt e, const DropJob& j, hipStream_t st) {
-  const dim3 g(row_grid(j.rows));
-  if (e == BF16) hipLaunchKernelGGL(k_dropout<uint16_t>, g, dim3(kThreads), 0, st, j);
-  else hipLaunchKernelGGL(k_dropout<float>, g, dim3(kThreads), 0, st, j);
+  const int64_t per = ((int64_t)j.cols + 7) / 8;
+  const int64_t chunks = j.rows > (INT64_MAX >> 2) / per ? INT64_MAX >> 2 : j.rows * per;
+  const int grid = (int)std::min<int64_t>((chunks + kThreads - 1) / kThreads, kResident);
+  const int64_t stride = (int64_t)grid * kThreads;
+  if (e == BF16)
+    hipLaunchKernelGGL(k_dropout<uint16_t>, dim3(grid), dim3(kThreads), 0, st, j, stride / per, (int)(stride % per));
+  else
+    hipLaunchKernelGGL(k_dropout<float>, dim3(grid), dim3(kThreads), 0, st, j, stride / per, (int)(stride % per));
   return hipGetLastError();
 }
 
 hipError_t launch_norm_forward(Elt e, const NormJob& j, hipStream_t st) {
-  const dim3 g(row_grid(j.rows));
-  if (e == BF16) hipLaunchKernelGGL(k_norm_forward<uint16_t>, g, dim3(kThreads), 0, st, j);
-  else hipLaunchKernelGGL(k_norm_forward<float>, g, dim3(kThreads), 0, st, j);
-  return hipGetLastError();
+  if (e == BF16) return j.r.p ? forward<uint16_t, true>(j, st) : forward<uint16_t, false>(j, st);
+  return j.r.p ? forward<float, true>(j, st) : forward<float, false>(j, st);
 }
 
 hipError_t launch_norm_backward(Elt e, const NormJob& j, hipStream_t st) {
