@@ -442,8 +442,8 @@ struct NormJob {
   int64_t rows;
 };
 
-// blocks of partial weight gradients (2 x cols floats each) that a backward
-// pass over rows x cols leaves in its workspace
+// workgroups of a backward pass over rows x cols; where there are several, each
+// leaves partial weight gradients (2 x cols floats) in the workspace
 int norm_parts(int64_t rows, int cols);
 hipError_t launch_dropout(Elt e, const DropJob& j, hipStream_t st);
 hipError_t launch_norm_forward(Elt e, const NormJob& j, hipStream_t st);

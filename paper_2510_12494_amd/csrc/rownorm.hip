@@ -17,8 +17,7 @@ namespace {
 
 using namespace dev;
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kMaxParts = 256;
+constexpr int kThreads = 256;
 
 // ------------------------------------------------------------------- chunks
 // Vectors at element alignment: gfx950 loads and stores 16 bytes at any
@@ -334,91 +333,182 @@ __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(No
 }
 
 // ----------------------------------------------------------------- backward
-// the sum over the workgroup's threads, in every thread
-__device__ __forceinline__ float block_sum(float v, float* lds) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-  __syncthreads();                               // the previous sum has been read
-  if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
-  __syncthreads();
-  float s = 0.f;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) s += lds[w];
-  return s;
-}
-
-// bit i: column 8q + i of the row is kept
-__device__ __forceinline__ uint32_t keep_bits(const DropKey& d, uint32_t step, int64_t row, uint32_t q) {
-  const uint64_t id = (uint64_t)row;
-  uint32_t c[4] = {step, (uint32_t)id, q, 0x80000000u | ((uint32_t)(id >> 32) << 16) | d.tag};
-  philox4x32_10(c, d.k0, d.k1);
-  uint32_t bits = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    bits |= ((c[i] & 0xffffu) >= d.thr ? 1u : 0u) << (2 * i);
-    bits |= ((c[i] >> 16) >= d.thr ? 1u : 0u) << (2 * i + 1);
+// The sum over the lanes of a wavefront that share lane % G, in lanes 0 .. G-1.
+template <int G>
+__device__ __forceinline__ float stride_sum(float v) {
+  if constexpr (G <= 8) v += dpp<0x128>(v);          // rotated by 8 in 16 lanes
+  if constexpr (G <= 4) v += dpp<0x124>(v);          // by 4
+  if constexpr (G <= 2) v += dpp<0x122>(v);          // by 2
+  if constexpr (G <= 1) v += dpp<0x121>(v);          // by 1
+  if constexpr (G <= 16) {
+    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
   }
-  return bits;
-}
-
-// Partial weight gradients: block (x, y) sums the rows of part y in columns
-// 256 x ..  It runs before k_norm_dx, which may write over dy.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void k_norm_part(NormJob j, int parts) {
-  const int c = blockIdx.x * kThreads + threadIdx.x;
-  if (c >= j.cols) return;
-  float dg = 0.f, db = 0.f;
-  for (int64_t r = blockIdx.y; r < j.rows; r += parts) {
-    const float dy = ld1<T>(row_of<T>(j.dy, r) + c);
-    dg += dy * ((ld1<T>(row_of<T>(j.v, r) + c) - j.stats[2 * r]) * j.stats[2 * r + 1]);
-    db += dy;
+  if constexpr (G <= 32) {
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
   }
-  j.part[(int64_t)(2 * blockIdx.y) * j.cols + c] = dg;
-  j.part[(int64_t)(2 * blockIdx.y + 1) * j.cols + c] = db;
+  return v;
 }
 
-__global__ __launch_bounds__(kThreads) void k_norm_reduce(NormJob j, int parts) {
-  const int c = blockIdx.x * kThreads + threadIdx.x;
-  if (c >= j.cols) return;
-  float dg = 0.f, db = 0.f;
-  for (int p = 0; p < parts; ++p) {
-    dg += j.part[(int64_t)(2 * p) * j.cols + c];
-    db += j.part[(int64_t)(2 * p + 1) * j.cols + c];
-  }
-  if (j.dgamma) j.dgamma[c] = dg;
-  if (j.dbeta) j.dbeta[c] = db;
-}
+// Rows as in the forward, one pass: both row sums and the weights' gradients
+// come from the same registers.  A thread keeps its columns' two sums over all
+// of its rows; at the end the workgroup's rows of threads meet in LDS and leave
+// one partial pair of float32 rows (2 x cols at j.part), or the result itself
+// where the grid is one workgroup.
+template <typename T, bool RES, int G, int CH, int NT>
+__global__ __launch_bounds__(NT) void k_norm_backward(NormJob j) {
+  constexpr int W = G > 64 ? G / 64 : 1;
+  constexpr int NW = NT / 64;
+  constexpr int RPB = NT / G;
+  constexpr int GL = G < 64 ? G : 64;
+  constexpr bool HOIST = G <= 64;
+  static_assert(G <= 64 || G == NT, "a workgroup holds whole rows");
+  __shared__ f32x2 slots[2][W];
+  __shared__ float sums[W > 1 ? 1 : NW][W > 1 ? 1 : GL * 8];
+  const Cols k(j.cols);
+  const int lane = threadIdx.x % G, wave = threadIdx.x / 64;
+  const float inv = 1.f / (float)k.n;
+  uint32_t step = 0;
+  if constexpr (RES) step = step_of(j.d);
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void k_norm_dx(NormJob j) {
-  __shared__ float lds[kWaves];
-  const uint32_t step = step_of(j.d);
-  const float inv = 1.f / (float)j.cols;
-  for (int64_t r = blockIdx.x; r < j.rows; r += gridDim.x) {
-    const T *v = row_of<T>(j.v, r), *dy = row_of<T>(j.dy, r);
-    const float mean = j.stats[2 * r], k = j.stats[2 * r + 1];
-    float sg = 0.f, sgh = 0.f;
-    for (int c = threadIdx.x; c < j.cols; c += kThreads) {
-      const float g = ld1<T>(dy + c) * (j.gamma ? j.gamma[c] : 1.f);
-      sg += g;
-      sgh += g * ((ld1<T>(v + c) - mean) * k);
+  float gm[HOIST ? CH : 1][8];
+  auto weights = [&](int c, int slot) {
+    const int q = c * G + lane;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) gm[slot][i] = 1.f;
+    if (j.gamma) chunk_values<G == 1>(load_chunk<G == 1>(j.gamma, q, k), q, k, gm[slot]);
+  };
+  if constexpr (HOIST)
+    for (int c = 0; c < CH; ++c) weights(c, c);
+  float ag[CH][8] = {}, ab[CH][8] = {};
+
+  int flip = 0;
+  for (int64_t r = (int64_t)blockIdx.x * RPB + threadIdx.x / G; r < j.rows; r += (int64_t)gridDim.x * RPB) {
+    Raw<T> xr[CH], yr[CH], sr[CH];
+    const f32x2 st = *(const f32x2*)(j.stats + 2 * r);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int q = c * G + lane;
+      xr[c] = load_chunk<G == 1>(row_of<T>(j.v, r), q, k);
+      yr[c] = load_chunk<G == 1>(row_of<T>(j.dy, r), q, k);
+      if constexpr (RES)
+        if (j.ds.p) sr[c] = load_chunk<G == 1>(row_of<T>(j.ds, r), q, k);
     }
-    const float mg = block_sum(sg, lds) * inv, mgh = block_sum(sgh, lds) * inv;
-    for (int q = threadIdx.x; q * 8 < j.cols; q += kThreads) {
-      const uint32_t keep = j.d.thr && j.dx.p ? keep_bits(j.d, step, j.d.row0 + r, q) : 0xffu;
-      for (int i = 0; i < 8 && q * 8 + i < j.cols; ++i) {
-        const int c = q * 8 + i;
-        const float g = ld1<T>(dy + c) * (j.gamma ? j.gamma[c] : 1.f);
-        float d = k * (g - mg - (ld1<T>(v + c) - mean) * k * mgh);
-        if (j.ds.p) d += ld1<T>(row_of<T>(j.ds, r) + c);
-        if (j.dr.p) st1<T>(out_row<T>(j.dr, r) + c, d);
-        if (j.dx.p) st1<T>(out_row<T>(j.dx, r) + c, (keep >> i & 1u) ? d * j.d.scale : 0.f);
+    float h[CH][8], g[CH][8];
+    float sg = 0.f, sgh = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int q = c * G + lane, at = HOIST ? c : 0;
+      if constexpr (!HOIST) weights(c, 0);
+      chunk_values<G == 1>(xr[c], q, k, h[c]);
+      chunk_values<G == 1>(yr[c], q, k, g[c]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        h[c][i] = (h[c][i] - st[0]) * st[1];
+        ag[c][i] = fmaf(g[c][i], h[c][i], ag[c][i]);
+        ab[c][i] += g[c][i];
+        g[c][i] *= gm[at][i];
+        sg += g[c][i];
+        sgh = fmaf(g[c][i], h[c][i], sgh);
+      }
+    }
+    sg = group_sum<GL>(sg);
+    sgh = group_sum<GL>(sgh);
+    if constexpr (W > 1) {
+      if (threadIdx.x % 64 == 0) slots[flip][wave] = f32x2{sg, sgh};
+      __syncthreads();
+      sg = sgh = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        sg += slots[flip][w][0];
+        sgh += slots[flip][w][1];
+      }
+      flip ^= 1;
+    }
+    const float mg = sg * inv, mgh = sgh * inv;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int q = c * G + lane;
+      float d[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) d[i] = st[1] * (g[c][i] - mg - h[c][i] * mgh);
+      if constexpr (RES) {
+        if (j.ds.p) {
+          float t[8];
+          chunk_values<G == 1>(sr[c], q, k, t);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) d[i] += t[i];
+        }
+      }
+      if (j.dr.p) store_chunk(out_row<T>(j.dr, r), q, k, d);
+      if constexpr (RES) {
+        if (j.dx.p) {
+          if (j.d.thr) drop_chunk(j.d, step, j.d.row0 + r, q, d);
+          store_chunk(out_row<T>(j.dx, r), q, k, d);
+        }
+      }
+    }
+  }
+
+  if (!j.dgamma && !j.dbeta) return;
+  float* const out[2] = {gridDim.x == 1 ? j.dgamma : j.part + (int64_t)(2 * blockIdx.x) * k.n,
+                         gridDim.x == 1 ? j.dbeta : j.part + (int64_t)(2 * blockIdx.x + 1) * k.n};
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+      float* const dst = out[a];
+      float(&acc)[8] = a == 0 ? ag[c] : ab[c];
+      if constexpr (W > 1) {
+        if (dst) store_chunk(dst, c * G + lane, k, acc);
+      } else {
+        if constexpr (GL < 64)
+          for (int i = 0; i < 8; ++i) acc[i] = stride_sum<GL>(acc[i]);
+        __syncthreads();                             // the previous sums have been read
+        if (threadIdx.x % 64 < GL) {
+          *(f32x4*)&sums[wave][lane * 8] = f32x4{acc[0], acc[1], acc[2], acc[3]};
+          *(f32x4*)&sums[wave][lane * 8 + 4] = f32x4{acc[4], acc[5], acc[6], acc[7]};
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < GL * 8; i += NT) {
+          const int col = c * G * 8 + i;
+          if (dst && col < k.n) {
+            float t = 0.f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) t += sums[w][i];
+            dst[col] = t;
+          }
+        }
       }
     }
   }
 }
 
-int row_grid(int64_t rows) { return (int)std::min<int64_t>(rows, 1 << 16); }
+// The partial pairs summed: a workgroup takes 64 of the 2 x cols columns, each
+// of its wavefronts every kSlices-th part; the wavefronts' sums meet in LDS.
+constexpr int kSlices = 16;
+__global__ __launch_bounds__(64 * kSlices) void k_norm_reduce(NormJob j, int parts) {
+  __shared__ float sums[kSlices][64];
+  const int lane = threadIdx.x % 64, slice = threadIdx.x / 64;
+  const int64_t pitch = 2 * (int64_t)j.cols;
+  const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+  float t = 0.f;
+  if (c < pitch) {
+    const float* p = j.part + c;
+#pragma unroll 8
+    for (int i = slice; i < parts; i += kSlices) t += p[i * pitch];
+  }
+  sums[slice][lane] = t;
+  __syncthreads();
+  if (slice == 0 && c < pitch) {
+    t = 0.f;
+#pragma unroll
+    for (int s = 0; s < kSlices; ++s) t += sums[s][lane];
+    float* const dst = c < j.cols ? j.dgamma : j.dbeta;
+    if (dst) dst[c < j.cols ? c : c - j.cols] = t;
+  }
+}
 
 // one round of resident workgroups: 256 CUs, eight workgroups of 256 threads
 constexpr int kResident = 2048;
@@ -431,6 +521,41 @@ hipError_t forward_with(const NormJob& j, hipStream_t st) {
   const int grid = (int)std::min<int64_t>(blocks, kResident * kThreads / nt);
   hipLaunchKernelGGL((k_norm_forward<T, RES, G, CH>), dim3(grid), dim3(nt), 0, st, j);
   return hipGetLastError();
+}
+
+// threads of a workgroup of the backward, and its rows at a time
+constexpr int backward_threads(int G) { return G > 512 ? G : 512; }
+
+// Lanes per row of a width (G of the kernels).
+int lanes_for(int cols) {
+  const int per = (cols + 7) / 8;
+  for (int g = 1; g <= 64; g *= 2)
+    if (per <= g) return g;
+  if (per <= 128) return 64;
+  return per <= 1024 ? 512 : 1024;
+}
+
+template <typename T, bool RES, int G, int CH>
+hipError_t backward_with(const NormJob& j, int parts, hipStream_t st) {
+  constexpr int nt = backward_threads(G);
+  hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt>), dim3(parts), dim3(nt), 0, st, j);
+  return hipGetLastError();
+}
+
+template <typename T, bool RES>
+hipError_t backward(const NormJob& j, int parts, hipStream_t st) {
+  const int per = (j.cols + 7) / 8;
+  switch (lanes_for(j.cols)) {
+    case 1: return backward_with<T, RES, 1, 1>(j, parts, st);
+    case 2: return backward_with<T, RES, 2, 1>(j, parts, st);
+    case 4: return backward_with<T, RES, 4, 1>(j, parts, st);
+    case 8: return backward_with<T, RES, 8, 1>(j, parts, st);
+    case 16: return backward_with<T, RES, 16, 1>(j, parts, st);
+    case 32: return backward_with<T, RES, 32, 1>(j, parts, st);
+    case 64: return per <= 64 ? backward_with<T, RES, 64, 1>(j, parts, st) : backward_with<T, RES, 64, 2>(j, parts, st);
+    case 512: return per <= 512 ? backward_with<T, RES, 512, 1>(j, parts, st) : backward_with<T, RES, 512, 2>(j, parts, st);
+    default: return per <= 2048 ? backward_with<T, RES, 1024, 2>(j, parts, st) : backward_with<T, RES, 1024, 4>(j, parts, st);
+  }
 }
 
 template <typename T, bool RES>
@@ -453,7 +578,14 @@ hipError_t forward(const NormJob& j, hipStream_t st) {
 
 }  // namespace
 
-int norm_parts(int64_t rows, int) { return (int)std::min<int64_t>(rows, kMaxParts); }
+// One round of resident workgroups (two of 512 threads a CU, or one of 1024),
+// the rows dealt out evenly.
+int norm_parts(int64_t rows, int cols) {
+  const int g = lanes_for(cols), nt = backward_threads(g), rpb = nt / g;
+  const int64_t blocks = (rows + rpb - 1) / rpb, resident = 256 * (1024 / nt);
+  const int64_t rounds = (blocks + resident - 1) / resident;
+  return rounds ? (int)((blocks + rounds - 1) / rounds) : 0;
+}
 
 hipError_t launch_dropout(Elt e, const DropJob& j, hipStream_t st) {
   const int64_t per = ((int64_t)j.cols + 7) / 8;
@@ -473,21 +605,18 @@ hipError_t launch_norm_forward(Elt e, const NormJob& j, hipStream_t st) {
 }
 
 hipError_t launch_norm_backward(Elt e, const NormJob& j, hipStream_t st) {
-  const int cb = (j.cols + kThreads - 1) / kThreads;
-  if (j.dgamma || j.dbeta) {
-    const int parts = norm_parts(j.rows, j.cols);
-    if (parts > 0) {
-      if (e == BF16) hipLaunchKernelGGL(k_norm_part<uint16_t>, dim3(cb, parts), dim3(kThreads), 0, st, j, parts);
-      else hipLaunchKernelGGL(k_norm_part<float>, dim3(cb, parts), dim3(kThreads), 0, st, j, parts);
-    }
-    hipLaunchKernelGGL(k_norm_reduce, dim3(cb), dim3(kThreads), 0, st, j, parts);
+  const int parts = norm_parts(j.rows, j.cols);
+  const bool residual = j.ds.p || j.dx.p || j.d.thr;
+  hipError_t err = hipSuccess;
+  if (parts > 0) {
+    if (e == BF16) err = residual ? backward<uint16_t, true>(j, parts, st) : backward<uint16_t, false>(j, parts, st);
+    else err = residual ? backward<float, true>(j, parts, st) : backward<float, false>(j, parts, st);
   }
-  if (j.rows > 0 && (j.dr.p || j.dx.p)) {
-    const dim3 g(row_grid(j.rows));
-    if (e == BF16) hipLaunchKernelGGL(k_norm_dx<uint16_t>, g, dim3(kThreads), 0, st, j);
-    else hipLaunchKernelGGL(k_norm_dx<float>, g, dim3(kThreads), 0, st, j);
+  if (err == hipSuccess && parts != 1 && (j.dgamma || j.dbeta)) {
+    hipLaunchKernelGGL(k_norm_reduce, dim3((j.cols + 31) / 32), dim3(64 * kSlices), 0, st, j, parts);
+    err = hipGetLastError();
   }
-  return hipGetLastError();
+  return err;
 }
 
 }  // namespace vfl

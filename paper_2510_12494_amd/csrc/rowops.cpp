@@ -109,6 +109,11 @@ NormJob norm_job(Checks& c, const Args& a) {
   return j;
 }
 
+size_t workspace_bytes(int64_t rows, int32_t cols) {
+  const int parts = norm_parts(rows, cols);
+  return parts > 1 ? (size_t)parts * 2 * (size_t)cols * sizeof(float) : 0;
+}
+
 // what every backward pass checks: the statistics, the weights' gradients and
 // the workspace that they need (*nomem: it is too small)
 template <typename Args>
@@ -118,10 +123,10 @@ void norm_grads(Checks& c, const Args& a, NormJob& j, bool* nomem) {
   if (c.why || (!a.dgamma && !a.dbeta)) return;
   j.dgamma = a.dgamma;
   j.dbeta = a.dbeta;
-  const size_t bytes = (size_t)norm_parts(a.rows, a.cols) * 2 * (size_t)a.cols * sizeof(float);
-  if (bytes == 0) return;
   c.need((uintptr_t)a.workspace % 16 == 0, "workspace must be 16-byte aligned");
   if (c.why) return;
+  const size_t bytes = workspace_bytes(a.rows, a.cols);
+  if (bytes == 0) return;
   if (!a.workspace || a.workspace_bytes < bytes) {
     c.why = "workspace smaller than vfl_norm_workspace_size()";
     *nomem = true;
@@ -153,7 +158,7 @@ vfl_status vfl_norm_workspace_size(int64_t rows, int32_t cols, size_t* bytes) {
   Checks c = begin(call, VFL_F32, rows, cols, VFL_NORM_MAX_COLS);
   c.need(bytes != nullptr, "bytes must not be NULL");
   if (c.why) return refuse(call, c.why);
-  *bytes = (size_t)norm_parts(rows, cols) * 2 * (size_t)cols * sizeof(float);
+  *bytes = workspace_bytes(rows, cols);
   return enqueued(call, hipSuccess);
 }
 

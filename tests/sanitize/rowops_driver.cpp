@@ -67,7 +67,7 @@ hipError_t launch_norm_backward(Elt e, const NormJob& j, hipStream_t) {
   for (const Mat* m : {&j.ds, &j.dr, &j.dx}) check_mat(*m, j.rows, j.cols, elt_size(e), false);
   expect(j.stats || j.rows == 0, "statistics");
   expect(j.dr.p || j.dx.p || j.dgamma || j.dbeta, "an output");
-  if ((j.dgamma || j.dbeta) && j.rows > 0)
+  if ((j.dgamma || j.dbeta) && norm_parts(j.rows, j.cols) > 1)
     expect(j.part && (size_t)norm_parts(j.rows, j.cols) * 8 * j.cols <= ws_bytes,
            "the workspace holds the partial sums");
   return hipSuccess;
