@@ -101,15 +101,17 @@ __device__ __forceinline__ int64_t pk_index(int n, int k, int kst) {
 }
 
 // Philox4x32-10 (Salmon et al., SC'11): 10 rounds of the 4x32 bijection
-// with Weyl-sequence key increments.
+// with Weyl-sequence key increments.  Both halves of a product come from one
+// v_mad_u64_u32, the three-way exclusive or is one v_bitop3_b32 (0x96).
 __device__ __forceinline__ void philox4x32_10(uint32_t (&c)[4], uint32_t k0, uint32_t k1) {
 #pragma unroll
   for (int r = 0; r < 10; ++r) {
     if (r) { k0 += 0x9E3779B9u; k1 += 0xBB67AE85u; }
-    const uint32_t hi0 = __umulhi(0xD2511F53u, c[0]), lo0 = 0xD2511F53u * c[0];
-    const uint32_t hi1 = __umulhi(0xCD9E8D57u, c[2]), lo1 = 0xCD9E8D57u * c[2];
-    const uint32_t n0 = hi1 ^ c[1] ^ k0, n2 = hi0 ^ c[3] ^ k1;
-    c[0] = n0; c[1] = lo1; c[2] = n2; c[3] = lo0;
+    const uint64_t p0 = (uint64_t)0xD2511F53u * c[0], p1 = (uint64_t)0xCD9E8D57u * c[2];
+    c[0] = __builtin_amdgcn_bitop3_b32((uint32_t)(p1 >> 32), c[1], k0, 0x96);
+    c[2] = __builtin_amdgcn_bitop3_b32((uint32_t)(p0 >> 32), c[3], k1, 0x96);
+    c[1] = (uint32_t)p1;
+    c[3] = (uint32_t)p0;
   }
 }
 

@@ -58,13 +58,19 @@ struct Cols {
   __device__ explicit Cols(int cols) : n(cols), per((cols + 7) >> 3), part(cols & 7) {}
 };
 
+// How the columns of a kernel's rows lie: kExact: each lane's chunks are all
+// whole; kRagged: a row may end inside a chunk, and lanes may have none of it
+// (rows of eight columns and more); kSmall: rows of one chunk of any width.
+enum Form { kExact, kRagged, kSmall };
+
 // Chunk q of a row, loaded without a branch: the last chunk of a row that ends
 // inside it, and chunks past the row's end, are read from the row's last eight
 // columns, so that no access leaves the row (rows of fewer than eight columns
-// are gathered; kSmall marks the kernels that meet them).
-template <bool kSmall, typename T>
+// are gathered).
+template <Form F, typename T>
 __device__ __forceinline__ Raw<T> load_chunk(const T* row, int q, const Cols& k) {
-  if constexpr (kSmall) {
+  if constexpr (F == kExact) return load_at(row + 8 * q);
+  if constexpr (F == kSmall) {
     if (k.n < 8) {
       T e[8] = {};
 #pragma unroll
@@ -78,12 +84,13 @@ __device__ __forceinline__ Raw<T> load_chunk(const T* row, int q, const Cols& k)
 
 // Its values: those of a partial chunk moved to their places, zero at and past
 // the row's end.
-template <bool kSmall, typename T>
+template <Form F, typename T>
 __device__ __forceinline__ void chunk_values(const Raw<T>& r, int q, const Cols& k, float (&v)[8]) {
   unpack(r, v);
-  if (kSmall && k.n < 8) return;
+  if constexpr (F == kExact) return;
+  if (F == kSmall && k.n < 8) return;
   if (k.part && q == k.per - 1) {
-    const int by = 8 - k.part;
+    const int by = 8 - k.part;                       // uniform
     if (by & 4) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = i + 4 < 8 ? v[(i + 4) & 7] : 0.f;
@@ -119,10 +126,10 @@ __device__ __forceinline__ void store8(float* p, const float* v) {
 
 // Stores chunk q of a row: whole, or the columns that the row has of it, in
 // pieces of four, two and one.
-template <typename T>
+template <Form F, typename T>
 __device__ __forceinline__ void store_chunk(T* row, int q, const Cols& k, const float (&v)[8]) {
   T* p = row + 8 * q;
-  if (8 * q + 8 <= k.n) {
+  if (F == kExact || 8 * q + 8 <= k.n) {
     store8(p, v);
   } else if (q < k.per) {
     const int m = k.part;                          // uniform
@@ -148,20 +155,25 @@ __device__ __forceinline__ uint32_t step_of(const DropKey& d) {
   return d.step + (d.step_dev ? *d.step_dev : 0u);
 }
 
-// v = dropout(v) of chunk q of global row id `row`.  One Philox block of
-// 16-bit numbers per chunk: with 32-bit numbers the two blocks' 40 wide
-// multiplications would take longer than the chunk's bytes.  A number u is at
-// least thr where u * 2^16 exceeds (thr - 1) * 2^16 + 65535, which compares a
-// word's high half without moving it.
-__device__ __forceinline__ void drop_chunk(const DropKey& d, uint32_t step, int64_t row, int q, float (&v)[8]) {
+// The numbers of chunk q of global row id `row`: one Philox block of 16-bit
+// numbers per chunk (32-bit numbers would take two blocks).
+struct Numbers { uint32_t w[4]; };
+__device__ __forceinline__ Numbers chunk_numbers(const DropKey& d, uint32_t step, int64_t row, int q) {
   const uint64_t id = (uint64_t)row;
-  uint32_t c[4] = {step, (uint32_t)id, (uint32_t)q, 0x80000000u | ((uint32_t)(id >> 32) << 16) | d.tag};
-  philox4x32_10(c, d.k0, d.k1);
+  Numbers n{{step, (uint32_t)id, (uint32_t)q, 0x80000000u | ((uint32_t)(id >> 32) << 16) | d.tag}};
+  philox4x32_10(n.w, d.k0, d.k1);
+  return n;
+}
+
+// v = dropout(v).  A number u is at least thr where it exceeds thr - 1, and a
+// word's high half does where the word exceeds (thr - 1) * 2^16 + 65535: neither
+// half is moved to be compared.
+__device__ __forceinline__ void drop_values(const DropKey& d, const Numbers& n, float (&v)[8]) {
   const uint32_t last = (d.thr << 16) - 1u;        // thr in 1 .. 65536
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    v[2 * i] = (c[i] << 16) > last ? v[2 * i] * d.scale : 0.f;
-    v[2 * i + 1] = c[i] > last ? v[2 * i + 1] * d.scale : 0.f;
+    v[2 * i] = (uint16_t)n.w[i] > (uint16_t)(d.thr - 1u) ? v[2 * i] * d.scale : 0.f;
+    v[2 * i + 1] = n.w[i] > last ? v[2 * i + 1] * d.scale : 0.f;
   }
 }
 
@@ -173,7 +185,7 @@ __device__ __forceinline__ T* out_row(const Mat& m, int64_t r) { return (T*)m.p 
 // The matrix's chunks dealt to the threads in order, so that a wavefront's are
 // consecutive whatever the width; a thread steps its (row, chunk) pair by
 // (drow, dq), a whole grid, without a division.
-template <typename T>
+template <typename T, Form F>
 __global__ __launch_bounds__(kThreads) void k_dropout(DropJob j, int64_t drow, int dq) {
   const Cols k(j.cols);
   const uint32_t step = step_of(j.d);
@@ -181,11 +193,13 @@ __global__ __launch_bounds__(kThreads) void k_dropout(DropJob j, int64_t drow, i
   int64_t r = first / (uint32_t)k.per;
   int q = (int)(first % (uint32_t)k.per);
   while (r < j.rows) {
-    const Raw<T> raw = load_chunk<true>(row_of<T>(j.x, r), q, k);
+    const Raw<T> raw = load_chunk<F>(row_of<T>(j.x, r), q, k);
+    Numbers n;
+    if (j.d.thr) n = chunk_numbers(j.d, step, j.d.row0 + r, q);
     float v[8];
-    chunk_values<true>(raw, q, k, v);
-    if (j.d.thr) drop_chunk(j.d, step, j.d.row0 + r, q, v);
-    store_chunk(out_row<T>(j.y, r), q, k, v);
+    chunk_values<F>(raw, q, k, v);
+    if (j.d.thr) drop_values(j.d, n, v);
+    store_chunk<F>(out_row<T>(j.y, r), q, k, v);
     r += drow;
     q += dq;
     if (q >= k.per) {
@@ -220,26 +234,49 @@ __device__ __forceinline__ float group_sum(float v) {
   return v;
 }
 
+// The row group of a thread: a scalar where a wavefront holds one row only.
+template <int G>
+__device__ __forceinline__ int group_of_thread() {
+  const int g = threadIdx.x / G;
+  return G >= 64 ? __builtin_amdgcn_readfirstlane(g) : g;
+}
+
 // ------------------------------------------------------------------ forward
 // G lanes hold a row, CH chunks each (chunk c * G + lane); a workgroup of
-// max(kThreads, G) threads holds kThreads / G rows, or one.  Mean and variance
-// in two sums over the registers.  Where a row spans W = G / 64 wavefronts,
-// each forms its own mean and sum of squares, and these meet in LDS: with
-// n_w, m_w, M_w of wavefront w, the row's sum of squares is the sum of
-// M_w + n_w (m_w - mean)^2, which takes one barrier a row (the slots alternate)
-// and loses nothing to cancellation.
-template <typename T, bool RES, int G, int CH>
+// max(kThreads, G) threads holds kThreads / G rows, or one.  The next row's
+// loads are in flight while a row is worked on.  Mean and variance in two sums
+// over the registers.  Where a row spans W = G / 64 wavefronts, each forms its
+// own mean and sum of squares, and these meet in LDS: with n_w, m_w, M_w of
+// wavefront w, the row's sum of squares is the sum of M_w + n_w (m_w -
+// mean)^2, which takes one barrier a row (the slots alternate) and loses
+// nothing to cancellation.  HOIST: a thread's gamma and beta are loaded before
+// its first row and kept.
+template <typename T, bool RES, int G, int CH, Form F, bool HOIST>
 __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(NormJob j) {
   constexpr int W = G > 64 ? G / 64 : 1;
   constexpr int RPB = G > 64 ? 1 : kThreads / G;
   constexpr int GL = G < 64 ? G : 64;
-  constexpr bool HOIST = G <= 64;
+  constexpr bool AHEAD = G < 1024;                 // the next row is loaded early
   static_assert(G <= 64 || G >= kThreads, "a workgroup holds whole rows");
-  __shared__ f32x2 slots[2][W];
+  __shared__ f32x2 slots[2][W];                    // a wavefront's mean and sum of squares
+  __shared__ float columns[W];                     // and its columns of a row
   const Cols k(j.cols);
   const int lane = threadIdx.x % G, wave = threadIdx.x / 64;
   const float inv = 1.f / (float)k.n;
-  const bool whole = k.n == 8 * G * CH;
+
+  Raw<T> x[CH], res[CH];
+  auto fetch = [&](int64_t r) {
+    const T* px = row_of<T>(j.x, r);
+    const T* pr = RES ? row_of<T>(j.r, r) : nullptr;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      x[c] = load_chunk<F>(px, c * G + lane, k);
+      if constexpr (RES) res[c] = load_chunk<F>(pr, c * G + lane, k);
+    }
+  };
+  const int64_t stride = (int64_t)gridDim.x * RPB;
+  int64_t r = (int64_t)blockIdx.x * RPB + group_of_thread<G>();
+  if (AHEAD && r < j.rows) fetch(r);
   uint32_t step = 0;
   if constexpr (RES) step = step_of(j.d);
 
@@ -248,73 +285,79 @@ __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(No
     const int q = c * G + lane;
 #pragma unroll
     for (int i = 0; i < 8; ++i) g[slot][i] = 1.f, b[slot][i] = 0.f;
-    if (j.gamma) chunk_values<G == 1>(load_chunk<G == 1>(j.gamma, q, k), q, k, g[slot]);
-    if (j.beta) chunk_values<G == 1>(load_chunk<G == 1>(j.beta, q, k), q, k, b[slot]);
+    if (j.gamma) chunk_values<F>(load_chunk<F>(j.gamma, q, k), q, k, g[slot]);
+    if (j.beta) chunk_values<F>(load_chunk<F>(j.beta, q, k), q, k, b[slot]);
   };
   if constexpr (HOIST)
     for (int c = 0; c < CH; ++c) weights(c, c);
-  // this wavefront's columns (W > 1)
   float nw = 0.f;
   if constexpr (W > 1) {
 #pragma unroll
     for (int c = 0; c < CH; ++c) nw += (float)min(max(k.n - 8 * (c * G + 64 * wave), 0), 512);
+    if (threadIdx.x % 64 == 0) columns[wave] = nw;   // read past the first row's barrier
   }
+  const float inv_nw = nw > 0.f ? 1.f / nw : 0.f;
 
   int flip = 0;
-  for (int64_t r = (int64_t)blockIdx.x * RPB + threadIdx.x / G; r < j.rows; r += (int64_t)gridDim.x * RPB) {
-    Raw<T> x[CH], res[CH];
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      x[c] = load_chunk<G == 1>(row_of<T>(j.x, r), c * G + lane, k);
-      if constexpr (RES) res[c] = load_chunk<G == 1>(row_of<T>(j.r, r), c * G + lane, k);
-    }
+  for (; r < j.rows; r += stride) {
+    if constexpr (!AHEAD) fetch(r);
     float v[CH][8];
     float sum = 0.f;
+    if constexpr (RES) {
+      Numbers n[CH];
+      if (AHEAD && j.d.thr) {                        // beside the row's loads
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      const int q = c * G + lane;
-      chunk_values<G == 1>(x[c], q, k, v[c]);
-      if constexpr (RES) {
-        if (j.d.thr) drop_chunk(j.d, step, j.d.row0 + r, q, v[c]);
+        for (int c = 0; c < CH; ++c) n[c] = chunk_numbers(j.d, step, j.d.row0 + r, c * G + lane);
+      }
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        const int q = c * G + lane;
+        chunk_values<F>(x[c], q, k, v[c]);
+        if (!AHEAD && j.d.thr) n[c] = chunk_numbers(j.d, step, j.d.row0 + r, q);
+        if (j.d.thr) drop_values(j.d, n[c], v[c]);
         float t[8];
-        chunk_values<G == 1>(res[c], q, k, t);
+        chunk_values<F>(res[c], q, k, t);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[c][i] += t[i];
-        if (j.s.p) store_chunk(out_row<T>(j.s, r), q, k, v[c]);
       }
+    } else {
+#pragma unroll
+      for (int c = 0; c < CH; ++c) chunk_values<F>(x[c], c * G + lane, k, v[c]);
+    }
+    if (AHEAD && r + stride < j.rows) fetch(r + stride);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      if constexpr (RES)
+        if (j.s.p) store_chunk<F>(out_row<T>(j.s, r), c * G + lane, k, v[c]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum += v[c][i];
     }
     sum = group_sum<GL>(sum);
-    float mean = sum * inv;
-    if constexpr (W > 1) mean = nw > 0.f ? sum / nw : 0.f;
+    float mean = sum * (W > 1 ? inv_nw : inv);
     float sq = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const int left = k.n - 8 * (c * G + lane);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float d = whole || i < left ? v[c][i] - mean : 0.f;
+        const float d = F == kExact || i < left ? v[c][i] - mean : 0.f;
         sq = fmaf(d, d, sq);
       }
     }
     sq = group_sum<GL>(sq);
     if constexpr (W > 1) {
-      if (threadIdx.x % 64 == 0) slots[flip][wave] = f32x2{sum, sq};
+      if (threadIdx.x % 64 == 0) slots[flip][wave] = f32x2{mean, sq};
       __syncthreads();
       sum = 0.f;
 #pragma unroll
-      for (int w = 0; w < W; ++w) sum += slots[flip][w][0];
+      for (int w = 0; w < W; ++w) sum = fmaf(columns[w], slots[flip][w][0], sum);
       mean = sum * inv;
       sq = 0.f;
 #pragma unroll
       for (int w = 0; w < W; ++w) {
-        float n = 0.f;
-#pragma unroll
-        for (int c = 0; c < CH; ++c) n += (float)min(max(k.n - 8 * (c * G + 64 * w), 0), 512);
         const f32x2 s = slots[flip][w];
-        const float d = n > 0.f ? s[0] / n - mean : 0.f;
-        sq += fmaf(n * d, d, s[1]);
+        const float d = s[0] - mean;
+        sq += fmaf(columns[w] * d, d, s[1]);
       }
       flip ^= 1;
     }
@@ -327,7 +370,7 @@ __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(No
       float y[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) y[i] = fmaf((v[c][i] - mean) * rs, g[at][i], b[at][i]);
-      store_chunk(out_row<T>(j.y, r), c * G + lane, k, y);
+      store_chunk<F>(out_row<T>(j.y, r), c * G + lane, k, y);
     }
   }
 }
@@ -356,7 +399,7 @@ __device__ __forceinline__ float stride_sum(float v) {
 // of its rows; at the end the workgroup's rows of threads meet in LDS and leave
 // one partial pair of float32 rows (2 x cols at j.part), or the result itself
 // where the grid is one workgroup.
-template <typename T, bool RES, int G, int CH, int NT>
+template <typename T, bool RES, int G, int CH, int NT, Form F>
 __global__ __launch_bounds__(NT) void k_norm_backward(NormJob j) {
   constexpr int W = G > 64 ? G / 64 : 1;
   constexpr int NW = NT / 64;
@@ -377,23 +420,23 @@ __global__ __launch_bounds__(NT) void k_norm_backward(NormJob j) {
     const int q = c * G + lane;
 #pragma unroll
     for (int i = 0; i < 8; ++i) gm[slot][i] = 1.f;
-    if (j.gamma) chunk_values<G == 1>(load_chunk<G == 1>(j.gamma, q, k), q, k, gm[slot]);
+    if (j.gamma) chunk_values<F>(load_chunk<F>(j.gamma, q, k), q, k, gm[slot]);
   };
   if constexpr (HOIST)
     for (int c = 0; c < CH; ++c) weights(c, c);
   float ag[CH][8] = {}, ab[CH][8] = {};
 
   int flip = 0;
-  for (int64_t r = (int64_t)blockIdx.x * RPB + threadIdx.x / G; r < j.rows; r += (int64_t)gridDim.x * RPB) {
+  for (int64_t r = (int64_t)blockIdx.x * RPB + group_of_thread<G>(); r < j.rows; r += (int64_t)gridDim.x * RPB) {
     Raw<T> xr[CH], yr[CH], sr[CH];
     const f32x2 st = *(const f32x2*)(j.stats + 2 * r);
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const int q = c * G + lane;
-      xr[c] = load_chunk<G == 1>(row_of<T>(j.v, r), q, k);
-      yr[c] = load_chunk<G == 1>(row_of<T>(j.dy, r), q, k);
+      xr[c] = load_chunk<F>(row_of<T>(j.v, r), q, k);
+      yr[c] = load_chunk<F>(row_of<T>(j.dy, r), q, k);
       if constexpr (RES)
-        if (j.ds.p) sr[c] = load_chunk<G == 1>(row_of<T>(j.ds, r), q, k);
+        if (j.ds.p) sr[c] = load_chunk<F>(row_of<T>(j.ds, r), q, k);
     }
     float h[CH][8], g[CH][8];
     float sg = 0.f, sgh = 0.f;
@@ -401,8 +444,8 @@ __global__ __launch_bounds__(NT) void k_norm_backward(NormJob j) {
     for (int c = 0; c < CH; ++c) {
       const int q = c * G + lane, at = HOIST ? c : 0;
       if constexpr (!HOIST) weights(c, 0);
-      chunk_values<G == 1>(xr[c], q, k, h[c]);
-      chunk_values<G == 1>(yr[c], q, k, g[c]);
+      chunk_values<F>(xr[c], q, k, h[c]);
+      chunk_values<F>(yr[c], q, k, g[c]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         h[c][i] = (h[c][i] - st[0]) * st[1];
@@ -436,16 +479,16 @@ __global__ __launch_bounds__(NT) void k_norm_backward(NormJob j) {
       if constexpr (RES) {
         if (j.ds.p) {
           float t[8];
-          chunk_values<G == 1>(sr[c], q, k, t);
+          chunk_values<F>(sr[c], q, k, t);
 #pragma unroll
           for (int i = 0; i < 8; ++i) d[i] += t[i];
         }
       }
-      if (j.dr.p) store_chunk(out_row<T>(j.dr, r), q, k, d);
+      if (j.dr.p) store_chunk<F>(out_row<T>(j.dr, r), q, k, d);
       if constexpr (RES) {
         if (j.dx.p) {
-          if (j.d.thr) drop_chunk(j.d, step, j.d.row0 + r, q, d);
-          store_chunk(out_row<T>(j.dx, r), q, k, d);
+          if (j.d.thr) drop_values(j.d, chunk_numbers(j.d, step, j.d.row0 + r, q), d);
+          store_chunk<F>(out_row<T>(j.dx, r), q, k, d);
         }
       }
     }
@@ -461,7 +504,7 @@ __global__ __launch_bounds__(NT) void k_norm_backward(NormJob j) {
       float* const dst = out[a];
       float(&acc)[8] = a == 0 ? ag[c] : ab[c];
       if constexpr (W > 1) {
-        if (dst) store_chunk(dst, c * G + lane, k, acc);
+        if (dst) store_chunk<F>(dst, c * G + lane, k, acc);
       } else {
         if constexpr (GL < 64)
           for (int i = 0; i < 8; ++i) acc[i] = stride_sum<GL>(acc[i]);
@@ -510,17 +553,37 @@ __global__ __launch_bounds__(64 * kSlices) void k_norm_reduce(NormJob j, int par
   }
 }
 
-// one round of resident workgroups: 256 CUs, eight workgroups of 256 threads
-constexpr int kResident = 2048;
+// The forward's workgroups (in units of 256 threads).  Rows of one chunk a lane
+// take one round of resident workgroups (two for the residual join, whose rows
+// differ more in time), so that a thread's gamma and beta serve several rows
+// and the next row's loads run beside a row's work: 120291 x 49 bf16 takes 7.8
+// us, 9.3 in two rounds; residual 118955 x 175 bf16 48.5 in two, 52.5 in one.
+// Wider rows are dealt out by the hardware: residual 32768 x 1024 bf16 46.6 us,
+// 48.5 in two rounds.
+constexpr int kResident = 2048, kMany = 16384;
 
-template <typename T, bool RES, int G, int CH>
+template <typename T, bool RES, int G, int CH, bool HOIST = G <= 64>
 hipError_t forward_with(const NormJob& j, hipStream_t st) {
   constexpr int nt = G > kThreads ? G : kThreads;
   constexpr int rpb = nt / G;
+  constexpr int most = G <= 64 && CH == 1 ? (RES ? 2 * kResident : kResident) : kMany;
   const int64_t blocks = (j.rows + rpb - 1) / rpb;
-  const int grid = (int)std::min<int64_t>(blocks, kResident * kThreads / nt);
-  hipLaunchKernelGGL((k_norm_forward<T, RES, G, CH>), dim3(grid), dim3(nt), 0, st, j);
+  const int grid = (int)std::min<int64_t>(blocks, most * kThreads / nt);
+  constexpr Form other = G == 1 ? kSmall : kRagged;
+  if (j.cols == 8 * G * CH)
+    hipLaunchKernelGGL((k_norm_forward<T, RES, G, CH, kExact, HOIST>), dim3(grid), dim3(nt), 0, st, j);
+  else
+    hipLaunchKernelGGL((k_norm_forward<T, RES, G, CH, other, HOIST>), dim3(grid), dim3(nt), 0, st, j);
   return hipGetLastError();
+}
+
+// Rows of several wavefronts: up to about a round of workgroups, gamma and beta
+// are fetched beside the row (378 x 5578 bf16: 8.2 us, 8.5 after it); beyond
+// that, reading them after the row's sums leaves the registers to more
+// wavefronts (7311 x 4040 bf16: 47.4 us, 50.3 before).
+template <typename T, bool RES, int G, int CH>
+hipError_t forward_wide(const NormJob& j, hipStream_t st) {
+  return j.rows <= 1024 ? forward_with<T, RES, G, CH, true>(j, st) : forward_with<T, RES, G, CH, false>(j, st);
 }
 
 // threads of a workgroup of the backward, and its rows at a time
@@ -538,7 +601,9 @@ int lanes_for(int cols) {
 template <typename T, bool RES, int G, int CH>
 hipError_t backward_with(const NormJob& j, int parts, hipStream_t st) {
   constexpr int nt = backward_threads(G);
-  hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt>), dim3(parts), dim3(nt), 0, st, j);
+  constexpr Form other = G == 1 ? kSmall : kRagged;
+  if (j.cols == 8 * G * CH) hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, kExact>), dim3(parts), dim3(nt), 0, st, j);
+  else hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, other>), dim3(parts), dim3(nt), 0, st, j);
   return hipGetLastError();
 }
 
@@ -569,11 +634,11 @@ hipError_t forward(const NormJob& j, hipStream_t st) {
   if (per <= 32) return forward_with<T, RES, 32, 1>(j, st);
   if (per <= 64) return forward_with<T, RES, 64, 1>(j, st);
   if (per <= 128) return forward_with<T, RES, 64, 2>(j, st);
-  if (per <= 256) return forward_with<T, RES, 256, 1>(j, st);
-  if (per <= 512) return forward_with<T, RES, 256, 2>(j, st);
-  if (per <= 1024) return forward_with<T, RES, 512, 2>(j, st);
-  if (per <= 2048) return forward_with<T, RES, 1024, 2>(j, st);
-  return forward_with<T, RES, 1024, 4>(j, st);
+  if (per <= 256) return forward_wide<T, RES, 256, 1>(j, st);
+  if (per <= 512) return forward_wide<T, RES, 256, 2>(j, st);
+  if (per <= 1024) return forward_wide<T, RES, 512, 2>(j, st);
+  if (per <= 2048) return forward_with<T, RES, 1024, 2, true>(j, st);
+  return forward_with<T, RES, 1024, 4, false>(j, st);   // registers: none left for gamma and beta
 }
 
 }  // namespace
@@ -587,16 +652,21 @@ int norm_parts(int64_t rows, int cols) {
   return rounds ? (int)((blocks + rounds - 1) / rounds) : 0;
 }
 
-hipError_t launch_dropout(Elt e, const DropJob& j, hipStream_t st) {
+template <typename T>
+hipError_t dropout(const DropJob& j, hipStream_t st) {
   const int64_t per = ((int64_t)j.cols + 7) / 8;
   const int64_t chunks = j.rows > (INT64_MAX >> 2) / per ? INT64_MAX >> 2 : j.rows * per;
-  const int grid = (int)std::min<int64_t>((chunks + kThreads - 1) / kThreads, kResident);
-  const int64_t stride = (int64_t)grid * kThreads;
-  if (e == BF16)
-    hipLaunchKernelGGL(k_dropout<uint16_t>, dim3(grid), dim3(kThreads), 0, st, j, stride / per, (int)(stride % per));
-  else
-    hipLaunchKernelGGL(k_dropout<float>, dim3(grid), dim3(kThreads), 0, st, j, stride / per, (int)(stride % per));
+  const int grid = (int)std::min<int64_t>((chunks + kThreads - 1) / kThreads, kMany);
+  const int64_t stride = (int64_t)grid * kThreads, drow = stride / per;
+  const int dq = (int)(stride % per);
+  if (j.cols % 8 == 0) hipLaunchKernelGGL((k_dropout<T, kExact>), dim3(grid), dim3(kThreads), 0, st, j, drow, dq);
+  else if (j.cols > 8) hipLaunchKernelGGL((k_dropout<T, kRagged>), dim3(grid), dim3(kThreads), 0, st, j, drow, dq);
+  else hipLaunchKernelGGL((k_dropout<T, kSmall>), dim3(grid), dim3(kThreads), 0, st, j, drow, dq);
   return hipGetLastError();
+}
+
+hipError_t launch_dropout(Elt e, const DropJob& j, hipStream_t st) {
+  return e == BF16 ? dropout<uint16_t>(j, st) : dropout<float>(j, st);
 }
 
 hipError_t launch_norm_forward(Elt e, const NormJob& j, hipStream_t st) {
