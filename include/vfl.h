@@ -421,7 +421,9 @@ vfl_status vfl_philox(uint64_t seed, uint32_t step, uint32_t tag, uint32_t row0,
 
 /* A row-major matrix: ld elements from row to row (0: as many as the
  * operator's columns; never fewer).  Element-aligned data of any ld is taken.
- * An output may be the same matrix as an input of its call (same data, same
+ * Between the matrix's first and last element, up to seven elements past a
+ * row's end may be read; they have no influence and are never written.  An
+ * output may be the same matrix as an input of its call (same data, same
  * ld); otherwise its elements must be none of an input's or of another
  * output's. */
 typedef struct {

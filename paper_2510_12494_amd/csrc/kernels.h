@@ -442,8 +442,9 @@ struct NormJob {
   int64_t rows;
 };
 
-// workgroups of a backward pass over rows x cols; where there are several, each
-// leaves partial weight gradients (2 x cols floats) in the workspace
+// the most partial pairs (2 x cols floats each) of weights' gradients that a
+// backward pass over rows x cols leaves in its workspace, whatever its element
+// type (1: none, the result is written at once)
 int norm_parts(int64_t rows, int cols);
 hipError_t launch_dropout(Elt e, const DropJob& j, hipStream_t st);
 hipError_t launch_norm_forward(Elt e, const NormJob& j, hipStream_t st);

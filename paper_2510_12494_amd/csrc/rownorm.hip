@@ -52,26 +52,34 @@ __device__ __forceinline__ void unpack(const Raw<float>& r, float (&v)[8]) {
 }
 
 // The columns of a row (kernel-uniform): n of them in `per` chunks, the last
-// one `part` columns wide when that is not 0.
+// one `part` columns wide when that is not 0.  Rows from `edge` on are so near
+// the matrix's end that a whole last chunk would pass it.
 struct Cols {
   int n, per, part;
-  __device__ explicit Cols(int cols) : n(cols), per((cols + 7) >> 3), part(cols & 7) {}
+  int64_t edge;
+  __device__ explicit Cols(int cols, int64_t rows) : n(cols), per((cols + 7) >> 3), part(cols & 7) {
+    const int past = 8 * per - n;                    // rows of n columns and more hold these
+    edge = past ? rows - (past + n - 1) / n : INT64_MAX;
+  }
 };
 
 // How the columns of a kernel's rows lie: kExact: each lane's chunks are all
 // whole; kRagged: a row may end inside a chunk, and lanes may have none of it
 // (rows of eight columns and more); kSmall: rows of one chunk of any width.
+// `whole`: this chunk is whole whatever the form.
 enum Form { kExact, kRagged, kSmall };
 
-// Chunk q of a row, loaded without a branch: the last chunk of a row that ends
-// inside it, and chunks past the row's end, are read from the row's last eight
-// columns, so that no access leaves the row (rows of fewer than eight columns
-// are gathered).
+// Chunk q of a row, loaded without a branch.  A row's last chunk is read whole:
+// past the row's end lie the next row or what is between the two.  Lanes
+// without a chunk read the last one.  On the matrix's edge rows the last eight
+// columns are read instead (rows of fewer are gathered), so that no access
+// passes the matrix.
 template <Form F, typename T>
-__device__ __forceinline__ Raw<T> load_chunk(const T* row, int q, const Cols& k) {
-  if constexpr (F == kExact) return load_at(row + 8 * q);
+__device__ __forceinline__ Raw<T> load_chunk(const T* row, int q, const Cols& k, bool edge, bool whole = false) {
+  if (F == kExact || whole) return load_at(row + 8 * q);
   if constexpr (F == kSmall) {
     if (k.n < 8) {
+      if (!edge) return load_at(row);
       T e[8] = {};
 #pragma unroll
       for (int i = 0; i < 7; ++i)
@@ -79,35 +87,40 @@ __device__ __forceinline__ Raw<T> load_chunk(const T* row, int q, const Cols& k)
       return __builtin_bit_cast(Raw<T>, e);
     }
   }
-  return load_at(row + min(8 * q, k.n - 8));
+  return load_at(row + min(8 * q, edge ? k.n - 8 : 8 * k.per - 8));
 }
 
-// Its values: those of a partial chunk moved to their places, zero at and past
-// the row's end.
+// Its values: zero at and past the row's end (on an edge row, those of a
+// partial chunk moved to their places).
 template <Form F, typename T>
-__device__ __forceinline__ void chunk_values(const Raw<T>& r, int q, const Cols& k, float (&v)[8]) {
+__device__ __forceinline__ void chunk_values(const Raw<T>& r, int q, const Cols& k, bool edge, float (&v)[8],
+                                             bool whole = false) {
   unpack(r, v);
-  if constexpr (F == kExact) return;
-  if (F == kSmall && k.n < 8) return;
-  if (k.part && q == k.per - 1) {
+  if (F == kExact || whole) return;
+  if (edge && k.n >= 8 && q == k.per - 1) {
     const int by = 8 - k.part;                       // uniform
     if (by & 4) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = i + 4 < 8 ? v[(i + 4) & 7] : 0.f;
+      for (int i = 0; i < 4; ++i) v[i] = v[i + 4];
     }
     if (by & 2) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = i + 2 < 8 ? v[(i + 2) & 7] : 0.f;
+      for (int i = 0; i < 6; ++i) v[i] = v[i + 2];
     }
     if (by & 1) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = i + 1 < 8 ? v[(i + 1) & 7] : 0.f;
+      for (int i = 0; i < 7; ++i) v[i] = v[i + 1];
     }
   }
-  if (q >= k.per) {
+  const int left = k.n - 8 * q;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = 0.f;
-  }
+  for (int i = 0; i < 8; ++i) v[i] = i < left ? v[i] : 0.f;
+}
+
+// Those of a row of its own (gamma, beta).
+template <Form F>
+__device__ __forceinline__ void vector_values(const float* p, int q, const Cols& k, float (&v)[8], bool whole) {
+  chunk_values<F>(load_chunk<F>(p, q, k, true, whole), q, k, true, v, whole);
 }
 
 __device__ __forceinline__ void store4(uint16_t* p, const float* v) {
@@ -127,9 +140,9 @@ __device__ __forceinline__ void store8(float* p, const float* v) {
 // Stores chunk q of a row: whole, or the columns that the row has of it, in
 // pieces of four, two and one.
 template <Form F, typename T>
-__device__ __forceinline__ void store_chunk(T* row, int q, const Cols& k, const float (&v)[8]) {
+__device__ __forceinline__ void store_chunk(T* row, int q, const Cols& k, const float (&v)[8], bool whole = false) {
   T* p = row + 8 * q;
-  if (F == kExact || 8 * q + 8 <= k.n) {
+  if (F == kExact || whole || 8 * q + 8 <= k.n) {
     store8(p, v);
   } else if (q < k.per) {
     const int m = k.part;                          // uniform
@@ -187,17 +200,18 @@ __device__ __forceinline__ T* out_row(const Mat& m, int64_t r) { return (T*)m.p 
 // (drow, dq), a whole grid, without a division.
 template <typename T, Form F>
 __global__ __launch_bounds__(kThreads) void k_dropout(DropJob j, int64_t drow, int dq) {
-  const Cols k(j.cols);
+  const Cols k(j.cols, j.rows);
   const uint32_t step = step_of(j.d);
   const uint32_t first = blockIdx.x * kThreads + threadIdx.x;
   int64_t r = first / (uint32_t)k.per;
   int q = (int)(first % (uint32_t)k.per);
   while (r < j.rows) {
-    const Raw<T> raw = load_chunk<F>(row_of<T>(j.x, r), q, k);
+    const bool edge = r >= k.edge;
+    const Raw<T> raw = load_chunk<F>(row_of<T>(j.x, r), q, k, edge);
     Numbers n;
     if (j.d.thr) n = chunk_numbers(j.d, step, j.d.row0 + r, q);
     float v[8];
-    chunk_values<F>(raw, q, k, v);
+    chunk_values<F>(raw, q, k, edge, v);
     if (j.d.thr) drop_values(j.d, n, v);
     store_chunk<F>(out_row<T>(j.y, r), q, k, v);
     r += drow;
@@ -260,7 +274,7 @@ __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(No
   static_assert(G <= 64 || G >= kThreads, "a workgroup holds whole rows");
   __shared__ f32x2 slots[2][W];                    // a wavefront's mean and sum of squares
   __shared__ float columns[W];                     // and its columns of a row
-  const Cols k(j.cols);
+  const Cols k(j.cols, j.rows);
   const int lane = threadIdx.x % G, wave = threadIdx.x / 64;
   const float inv = 1.f / (float)k.n;
 
@@ -268,10 +282,11 @@ __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(No
   auto fetch = [&](int64_t r) {
     const T* px = row_of<T>(j.x, r);
     const T* pr = RES ? row_of<T>(j.r, r) : nullptr;
+    const bool edge = r >= k.edge;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      x[c] = load_chunk<F>(px, c * G + lane, k);
-      if constexpr (RES) res[c] = load_chunk<F>(pr, c * G + lane, k);
+      x[c] = load_chunk<F>(px, c * G + lane, k, edge, c < CH / 2);
+      if constexpr (RES) res[c] = load_chunk<F>(pr, c * G + lane, k, edge, c < CH / 2);
     }
   };
   const int64_t stride = (int64_t)gridDim.x * RPB;
@@ -285,8 +300,8 @@ __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(No
     const int q = c * G + lane;
 #pragma unroll
     for (int i = 0; i < 8; ++i) g[slot][i] = 1.f, b[slot][i] = 0.f;
-    if (j.gamma) chunk_values<F>(load_chunk<F>(j.gamma, q, k), q, k, g[slot]);
-    if (j.beta) chunk_values<F>(load_chunk<F>(j.beta, q, k), q, k, b[slot]);
+    if (j.gamma) vector_values<F>(j.gamma, q, k, g[slot], c < CH / 2);
+    if (j.beta) vector_values<F>(j.beta, q, k, b[slot], c < CH / 2);
   };
   if constexpr (HOIST)
     for (int c = 0; c < CH; ++c) weights(c, c);
@@ -301,6 +316,7 @@ __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(No
   int flip = 0;
   for (; r < j.rows; r += stride) {
     if constexpr (!AHEAD) fetch(r);
+    const bool edge = r >= k.edge;
     float v[CH][8];
     float sum = 0.f;
     if constexpr (RES) {
@@ -312,23 +328,23 @@ __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(No
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
         const int q = c * G + lane;
-        chunk_values<F>(x[c], q, k, v[c]);
+        chunk_values<F>(x[c], q, k, edge, v[c], c < CH / 2);
         if (!AHEAD && j.d.thr) n[c] = chunk_numbers(j.d, step, j.d.row0 + r, q);
         if (j.d.thr) drop_values(j.d, n[c], v[c]);
         float t[8];
-        chunk_values<F>(res[c], q, k, t);
+        chunk_values<F>(res[c], q, k, edge, t, c < CH / 2);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[c][i] += t[i];
       }
     } else {
 #pragma unroll
-      for (int c = 0; c < CH; ++c) chunk_values<F>(x[c], c * G + lane, k, v[c]);
+      for (int c = 0; c < CH; ++c) chunk_values<F>(x[c], c * G + lane, k, edge, v[c], c < CH / 2);
     }
     if (AHEAD && r + stride < j.rows) fetch(r + stride);
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       if constexpr (RES)
-        if (j.s.p) store_chunk<F>(out_row<T>(j.s, r), c * G + lane, k, v[c]);
+        if (j.s.p) store_chunk<F>(out_row<T>(j.s, r), c * G + lane, k, v[c], c < CH / 2);
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum += v[c][i];
     }
@@ -340,7 +356,7 @@ __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(No
       const int left = k.n - 8 * (c * G + lane);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float d = F == kExact || i < left ? v[c][i] - mean : 0.f;
+        const float d = F == kExact || c < CH / 2 || i < left ? v[c][i] - mean : 0.f;
         sq = fmaf(d, d, sq);
       }
     }
@@ -370,7 +386,7 @@ __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(No
       float y[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) y[i] = fmaf((v[c][i] - mean) * rs, g[at][i], b[at][i]);
-      store_chunk<F>(out_row<T>(j.y, r), c * G + lane, k, y);
+      store_chunk<F>(out_row<T>(j.y, r), c * G + lane, k, y, c < CH / 2);
     }
   }
 }
@@ -394,24 +410,38 @@ __device__ __forceinline__ float stride_sum(float v) {
   return v;
 }
 
-// Rows as in the forward, one pass: both row sums and the weights' gradients
-// come from the same registers.  A thread keeps its columns' two sums over all
-// of its rows; at the end the workgroup's rows of threads meet in LDS and leave
-// one partial pair of float32 rows (2 x cols at j.part), or the result itself
-// where the grid is one workgroup.
-template <typename T, bool RES, int G, int CH, int NT, Form F>
-__global__ __launch_bounds__(NT) void k_norm_backward(NormJob j) {
+// Rows first, first + stride, ... as in the forward, one pass.  ACC: a thread
+// also adds its columns' terms of the weights' gradients to ag and ab.  Four
+// chunks a lane are too many registers to keep beside those: such rows are read
+// again (from the L2) after their sums.
+template <typename T, bool RES, int G, int CH, Form F, bool ACC>
+__device__ __forceinline__ void backward_rows(const NormJob& j, int64_t r, int64_t stride, float (&ag)[CH][8],
+                                              float (&ab)[CH][8]) {
   constexpr int W = G > 64 ? G / 64 : 1;
-  constexpr int NW = NT / 64;
-  constexpr int RPB = NT / G;
   constexpr int GL = G < 64 ? G : 64;
-  constexpr bool HOIST = G <= 64;
-  static_assert(G <= 64 || G == NT, "a workgroup holds whole rows");
+  constexpr bool AHEAD = G < 1024, AGAIN = CH > 2, HOIST = !AGAIN;
+  static_assert(!(AHEAD && AGAIN), "a row that is read again is not loaded early");
   __shared__ f32x2 slots[2][W];
-  __shared__ float sums[W > 1 ? 1 : NW][W > 1 ? 1 : GL * 8];
-  const Cols k(j.cols);
+  const Cols k(j.cols, j.rows);
   const int lane = threadIdx.x % G, wave = threadIdx.x / 64;
   const float inv = 1.f / (float)k.n;
+  const bool add = RES && j.ds.p, drop = RES && j.dx.p && j.d.thr;
+
+  Raw<T> xr[CH], yr[CH], sr[CH];
+  f32x2 st = {0.f, 0.f};
+  auto fetch = [&](int64_t r) {
+    st = *(const f32x2*)(j.stats + 2 * r);
+    const bool edge = r >= k.edge;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int q = c * G + lane;
+      xr[c] = load_chunk<F>(row_of<T>(j.v, r), q, k, edge, c < CH / 2);
+      yr[c] = load_chunk<F>(row_of<T>(j.dy, r), q, k, edge, c < CH / 2);
+      if constexpr (RES)
+        if (add) sr[c] = load_chunk<F>(row_of<T>(j.ds, r), q, k, edge, c < CH / 2);
+    }
+  };
+  if (AHEAD && r < j.rows) fetch(r);
   uint32_t step = 0;
   if constexpr (RES) step = step_of(j.d);
 
@@ -420,42 +450,50 @@ __global__ __launch_bounds__(NT) void k_norm_backward(NormJob j) {
     const int q = c * G + lane;
 #pragma unroll
     for (int i = 0; i < 8; ++i) gm[slot][i] = 1.f;
-    if (j.gamma) chunk_values<F>(load_chunk<F>(j.gamma, q, k), q, k, gm[slot]);
+    if (j.gamma) vector_values<F>(j.gamma, q, k, gm[slot], c < CH / 2);
   };
   if constexpr (HOIST)
     for (int c = 0; c < CH; ++c) weights(c, c);
-  float ag[CH][8] = {}, ab[CH][8] = {};
 
   int flip = 0;
-  for (int64_t r = (int64_t)blockIdx.x * RPB + group_of_thread<G>(); r < j.rows; r += (int64_t)gridDim.x * RPB) {
-    Raw<T> xr[CH], yr[CH], sr[CH];
-    const f32x2 st = *(const f32x2*)(j.stats + 2 * r);
+  for (; r < j.rows; r += stride) {
+    if constexpr (!AHEAD && !AGAIN) fetch(r);
+    if constexpr (AGAIN) st = *(const f32x2*)(j.stats + 2 * r);
+    Numbers n[CH];
+    if (AHEAD && drop) {                             // beside the row's loads
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      const int q = c * G + lane;
-      xr[c] = load_chunk<F>(row_of<T>(j.v, r), q, k);
-      yr[c] = load_chunk<F>(row_of<T>(j.dy, r), q, k);
-      if constexpr (RES)
-        if (j.ds.p) sr[c] = load_chunk<F>(row_of<T>(j.ds, r), q, k);
+      for (int c = 0; c < CH; ++c) n[c] = chunk_numbers(j.d, step, j.d.row0 + r, c * G + lane);
     }
-    float h[CH][8], g[CH][8];
+    const float mean = st[0], rs = st[1];
+    const bool edge = r >= k.edge;
+    Raw<T> sc[CH];
+    float h[AGAIN ? 1 : CH][8], g[AGAIN ? 1 : CH][8];
     float sg = 0.f, sgh = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      const int q = c * G + lane, at = HOIST ? c : 0;
-      if constexpr (!HOIST) weights(c, 0);
-      chunk_values<F>(xr[c], q, k, h[c]);
-      chunk_values<F>(yr[c], q, k, g[c]);
+      const int q = c * G + lane, at = AGAIN ? 0 : c;
+      if constexpr (AGAIN) {
+        __builtin_amdgcn_sched_barrier(0);           // one chunk's registers at a time
+        weights(c, 0);
+        xr[c] = load_chunk<F>(row_of<T>(j.v, r), q, k, edge, c < CH / 2);
+        yr[c] = load_chunk<F>(row_of<T>(j.dy, r), q, k, edge, c < CH / 2);
+      }
+      chunk_values<F>(xr[c], q, k, edge, h[at], c < CH / 2);
+      chunk_values<F>(yr[c], q, k, edge, g[at], c < CH / 2);
+      if constexpr (RES && !AGAIN) sc[c] = sr[c];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        h[c][i] = (h[c][i] - st[0]) * st[1];
-        ag[c][i] = fmaf(g[c][i], h[c][i], ag[c][i]);
-        ab[c][i] += g[c][i];
-        g[c][i] *= gm[at][i];
-        sg += g[c][i];
-        sgh = fmaf(g[c][i], h[c][i], sgh);
+        h[at][i] = (h[at][i] - mean) * rs;
+        if constexpr (ACC) {
+          ag[c][i] = fmaf(g[at][i], h[at][i], ag[c][i]);
+          ab[c][i] += g[at][i];
+        }
+        g[at][i] *= gm[HOIST ? c : 0][i];
+        sg += g[at][i];
+        sgh = fmaf(g[at][i], h[at][i], sgh);
       }
     }
+    if (AHEAD && r + stride < j.rows) fetch(r + stride);
     sg = group_sum<GL>(sg);
     sgh = group_sum<GL>(sgh);
     if constexpr (W > 1) {
@@ -472,29 +510,58 @@ __global__ __launch_bounds__(NT) void k_norm_backward(NormJob j) {
     const float mg = sg * inv, mgh = sgh * inv;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      const int q = c * G + lane;
+      const int q = c * G + lane, at = AGAIN ? 0 : c;
+      if constexpr (AGAIN) {
+        __builtin_amdgcn_sched_barrier(0);
+        weights(c, 0);
+        chunk_values<F>(load_chunk<F>(row_of<T>(j.v, r), q, k, edge, c < CH / 2), q, k, edge, h[0], c < CH / 2);
+        chunk_values<F>(load_chunk<F>(row_of<T>(j.dy, r), q, k, edge, c < CH / 2), q, k, edge, g[0], c < CH / 2);
+        if constexpr (RES)
+          if (add) sc[c] = load_chunk<F>(row_of<T>(j.ds, r), q, k, edge, c < CH / 2);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          h[0][i] = (h[0][i] - mean) * rs;
+          g[0][i] *= gm[0][i];
+        }
+      }
       float d[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) d[i] = st[1] * (g[c][i] - mg - h[c][i] * mgh);
+      for (int i = 0; i < 8; ++i) d[i] = rs * (g[at][i] - mg - h[at][i] * mgh);
       if constexpr (RES) {
-        if (j.ds.p) {
+        if (add) {
           float t[8];
-          chunk_values<F>(sr[c], q, k, t);
+          chunk_values<F>(sc[c], q, k, edge, t, c < CH / 2);
 #pragma unroll
           for (int i = 0; i < 8; ++i) d[i] += t[i];
         }
       }
-      if (j.dr.p) store_chunk<F>(out_row<T>(j.dr, r), q, k, d);
+      if (j.dr.p) store_chunk<F>(out_row<T>(j.dr, r), q, k, d, c < CH / 2);
       if constexpr (RES) {
         if (j.dx.p) {
-          if (j.d.thr) drop_values(j.d, chunk_numbers(j.d, step, j.d.row0 + r, q), d);
-          store_chunk<F>(out_row<T>(j.dx, r), q, k, d);
+          if (!AHEAD && drop) n[c] = chunk_numbers(j.d, step, j.d.row0 + r, q);
+          if (drop) drop_values(j.d, n[c], d);
+          store_chunk<F>(out_row<T>(j.dx, r), q, k, d, c < CH / 2);
         }
       }
     }
   }
+}
 
-  if (!j.dgamma && !j.dbeta) return;
+// Many rows: rows and weights' gradients from the same registers.  At the end
+// the workgroup's rows of threads meet in LDS and leave one partial pair of
+// float32 rows (2 x cols at j.part), or the result itself where the grid is
+// one workgroup.
+template <typename T, bool RES, int G, int CH, int NT, Form F>
+__global__ __launch_bounds__(NT) void k_norm_backward(NormJob j) {
+  constexpr int NW = NT / 64, RPB = NT / G;
+  constexpr int GL = G < 64 ? G : 64;
+  static_assert(G <= 64 || G == NT, "a workgroup holds whole rows");
+  __shared__ float sums[G > 64 ? 1 : NW][G > 64 ? 1 : GL * 8];
+  float ag[CH][8] = {}, ab[CH][8] = {};
+  backward_rows<T, RES, G, CH, F, true>(j, (int64_t)blockIdx.x * RPB + group_of_thread<G>(),
+                                        (int64_t)gridDim.x * RPB, ag, ab);
+  const Cols k(j.cols, j.rows);
+  const int lane = threadIdx.x % G, wave = threadIdx.x / 64;
   float* const out[2] = {gridDim.x == 1 ? j.dgamma : j.part + (int64_t)(2 * blockIdx.x) * k.n,
                          gridDim.x == 1 ? j.dbeta : j.part + (int64_t)(2 * blockIdx.x + 1) * k.n};
 #pragma unroll
@@ -503,8 +570,8 @@ __global__ __launch_bounds__(NT) void k_norm_backward(NormJob j) {
     for (int a = 0; a < 2; ++a) {
       float* const dst = out[a];
       float(&acc)[8] = a == 0 ? ag[c] : ab[c];
-      if constexpr (W > 1) {
-        if (dst) store_chunk<F>(dst, c * G + lane, k, acc);
+      if constexpr (G > 64) {
+        if (dst) store_chunk<F>(dst, c * G + lane, k, acc, c < CH / 2);
       } else {
         if constexpr (GL < 64)
           for (int i = 0; i < 8; ++i) acc[i] = stride_sum<GL>(acc[i]);
@@ -528,26 +595,104 @@ __global__ __launch_bounds__(NT) void k_norm_backward(NormJob j) {
   }
 }
 
-// The partial pairs summed: a workgroup takes 64 of the 2 x cols columns, each
-// of its wavefronts every kSlices-th part; the wavefronts' sums meet in LDS.
-constexpr int kSlices = 16;
-__global__ __launch_bounds__(64 * kSlices) void k_norm_reduce(NormJob j, int parts) {
-  __shared__ float sums[kSlices][64];
-  const int lane = threadIdx.x % 64, slice = threadIdx.x / 64;
+// Chunks of the columns that a workgroup of backward_columns takes.
+constexpr int column_lanes(int G) { return G > 64 ? 8 : 4; }
+
+// Few rows: the first workgroups take 32 columns of the weights' gradients each
+// over all rows (64 of wide rows), the others the rows; x and dy are read twice
+// (the second time from a cache), but nothing has to meet between workgroups.
+template <typename T, int NT, int LC, Form F>
+__device__ __forceinline__ void backward_columns(const NormJob& j, int block) {
+  constexpr int NW = NT / 64, SL = NT / LC, U = sizeof(T) == 2 && LC == 4 ? 8 : 4;
+  __shared__ float sums[NW][2][8 * LC];
+  const Cols k(j.cols, j.rows);
+  const int lane = threadIdx.x % LC, q = block * LC + lane;
+  float acc[2][8] = {};
+  for (int64_t r = threadIdx.x / LC; r < j.rows; r += U * SL) {
+    Raw<T> x[U], y[U];
+    f32x2 st[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t ru = r + u * SL;
+      if (ru < j.rows) {
+        st[u] = *(const f32x2*)(j.stats + 2 * ru);
+        x[u] = load_chunk<F>(row_of<T>(j.v, ru), q, k, ru >= k.edge);
+        y[u] = load_chunk<F>(row_of<T>(j.dy, ru), q, k, ru >= k.edge);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t ru = r + u * SL;
+      if (ru < j.rows) {
+        float h[8], d[8];
+        chunk_values<F>(x[u], q, k, ru >= k.edge, h);
+        chunk_values<F>(y[u], q, k, ru >= k.edge, d);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          acc[0][i] = fmaf(d[i], (h[i] - st[u][0]) * st[u][1], acc[0][i]);
+          acc[1][i] += d[i];
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int a = 0; a < 2; ++a) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[a][i] = stride_sum<LC>(acc[a][i]);
+    if (threadIdx.x % 64 < LC) {
+      *(f32x4*)&sums[threadIdx.x / 64][a][lane * 8] = f32x4{acc[a][0], acc[a][1], acc[a][2], acc[a][3]};
+      *(f32x4*)&sums[threadIdx.x / 64][a][lane * 8 + 4] = f32x4{acc[a][4], acc[a][5], acc[a][6], acc[a][7]};
+    }
+  }
+  __syncthreads();
+  const int a = threadIdx.x / (8 * LC), i = threadIdx.x % (8 * LC), col = block * 8 * LC + i;
+  if (a < 2 && col < k.n) {
+    float* const dst = a == 0 ? j.dgamma : j.dbeta;
+    float t = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) t += sums[w][a][i];
+    if (dst) dst[col] = t;
+  }
+}
+
+template <typename T, bool RES, int G, int CH, int NT, Form F>
+__global__ __launch_bounds__(NT) void k_norm_backward_split(NormJob j, int col_blocks) {
+  constexpr int RPB = NT / G;
+  constexpr int LC = column_lanes(G);
+  constexpr Form FC = F == kExact && G * CH % LC != 0 ? (G == 1 ? kSmall : kRagged) : F;
+  if ((int)blockIdx.x < col_blocks) {
+    backward_columns<T, NT, LC, FC>(j, blockIdx.x);
+  } else {
+    float none[CH][8];
+    backward_rows<T, RES, G, CH, F, false>(j, (int64_t)(blockIdx.x - col_blocks) * RPB + group_of_thread<G>(),
+                                           (int64_t)(gridDim.x - col_blocks) * RPB, none, none);
+  }
+}
+
+// The partial pairs summed: a workgroup takes RC of the 2 x cols columns, each
+// group of RC lanes every (kReduceThreads / RC)-th part; the groups meet in the
+// wavefront, the wavefronts in LDS, always in the same order.
+constexpr int kReduceThreads = 1024;
+template <int RC>
+__global__ __launch_bounds__(kReduceThreads) void k_norm_reduce(NormJob j, int parts) {
+  constexpr int slices = kReduceThreads / RC, waves = kReduceThreads / 64;
+  __shared__ float sums[waves][RC];
+  const int lane = threadIdx.x % RC, slice = threadIdx.x / RC;
   const int64_t pitch = 2 * (int64_t)j.cols;
-  const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+  const int64_t c = (int64_t)blockIdx.x * RC + lane;
   float t = 0.f;
   if (c < pitch) {
     const float* p = j.part + c;
 #pragma unroll 8
-    for (int i = slice; i < parts; i += kSlices) t += p[i * pitch];
+    for (int i = slice; i < parts; i += slices) t += p[i * pitch];
   }
-  sums[slice][lane] = t;
+  if constexpr (RC < 64) t = stride_sum<RC>(t);
+  if (threadIdx.x % 64 < RC) sums[threadIdx.x / 64][lane] = t;
   __syncthreads();
   if (slice == 0 && c < pitch) {
     t = 0.f;
 #pragma unroll
-    for (int s = 0; s < kSlices; ++s) t += sums[s][lane];
+    for (int w = 0; w < waves; ++w) t += sums[w][lane];
     float* const dst = c < j.cols ? j.dgamma : j.dbeta;
     if (dst) dst[c < j.cols ? c : c - j.cols] = t;
   }
@@ -586,40 +731,85 @@ hipError_t forward_wide(const NormJob& j, hipStream_t st) {
   return j.rows <= 1024 ? forward_with<T, RES, G, CH, true>(j, st) : forward_with<T, RES, G, CH, false>(j, st);
 }
 
-// threads of a workgroup of the backward, and its rows at a time
+// threads of a workgroup of the backward
 constexpr int backward_threads(int G) { return G > 512 ? G : 512; }
 
-// Lanes per row of a width (G of the kernels).
-int lanes_for(int cols) {
+// Rows up to which a backward pass reads x and dy twice in one launch instead of
+// leaving partial sums to a second one.  The columns' workgroups take a time
+// that grows with the rows; the second launch costs about 4 us, and writing and
+// reading the partial sums most for wide rows.  Both ways: 920 x 656 float32
+// 7.2 us against 7.8, 473 x 736 bf16 5.6 against 7.9; 1190 x 1388 float32 15.4
+// either way, 286 x 3791 7.8 against 11.5, 1010 x 7164 bf16 14.1 against 20.1.
+constexpr int kFew = 1024, kFewWide = 1536;
+
+// How a backward pass over rows x cols runs.
+struct BackwardPlan {
+  int lanes;             // G of the kernels
+  int parts;             // workgroups of k_norm_backward (0: k_norm_backward_split)
+  int col_blocks, row_blocks;   // of k_norm_backward_split
+};
+
+BackwardPlan backward_plan(int64_t rows, int cols, bool weights) {
   const int per = (cols + 7) / 8;
-  for (int g = 1; g <= 64; g *= 2)
-    if (per <= g) return g;
-  if (per <= 128) return 64;
-  return per <= 1024 ? 512 : 1024;
+  BackwardPlan p{};
+  for (p.lanes = 1; p.lanes < 64 && p.lanes < per; p.lanes *= 2) {}
+  if (per > 128) p.lanes = per <= 1024 ? 512 : 1024;
+  const int nt = backward_threads(p.lanes), rpb = nt / p.lanes;
+  const int64_t blocks = (rows + rpb - 1) / rpb;
+  if (weights && blocks == 1) {
+    p.parts = 1;
+  } else if (weights && rows > (per > 128 ? kFewWide : kFew)) {
+    const int64_t rounds = (blocks + 255) / 256;     // rows dealt out evenly to a workgroup a CU
+    p.parts = (int)((blocks + rounds - 1) / rounds);
+  } else {
+    p.col_blocks = weights ? (per + column_lanes(p.lanes) - 1) / column_lanes(p.lanes) : 0;
+    p.row_blocks = (int)std::min<int64_t>(blocks, 16384);
+  }
+  return p;
 }
 
 template <typename T, bool RES, int G, int CH>
-hipError_t backward_with(const NormJob& j, int parts, hipStream_t st) {
+hipError_t backward_with(const NormJob& j, const BackwardPlan& p, hipStream_t st) {
   constexpr int nt = backward_threads(G);
   constexpr Form other = G == 1 ? kSmall : kRagged;
-  if (j.cols == 8 * G * CH) hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, kExact>), dim3(parts), dim3(nt), 0, st, j);
-  else hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, other>), dim3(parts), dim3(nt), 0, st, j);
+  const bool exact = j.cols == 8 * G * CH;
+  if (p.parts > 0) {
+    if (exact) hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, kExact>), dim3(p.parts), dim3(nt), 0, st, j);
+    else hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, other>), dim3(p.parts), dim3(nt), 0, st, j);
+    return hipGetLastError();
+  }
+  auto run = [&](int col_blocks, int row_blocks) {
+    const dim3 grid(col_blocks + row_blocks);
+    if (grid.x == 0) return;
+    if (exact)
+      hipLaunchKernelGGL((k_norm_backward_split<T, RES, G, CH, nt, kExact>), grid, dim3(nt), 0, st, j, col_blocks);
+    else
+      hipLaunchKernelGGL((k_norm_backward_split<T, RES, G, CH, nt, other>), grid, dim3(nt), 0, st, j, col_blocks);
+  };
+  const int row_blocks = j.dr.p || j.dx.p ? p.row_blocks : 0;
+  auto over = [&](const Mat& m) { return m.p && (m.p == j.dy.p || m.p == j.v.p); };
+  if (row_blocks > 0 && (over(j.dr) || over(j.dx))) {   // in place: the columns first
+    run(p.col_blocks, 0);
+    run(0, row_blocks);
+  } else {
+    run(p.col_blocks, row_blocks);
+  }
   return hipGetLastError();
 }
 
 template <typename T, bool RES>
-hipError_t backward(const NormJob& j, int parts, hipStream_t st) {
+hipError_t backward(const NormJob& j, const BackwardPlan& p, hipStream_t st) {
   const int per = (j.cols + 7) / 8;
-  switch (lanes_for(j.cols)) {
-    case 1: return backward_with<T, RES, 1, 1>(j, parts, st);
-    case 2: return backward_with<T, RES, 2, 1>(j, parts, st);
-    case 4: return backward_with<T, RES, 4, 1>(j, parts, st);
-    case 8: return backward_with<T, RES, 8, 1>(j, parts, st);
-    case 16: return backward_with<T, RES, 16, 1>(j, parts, st);
-    case 32: return backward_with<T, RES, 32, 1>(j, parts, st);
-    case 64: return per <= 64 ? backward_with<T, RES, 64, 1>(j, parts, st) : backward_with<T, RES, 64, 2>(j, parts, st);
-    case 512: return per <= 512 ? backward_with<T, RES, 512, 1>(j, parts, st) : backward_with<T, RES, 512, 2>(j, parts, st);
-    default: return per <= 2048 ? backward_with<T, RES, 1024, 2>(j, parts, st) : backward_with<T, RES, 1024, 4>(j, parts, st);
+  switch (p.lanes) {
+    case 1: return backward_with<T, RES, 1, 1>(j, p, st);
+    case 2: return backward_with<T, RES, 2, 1>(j, p, st);
+    case 4: return backward_with<T, RES, 4, 1>(j, p, st);
+    case 8: return backward_with<T, RES, 8, 1>(j, p, st);
+    case 16: return backward_with<T, RES, 16, 1>(j, p, st);
+    case 32: return backward_with<T, RES, 32, 1>(j, p, st);
+    case 64: return per <= 64 ? backward_with<T, RES, 64, 1>(j, p, st) : backward_with<T, RES, 64, 2>(j, p, st);
+    case 512: return per <= 512 ? backward_with<T, RES, 512, 1>(j, p, st) : backward_with<T, RES, 512, 2>(j, p, st);
+    default: return per <= 2048 ? backward_with<T, RES, 1024, 2>(j, p, st) : backward_with<T, RES, 1024, 4>(j, p, st);
   }
 }
 
@@ -643,13 +833,9 @@ hipError_t forward(const NormJob& j, hipStream_t st) {
 
 }  // namespace
 
-// One round of resident workgroups (two of 512 threads a CU, or one of 1024),
-// the rows dealt out evenly.
 int norm_parts(int64_t rows, int cols) {
-  const int g = lanes_for(cols), nt = backward_threads(g), rpb = nt / g;
-  const int64_t blocks = (rows + rpb - 1) / rpb, resident = 256 * (1024 / nt);
-  const int64_t rounds = (blocks + resident - 1) / resident;
-  return rounds ? (int)((blocks + rounds - 1) / rounds) : 0;
+  const BackwardPlan p = backward_plan(rows, cols, true);
+  return p.parts > 0 ? p.parts : 1;
 }
 
 template <typename T>
@@ -675,18 +861,19 @@ hipError_t launch_norm_forward(Elt e, const NormJob& j, hipStream_t st) {
 }
 
 hipError_t launch_norm_backward(Elt e, const NormJob& j, hipStream_t st) {
-  const int parts = norm_parts(j.rows, j.cols);
-  const bool residual = j.ds.p || j.dx.p || j.d.thr;
-  hipError_t err = hipSuccess;
-  if (parts > 0) {
-    if (e == BF16) err = residual ? backward<uint16_t, true>(j, parts, st) : backward<uint16_t, false>(j, parts, st);
-    else err = residual ? backward<float, true>(j, parts, st) : backward<float, false>(j, parts, st);
-  }
-  if (err == hipSuccess && parts != 1 && (j.dgamma || j.dbeta)) {
-    hipLaunchKernelGGL(k_norm_reduce, dim3((j.cols + 31) / 32), dim3(64 * kSlices), 0, st, j, parts);
-    err = hipGetLastError();
-  }
-  return err;
+  const bool weights = j.dgamma || j.dbeta, residual = j.ds.p || j.dx.p;
+  const BackwardPlan p = backward_plan(j.rows, j.cols, weights);
+  hipError_t err;
+  if (e == BF16) err = residual ? backward<uint16_t, true>(j, p, st) : backward<uint16_t, false>(j, p, st);
+  else err = residual ? backward<float, true>(j, p, st) : backward<float, false>(j, p, st);
+  const int parts = p.parts;
+  if (err != hipSuccess || parts <= 1) return err;
+  // 64 columns a workgroup once they fill the CUs, else 16
+  if (2 * j.cols > 256 * 16)
+    hipLaunchKernelGGL((k_norm_reduce<64>), dim3((2 * j.cols + 63) / 64), dim3(kReduceThreads), 0, st, j, parts);
+  else
+    hipLaunchKernelGGL((k_norm_reduce<16>), dim3((2 * j.cols + 15) / 16), dim3(kReduceThreads), 0, st, j, parts);
+  return hipGetLastError();
 }
 
 }  // namespace vfl
