@@ -256,26 +256,26 @@ __device__ __forceinline__ int group_of_thread() {
 }
 
 // ------------------------------------------------------------------ forward
-// G lanes hold a row, CH chunks each (chunk c * G + lane); a workgroup of
-// max(kThreads, G) threads holds kThreads / G rows, or one.  The next row's
-// loads are in flight while a row is worked on.  Mean and variance in two sums
-// over the registers.  Where a row spans W = G / 64 wavefronts, each forms its
-// own mean and sum of squares, and these meet in LDS: with n_w, m_w, M_w of
-// wavefront w, the row's sum of squares is the sum of M_w + n_w (m_w -
-// mean)^2, which takes one barrier a row (the slots alternate) and loses
-// nothing to cancellation.  HOIST: a thread's gamma and beta are loaded before
+// Up to G = 64 lanes hold a row, CH chunks each (chunk c * G + lane), and a
+// workgroup kThreads / G rows; wider rows (G = 512 or 1024) take a workgroup of
+// as many wavefronts as they fill, G threads at most.  The next row's loads are
+// in flight while a row is worked on.  Mean and variance in two sums over the
+// registers.  Where a row spans several wavefronts, each forms its own mean and
+// sum of squares, and these meet in LDS: with n_w, m_w, M_w of wavefront w, the
+// row's sum of squares is the sum of M_w + n_w (m_w - mean)^2, which takes one
+// barrier a row (the slots alternate) and loses nothing to cancellation.  HOIST: a thread's gamma and beta are loaded before
 // its first row and kept.
 template <typename T, bool RES, int G, int CH, Form F, bool HOIST>
 __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(NormJob j) {
-  constexpr int W = G > 64 ? G / 64 : 1;
-  constexpr int RPB = G > 64 ? 1 : kThreads / G;
+  constexpr bool WIDE = G > 64;
+  constexpr int RPB = WIDE ? 1 : kThreads / G;
   constexpr int GL = G < 64 ? G : 64;
   constexpr bool AHEAD = G < 1024;                 // the next row is loaded early
-  static_assert(G <= 64 || G >= kThreads, "a workgroup holds whole rows");
-  __shared__ f32x2 slots[2][W];                    // a wavefront's mean and sum of squares
-  __shared__ float columns[W];                     // and its columns of a row
+  __shared__ f32x2 slots[2][WIDE ? 16 : 1];        // a wavefront's mean and sum of squares
+  __shared__ float columns[WIDE ? 16 : 1];         // and its columns of a row
   const Cols k(j.cols, j.rows);
-  const int lane = threadIdx.x % G, wave = threadIdx.x / 64;
+  const int lanes = WIDE ? (int)blockDim.x : G;
+  const int lane = WIDE ? (int)threadIdx.x : threadIdx.x % G, wave = threadIdx.x / 64;
   const float inv = 1.f / (float)k.n;
 
   Raw<T> x[CH], res[CH];
@@ -285,8 +285,8 @@ __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(No
     const bool edge = r >= k.edge;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      x[c] = load_chunk<F>(px, c * G + lane, k, edge, c < CH / 2);
-      if constexpr (RES) res[c] = load_chunk<F>(pr, c * G + lane, k, edge, c < CH / 2);
+      x[c] = load_chunk<F>(px, c * lanes + lane, k, edge, c < CH / 2);
+      if constexpr (RES) res[c] = load_chunk<F>(pr, c * lanes + lane, k, edge, c < CH / 2);
     }
   };
   const int64_t stride = (int64_t)gridDim.x * RPB;
@@ -297,7 +297,7 @@ __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(No
 
   float g[HOIST ? CH : 1][8], b[HOIST ? CH : 1][8];
   auto weights = [&](int c, int slot) {
-    const int q = c * G + lane;
+    const int q = c * lanes + lane;
 #pragma unroll
     for (int i = 0; i < 8; ++i) g[slot][i] = 1.f, b[slot][i] = 0.f;
     if (j.gamma) vector_values<F>(j.gamma, q, k, g[slot], c < CH / 2);
@@ -306,9 +306,9 @@ __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(No
   if constexpr (HOIST)
     for (int c = 0; c < CH; ++c) weights(c, c);
   float nw = 0.f;
-  if constexpr (W > 1) {
+  if constexpr (WIDE) {
 #pragma unroll
-    for (int c = 0; c < CH; ++c) nw += (float)min(max(k.n - 8 * (c * G + 64 * wave), 0), 512);
+    for (int c = 0; c < CH; ++c) nw += (float)min(max(k.n - 8 * (c * lanes + 64 * wave), 0), 512);
     if (threadIdx.x % 64 == 0) columns[wave] = nw;   // read past the first row's barrier
   }
   const float inv_nw = nw > 0.f ? 1.f / nw : 0.f;
@@ -323,11 +323,11 @@ __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(No
       Numbers n[CH];
       if (AHEAD && j.d.thr) {                        // beside the row's loads
 #pragma unroll
-        for (int c = 0; c < CH; ++c) n[c] = chunk_numbers(j.d, step, j.d.row0 + r, c * G + lane);
+        for (int c = 0; c < CH; ++c) n[c] = chunk_numbers(j.d, step, j.d.row0 + r, c * lanes + lane);
       }
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
-        const int q = c * G + lane;
+        const int q = c * lanes + lane;
         chunk_values<F>(x[c], q, k, edge, v[c], c < CH / 2);
         if (!AHEAD && j.d.thr) n[c] = chunk_numbers(j.d, step, j.d.row0 + r, q);
         if (j.d.thr) drop_values(j.d, n[c], v[c]);
@@ -338,22 +338,22 @@ __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(No
       }
     } else {
 #pragma unroll
-      for (int c = 0; c < CH; ++c) chunk_values<F>(x[c], c * G + lane, k, edge, v[c], c < CH / 2);
+      for (int c = 0; c < CH; ++c) chunk_values<F>(x[c], c * lanes + lane, k, edge, v[c], c < CH / 2);
     }
     if (AHEAD && r + stride < j.rows) fetch(r + stride);
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       if constexpr (RES)
-        if (j.s.p) store_chunk<F>(out_row<T>(j.s, r), c * G + lane, k, v[c], c < CH / 2);
+        if (j.s.p) store_chunk<F>(out_row<T>(j.s, r), c * lanes + lane, k, v[c], c < CH / 2);
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum += v[c][i];
     }
     sum = group_sum<GL>(sum);
-    float mean = sum * (W > 1 ? inv_nw : inv);
+    float mean = sum * (WIDE ? inv_nw : inv);
     float sq = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      const int left = k.n - 8 * (c * G + lane);
+      const int left = k.n - 8 * (c * lanes + lane);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float d = F == kExact || c < CH / 2 || i < left ? v[c][i] - mean : 0.f;
@@ -361,20 +361,17 @@ __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(No
       }
     }
     sq = group_sum<GL>(sq);
-    if constexpr (W > 1) {
+    if constexpr (WIDE) {
       if (threadIdx.x % 64 == 0) slots[flip][wave] = f32x2{mean, sq};
       __syncthreads();
-      sum = 0.f;
-#pragma unroll
-      for (int w = 0; w < W; ++w) sum = fmaf(columns[w], slots[flip][w][0], sum);
-      mean = sum * inv;
-      sq = 0.f;
-#pragma unroll
-      for (int w = 0; w < W; ++w) {
-        const f32x2 s = slots[flip][w];
-        const float d = s[0] - mean;
-        sq += fmaf(columns[w] * d, d, s[1]);
-      }
+      // every 16 lanes add the wavefronts' values, a lane each
+      const int w = threadIdx.x % 16;
+      const bool has = 64 * w < lanes;
+      const f32x2 s = has ? slots[flip][w] : f32x2{0.f, 0.f};
+      const float n = has ? columns[w] : 0.f;
+      mean = group_sum<16>(n * s[0]) * inv;
+      const float d = s[0] - mean;
+      sq = group_sum<16>(fmaf(n * d, d, s[1]));
       flip ^= 1;
     }
     const float rs = 1.f / sqrtf(fmaf(sq, inv, j.eps));
@@ -386,7 +383,7 @@ __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(No
       float y[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) y[i] = fmaf((v[c][i] - mean) * rs, g[at][i], b[at][i]);
-      store_chunk<F>(out_row<T>(j.y, r), c * G + lane, k, y, c < CH / 2);
+      store_chunk<F>(out_row<T>(j.y, r), c * lanes + lane, k, y, c < CH / 2);
     }
   }
 }
@@ -411,19 +408,19 @@ __device__ __forceinline__ float stride_sum(float v) {
 }
 
 // Rows first, first + stride, ... as in the forward, one pass.  ACC: a thread
-// also adds its columns' terms of the weights' gradients to ag and ab.  Four
-// chunks a lane are too many registers to keep beside those: such rows are read
-// again (from the L2) after their sums.
+// also adds its columns' terms of the weights' gradients to ag and ab (not with
+// four chunks a lane, which leave no registers for those).
 template <typename T, bool RES, int G, int CH, Form F, bool ACC>
 __device__ __forceinline__ void backward_rows(const NormJob& j, int64_t r, int64_t stride, float (&ag)[CH][8],
                                               float (&ab)[CH][8]) {
-  constexpr int W = G > 64 ? G / 64 : 1;
+  constexpr bool WIDE = G > 64;
   constexpr int GL = G < 64 ? G : 64;
-  constexpr bool AHEAD = G < 1024, AGAIN = CH > 2, HOIST = !AGAIN;
-  static_assert(!(AHEAD && AGAIN), "a row that is read again is not loaded early");
-  __shared__ f32x2 slots[2][W];
+  constexpr bool AHEAD = G < 1024, HOIST = CH <= 2;
+  static_assert(!(ACC && CH > 2), "registers");
+  __shared__ f32x2 slots[2][WIDE ? 16 : 1];
   const Cols k(j.cols, j.rows);
-  const int lane = threadIdx.x % G, wave = threadIdx.x / 64;
+  const int lanes = WIDE ? (int)blockDim.x : G;
+  const int lane = WIDE ? (int)threadIdx.x : threadIdx.x % G;
   const float inv = 1.f / (float)k.n;
   const bool add = RES && j.ds.p, drop = RES && j.dx.p && j.d.thr;
 
@@ -434,7 +431,7 @@ __device__ __forceinline__ void backward_rows(const NormJob& j, int64_t r, int64
     const bool edge = r >= k.edge;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      const int q = c * G + lane;
+      const int q = c * lanes + lane;
       xr[c] = load_chunk<F>(row_of<T>(j.v, r), q, k, edge, c < CH / 2);
       yr[c] = load_chunk<F>(row_of<T>(j.dy, r), q, k, edge, c < CH / 2);
       if constexpr (RES)
@@ -447,7 +444,7 @@ __device__ __forceinline__ void backward_rows(const NormJob& j, int64_t r, int64
 
   float gm[HOIST ? CH : 1][8];
   auto weights = [&](int c, int slot) {
-    const int q = c * G + lane;
+    const int q = c * lanes + lane;
 #pragma unroll
     for (int i = 0; i < 8; ++i) gm[slot][i] = 1.f;
     if (j.gamma) vector_values<F>(j.gamma, q, k, gm[slot], c < CH / 2);
@@ -457,76 +454,55 @@ __device__ __forceinline__ void backward_rows(const NormJob& j, int64_t r, int64
 
   int flip = 0;
   for (; r < j.rows; r += stride) {
-    if constexpr (!AHEAD && !AGAIN) fetch(r);
-    if constexpr (AGAIN) st = *(const f32x2*)(j.stats + 2 * r);
+    if constexpr (!AHEAD) fetch(r);
     Numbers n[CH];
     if (AHEAD && drop) {                             // beside the row's loads
 #pragma unroll
-      for (int c = 0; c < CH; ++c) n[c] = chunk_numbers(j.d, step, j.d.row0 + r, c * G + lane);
+      for (int c = 0; c < CH; ++c) n[c] = chunk_numbers(j.d, step, j.d.row0 + r, c * lanes + lane);
     }
     const float mean = st[0], rs = st[1];
     const bool edge = r >= k.edge;
     Raw<T> sc[CH];
-    float h[AGAIN ? 1 : CH][8], g[AGAIN ? 1 : CH][8];
+    float h[CH][8], g[CH][8];
     float sg = 0.f, sgh = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      const int q = c * G + lane, at = AGAIN ? 0 : c;
-      if constexpr (AGAIN) {
-        __builtin_amdgcn_sched_barrier(0);           // one chunk's registers at a time
-        weights(c, 0);
-        xr[c] = load_chunk<F>(row_of<T>(j.v, r), q, k, edge, c < CH / 2);
-        yr[c] = load_chunk<F>(row_of<T>(j.dy, r), q, k, edge, c < CH / 2);
-      }
-      chunk_values<F>(xr[c], q, k, edge, h[at], c < CH / 2);
-      chunk_values<F>(yr[c], q, k, edge, g[at], c < CH / 2);
-      if constexpr (RES && !AGAIN) sc[c] = sr[c];
+      const int q = c * lanes + lane;
+      if constexpr (!HOIST) weights(c, 0);
+      chunk_values<F>(xr[c], q, k, edge, h[c], c < CH / 2);
+      chunk_values<F>(yr[c], q, k, edge, g[c], c < CH / 2);
+      if constexpr (RES) sc[c] = sr[c];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        h[at][i] = (h[at][i] - mean) * rs;
+        h[c][i] = (h[c][i] - mean) * rs;
         if constexpr (ACC) {
-          ag[c][i] = fmaf(g[at][i], h[at][i], ag[c][i]);
-          ab[c][i] += g[at][i];
+          ag[c][i] = fmaf(g[c][i], h[c][i], ag[c][i]);
+          ab[c][i] += g[c][i];
         }
-        g[at][i] *= gm[HOIST ? c : 0][i];
-        sg += g[at][i];
-        sgh = fmaf(g[at][i], h[at][i], sgh);
+        g[c][i] *= gm[HOIST ? c : 0][i];
+        sg += g[c][i];
+        sgh = fmaf(g[c][i], h[c][i], sgh);
       }
     }
     if (AHEAD && r + stride < j.rows) fetch(r + stride);
     sg = group_sum<GL>(sg);
     sgh = group_sum<GL>(sgh);
-    if constexpr (W > 1) {
-      if (threadIdx.x % 64 == 0) slots[flip][wave] = f32x2{sg, sgh};
+    if constexpr (WIDE) {
+      if (threadIdx.x % 64 == 0) slots[flip][threadIdx.x / 64] = f32x2{sg, sgh};
       __syncthreads();
-      sg = sgh = 0.f;
-#pragma unroll
-      for (int w = 0; w < W; ++w) {
-        sg += slots[flip][w][0];
-        sgh += slots[flip][w][1];
-      }
+      const int w = threadIdx.x % 16;
+      const f32x2 s = 64 * w < lanes ? slots[flip][w] : f32x2{0.f, 0.f};
+      sg = group_sum<16>(s[0]);
+      sgh = group_sum<16>(s[1]);
       flip ^= 1;
     }
     const float mg = sg * inv, mgh = sgh * inv;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      const int q = c * G + lane, at = AGAIN ? 0 : c;
-      if constexpr (AGAIN) {
-        __builtin_amdgcn_sched_barrier(0);
-        weights(c, 0);
-        chunk_values<F>(load_chunk<F>(row_of<T>(j.v, r), q, k, edge, c < CH / 2), q, k, edge, h[0], c < CH / 2);
-        chunk_values<F>(load_chunk<F>(row_of<T>(j.dy, r), q, k, edge, c < CH / 2), q, k, edge, g[0], c < CH / 2);
-        if constexpr (RES)
-          if (add) sc[c] = load_chunk<F>(row_of<T>(j.ds, r), q, k, edge, c < CH / 2);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          h[0][i] = (h[0][i] - mean) * rs;
-          g[0][i] *= gm[0][i];
-        }
-      }
+      const int q = c * lanes + lane;
       float d[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) d[i] = rs * (g[at][i] - mg - h[at][i] * mgh);
+      for (int i = 0; i < 8; ++i) d[i] = rs * (g[c][i] - mg - h[c][i] * mgh);
       if constexpr (RES) {
         if (add) {
           float t[8];
@@ -553,15 +529,14 @@ __device__ __forceinline__ void backward_rows(const NormJob& j, int64_t r, int64
 // one workgroup.
 template <typename T, bool RES, int G, int CH, int NT, Form F>
 __global__ __launch_bounds__(NT) void k_norm_backward(NormJob j) {
-  constexpr int NW = NT / 64, RPB = NT / G;
+  constexpr int NW = NT / 64, RPB = G > 64 ? 1 : NT / G;
   constexpr int GL = G < 64 ? G : 64;
-  static_assert(G <= 64 || G == NT, "a workgroup holds whole rows");
   __shared__ float sums[G > 64 ? 1 : NW][G > 64 ? 1 : GL * 8];
   float ag[CH][8] = {}, ab[CH][8] = {};
   backward_rows<T, RES, G, CH, F, true>(j, (int64_t)blockIdx.x * RPB + group_of_thread<G>(),
                                         (int64_t)gridDim.x * RPB, ag, ab);
   const Cols k(j.cols, j.rows);
-  const int lane = threadIdx.x % G, wave = threadIdx.x / 64;
+  const int lane = G > 64 ? (int)threadIdx.x : threadIdx.x % G, wave = threadIdx.x / 64;
   float* const out[2] = {gridDim.x == 1 ? j.dgamma : j.part + (int64_t)(2 * blockIdx.x) * k.n,
                          gridDim.x == 1 ? j.dbeta : j.part + (int64_t)(2 * blockIdx.x + 1) * k.n};
 #pragma unroll
@@ -571,7 +546,7 @@ __global__ __launch_bounds__(NT) void k_norm_backward(NormJob j) {
       float* const dst = out[a];
       float(&acc)[8] = a == 0 ? ag[c] : ab[c];
       if constexpr (G > 64) {
-        if (dst) store_chunk<F>(dst, c * G + lane, k, acc, c < CH / 2);
+        if (dst) store_chunk<F>(dst, c * (int)blockDim.x + lane, k, acc, c < CH / 2);
       } else {
         if constexpr (GL < 64)
           for (int i = 0; i < 8; ++i) acc[i] = stride_sum<GL>(acc[i]);
@@ -657,7 +632,7 @@ __device__ __forceinline__ void backward_columns(const NormJob& j, int block) {
 
 template <typename T, bool RES, int G, int CH, int NT, Form F>
 __global__ __launch_bounds__(NT) void k_norm_backward_split(NormJob j, int col_blocks) {
-  constexpr int RPB = NT / G;
+  constexpr int RPB = G > 64 ? 1 : NT / G;
   constexpr int LC = column_lanes(G);
   constexpr Form FC = F == kExact && G * CH % LC != 0 ? (G == 1 ? kSmall : kRagged) : F;
   if ((int)blockIdx.x < col_blocks) {
@@ -703,19 +678,31 @@ __global__ __launch_bounds__(kReduceThreads) void k_norm_reduce(NormJob j, int p
 // differ more in time), so that a thread's gamma and beta serve several rows
 // and the next row's loads run beside a row's work: 120291 x 49 bf16 takes 7.8
 // us, 9.3 in two rounds; residual 118955 x 175 bf16 48.5 in two, 52.5 in one.
-// Wider rows are dealt out by the hardware: residual 32768 x 1024 bf16 46.6 us,
-// 48.5 in two rounds.
+// Wider rows are dealt out by the hardware (residual 32768 x 1024 bf16 46.6 us,
+// 48.5 in two rounds) up to 8192 columns, beyond which gamma and beta are too
+// many bytes to read for each row: 2000 x 16384 bf16 28.9
+// us with a workgroup a CU, 38 with one a row.
 constexpr int kResident = 2048, kMany = 16384;
+
+// threads for a row of `per` chunks, CH a thread, that takes several wavefronts
+int wide_threads(int per, int CH) { return (per + 64 * CH - 1) / (64 * CH) * 64; }
+
+// What a kernel of G lanes a row and CH chunks a lane takes for granted: the
+// chunks fit, and the first half of a lane's are whole.
+bool chunks_fit(int per, int lanes, int CH) { return per <= lanes * CH && (CH == 1 || per > lanes * (CH / 2)); }
 
 template <typename T, bool RES, int G, int CH, bool HOIST = G <= 64>
 hipError_t forward_with(const NormJob& j, hipStream_t st) {
-  constexpr int nt = G > kThreads ? G : kThreads;
-  constexpr int rpb = nt / G;
-  constexpr int most = G <= 64 && CH == 1 ? (RES ? 2 * kResident : kResident) : kMany;
+  const int per = (j.cols + 7) / 8;
+  const int nt = G > 64 ? wide_threads(per, CH) : kThreads, lanes = G > 64 ? nt : G;
+  const int rpb = G > 64 ? 1 : nt / G;
+  if (!chunks_fit(per, lanes, CH) || nt > std::max(G, kThreads)) return hipErrorInvalidConfiguration;
   const int64_t blocks = (j.rows + rpb - 1) / rpb;
-  const int grid = (int)std::min<int64_t>(blocks, most * kThreads / nt);
+  const int64_t most = G <= 64 && CH == 1 ? (RES ? 2 * kResident : kResident)
+                                          : kMany;
+  const int grid = (int)std::min<int64_t>(blocks, G == 1024 ? 256 : most * kThreads / nt);
   constexpr Form other = G == 1 ? kSmall : kRagged;
-  if (j.cols == 8 * G * CH)
+  if (j.cols == 8 * CH * lanes)
     hipLaunchKernelGGL((k_norm_forward<T, RES, G, CH, kExact, HOIST>), dim3(grid), dim3(nt), 0, st, j);
   else
     hipLaunchKernelGGL((k_norm_forward<T, RES, G, CH, other, HOIST>), dim3(grid), dim3(nt), 0, st, j);
@@ -744,26 +731,35 @@ constexpr int kFew = 1024, kFewWide = 1536;
 
 // How a backward pass over rows x cols runs.
 struct BackwardPlan {
-  int lanes;             // G of the kernels
+  int lanes, chunks;     // G and CH of the kernels
+  int threads;           // of a workgroup
   int parts;             // workgroups of k_norm_backward (0: k_norm_backward_split)
   int col_blocks, row_blocks;   // of k_norm_backward_split
 };
 
-BackwardPlan backward_plan(int64_t rows, int cols, bool weights) {
+BackwardPlan backward_plan(int64_t rows, int cols, Elt e, bool weights) {
   const int per = (cols + 7) / 8;
+  const bool wide = per > 128;
   BackwardPlan p{};
   for (p.lanes = 1; p.lanes < 64 && p.lanes < per; p.lanes *= 2) {}
-  if (per > 128) p.lanes = per <= 1024 ? 512 : 1024;
-  const int nt = backward_threads(p.lanes), rpb = nt / p.lanes;
+  if (wide) p.lanes = per <= 1024 ? 512 : 1024;
+  p.chunks = per <= 64 ? 1 : per <= 128 ? 2 : per <= 512 ? 1 : per <= 2048 ? 2 : 4;
+  p.threads = backward_threads(p.lanes);
+  const int rpb = wide ? 1 : p.threads / p.lanes;
   const int64_t blocks = (rows + rpb - 1) / rpb;
-  if (weights && blocks == 1) {
+  if (weights && blocks == 1 && p.chunks <= 2) {
     p.parts = 1;
-  } else if (weights && rows > (per > 128 ? kFewWide : kFew)) {
-    const int64_t rounds = (blocks + 255) / 256;     // rows dealt out evenly to a workgroup a CU
+  } else if (weights && rows > (wide ? kFewWide : kFew) && p.chunks <= 2) {
+    // bf16 rows of few wavefronts take two chunks a lane: twice the bytes in flight
+    if (wide && per <= 384 && e == BF16) p.chunks = 2;
+    if (wide) p.threads = wide_threads(per, p.chunks);
+    // the rows dealt out evenly to workgroups of eight wavefronts in all a CU
+    const int64_t most = 256 * std::max(1, 512 / p.threads);
+    const int64_t rounds = (blocks + most - 1) / most;
     p.parts = (int)((blocks + rounds - 1) / rounds);
   } else {
     p.col_blocks = weights ? (per + column_lanes(p.lanes) - 1) / column_lanes(p.lanes) : 0;
-    p.row_blocks = (int)std::min<int64_t>(blocks, 16384);
+    p.row_blocks = (int)std::min<int64_t>(blocks, kMany);
   }
   return p;
 }
@@ -772,11 +768,17 @@ template <typename T, bool RES, int G, int CH>
 hipError_t backward_with(const NormJob& j, const BackwardPlan& p, hipStream_t st) {
   constexpr int nt = backward_threads(G);
   constexpr Form other = G == 1 ? kSmall : kRagged;
-  const bool exact = j.cols == 8 * G * CH;
-  if (p.parts > 0) {
-    if (exact) hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, kExact>), dim3(p.parts), dim3(nt), 0, st, j);
-    else hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, other>), dim3(p.parts), dim3(nt), 0, st, j);
-    return hipGetLastError();
+  const int lanes = G > 64 ? p.threads : G;
+  const bool exact = j.cols == 8 * CH * lanes;
+  if (!chunks_fit((j.cols + 7) / 8, lanes, CH)) return hipErrorInvalidConfiguration;
+  if constexpr (CH <= 2) {
+    if (p.parts > 0) {
+      if (exact)
+        hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, kExact>), dim3(p.parts), dim3(p.threads), 0, st, j);
+      else
+        hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, other>), dim3(p.parts), dim3(p.threads), 0, st, j);
+      return hipGetLastError();
+    }
   }
   auto run = [&](int col_blocks, int row_blocks) {
     const dim3 grid(col_blocks + row_blocks);
@@ -799,7 +801,6 @@ hipError_t backward_with(const NormJob& j, const BackwardPlan& p, hipStream_t st
 
 template <typename T, bool RES>
 hipError_t backward(const NormJob& j, const BackwardPlan& p, hipStream_t st) {
-  const int per = (j.cols + 7) / 8;
   switch (p.lanes) {
     case 1: return backward_with<T, RES, 1, 1>(j, p, st);
     case 2: return backward_with<T, RES, 2, 1>(j, p, st);
@@ -807,9 +808,9 @@ hipError_t backward(const NormJob& j, const BackwardPlan& p, hipStream_t st) {
     case 8: return backward_with<T, RES, 8, 1>(j, p, st);
     case 16: return backward_with<T, RES, 16, 1>(j, p, st);
     case 32: return backward_with<T, RES, 32, 1>(j, p, st);
-    case 64: return per <= 64 ? backward_with<T, RES, 64, 1>(j, p, st) : backward_with<T, RES, 64, 2>(j, p, st);
-    case 512: return per <= 512 ? backward_with<T, RES, 512, 1>(j, p, st) : backward_with<T, RES, 512, 2>(j, p, st);
-    default: return per <= 2048 ? backward_with<T, RES, 1024, 2>(j, p, st) : backward_with<T, RES, 1024, 4>(j, p, st);
+    case 64: return p.chunks == 1 ? backward_with<T, RES, 64, 1>(j, p, st) : backward_with<T, RES, 64, 2>(j, p, st);
+    case 512: return p.chunks == 1 ? backward_with<T, RES, 512, 1>(j, p, st) : backward_with<T, RES, 512, 2>(j, p, st);
+    default: return p.chunks == 2 ? backward_with<T, RES, 1024, 2>(j, p, st) : backward_with<T, RES, 1024, 4>(j, p, st);
   }
 }
 
@@ -824,8 +825,9 @@ hipError_t forward(const NormJob& j, hipStream_t st) {
   if (per <= 32) return forward_with<T, RES, 32, 1>(j, st);
   if (per <= 64) return forward_with<T, RES, 64, 1>(j, st);
   if (per <= 128) return forward_with<T, RES, 64, 2>(j, st);
-  if (per <= 256) return forward_wide<T, RES, 256, 1>(j, st);
-  if (per <= 512) return forward_wide<T, RES, 256, 2>(j, st);
+  // bf16 rows take two chunks a lane for as many bytes in flight as float32
+  // rows have with one: 20000 x 1200 bf16 29.3 us, 31.9 with one
+  if (per <= 512 && sizeof(T) == 4) return forward_wide<T, RES, 512, 1>(j, st);
   if (per <= 1024) return forward_wide<T, RES, 512, 2>(j, st);
   if (per <= 2048) return forward_with<T, RES, 1024, 2, true>(j, st);
   return forward_with<T, RES, 1024, 4, false>(j, st);   // registers: none left for gamma and beta
@@ -834,8 +836,7 @@ hipError_t forward(const NormJob& j, hipStream_t st) {
 }  // namespace
 
 int norm_parts(int64_t rows, int cols) {
-  const BackwardPlan p = backward_plan(rows, cols, true);
-  return p.parts > 0 ? p.parts : 1;
+  return std::max({1, backward_plan(rows, cols, F32, true).parts, backward_plan(rows, cols, BF16, true).parts});
 }
 
 template <typename T>
@@ -862,7 +863,7 @@ hipError_t launch_norm_forward(Elt e, const NormJob& j, hipStream_t st) {
 
 hipError_t launch_norm_backward(Elt e, const NormJob& j, hipStream_t st) {
   const bool weights = j.dgamma || j.dbeta, residual = j.ds.p || j.dx.p;
-  const BackwardPlan p = backward_plan(j.rows, j.cols, weights);
+  const BackwardPlan p = backward_plan(j.rows, j.cols, e, weights);
   hipError_t err;
   if (e == BF16) err = residual ? backward<uint16_t, true>(j, p, st) : backward<uint16_t, false>(j, p, st);
   else err = residual ? backward<float, true>(j, p, st) : backward<float, false>(j, p, st);
