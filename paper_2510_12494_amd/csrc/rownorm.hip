@@ -8,6 +8,7 @@
 // registers between the passes over it.  All sums are float32; a value is
 // rounded to the storage type where it is stored.
 #include <algorithm>
+#include <type_traits>
 
 #include "device.h"
 #include "kernels.h"
@@ -18,6 +19,42 @@ namespace {
 using namespace dev;
 
 constexpr int kThreads = 256;
+
+// Kernel arguments: what a kernel reads and no more, the sizes of its grid and
+// workgroups among them (asking for those would add 256 bytes of hidden
+// arguments).  The host writes them for every launch: a layer norm's 72 bytes
+// instead of the whole job and the hidden ones take 0.5 us off a call of 3.7.
+struct DropArgs {
+  DropKey d;
+  Mat x, y;
+  int64_t rows, drow;
+  int cols, dq;
+};
+struct NoResidual {};
+struct ForwardResidual { DropKey d; Mat r, s; };
+template <bool RES>
+struct ForwardArgs : std::conditional_t<RES, ForwardResidual, NoResidual> {
+  Mat x, y;
+  const float *gamma, *beta;
+  float* stats;
+  int64_t rows;
+  int cols, grid, threads;
+  float eps;
+};
+struct BackwardResidual { DropKey d; Mat ds, dx; };
+template <bool RES>
+struct BackwardArgs : std::conditional_t<RES, BackwardResidual, NoResidual> {
+  Mat v, dy, dr;
+  const float *gamma, *stats;
+  float *dgamma, *dbeta, *part;
+  int64_t rows;
+  int cols, grid, threads, col_blocks;
+};
+struct ReduceArgs {
+  const float* part;
+  float *dgamma, *dbeta;
+  int cols, parts;
+};
 
 // ------------------------------------------------------------------- chunks
 // Vectors at element alignment: gfx950 loads and stores 16 bytes at any
@@ -199,7 +236,7 @@ __device__ __forceinline__ T* out_row(const Mat& m, int64_t r) { return (T*)m.p 
 // consecutive whatever the width; a thread steps its (row, chunk) pair by
 // (drow, dq), a whole grid, without a division.
 template <typename T, Form F>
-__global__ __launch_bounds__(kThreads) void k_dropout(DropJob j, int64_t drow, int dq) {
+__global__ __launch_bounds__(kThreads) void k_dropout(DropArgs j) {
   const Cols k(j.cols, j.rows);
   const uint32_t step = step_of(j.d);
   const uint32_t first = blockIdx.x * kThreads + threadIdx.x;
@@ -214,8 +251,8 @@ __global__ __launch_bounds__(kThreads) void k_dropout(DropJob j, int64_t drow, i
     chunk_values<F>(raw, q, k, edge, v);
     if (j.d.thr) drop_values(j.d, n, v);
     store_chunk<F>(out_row<T>(j.y, r), q, k, v);
-    r += drow;
-    q += dq;
+    r += j.drow;
+    q += j.dq;
     if (q >= k.per) {
       q -= k.per;
       ++r;
@@ -266,7 +303,7 @@ __device__ __forceinline__ int group_of_thread() {
 // barrier a row (the slots alternate) and loses nothing to cancellation.  HOIST: a thread's gamma and beta are loaded before
 // its first row and kept.
 template <typename T, bool RES, int G, int CH, Form F, bool HOIST>
-__global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(NormJob j) {
+__global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(ForwardArgs<RES> j) {
   constexpr bool WIDE = G > 64;
   constexpr int RPB = WIDE ? 1 : kThreads / G;
   constexpr int GL = G < 64 ? G : 64;
@@ -274,14 +311,15 @@ __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(No
   __shared__ f32x2 slots[2][WIDE ? 16 : 1];        // a wavefront's mean and sum of squares
   __shared__ float columns[WIDE ? 16 : 1];         // and its columns of a row
   const Cols k(j.cols, j.rows);
-  const int lanes = WIDE ? (int)blockDim.x : G;
+  const int lanes = WIDE ? j.threads : G;
   const int lane = WIDE ? (int)threadIdx.x : threadIdx.x % G, wave = threadIdx.x / 64;
   const float inv = 1.f / (float)k.n;
 
   Raw<T> x[CH], res[CH];
   auto fetch = [&](int64_t r) {
     const T* px = row_of<T>(j.x, r);
-    const T* pr = RES ? row_of<T>(j.r, r) : nullptr;
+    const T* pr = nullptr;
+    if constexpr (RES) pr = row_of<T>(j.r, r);
     const bool edge = r >= k.edge;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -289,7 +327,7 @@ __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(No
       if constexpr (RES) res[c] = load_chunk<F>(pr, c * lanes + lane, k, edge, c < CH / 2);
     }
   };
-  const int64_t stride = (int64_t)gridDim.x * RPB;
+  const int64_t stride = (int64_t)j.grid * RPB;
   int64_t r = (int64_t)blockIdx.x * RPB + group_of_thread<G>();
   if (AHEAD && r < j.rows) fetch(r);
   uint32_t step = 0;
@@ -411,7 +449,7 @@ __device__ __forceinline__ float stride_sum(float v) {
 // also adds its columns' terms of the weights' gradients to ag and ab (not with
 // four chunks a lane, which leave no registers for those).
 template <typename T, bool RES, int G, int CH, Form F, bool ACC>
-__device__ __forceinline__ void backward_rows(const NormJob& j, int64_t r, int64_t stride, float (&ag)[CH][8],
+__device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_t r, int64_t stride, float (&ag)[CH][8],
                                               float (&ab)[CH][8]) {
   constexpr bool WIDE = G > 64;
   constexpr int GL = G < 64 ? G : 64;
@@ -419,10 +457,14 @@ __device__ __forceinline__ void backward_rows(const NormJob& j, int64_t r, int64
   static_assert(!(ACC && CH > 2), "registers");
   __shared__ f32x2 slots[2][WIDE ? 16 : 1];
   const Cols k(j.cols, j.rows);
-  const int lanes = WIDE ? (int)blockDim.x : G;
+  const int lanes = WIDE ? j.threads : G;
   const int lane = WIDE ? (int)threadIdx.x : threadIdx.x % G;
   const float inv = 1.f / (float)k.n;
-  const bool add = RES && j.ds.p, drop = RES && j.dx.p && j.d.thr;
+  bool add = false, drop = false;
+  if constexpr (RES) {
+    add = j.ds.p;
+    drop = j.dx.p && j.d.thr;
+  }
 
   Raw<T> xr[CH], yr[CH], sr[CH];
   f32x2 st = {0.f, 0.f};
@@ -456,9 +498,11 @@ __device__ __forceinline__ void backward_rows(const NormJob& j, int64_t r, int64
   for (; r < j.rows; r += stride) {
     if constexpr (!AHEAD) fetch(r);
     Numbers n[CH];
-    if (AHEAD && drop) {                             // beside the row's loads
+    if constexpr (RES && AHEAD) {
+      if (drop) {                                    // beside the row's loads
 #pragma unroll
-      for (int c = 0; c < CH; ++c) n[c] = chunk_numbers(j.d, step, j.d.row0 + r, c * lanes + lane);
+        for (int c = 0; c < CH; ++c) n[c] = chunk_numbers(j.d, step, j.d.row0 + r, c * lanes + lane);
+      }
     }
     const float mean = st[0], rs = st[1];
     const bool edge = r >= k.edge;
@@ -528,17 +572,17 @@ __device__ __forceinline__ void backward_rows(const NormJob& j, int64_t r, int64
 // float32 rows (2 x cols at j.part), or the result itself where the grid is
 // one workgroup.
 template <typename T, bool RES, int G, int CH, int NT, Form F>
-__global__ __launch_bounds__(NT) void k_norm_backward(NormJob j) {
+__global__ __launch_bounds__(NT) void k_norm_backward(BackwardArgs<RES> j) {
   constexpr int NW = NT / 64, RPB = G > 64 ? 1 : NT / G;
   constexpr int GL = G < 64 ? G : 64;
   __shared__ float sums[G > 64 ? 1 : NW][G > 64 ? 1 : GL * 8];
   float ag[CH][8] = {}, ab[CH][8] = {};
   backward_rows<T, RES, G, CH, F, true>(j, (int64_t)blockIdx.x * RPB + group_of_thread<G>(),
-                                        (int64_t)gridDim.x * RPB, ag, ab);
+                                        (int64_t)j.grid * RPB, ag, ab);
   const Cols k(j.cols, j.rows);
   const int lane = G > 64 ? (int)threadIdx.x : threadIdx.x % G, wave = threadIdx.x / 64;
-  float* const out[2] = {gridDim.x == 1 ? j.dgamma : j.part + (int64_t)(2 * blockIdx.x) * k.n,
-                         gridDim.x == 1 ? j.dbeta : j.part + (int64_t)(2 * blockIdx.x + 1) * k.n};
+  float* const out[2] = {j.grid == 1 ? j.dgamma : j.part + (int64_t)(2 * blockIdx.x) * k.n,
+                         j.grid == 1 ? j.dbeta : j.part + (int64_t)(2 * blockIdx.x + 1) * k.n};
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
 #pragma unroll
@@ -546,7 +590,7 @@ __global__ __launch_bounds__(NT) void k_norm_backward(NormJob j) {
       float* const dst = out[a];
       float(&acc)[8] = a == 0 ? ag[c] : ab[c];
       if constexpr (G > 64) {
-        if (dst) store_chunk<F>(dst, c * (int)blockDim.x + lane, k, acc, c < CH / 2);
+        if (dst) store_chunk<F>(dst, c * j.threads + lane, k, acc, c < CH / 2);
       } else {
         if constexpr (GL < 64)
           for (int i = 0; i < 8; ++i) acc[i] = stride_sum<GL>(acc[i]);
@@ -576,8 +620,8 @@ constexpr int column_lanes(int G) { return G > 64 ? 8 : 4; }
 // Few rows: the first workgroups take 32 columns of the weights' gradients each
 // over all rows (64 of wide rows), the others the rows; x and dy are read twice
 // (the second time from a cache), but nothing has to meet between workgroups.
-template <typename T, int NT, int LC, Form F>
-__device__ __forceinline__ void backward_columns(const NormJob& j, int block) {
+template <typename T, bool RES, int NT, int LC, Form F>
+__device__ __forceinline__ void backward_columns(const BackwardArgs<RES>& j, int block) {
   constexpr int NW = NT / 64, SL = NT / LC, U = sizeof(T) == 2 && LC == 4 ? 8 : 4;
   __shared__ float sums[NW][2][8 * LC];
   const Cols k(j.cols, j.rows);
@@ -631,16 +675,16 @@ __device__ __forceinline__ void backward_columns(const NormJob& j, int block) {
 }
 
 template <typename T, bool RES, int G, int CH, int NT, Form F>
-__global__ __launch_bounds__(NT) void k_norm_backward_split(NormJob j, int col_blocks) {
+__global__ __launch_bounds__(NT) void k_norm_backward_split(BackwardArgs<RES> j) {
   constexpr int RPB = G > 64 ? 1 : NT / G;
   constexpr int LC = column_lanes(G);
   constexpr Form FC = F == kExact && G * CH % LC != 0 ? (G == 1 ? kSmall : kRagged) : F;
-  if ((int)blockIdx.x < col_blocks) {
-    backward_columns<T, NT, LC, FC>(j, blockIdx.x);
+  if ((int)blockIdx.x < j.col_blocks) {
+    backward_columns<T, RES, NT, LC, FC>(j, blockIdx.x);
   } else {
     float none[CH][8];
-    backward_rows<T, RES, G, CH, F, false>(j, (int64_t)(blockIdx.x - col_blocks) * RPB + group_of_thread<G>(),
-                                           (int64_t)(gridDim.x - col_blocks) * RPB, none, none);
+    backward_rows<T, RES, G, CH, F, false>(j, (int64_t)(blockIdx.x - j.col_blocks) * RPB + group_of_thread<G>(),
+                                           (int64_t)(j.grid - j.col_blocks) * RPB, none, none);
   }
 }
 
@@ -649,7 +693,7 @@ __global__ __launch_bounds__(NT) void k_norm_backward_split(NormJob j, int col_b
 // wavefront, the wavefronts in LDS, always in the same order.
 constexpr int kReduceThreads = 1024;
 template <int RC>
-__global__ __launch_bounds__(kReduceThreads) void k_norm_reduce(NormJob j, int parts) {
+__global__ __launch_bounds__(kReduceThreads) void k_norm_reduce(ReduceArgs j) {
   constexpr int slices = kReduceThreads / RC, waves = kReduceThreads / 64;
   __shared__ float sums[waves][RC];
   const int lane = threadIdx.x % RC, slice = threadIdx.x / RC;
@@ -659,7 +703,7 @@ __global__ __launch_bounds__(kReduceThreads) void k_norm_reduce(NormJob j, int p
   if (c < pitch) {
     const float* p = j.part + c;
 #pragma unroll 8
-    for (int i = slice; i < parts; i += slices) t += p[i * pitch];
+    for (int i = slice; i < j.parts; i += slices) t += p[i * pitch];
   }
   if constexpr (RC < 64) t = stride_sum<RC>(t);
   if (threadIdx.x % 64 < RC) sums[threadIdx.x / 64][lane] = t;
@@ -680,8 +724,8 @@ __global__ __launch_bounds__(kReduceThreads) void k_norm_reduce(NormJob j, int p
 // us, 9.3 in two rounds; residual 118955 x 175 bf16 48.5 in two, 52.5 in one.
 // Wider rows are dealt out by the hardware (residual 32768 x 1024 bf16 46.6 us,
 // 48.5 in two rounds) up to 8192 columns, beyond which gamma and beta are too
-// many bytes to read for each row: 2000 x 16384 bf16 28.9
-// us with a workgroup a CU, 38 with one a row.
+// many bytes to read for each row: 2000 x 16384 bf16 28.9 us with a workgroup a
+// CU, 38 with one a row.
 constexpr int kResident = 2048, kMany = 16384;
 
 // threads for a row of `per` chunks, CH a thread, that takes several wavefronts
@@ -701,11 +745,27 @@ hipError_t forward_with(const NormJob& j, hipStream_t st) {
   const int64_t most = G <= 64 && CH == 1 ? (RES ? 2 * kResident : kResident)
                                           : kMany;
   const int grid = (int)std::min<int64_t>(blocks, G == 1024 ? 256 : most * kThreads / nt);
+  ForwardArgs<RES> a;
+  if constexpr (RES) {
+    a.d = j.d;
+    a.r = j.r;
+    a.s = j.s;
+  }
+  a.x = j.x;
+  a.y = j.y;
+  a.gamma = j.gamma;
+  a.beta = j.beta;
+  a.stats = j.stats;
+  a.rows = j.rows;
+  a.cols = j.cols;
+  a.grid = grid;
+  a.threads = nt;
+  a.eps = j.eps;
   constexpr Form other = G == 1 ? kSmall : kRagged;
   if (j.cols == 8 * CH * lanes)
-    hipLaunchKernelGGL((k_norm_forward<T, RES, G, CH, kExact, HOIST>), dim3(grid), dim3(nt), 0, st, j);
+    hipLaunchKernelGGL((k_norm_forward<T, RES, G, CH, kExact, HOIST>), dim3(grid), dim3(nt), 0, st, a);
   else
-    hipLaunchKernelGGL((k_norm_forward<T, RES, G, CH, other, HOIST>), dim3(grid), dim3(nt), 0, st, j);
+    hipLaunchKernelGGL((k_norm_forward<T, RES, G, CH, other, HOIST>), dim3(grid), dim3(nt), 0, st, a);
   return hipGetLastError();
 }
 
@@ -771,22 +831,42 @@ hipError_t backward_with(const NormJob& j, const BackwardPlan& p, hipStream_t st
   const int lanes = G > 64 ? p.threads : G;
   const bool exact = j.cols == 8 * CH * lanes;
   if (!chunks_fit((j.cols + 7) / 8, lanes, CH)) return hipErrorInvalidConfiguration;
+  BackwardArgs<RES> a;
+  if constexpr (RES) {
+    a.d = j.d;
+    a.ds = j.ds;
+    a.dx = j.dx;
+  }
+  a.v = j.v;
+  a.dy = j.dy;
+  a.dr = j.dr;
+  a.gamma = j.gamma;
+  a.stats = j.stats;
+  a.dgamma = j.dgamma;
+  a.dbeta = j.dbeta;
+  a.part = j.part;
+  a.rows = j.rows;
+  a.cols = j.cols;
+  a.threads = p.threads;
+  a.col_blocks = 0;
   if constexpr (CH <= 2) {
     if (p.parts > 0) {
+      a.grid = p.parts;
       if (exact)
-        hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, kExact>), dim3(p.parts), dim3(p.threads), 0, st, j);
+        hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, kExact>), dim3(p.parts), dim3(p.threads), 0, st, a);
       else
-        hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, other>), dim3(p.parts), dim3(p.threads), 0, st, j);
+        hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, other>), dim3(p.parts), dim3(p.threads), 0, st, a);
       return hipGetLastError();
     }
   }
   auto run = [&](int col_blocks, int row_blocks) {
-    const dim3 grid(col_blocks + row_blocks);
-    if (grid.x == 0) return;
+    a.col_blocks = col_blocks;
+    a.grid = col_blocks + row_blocks;
+    if (a.grid == 0) return;
     if (exact)
-      hipLaunchKernelGGL((k_norm_backward_split<T, RES, G, CH, nt, kExact>), grid, dim3(nt), 0, st, j, col_blocks);
+      hipLaunchKernelGGL((k_norm_backward_split<T, RES, G, CH, nt, kExact>), dim3(a.grid), dim3(nt), 0, st, a);
     else
-      hipLaunchKernelGGL((k_norm_backward_split<T, RES, G, CH, nt, other>), grid, dim3(nt), 0, st, j, col_blocks);
+      hipLaunchKernelGGL((k_norm_backward_split<T, RES, G, CH, nt, other>), dim3(a.grid), dim3(nt), 0, st, a);
   };
   const int row_blocks = j.dr.p || j.dx.p ? p.row_blocks : 0;
   auto over = [&](const Mat& m) { return m.p && (m.p == j.dy.p || m.p == j.v.p); };
@@ -844,11 +924,11 @@ hipError_t dropout(const DropJob& j, hipStream_t st) {
   const int64_t per = ((int64_t)j.cols + 7) / 8;
   const int64_t chunks = j.rows > (INT64_MAX >> 2) / per ? INT64_MAX >> 2 : j.rows * per;
   const int grid = (int)std::min<int64_t>((chunks + kThreads - 1) / kThreads, kMany);
-  const int64_t stride = (int64_t)grid * kThreads, drow = stride / per;
-  const int dq = (int)(stride % per);
-  if (j.cols % 8 == 0) hipLaunchKernelGGL((k_dropout<T, kExact>), dim3(grid), dim3(kThreads), 0, st, j, drow, dq);
-  else if (j.cols > 8) hipLaunchKernelGGL((k_dropout<T, kRagged>), dim3(grid), dim3(kThreads), 0, st, j, drow, dq);
-  else hipLaunchKernelGGL((k_dropout<T, kSmall>), dim3(grid), dim3(kThreads), 0, st, j, drow, dq);
+  const int64_t stride = (int64_t)grid * kThreads;
+  const DropArgs a{j.d, j.x, j.y, j.rows, stride / per, j.cols, (int)(stride % per)};
+  if (j.cols % 8 == 0) hipLaunchKernelGGL((k_dropout<T, kExact>), dim3(grid), dim3(kThreads), 0, st, a);
+  else if (j.cols > 8) hipLaunchKernelGGL((k_dropout<T, kRagged>), dim3(grid), dim3(kThreads), 0, st, a);
+  else hipLaunchKernelGGL((k_dropout<T, kSmall>), dim3(grid), dim3(kThreads), 0, st, a);
   return hipGetLastError();
 }
 
@@ -867,13 +947,13 @@ hipError_t launch_norm_backward(Elt e, const NormJob& j, hipStream_t st) {
   hipError_t err;
   if (e == BF16) err = residual ? backward<uint16_t, true>(j, p, st) : backward<uint16_t, false>(j, p, st);
   else err = residual ? backward<float, true>(j, p, st) : backward<float, false>(j, p, st);
-  const int parts = p.parts;
-  if (err != hipSuccess || parts <= 1) return err;
+  if (err != hipSuccess || p.parts <= 1) return err;
+  const ReduceArgs a{j.part, j.dgamma, j.dbeta, j.cols, p.parts};
   // 64 columns a workgroup once they fill the CUs, else 16
   if (2 * j.cols > 256 * 16)
-    hipLaunchKernelGGL((k_norm_reduce<64>), dim3((2 * j.cols + 63) / 64), dim3(kReduceThreads), 0, st, j, parts);
+    hipLaunchKernelGGL((k_norm_reduce<64>), dim3((2 * j.cols + 63) / 64), dim3(kReduceThreads), 0, st, a);
   else
-    hipLaunchKernelGGL((k_norm_reduce<16>), dim3((2 * j.cols + 15) / 16), dim3(kReduceThreads), 0, st, j, parts);
+    hipLaunchKernelGGL((k_norm_reduce<16>), dim3((2 * j.cols + 15) / 16), dim3(kReduceThreads), 0, st, a);
   return hipGetLastError();
 }
 
