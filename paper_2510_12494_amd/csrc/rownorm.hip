@@ -695,6 +695,7 @@ constexpr int kReduceThreads = 1024;
 template <int RC>
 __global__ __launch_bounds__(kReduceThreads) void k_norm_reduce(ReduceArgs j) {
   constexpr int slices = kReduceThreads / RC, waves = kReduceThreads / 64;
+  constexpr int U = 256 / slices;                  // the loads of 256 parts in flight
   __shared__ float sums[waves][RC];
   const int lane = threadIdx.x % RC, slice = threadIdx.x / RC;
   const int64_t pitch = 2 * (int64_t)j.cols;
@@ -702,8 +703,13 @@ __global__ __launch_bounds__(kReduceThreads) void k_norm_reduce(ReduceArgs j) {
   float t = 0.f;
   if (c < pitch) {
     const float* p = j.part + c;
-#pragma unroll 8
-    for (int i = slice; i < j.parts; i += slices) t += p[i * pitch];
+    for (int i = slice; i < j.parts; i += U * slices) {
+      float v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = i + u * slices < j.parts ? p[(i + u * slices) * pitch] : 0.f;
+#pragma unroll
+      for (int u = 0; u < U; ++u) t += v[u];
+    }
   }
   if constexpr (RC < 64) t = stride_sum<RC>(t);
   if (threadIdx.x % 64 < RC) sums[threadIdx.x / 64][lane] = t;

@@ -645,3 +645,69 @@ def test_backward_in_a_replayed_graph(V):
         g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, outs))
+
+
+# widths at which a row takes another number of chunks a lane or of wavefronts,
+# one chunk more, and one that ends inside a chunk; more rows than the backward
+# pass reads twice
+EDGES = [8, 9, 16, 17, 32, 64, 72, 128, 136, 256, 264, 511, 512, 520, 1024, 1032, 1535, 1536, 1544, 3071, 3080, 4096,
+         4104, 8192, 8193, 9000, 16384, 16385]
+
+
+@pytest.mark.parametrize("dt", DTS)
+@pytest.mark.parametrize("cols", EDGES)
+def test_widths_where_the_layout_changes(V, dt, cols):
+    rows = 1540 if cols > 1024 else 1100
+    c = Call(V, "residual", dt, rows, cols, p=0.2)
+    c.forward()
+    c.check_forward()
+    c.backward()
+    c.check_backward()
+    c.guards()
+    few = Call(V, "norm", dt, 5, cols, (cols + 7) // 8 * 8, 1)
+    few.forward()
+    few.check_forward()
+    few.backward()
+    few.check_backward()
+    few.guards()
+
+
+@pytest.mark.parametrize("dt", DTS)
+@pytest.mark.parametrize("rows,cols", [(1100, 24), (1600, 1300), (1600, 9000), (40, 20000)])
+def test_in_place_with_many_rows(V, dt, rows, cols):
+    """dx over dy and dr over ds, whichever way the weights' gradients are made."""
+    ref = Call(V, "residual", dt, rows, cols, p=0.3)
+    ref.forward()
+    ref.backward()
+    c = Call(V, "residual", dt, rows, cols, p=0.3)
+    c.forward()
+    c.ds.put(c.a.dr)
+    c.dy.put(c.a.dx)
+    c.backward()
+    assert torch.equal(c.ds.t, ref.dr.t) and torch.equal(c.dy.t, ref.dx.t)
+    assert torch.equal(c.dgamma, ref.dgamma) and torch.equal(c.dbeta, ref.dbeta)
+
+
+@pytest.mark.parametrize("dt", DTS)
+@pytest.mark.parametrize("cols", [3, 13, 100, 1001, 9001])
+def test_values_between_rows_have_no_influence(V, dt, cols):
+    """NaN behind every row's end (read along with a row's last chunk)."""
+    rows = 23
+    ref = Call(V, "residual", dt, rows, cols, cols + 9, 0, p=0.3)
+    ref.forward()
+    ref.backward()
+    c = Call(V, "residual", dt, rows, cols, cols + 9, 0, p=0.3)
+    for m in (c.x, c.r, c.s, c.dy, c.ds):
+        m.buf[:rows * m.ld].view(rows, m.ld)[:, cols:] = float("nan")
+    c.forward()
+    c.backward()
+    for name in ("y", "s", "dr", "dx"):
+        assert torch.equal(c.m[name].t, ref.m[name].t)
+    assert torch.equal(c.stats, ref.stats) and torch.equal(c.dgamma, ref.dgamma) and torch.equal(c.dbeta, ref.dbeta)
+    d, y = V.vfl_dropout_args(), Mat(dt, rows, cols)
+    d.dtype, d.rows, d.cols = c.a.dtype, rows, cols
+    key(d.drop, 0.5)
+    c.x.put(d.x)
+    y.put(d.y)
+    V.vfl_dropout(d)
+    assert not bool(y.t.isnan().any())
