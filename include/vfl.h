@@ -466,10 +466,10 @@ typedef struct {
 } vfl_dropout_args;
 vfl_status vfl_dropout(const vfl_dropout_args* a, void* stream);
 
-/* Device workspace (16-byte aligned) that a backward pass over rows x cols
- * needs for its weights' gradients; its contents need no preparation and mean
- * nothing between calls.  Calls that may run at the same time need one each.
- * Host-only. */
+/* Device workspace (16-byte aligned) that a backward pass over rows x cols, or
+ * over fewer rows, needs for its weights' gradients (0 bytes: none); its
+ * contents need no preparation and mean nothing between calls.  Calls that may
+ * run at the same time need one each.  Host-only. */
 #define VFL_NORM_MAX_COLS 32768
 vfl_status vfl_norm_workspace_size(int64_t rows, int32_t cols, size_t* bytes);
 

@@ -443,8 +443,8 @@ struct NormJob {
 };
 
 // the most partial pairs (2 x cols floats each) of weights' gradients that a
-// backward pass over rows x cols leaves in its workspace, whatever its element
-// type (1: none, the result is written at once)
+// backward pass over rows x cols, or fewer rows, leaves in its workspace,
+// whatever its element type (1: none, the result is written at once)
 int norm_parts(int64_t rows, int cols);
 hipError_t launch_dropout(Elt e, const DropJob& j, hipStream_t st);
 hipError_t launch_norm_forward(Elt e, const NormJob& j, hipStream_t st);

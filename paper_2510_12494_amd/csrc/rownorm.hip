@@ -800,6 +800,7 @@ struct BackwardPlan {
   int lanes, chunks;     // G and CH of the kernels
   int threads;           // of a workgroup
   int parts;             // workgroups of k_norm_backward (0: k_norm_backward_split)
+  int room;              // parts that these or fewer rows may take
   int col_blocks, row_blocks;   // of k_norm_backward_split
 };
 
@@ -823,6 +824,7 @@ BackwardPlan backward_plan(int64_t rows, int cols, Elt e, bool weights) {
     const int64_t most = 256 * std::max(1, 512 / p.threads);
     const int64_t rounds = (blocks + most - 1) / most;
     p.parts = (int)((blocks + rounds - 1) / rounds);
+    p.room = (int)std::min(blocks, most);
   } else {
     p.col_blocks = weights ? (per + column_lanes(p.lanes) - 1) / column_lanes(p.lanes) : 0;
     p.row_blocks = (int)std::min<int64_t>(blocks, kMany);
@@ -922,7 +924,7 @@ hipError_t forward(const NormJob& j, hipStream_t st) {
 }  // namespace
 
 int norm_parts(int64_t rows, int cols) {
-  return std::max({1, backward_plan(rows, cols, F32, true).parts, backward_plan(rows, cols, BF16, true).parts});
+  return std::max({1, backward_plan(rows, cols, F32, true).room, backward_plan(rows, cols, BF16, true).room});
 }
 
 template <typename T>

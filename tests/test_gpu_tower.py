@@ -1,0 +1,93 @@
+"""GPU tests of the residual tower: its gradients against float64 autograd on the
+same masks, a batch in two halves, and the example end to end."""
+import importlib.util
+import os
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import rowops as R
+
+pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("needs an MI355X")
+
+
+def _reference(t, x, dz, row0, step):
+    """Embedding and gradients of tower t in float64 on the CPU."""
+    P = {k: v.double().cpu().requires_grad_() for k, v in t.params.items()}
+    ids = np.arange(row0, row0 + len(x))
+
+    def drop(v, tag):
+        k = torch.from_numpy(R.keep_mask(t.p, t.seed, step, tag, ids, v.shape[1]))
+        return torch.where(k, v * R.scale(t.p), 0.0)
+
+    def norm(s, l):
+        return torch.nn.functional.layer_norm(s, (t.width,), P[f"gamma.{l}"], P[f"beta.{l}"], 1e-5)
+
+    s = x.double().cpu() @ P["W_in"].T
+    y = norm(s, 0)
+    for l in range(t.blocks):
+        a = drop(torch.relu(y @ P[f"W1.{l}"].T + P[f"b.{l}"]), 2 * l)
+        s = s + drop(a @ P[f"W2.{l}"].T, 2 * l + 1)
+        y = norm(s, l + 1)
+    y.backward(dz.double().cpu())
+    return y.detach(), {k: v.grad for k, v in P.items()}
+
+
+@pytest.mark.parametrize("width,hidden,blocks,rows", [(64, 96, 2, 300), (40, 33, 1, 77), (256, 256, 3, 1500)])
+def test_gradients_equal_float64_autograd(width, hidden, blocks, rows):
+    """float32: products of up to 256 terms and sums over the rows, a few
+    layers deep: within 1e-4 of the largest entry (the bound of the float32
+    workloads), apart from ReLUs within rounding of zero, of which a handful
+    may flip (each moves an entry by at most one row's share)."""
+    from paper_2510_12494_amd.tower import ResidualTower
+    t = ResidualTower(24, width, hidden, blocks, rows + 50, "f32", p=0.25, seed=5)
+    g = torch.Generator().manual_seed(rows)
+    x, dz = torch.randn(rows, 24, generator=g), torch.randn(rows, width, generator=g) / rows
+    z = t.forward(x.cuda(), row0=900, step=4)
+    want, grads = _reference(t, x, dz, 900, 4)
+    assert (z.double().cpu() - want).abs().max() <= 1e-4 * want.abs().max()
+    t.backward(dz.cuda())
+    for k, v in grads.items():
+        err = (t.grads[k].double().cpu() - v).abs().max() / v.abs().max()
+        assert err <= 1e-4 + 4.0 / rows * 0.05, (k, float(err))
+
+
+def test_a_sample_does_not_depend_on_its_batch():
+    from paper_2510_12494_amd.tower import ResidualTower
+    t = ResidualTower(16, 64, 64, 2, 512, "f32", p=0.3, seed=3)
+    x = torch.randn(512, 16, generator=torch.Generator().manual_seed(1)).cuda()
+    whole = t.forward(x, row0=100, step=9).clone()
+    halves = torch.cat([t.forward(x[:200], row0=100, step=9).clone(), t.forward(x[200:], row0=300, step=9).clone()])
+    assert (whole - halves).abs().max() <= 1e-4 * whole.abs().max()
+    assert (whole - t.forward(x, row0=100, step=10)).abs().max() > 0.1         # another step, other masks
+    one = t.forward(x[7:8], train=False).clone()
+    assert (one - t.forward(x, train=False)[7:8]).abs().max() <= 1e-4 * one.abs().max()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_example_learns(dtype, capsys):
+    spec = importlib.util.spec_from_file_location("residual_towers", os.path.join(ROOT, "examples", "residual_towers.py"))
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    losses, right = m.main(["--steps", "120", "--rows", "9000", "--batch", "2048", "--width", "128", "--blocks", "2",
+                            "--dtype", dtype])
+    assert abs(losses[0] - np.log(2)) < 1e-3                  # a zero head: the logit is 0
+    assert np.mean(losses[-10:]) < 0.9 * losses[0]
+    assert right >= 0.5
+    assert "scored 64 samples" in capsys.readouterr().out
+
+
+def test_refusals():
+    from paper_2510_12494_amd.tower import ResidualTower
+    t = ResidualTower(16, 32, 32, 1, 64, "f32")
+    for bad in (torch.zeros(65, 16), torch.zeros(4, 15), torch.zeros(4, 16, dtype=torch.bfloat16), torch.zeros(0, 16)):
+        with pytest.raises(ValueError):
+            t.forward(bad.cuda())

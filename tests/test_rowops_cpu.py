@@ -151,3 +151,13 @@ def test_binding_matches_the_header_layout(V, tmp_path):
         want.append(C.sizeof(s))
         want += [getattr(s, f[0]).offset for f in s._fields_]
     assert got == want
+
+
+@pytest.mark.parametrize("cols", [1, 8, 64, 65, 500, 1024, 1025, 2400, 4096, 5001, 16384, 16392, 32768])
+def test_a_workspace_serves_every_smaller_batch(V, cols):
+    """Sizes never shrink with the rows."""
+    last = 0
+    for rows in list(range(0, 5000, 7)) + [2**k for k in range(13, 40)]:
+        n = V.vfl_norm_workspace_size(rows, cols)
+        assert n >= last
+        last = n
