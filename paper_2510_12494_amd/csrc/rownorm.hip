@@ -41,7 +41,7 @@ struct ForwardArgs : std::conditional_t<RES, ForwardResidual, NoResidual> {
   int cols, grid, threads;
   float eps;
 };
-struct BackwardResidual { DropKey d; Mat ds, dx; };
+struct BackwardResidual { DropKey d; Mat ds, dx; int add; };
 template <bool RES>
 struct BackwardArgs : std::conditional_t<RES, BackwardResidual, NoResidual> {
   Mat v, dy, dr;
@@ -448,7 +448,7 @@ __device__ __forceinline__ float stride_sum(float v) {
 // Rows first, first + stride, ... as in the forward, one pass.  ACC: a thread
 // also adds its columns' terms of the weights' gradients to ag and ab (not with
 // four chunks a lane, which leave no registers for those).
-template <typename T, bool RES, int G, int CH, Form F, bool ACC>
+template <typename T, bool RES, int G, int CH, Form F, bool ACC, bool OUT>
 __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_t r, int64_t stride, float (&ag)[CH][8],
                                               float (&ab)[CH][8]) {
   constexpr bool WIDE = G > 64;
@@ -462,8 +462,8 @@ __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_
   const float inv = 1.f / (float)k.n;
   bool add = false, drop = false;
   if constexpr (RES) {
-    add = j.ds.p;
-    drop = j.dx.p && j.d.thr;
+    add = j.add;
+    drop = j.d.thr;
   }
 
   Raw<T> xr[CH], yr[CH], sr[CH];
@@ -476,8 +476,7 @@ __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_
       const int q = c * lanes + lane;
       xr[c] = load_chunk<F>(row_of<T>(j.v, r), q, k, edge, c < CH / 2);
       yr[c] = load_chunk<F>(row_of<T>(j.dy, r), q, k, edge, c < CH / 2);
-      if constexpr (RES)
-        if (add) sr[c] = load_chunk<F>(row_of<T>(j.ds, r), q, k, edge, c < CH / 2);
+      if constexpr (RES && OUT) sr[c] = load_chunk<F>(row_of<T>(j.ds, r), q, k, edge, c < CH / 2);
     }
   };
   if (AHEAD && r < j.rows) fetch(r);
@@ -498,7 +497,7 @@ __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_
   for (; r < j.rows; r += stride) {
     if constexpr (!AHEAD) fetch(r);
     Numbers n[CH];
-    if constexpr (RES && AHEAD) {
+    if constexpr (RES && AHEAD && OUT) {
       if (drop) {                                    // beside the row's loads
 #pragma unroll
         for (int c = 0; c < CH; ++c) n[c] = chunk_numbers(j.d, step, j.d.row0 + r, c * lanes + lane);
@@ -515,7 +514,7 @@ __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_
       if constexpr (!HOIST) weights(c, 0);
       chunk_values<F>(xr[c], q, k, edge, h[c], c < CH / 2);
       chunk_values<F>(yr[c], q, k, edge, g[c], c < CH / 2);
-      if constexpr (RES) sc[c] = sr[c];
+      if constexpr (RES && OUT) sc[c] = sr[c];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         h[c][i] = (h[c][i] - mean) * rs;
@@ -528,7 +527,8 @@ __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_
         sgh = fmaf(g[c][i], h[c][i], sgh);
       }
     }
-    if (AHEAD && r + stride < j.rows) fetch(r + stride);
+    if (AHEAD) fetch(r + stride < j.rows ? r + stride : r);
+    if constexpr (!OUT) continue;
     sg = group_sum<GL>(sg);
     sgh = group_sum<GL>(sgh);
     if constexpr (WIDE) {
@@ -555,13 +555,11 @@ __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_
           for (int i = 0; i < 8; ++i) d[i] += t[i];
         }
       }
-      if (j.dr.p) store_chunk<F>(out_row<T>(j.dr, r), q, k, d, c < CH / 2);
+      store_chunk<F>(out_row<T>(j.dr, r), q, k, d, c < CH / 2);
       if constexpr (RES) {
-        if (j.dx.p) {
-          if (!AHEAD && drop) n[c] = chunk_numbers(j.d, step, j.d.row0 + r, q);
-          if (drop) drop_values(j.d, n[c], d);
-          store_chunk<F>(out_row<T>(j.dx, r), q, k, d, c < CH / 2);
-        }
+        if (!AHEAD && drop) n[c] = chunk_numbers(j.d, step, j.d.row0 + r, q);
+        if (drop) drop_values(j.d, n[c], d);
+        store_chunk<F>(out_row<T>(j.dx, r), q, k, d, c < CH / 2);
       }
     }
   }
@@ -577,8 +575,9 @@ __global__ __launch_bounds__(NT) void k_norm_backward(BackwardArgs<RES> j) {
   constexpr int GL = G < 64 ? G : 64;
   __shared__ float sums[G > 64 ? 1 : NW][G > 64 ? 1 : GL * 8];
   float ag[CH][8] = {}, ab[CH][8] = {};
-  backward_rows<T, RES, G, CH, F, true>(j, (int64_t)blockIdx.x * RPB + group_of_thread<G>(),
-                                        (int64_t)j.grid * RPB, ag, ab);
+  const int64_t first = (int64_t)blockIdx.x * RPB + group_of_thread<G>(), stride = (int64_t)j.grid * RPB;
+  if (j.dr.p) backward_rows<T, RES, G, CH, F, true, true>(j, first, stride, ag, ab);
+  else backward_rows<T, RES, G, CH, F, true, false>(j, first, stride, ag, ab);
   const Cols k(j.cols, j.rows);
   const int lane = G > 64 ? (int)threadIdx.x : threadIdx.x % G, wave = threadIdx.x / 64;
   float* const out[2] = {j.grid == 1 ? j.dgamma : j.part + (int64_t)(2 * blockIdx.x) * k.n,
@@ -683,7 +682,7 @@ __global__ __launch_bounds__(NT) void k_norm_backward_split(BackwardArgs<RES> j)
     backward_columns<T, RES, NT, LC, FC>(j, blockIdx.x);
   } else {
     float none[CH][8];
-    backward_rows<T, RES, G, CH, F, false>(j, (int64_t)(blockIdx.x - j.col_blocks) * RPB + group_of_thread<G>(),
+    backward_rows<T, RES, G, CH, F, false, true>(j, (int64_t)(blockIdx.x - j.col_blocks) * RPB + group_of_thread<G>(),
                                            (int64_t)(j.grid - j.col_blocks) * RPB, none, none);
   }
 }
@@ -841,13 +840,17 @@ hipError_t backward_with(const NormJob& j, const BackwardPlan& p, hipStream_t st
   if (!chunks_fit((j.cols + 7) / 8, lanes, CH)) return hipErrorInvalidConfiguration;
   BackwardArgs<RES> a;
   if constexpr (RES) {
+    // an absent operand becomes one that changes nothing: ds is read from v and
+    // not added, dr goes where dx is written after it, dx where dr is, undropped
     a.d = j.d;
-    a.ds = j.ds;
-    a.dx = j.dx;
+    a.add = j.ds.p != nullptr;
+    a.ds = j.ds.p ? j.ds : j.v;
+    a.dx = j.dx.p ? j.dx : j.dr;
+    if (!j.dx.p) a.d.thr = 0;
   }
   a.v = j.v;
   a.dy = j.dy;
-  a.dr = j.dr;
+  a.dr = j.dr.p ? j.dr : j.dx;
   a.gamma = j.gamma;
   a.stats = j.stats;
   a.dgamma = j.dgamma;
