@@ -34,6 +34,7 @@
 
 #include "../../include/vfl.h"
 #include "kernels.h"
+#include "rowops.h"
 
 using namespace vfl;
 

@@ -11,7 +11,7 @@
 #include <type_traits>
 
 #include "device.h"
-#include "kernels.h"
+#include "rowops.h"
 
 namespace vfl {
 namespace {

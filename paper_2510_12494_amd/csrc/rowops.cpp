@@ -6,7 +6,7 @@
 #include <cstring>
 
 #include "../../include/vfl.h"
-#include "kernels.h"
+#include "rowops.h"
 
 using namespace vfl;
 

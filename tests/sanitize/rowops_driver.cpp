@@ -12,7 +12,7 @@
 #include <random>
 
 #include "../../include/vfl.h"
-#include "../../paper_2510_12494_amd/csrc/kernels.h"
+#include "../../paper_2510_12494_amd/csrc/rowops.h"
 
 namespace {
 int launched = 0, fails = 0;
