@@ -8,7 +8,8 @@ that train their own party model.
 
 and the embedding is the last y.  The dropouts, norms and joins run in the
 library's kernels (vfl_dropout, vfl_layernorm_*, vfl_residual_*), the products
-in torch's matmul.  Parameters are float32 masters with operand copies in the
+in torch's matmul, whose results have the tower's dtype (a weight gradient is
+rounded to it once, as the gradients it is a product of are).  Parameters are float32 masters with operand copies in the
 tower's dtype, as in the library's own models; buffers and call descriptors are
 made once, for at most ``max_rows`` rows.  A dropout mask follows from (seed,
 step, layer, sample id), so the backward pass stores none and a sample's mask
@@ -24,7 +25,8 @@ EPS = 1e-5
 
 
 def _set(m, t: torch.Tensor):
-    m.data, m.ld = t.data_ptr(), t.stride(0)
+    # a single row's stride is of no use and may be anything
+    m.data, m.ld = t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
 class ResidualTower:
@@ -35,7 +37,11 @@ class ResidualTower:
                  p: float = 0.1, seed: int = 0, device: str = "cuda:0"):
         self.d_in, self.width, self.hidden, self.blocks, self.max_rows = d_in, width, hidden, blocks, max_rows
         self.p, self.seed = p, seed
-        self.dev, self.bf16 = torch.device(device), dtype == "bf16"
+        if dtype not in ("bf16", "f32"):
+            raise ValueError(f"dtype must be 'bf16' or 'f32', not {dtype!r}")
+        dev = torch.device(device)
+        self.dev = dev if dev.index is not None else torch.device(dev.type, torch.cuda.current_device())
+        self.bf16, self.trained = dtype == "bf16", 0        # rows whose training forward the buffers hold
         self.tdt = torch.bfloat16 if self.bf16 else torch.float32
         g = torch.Generator().manual_seed(seed)
 
@@ -110,13 +116,16 @@ class ResidualTower:
         self.norm0.rows = rows
         return torch.cuda.current_stream(self.dev).cuda_stream
 
+    @torch.no_grad()
     def forward(self, x: torch.Tensor, row0: int = 0, step: int = 0, train: bool = True) -> torch.Tensor:
-        """The embedding of rows ``x`` (global sample ids from ``row0``); without
-        ``train`` nothing is dropped (scoring)."""
-        rows = x.shape[0]
-        if not 1 <= rows <= self.max_rows or x.shape[1] != self.d_in or x.dtype != self.tdt:
-            raise ValueError(f"x must be [1..{self.max_rows} x {self.d_in}] of {self.tdt}")
-        c = self.copies
+        """The embedding of rows ``x`` (global sample ids from ``row0``), a view of
+        the tower's buffer that the next forward overwrites; without ``train``
+        nothing is dropped (scoring)."""
+        if (x.dim() != 2 or not 1 <= x.shape[0] <= self.max_rows or x.shape[1] != self.d_in or x.dtype != self.tdt
+                or x.device != self.dev):
+            raise ValueError(f"x must be [1..{self.max_rows} x {self.d_in}] of {self.tdt} on {self.dev}")
+        rows, c = x.shape[0], self.copies
+        self.trained = 0
         with torch.cuda.device(self.dev):
             st = self._call(rows, row0, step, self.p if train else 0.0)
             self.x = x
@@ -129,11 +138,16 @@ class ResidualTower:
                 V.vfl_dropout(self.drops[l], st)
                 torch.matmul(a, c[f"W2.{l}"].T, out=self.branch[:rows])
                 V.vfl_residual_forward(self.joins[l], st)
+        if train:
+            self.trained = rows
         return self.y[self.blocks][:rows]
 
+    @torch.no_grad()
     def backward(self, dz: torch.Tensor):
         """Gradients of every parameter into ``grads`` for the gradient ``dz`` of
-        the last training forward's embedding."""
+        the last forward's embedding, which has to be a training one."""
+        if not self.trained or dz.shape != (self.trained, self.width) or dz.device != self.dev:
+            raise ValueError(f"dz must be [{self.trained} x {self.width}] on {self.dev}, of a training forward's rows")
         rows, G, c = dz.shape[0], self.grads, self.copies
         with torch.cuda.device(self.dev):
             st = torch.cuda.current_stream(self.dev).cuda_stream
@@ -158,6 +172,7 @@ class ResidualTower:
             ds += self.dbranch[:rows]
             G["W_in"].copy_(torch.matmul(ds.T, self.x))
 
+    @torch.no_grad()
     def sgd(self, lr: float):
         for k, v in self.params.items():
             v.add_(self.grads[k], alpha=-lr)

@@ -91,3 +91,36 @@ def test_refusals():
     for bad in (torch.zeros(65, 16), torch.zeros(4, 15), torch.zeros(4, 16, dtype=torch.bfloat16), torch.zeros(0, 16)):
         with pytest.raises(ValueError):
             t.forward(bad.cuda())
+
+
+def test_backward_needs_the_training_forward_of_its_rows():
+    from paper_2510_12494_amd.tower import ResidualTower
+    t = ResidualTower(16, 32, 32, 1, 64, "f32")
+    x = torch.randn(64, 16, generator=torch.Generator().manual_seed(1)).cuda()
+    dz = torch.ones(64, 32, device="cuda")
+    with pytest.raises(ValueError):
+        t.backward(dz)                                        # no forward yet
+    t.forward(x)
+    for bad in (dz[:63], dz[:, :31], dz.cpu()):
+        with pytest.raises(ValueError):
+            t.backward(bad)
+    t.backward(dz)
+    t.forward(x[:1], train=False)                             # scoring takes the buffers
+    with pytest.raises(ValueError):
+        t.backward(dz)
+    with pytest.raises(ValueError):
+        ResidualTower(16, 32, 32, 1, 64, "f16")
+
+
+def test_gradient_of_one_row_in_any_layout():
+    """A single row's stride says nothing about its length."""
+    from paper_2510_12494_amd.tower import ResidualTower
+    t = ResidualTower(16, 32, 32, 1, 64, "f32")
+    g = torch.Generator().manual_seed(2)
+    x, dz = torch.randn(1, 16, generator=g).cuda(), torch.randn(32, 1, generator=g).cuda()
+    t.forward(x)
+    t.backward(dz.T)                                          # strides (1, 1)
+    got = {k: v.clone() for k, v in t.grads.items()}
+    t.backward(dz.T.reshape(-1).reshape(1, 32).clone())
+    assert all(torch.equal(got[k], v) for k, v in t.grads.items())
+    assert t.grads["gamma.0"].abs().max() > 0
