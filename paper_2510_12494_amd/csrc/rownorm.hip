@@ -453,7 +453,7 @@ __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_
                                               float (&ab)[CH][8]) {
   constexpr bool WIDE = G > 64;
   constexpr int GL = G < 64 ? G : 64;
-  constexpr bool AHEAD = G < 1024, HOIST = CH <= 2;
+  constexpr bool AHEAD = G < 1024 || CH == 1, HOIST = CH <= 2;
   static_assert(!(ACC && CH > 2), "registers");
   __shared__ f32x2 slots[2][WIDE ? 16 : 1];
   const Cols k(j.cols, j.rows);
@@ -818,6 +818,11 @@ BackwardPlan backward_plan(int64_t rows, int cols, Elt e, bool weights) {
   } else if (weights && rows > (wide ? kFewWide : kFew) && p.chunks <= 2) {
     // bf16 rows of few wavefronts take two chunks a lane: twice the bytes in flight
     if (wide && per <= 384 && e == BF16) p.chunks = 2;
+    // one chunk a lane in twice the wavefronts: their number then differs less
+    // from SIMD to SIMD (1537 x 5001 residual, float32 40.7 -> 38.4 us, bf16
+    // 29.0 -> 26.0; at 8192 columns, whole wavefronts either way, 59.1 -> 57.9
+    // and 33.1 both)
+    if (per > 512 && per <= 1024) p.lanes = 1024, p.chunks = 1;
     if (wide) p.threads = wide_threads(per, p.chunks);
     // the rows dealt out evenly to workgroups of eight wavefronts in all a CU
     const int64_t most = 256 * std::max(1, 512 / p.threads);
@@ -870,24 +875,28 @@ hipError_t backward_with(const NormJob& j, const BackwardPlan& p, hipStream_t st
       return hipGetLastError();
     }
   }
-  auto run = [&](int col_blocks, int row_blocks) {
-    a.col_blocks = col_blocks;
-    a.grid = col_blocks + row_blocks;
-    if (a.grid == 0) return;
-    if (exact)
-      hipLaunchKernelGGL((k_norm_backward_split<T, RES, G, CH, nt, kExact>), dim3(a.grid), dim3(nt), 0, st, a);
-    else
-      hipLaunchKernelGGL((k_norm_backward_split<T, RES, G, CH, nt, other>), dim3(a.grid), dim3(nt), 0, st, a);
-  };
-  const int row_blocks = j.dr.p || j.dx.p ? p.row_blocks : 0;
-  auto over = [&](const Mat& m) { return m.p && (m.p == j.dy.p || m.p == j.v.p); };
-  if (row_blocks > 0 && (over(j.dr) || over(j.dx))) {   // in place: the columns first
-    run(p.col_blocks, 0);
-    run(0, row_blocks);
+  if constexpr (G == 1024 && CH == 1) {              // many rows only
+    return hipErrorInvalidConfiguration;
   } else {
-    run(p.col_blocks, row_blocks);
+    auto run = [&](int col_blocks, int row_blocks) {
+      a.col_blocks = col_blocks;
+      a.grid = col_blocks + row_blocks;
+      if (a.grid == 0) return;
+      if (exact)
+        hipLaunchKernelGGL((k_norm_backward_split<T, RES, G, CH, nt, kExact>), dim3(a.grid), dim3(nt), 0, st, a);
+      else
+        hipLaunchKernelGGL((k_norm_backward_split<T, RES, G, CH, nt, other>), dim3(a.grid), dim3(nt), 0, st, a);
+    };
+    const int row_blocks = j.dr.p || j.dx.p ? p.row_blocks : 0;
+    auto over = [&](const Mat& m) { return m.p && (m.p == j.dy.p || m.p == j.v.p); };
+    if (row_blocks > 0 && (over(j.dr) || over(j.dx))) {   // in place: the columns first
+      run(p.col_blocks, 0);
+      run(0, row_blocks);
+    } else {
+      run(p.col_blocks, row_blocks);
+    }
+    return hipGetLastError();
   }
-  return hipGetLastError();
 }
 
 template <typename T, bool RES>
@@ -901,7 +910,9 @@ hipError_t backward(const NormJob& j, const BackwardPlan& p, hipStream_t st) {
     case 32: return backward_with<T, RES, 32, 1>(j, p, st);
     case 64: return p.chunks == 1 ? backward_with<T, RES, 64, 1>(j, p, st) : backward_with<T, RES, 64, 2>(j, p, st);
     case 512: return p.chunks == 1 ? backward_with<T, RES, 512, 1>(j, p, st) : backward_with<T, RES, 512, 2>(j, p, st);
-    default: return p.chunks == 2 ? backward_with<T, RES, 1024, 2>(j, p, st) : backward_with<T, RES, 1024, 4>(j, p, st);
+    default:
+      if (p.chunks == 1) return backward_with<T, RES, 1024, 1>(j, p, st);
+      return p.chunks == 2 ? backward_with<T, RES, 1024, 2>(j, p, st) : backward_with<T, RES, 1024, 4>(j, p, st);
   }
 }
 
