@@ -48,7 +48,7 @@ struct BackwardArgs : std::conditional_t<RES, BackwardResidual, NoResidual> {
   const float *gamma, *stats;
   float *dgamma, *dbeta, *part;
   int64_t rows;
-  int cols, grid, threads, col_blocks;
+  int cols, grid, lanes, groups, col_blocks;       // lanes: threads of a wide row
 };
 struct ReduceArgs {
   const float* part;
@@ -292,6 +292,11 @@ __device__ __forceinline__ int group_of_thread() {
   return G >= 64 ? __builtin_amdgcn_readfirstlane(g) : g;
 }
 
+// That of a wavefront where `lanes` threads hold a row.
+__device__ __forceinline__ int group_of_wave(int lanes) {
+  return __builtin_amdgcn_readfirstlane(threadIdx.x / 64) / (lanes / 64);
+}
+
 // ------------------------------------------------------------------ forward
 // Up to G = 64 lanes hold a row, CH chunks each (chunk c * G + lane), and a
 // workgroup kThreads / G rows; wider rows (G = 512 or 1024) take a workgroup of
@@ -445,20 +450,24 @@ __device__ __forceinline__ float stride_sum(float v) {
   return v;
 }
 
-// Rows first, first + stride, ... as in the forward, one pass.  ACC: a thread
-// also adds its columns' terms of the weights' gradients to ag and ab (not with
-// four chunks a lane, which leave no registers for those).
+// Rows first, first + stride, ... as in the forward, one pass.  G = 256: a
+// workgroup's groups of wavefronts take a row each, with barriers in common;
+// those without a row left go along.  ACC: a thread also adds its columns' terms
+// of the weights' gradients to ag and ab (not with four chunks a lane, which
+// leave no registers for those).
 template <typename T, bool RES, int G, int CH, Form F, bool ACC, bool OUT>
 __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_t r, int64_t stride, float (&ag)[CH][8],
                                               float (&ab)[CH][8]) {
   constexpr bool WIDE = G > 64;
   constexpr int GL = G < 64 ? G : 64;
+  constexpr bool GROUPS = G == 256;
   constexpr bool AHEAD = G < 1024 || CH == 1, HOIST = CH <= 2;
   static_assert(!(ACC && CH > 2), "registers");
   __shared__ f32x2 slots[2][WIDE ? 16 : 1];
   const Cols k(j.cols, j.rows);
-  const int lanes = WIDE ? j.threads : G;
-  const int lane = WIDE ? (int)threadIdx.x : threadIdx.x % G;
+  const int lanes = WIDE ? j.lanes : G;
+  const int group = GROUPS ? group_of_wave(lanes) : 0;
+  const int lane = WIDE ? (int)threadIdx.x - group * lanes : threadIdx.x % G;
   const float inv = 1.f / (float)k.n;
   bool add = false, drop = false;
   if constexpr (RES) {
@@ -479,7 +488,8 @@ __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_
       if constexpr (RES && OUT) sr[c] = load_chunk<F>(row_of<T>(j.ds, r), q, k, edge, c < CH / 2);
     }
   };
-  if (AHEAD && r < j.rows) fetch(r);
+  if constexpr (GROUPS) fetch(min(r, j.rows - 1));
+  else if (AHEAD && r < j.rows) fetch(r);
   uint32_t step = 0;
   if constexpr (RES) step = step_of(j.d);
 
@@ -494,7 +504,8 @@ __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_
     for (int c = 0; c < CH; ++c) weights(c, c);
 
   int flip = 0;
-  for (; r < j.rows; r += stride) {
+  for (; r - group < j.rows; r += stride) {          // as often for every group
+    const bool live = !GROUPS || r < j.rows;
     if constexpr (!AHEAD) fetch(r);
     Numbers n[CH];
     if constexpr (RES && AHEAD && OUT) {
@@ -508,26 +519,28 @@ __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_
     Raw<T> sc[CH];
     float h[CH][8], g[CH][8];
     float sg = 0.f, sgh = 0.f;
+    if (live) {
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      const int q = c * lanes + lane;
-      if constexpr (!HOIST) weights(c, 0);
-      chunk_values<F>(xr[c], q, k, edge, h[c], c < CH / 2);
-      chunk_values<F>(yr[c], q, k, edge, g[c], c < CH / 2);
-      if constexpr (RES && OUT) sc[c] = sr[c];
+      for (int c = 0; c < CH; ++c) {
+        const int q = c * lanes + lane;
+        if constexpr (!HOIST) weights(c, 0);
+        chunk_values<F>(xr[c], q, k, edge, h[c], c < CH / 2);
+        chunk_values<F>(yr[c], q, k, edge, g[c], c < CH / 2);
+        if constexpr (RES && OUT) sc[c] = sr[c];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        h[c][i] = (h[c][i] - mean) * rs;
-        if constexpr (ACC) {
-          ag[c][i] = fmaf(g[c][i], h[c][i], ag[c][i]);
-          ab[c][i] += g[c][i];
+        for (int i = 0; i < 8; ++i) {
+          h[c][i] = (h[c][i] - mean) * rs;
+          if constexpr (ACC) {
+            ag[c][i] = fmaf(g[c][i], h[c][i], ag[c][i]);
+            ab[c][i] += g[c][i];
+          }
+          g[c][i] *= gm[HOIST ? c : 0][i];
+          sg += g[c][i];
+          sgh = fmaf(g[c][i], h[c][i], sgh);
         }
-        g[c][i] *= gm[HOIST ? c : 0][i];
-        sg += g[c][i];
-        sgh = fmaf(g[c][i], h[c][i], sgh);
       }
     }
-    if (AHEAD) fetch(r + stride < j.rows ? r + stride : r);
+    if (AHEAD) fetch(r + stride < j.rows ? r + stride : GROUPS ? min(r, j.rows - 1) : r);
     if constexpr (!OUT) continue;
     sg = group_sum<GL>(sg);
     sgh = group_sum<GL>(sgh);
@@ -535,11 +548,12 @@ __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_
       if (threadIdx.x % 64 == 0) slots[flip][threadIdx.x / 64] = f32x2{sg, sgh};
       __syncthreads();
       const int w = threadIdx.x % 16;
-      const f32x2 s = 64 * w < lanes ? slots[flip][w] : f32x2{0.f, 0.f};
+      const f32x2 s = 64 * w < lanes ? slots[flip][group * (lanes / 64) + w] : f32x2{0.f, 0.f};
       sg = group_sum<16>(s[0]);
       sgh = group_sum<16>(s[1]);
       flip ^= 1;
     }
+    if (!live) continue;
     const float mg = sg * inv, mgh = sgh * inv;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -571,15 +585,18 @@ __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_
 // one workgroup.
 template <typename T, bool RES, int G, int CH, int NT, Form F>
 __global__ __launch_bounds__(NT) void k_norm_backward(BackwardArgs<RES> j) {
-  constexpr int NW = NT / 64, RPB = G > 64 ? 1 : NT / G;
+  constexpr int NW = NT / 64;
   constexpr int GL = G < 64 ? G : 64;
-  __shared__ float sums[G > 64 ? 1 : NW][G > 64 ? 1 : GL * 8];
+  constexpr bool GROUPS = G == 256;
+  __shared__ float sums[G > 256 ? 1 : NW][G > 256 ? 1 : GL * 8];
   float ag[CH][8] = {}, ab[CH][8] = {};
-  const int64_t first = (int64_t)blockIdx.x * RPB + group_of_thread<G>(), stride = (int64_t)j.grid * RPB;
+  const int group = GROUPS ? group_of_wave(j.lanes) : G > 64 ? 0 : group_of_thread<G>();
+  const int rpb = GROUPS ? j.groups : G > 64 ? 1 : NT / G;
+  const int64_t first = (int64_t)blockIdx.x * rpb + group, stride = (int64_t)j.grid * rpb;
   if (j.dr.p) backward_rows<T, RES, G, CH, F, true, true>(j, first, stride, ag, ab);
   else backward_rows<T, RES, G, CH, F, true, false>(j, first, stride, ag, ab);
   const Cols k(j.cols, j.rows);
-  const int lane = G > 64 ? (int)threadIdx.x : threadIdx.x % G, wave = threadIdx.x / 64;
+  const int lane = G > 64 ? (int)threadIdx.x - group * j.lanes : threadIdx.x % G, wave = threadIdx.x / 64;
   float* const out[2] = {j.grid == 1 ? j.dgamma : j.part + (int64_t)(2 * blockIdx.x) * k.n,
                          j.grid == 1 ? j.dbeta : j.part + (int64_t)(2 * blockIdx.x + 1) * k.n};
 #pragma unroll
@@ -589,7 +606,21 @@ __global__ __launch_bounds__(NT) void k_norm_backward(BackwardArgs<RES> j) {
       float* const dst = out[a];
       float(&acc)[8] = a == 0 ? ag[c] : ab[c];
       if constexpr (G > 64) {
-        if (dst) store_chunk<F>(dst, c * j.threads + lane, k, acc, c < CH / 2);
+        if (GROUPS && j.groups > 1) {
+          f32x4* const mine = (f32x4*)&sums[0][8 * threadIdx.x];
+          __syncthreads();                           // the previous sums have been read
+          if (group > 0) {
+            mine[0] = f32x4{acc[0], acc[1], acc[2], acc[3]};
+            mine[1] = f32x4{acc[4], acc[5], acc[6], acc[7]};
+          }
+          __syncthreads();
+          if (group > 0) continue;
+          for (int g = 1; g < j.groups; ++g) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[i] += (&sums[0][0])[8 * (g * j.lanes + lane) + i];
+          }
+        }
+        if (dst) store_chunk<F>(dst, c * j.lanes + lane, k, acc, c < CH / 2);
       } else {
         if constexpr (GL < 64)
           for (int i = 0; i < 8; ++i) acc[i] = stride_sum<GL>(acc[i]);
@@ -797,7 +828,8 @@ constexpr int kFew = 1024, kFewWide = 1536;
 // How a backward pass over rows x cols runs.
 struct BackwardPlan {
   int lanes, chunks;     // G and CH of the kernels
-  int threads;           // of a workgroup
+  int threads;           // of a row that takes several wavefronts, else of a workgroup
+  int groups;            // rows that k_norm_backward's workgroup holds, where wide
   int parts;             // workgroups of k_norm_backward (0: k_norm_backward_split)
   int room;              // parts that these or fewer rows may take
   int col_blocks, row_blocks;   // of k_norm_backward_split
@@ -811,21 +843,32 @@ BackwardPlan backward_plan(int64_t rows, int cols, Elt e, bool weights) {
   if (wide) p.lanes = per <= 1024 ? 512 : 1024;
   p.chunks = per <= 64 ? 1 : per <= 128 ? 2 : per <= 512 ? 1 : per <= 2048 ? 2 : 4;
   p.threads = backward_threads(p.lanes);
+  p.groups = 1;
   const int rpb = wide ? 1 : p.threads / p.lanes;
-  const int64_t blocks = (rows + rpb - 1) / rpb;
+  int64_t blocks = (rows + rpb - 1) / rpb;
   if (weights && blocks == 1 && p.chunks <= 2) {
     p.parts = 1;
   } else if (weights && rows > (wide ? kFewWide : kFew) && p.chunks <= 2) {
     // bf16 rows of few wavefronts take two chunks a lane: twice the bytes in flight
     if (wide && per <= 384 && e == BF16) p.chunks = 2;
+    // the workgroups of narrow wide rows hold as many of them as fill eight
+    // wavefronts, so that fewer partial pairs are written and read: 2500 x 2048
+    // bf16 12.4 us, 15.6 with a row each; residual 8000 x 1500 bf16 33.1, 35.6;
+    // 8000 x 2048 float32 40.8, 42.1.  Not float32 rows of three wavefronts:
+    // 8000 x 1032 26.9, 25.3 with a row each
+    if (wide && per <= 256 && (e == BF16 || per > 192)) p.lanes = 256;
     // one chunk a lane in twice the wavefronts: their number then differs less
     // from SIMD to SIMD (1537 x 5001 residual, float32 40.7 -> 38.4 us, bf16
     // 29.0 -> 26.0; at 8192 columns, whole wavefronts either way, 59.1 -> 57.9
     // and 33.1 both)
     if (per > 512 && per <= 1024) p.lanes = 1024, p.chunks = 1;
     if (wide) p.threads = wide_threads(per, p.chunks);
+    if (p.lanes == 256) {
+      p.groups = 512 / p.threads;
+      blocks = (rows + p.groups - 1) / p.groups;
+    }
     // the rows dealt out evenly to workgroups of eight wavefronts in all a CU
-    const int64_t most = 256 * std::max(1, 512 / p.threads);
+    const int64_t most = 256 * std::max(1, 512 / (p.threads * p.groups));
     const int64_t rounds = (blocks + most - 1) / most;
     p.parts = (int)((blocks + rounds - 1) / rounds);
     p.room = (int)std::min(blocks, most);
@@ -863,19 +906,21 @@ hipError_t backward_with(const NormJob& j, const BackwardPlan& p, hipStream_t st
   a.part = j.part;
   a.rows = j.rows;
   a.cols = j.cols;
-  a.threads = p.threads;
+  a.lanes = p.threads;
+  a.groups = p.groups;
   a.col_blocks = 0;
   if constexpr (CH <= 2) {
     if (p.parts > 0) {
       a.grid = p.parts;
+      const dim3 threads(p.threads * p.groups);
       if (exact)
-        hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, kExact>), dim3(p.parts), dim3(p.threads), 0, st, a);
+        hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, kExact>), dim3(p.parts), threads, 0, st, a);
       else
-        hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, other>), dim3(p.parts), dim3(p.threads), 0, st, a);
+        hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, other>), dim3(p.parts), threads, 0, st, a);
       return hipGetLastError();
     }
   }
-  if constexpr (G == 1024 && CH == 1) {              // many rows only
+  if constexpr (G == 256 || (G == 1024 && CH == 1)) {   // many rows only
     return hipErrorInvalidConfiguration;
   } else {
     auto run = [&](int col_blocks, int row_blocks) {
@@ -909,6 +954,7 @@ hipError_t backward(const NormJob& j, const BackwardPlan& p, hipStream_t st) {
     case 16: return backward_with<T, RES, 16, 1>(j, p, st);
     case 32: return backward_with<T, RES, 32, 1>(j, p, st);
     case 64: return p.chunks == 1 ? backward_with<T, RES, 64, 1>(j, p, st) : backward_with<T, RES, 64, 2>(j, p, st);
+    case 256: return backward_with<T, RES, 256, sizeof(T) == 2 ? 2 : 1>(j, p, st);
     case 512: return p.chunks == 1 ? backward_with<T, RES, 512, 1>(j, p, st) : backward_with<T, RES, 512, 2>(j, p, st);
     default:
       if (p.chunks == 1) return backward_with<T, RES, 1024, 1>(j, p, st);

@@ -711,3 +711,22 @@ def test_values_between_rows_have_no_influence(V, dt, cols):
     y.put(d.y)
     V.vfl_dropout(d)
     assert not bool(y.t.isnan().any())
+
+
+@pytest.mark.parametrize("dt", DTS)
+@pytest.mark.parametrize("rows,cols", [(1537, 1025), (1538, 1600), (1541, 2048), (1543, 1800), (2049, 2041), (1539, 2049),
+                                       (1537, 8191)])
+def test_rows_that_leave_part_of_a_workgroup_idle(V, dt, rows, cols):
+    c = Call(V, "residual", dt, rows, cols, (cols + 15) // 8 * 8 + 1, 3, p=0.4)
+    c.forward()
+    c.backward()
+    c.check_backward()
+    c.guards()
+    dgamma, dbeta = c.dgamma.clone(), c.dbeta.clone()
+    c.backward()
+    assert torch.equal(dgamma, c.dgamma) and torch.equal(dbeta, c.dbeta)       # the same sums in the same order
+    c.a.dr.data = c.a.dx.data = None                                           # weights' gradients alone
+    c.dgamma.fill_(0.0)
+    c.dbeta.fill_(0.0)
+    c.backward()
+    assert torch.equal(dgamma[:cols], c.dgamma[:cols]) and torch.equal(dbeta[:cols], c.dbeta[:cols])
