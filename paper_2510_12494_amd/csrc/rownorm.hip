@@ -819,11 +819,17 @@ constexpr int backward_threads(int G) { return G > 512 ? G : 512; }
 
 // Rows up to which a backward pass reads x and dy twice in one launch instead of
 // leaving partial sums to a second one.  The columns' workgroups take a time
-// that grows with the rows; the second launch costs about 4 us, and writing and
-// reading the partial sums most for wide rows.  Both ways: 920 x 656 float32
-// 7.2 us against 7.8, 473 x 736 bf16 5.6 against 7.9; 1190 x 1388 float32 15.4
-// either way, 286 x 3791 7.8 against 11.5, 1010 x 7164 bf16 14.1 against 20.1.
-constexpr int kFew = 1024, kFewWide = 1536;
+// that grows with the rows, and with their bytes once these no longer come from
+// one cache; the second launch costs 2 to 4 us.  One launch against two, us:
+// 1536 x 64 6.6, 7.9, 2048 x 64 7.7, 8.0; 1280 x 256 float32 8.1, 7.9; bf16
+// layer norm 1024 x 500 7.9, 7.9, 1024 x 2048 9.9, 9.9, 768 x 5001 14.7, 13.8,
+// residual 1536 x 1500 13.8, 14.5; float32 layer norm 768 x 500 7.9, 7.9,
+// 768 x 1500 11.8, 9.8, residual 768 x 3000 17.5, 18.1, 1024 x 5001 34.4, 28.8.
+int64_t few_rows(int per, Elt e) {
+  if (per <= 16) return 1920;
+  if (per <= 32) return 1280;
+  return e == BF16 && per <= 512 ? 1152 : 768;
+}
 
 // How a backward pass over rows x cols runs.
 struct BackwardPlan {
@@ -848,7 +854,7 @@ BackwardPlan backward_plan(int64_t rows, int cols, Elt e, bool weights) {
   int64_t blocks = (rows + rpb - 1) / rpb;
   if (weights && blocks == 1 && p.chunks <= 2) {
     p.parts = 1;
-  } else if (weights && rows > (wide ? kFewWide : kFew) && p.chunks <= 2) {
+  } else if (weights && rows > few_rows(per, e) && p.chunks <= 2) {
     // bf16 rows of few wavefronts take two chunks a lane: twice the bytes in flight
     if (wide && per <= 384 && e == BF16) p.chunks = 2;
     // the workgroups of narrow wide rows hold as many of them as fill eight

@@ -730,3 +730,14 @@ def test_rows_that_leave_part_of_a_workgroup_idle(V, dt, rows, cols):
     c.dbeta.fill_(0.0)
     c.backward()
     assert torch.equal(dgamma[:cols], c.dgamma[:cols]) and torch.equal(dbeta[:cols], c.dbeta[:cols])
+
+
+@pytest.mark.parametrize("dt", DTS)
+@pytest.mark.parametrize("cols", [1, 5, 8, 9, 16, 24, 64, 72, 128, 129, 256, 260, 500, 512, 1000])
+@pytest.mark.parametrize("rows", [770, 1281, 1999])
+def test_narrow_rows_by_either_way_of_the_weights_gradients(V, dt, rows, cols):
+    c = Call(V, "norm", dt, rows, cols, (cols + 7) // 8 * 8, 1)
+    c.forward()
+    c.backward()
+    c.check_backward()
+    c.guards()
