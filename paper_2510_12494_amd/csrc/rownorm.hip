@@ -819,13 +819,17 @@ hipError_t forward_with(const NormJob& j, hipStream_t st) {
   return hipGetLastError();
 }
 
-// Rows of several wavefronts: up to about a round of workgroups, gamma and beta
-// are fetched beside the row (378 x 5578 bf16: 8.2 us, 8.5 after it); beyond
-// that, reading them after the row's sums leaves the registers to more
-// wavefronts (7311 x 4040 bf16: 47.4 us, 50.3 before).
+// Rows of several wavefronts: where a round of workgroups takes them all, gamma
+// and beta are fetched beside the row (residual 1024 x 2048 float32: 8.1 us, 8.8
+// after it); beyond that, reading them after the row's sums leaves the registers
+// to more workgroups (residual 896 x 5001 bf16 11.2 us, 16.8 before; 7311 x 4040
+// bf16 47.4, 50.3).  Eight wavefronts of two chunks a lane gain no workgroup by
+// it (residual 1024 x 8192 bf16 13.7 after, 12.8 before).
 template <typename T, bool RES, int G, int CH>
 hipError_t forward_wide(const NormJob& j, hipStream_t st) {
-  return j.rows <= 1024 ? forward_with<T, RES, G, CH, true>(j, st) : forward_with<T, RES, G, CH, false>(j, st);
+  const int per = (j.cols + 7) / 8;
+  const int64_t most = per <= 256 || per > 896 ? 1024 : 256;
+  return j.rows <= most ? forward_with<T, RES, G, CH, true>(j, st) : forward_with<T, RES, G, CH, false>(j, st);
 }
 
 // threads of a workgroup of the backward
