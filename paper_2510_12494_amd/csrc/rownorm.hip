@@ -166,21 +166,32 @@ __device__ __forceinline__ void store4(uint16_t* p, const float* v) {
 __device__ __forceinline__ void store4(float* p, const float* v) { *(f32x4_a4*)p = f32x4{v[0], v[1], v[2], v[3]}; }
 __device__ __forceinline__ void store2(uint16_t* p, const float* v) { *(u32_a2*)p = pack_bf16(v[0], v[1]); }
 __device__ __forceinline__ void store2(float* p, const float* v) { *(f32x2_a4*)p = f32x2{v[0], v[1]}; }
+// EARLY: the lines leave the L2 as they are written (a non-temporal store)
+// instead of all at the kernel's end.
+template <bool EARLY>
 __device__ __forceinline__ void store8(uint16_t* p, const float* v) {
-  *(u32x4_a2*)p = u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+  const u32x4_a2 w{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+  if constexpr (EARLY) __builtin_nontemporal_store(w, (u32x4_a2*)p);
+  else *(u32x4_a2*)p = w;
 }
+template <bool EARLY>
 __device__ __forceinline__ void store8(float* p, const float* v) {
-  store4(p, v);
-  store4(p + 4, v + 4);
+  if constexpr (EARLY) {
+    __builtin_nontemporal_store(f32x4_a4{v[0], v[1], v[2], v[3]}, (f32x4_a4*)p);
+    __builtin_nontemporal_store(f32x4_a4{v[4], v[5], v[6], v[7]}, (f32x4_a4*)(p + 4));
+  } else {
+    store4(p, v);
+    store4(p + 4, v + 4);
+  }
 }
 
 // Stores chunk q of a row: whole, or the columns that the row has of it, in
 // pieces of four, two and one.
-template <Form F, typename T>
+template <Form F, bool EARLY = false, typename T>
 __device__ __forceinline__ void store_chunk(T* row, int q, const Cols& k, const float (&v)[8], bool whole = false) {
   T* p = row + 8 * q;
   if (F == kExact || whole || 8 * q + 8 <= k.n) {
-    store8(p, v);
+    store8<EARLY>(p, v);
   } else if (q < k.per) {
     const int m = k.part;                          // uniform
     if (m & 4) {
@@ -313,7 +324,7 @@ __device__ __forceinline__ int group_of_wave(int lanes) {
 // bounds it: residual 32768 x 1024 bf16 46.3 us (5.8 TB/s), layer norm 32768 x
 // 512 bf16 11.1 us (6.1 TB/s, partly from the last-level cache); one row takes
 // 2.1 us, a kernel's launch.
-template <typename T, bool RES, int G, int CH, Form F, bool HOIST>
+template <typename T, bool RES, int G, int CH, Form F, bool HOIST, bool EARLY>
 __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(ForwardArgs<RES> j) {
   constexpr bool WIDE = G > 64;
   constexpr int RPB = WIDE ? 1 : kThreads / G;
@@ -393,7 +404,7 @@ __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(Fo
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       if constexpr (RES)
-        if (j.s.p) store_chunk<F>(out_row<T>(j.s, r), c * lanes + lane, k, v[c], c < CH / 2);
+        if (j.s.p) store_chunk<F, EARLY>(out_row<T>(j.s, r), c * lanes + lane, k, v[c], c < CH / 2);
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum += v[c][i];
     }
@@ -432,7 +443,7 @@ __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(Fo
       float y[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) y[i] = fmaf((v[c][i] - mean) * rs, g[at][i], b[at][i]);
-      store_chunk<F>(out_row<T>(j.y, r), c * lanes + lane, k, y, c < CH / 2);
+      store_chunk<F, EARLY>(out_row<T>(j.y, r), c * lanes + lane, k, y, c < CH / 2);
     }
   }
 }
@@ -461,7 +472,7 @@ __device__ __forceinline__ float stride_sum(float v) {
 // those without a row left go along.  ACC: a thread also adds its columns' terms
 // of the weights' gradients to ag and ab (not with four chunks a lane, which
 // leave no registers for those).
-template <typename T, bool RES, int G, int CH, Form F, bool ACC, bool OUT>
+template <typename T, bool RES, int G, int CH, Form F, bool ACC, bool OUT, bool EARLY>
 __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_t r, int64_t stride, float (&ag)[CH][8],
                                               float (&ab)[CH][8]) {
   constexpr bool WIDE = G > 64;
@@ -575,11 +586,11 @@ __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_
           for (int i = 0; i < 8; ++i) d[i] += t[i];
         }
       }
-      store_chunk<F>(out_row<T>(j.dr, r), q, k, d, c < CH / 2);
+      store_chunk<F, EARLY>(out_row<T>(j.dr, r), q, k, d, c < CH / 2);
       if constexpr (RES) {
         if (!AHEAD && drop) n[c] = chunk_numbers(j.d, step, j.d.row0 + r, q);
         if (drop) drop_values(j.d, n[c], d);
-        store_chunk<F>(out_row<T>(j.dx, r), q, k, d, c < CH / 2);
+        store_chunk<F, EARLY>(out_row<T>(j.dx, r), q, k, d, c < CH / 2);
       }
     }
   }
@@ -593,7 +604,7 @@ __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_
 // launch, about 8 us in all: residual 32768 x 1024 bf16 67.0 us (5.0 TB/s),
 // 1537 x 5001 float32 38.7 (4.0 TB/s), layer norm 262144 x 64 bf16 22.8 (4.5
 // TB/s; 24.2 with two workgroups a CU).
-template <typename T, bool RES, int G, int CH, int NT, Form F>
+template <typename T, bool RES, int G, int CH, int NT, Form F, bool EARLY>
 __global__ __launch_bounds__(NT) void k_norm_backward(BackwardArgs<RES> j) {
   constexpr int NW = NT / 64;
   constexpr int GL = G < 64 ? G : 64;
@@ -603,8 +614,8 @@ __global__ __launch_bounds__(NT) void k_norm_backward(BackwardArgs<RES> j) {
   const int group = GROUPS ? group_of_wave(j.lanes) : G > 64 ? 0 : group_of_thread<G>();
   const int rpb = GROUPS ? j.groups : G > 64 ? 1 : NT / G;
   const int64_t first = (int64_t)blockIdx.x * rpb + group, stride = (int64_t)j.grid * rpb;
-  if (j.dr.p) backward_rows<T, RES, G, CH, F, true, true>(j, first, stride, ag, ab);
-  else backward_rows<T, RES, G, CH, F, true, false>(j, first, stride, ag, ab);
+  if (j.dr.p) backward_rows<T, RES, G, CH, F, true, true, EARLY>(j, first, stride, ag, ab);
+  else backward_rows<T, RES, G, CH, F, true, false, false>(j, first, stride, ag, ab);
   const Cols k(j.cols, j.rows);
   const int lane = G > 64 ? (int)threadIdx.x - group * j.lanes : threadIdx.x % G, wave = threadIdx.x / 64;
   float* const out[2] = {j.grid == 1 ? j.dgamma : j.part + (int64_t)(2 * blockIdx.x) * k.n,
@@ -725,7 +736,7 @@ __global__ __launch_bounds__(NT) void k_norm_backward_split(BackwardArgs<RES> j)
     backward_columns<T, RES, NT, LC, FC>(j, blockIdx.x);
   } else {
     float none[CH][8];
-    backward_rows<T, RES, G, CH, F, false, true>(j, (int64_t)(blockIdx.x - j.col_blocks) * RPB + group_of_thread<G>(),
+    backward_rows<T, RES, G, CH, F, false, true, false>(j, (int64_t)(blockIdx.x - j.col_blocks) * RPB + group_of_thread<G>(),
                                            (int64_t)(j.grid - j.col_blocks) * RPB, none, none);
   }
 }
@@ -785,6 +796,25 @@ int wide_threads(int per, int CH) { return (per + 64 * CH - 1) / (64 * CH) * 64;
 // chunks fit, and the first half of a lane's are whole.
 bool chunks_fit(int per, int lanes, int CH) { return per <= lanes * CH && (CH == 1 || per > lanes * (CH / 2)); }
 
+// Whether the results of a call over many rows leave the L2s early.  These hold up
+// to 32 MB that a kernel's end has to write back; written early, that overlaps
+// with the rows' work, but what reads a large result next no longer finds a part
+// of it in a cache.  The time of the call, and of the call and a layer norm of
+// its result, us, late and early: layer norm of 8 MB (4194 x 1000 bf16) 5.5, 4.8
+// and 10.2, 9.2; 16 MB (4096 x 1024 float32) 7.6, 6.2 and 15.7, 12.6; 32 MB 12.0,
+// 11.2 and 25.8, 26.9; residual join of 12 MB each (6144 x 1024 bf16) 8.9, 6.2 and
+// 14.5, 13.8, its backward 14.9, 14.4 and 20.5, 19.9; of 24 MB each 24.9, 26.6
+// and 35.2, 37.7 (float32).  Rows of few bytes, whose stores end inside a line,
+// take longer (layer norm 262144 x 13 float32 10.2, 11.8).
+constexpr int64_t kEarlyOne = 16 << 20, kEarlyTwo = 12 << 20, kEarlyRow = 256;
+template <typename T>
+constexpr bool can_store_early(int chunks) { return chunks * 8 * (int)sizeof(T) >= kEarlyRow; }
+template <typename T>
+bool stores_early(int64_t rows, int cols, int results) {
+  const int64_t row = (int64_t)cols * (int64_t)sizeof(T), most = results > 1 ? kEarlyTwo : kEarlyOne;
+  return row >= kEarlyRow && rows <= most / row;
+}
+
 template <typename T, bool RES, int G, int CH, bool HOIST = G <= 64>
 hipError_t forward_with(const NormJob& j, hipStream_t st) {
   const int per = (j.cols + 7) / 8;
@@ -812,10 +842,16 @@ hipError_t forward_with(const NormJob& j, hipStream_t st) {
   a.threads = nt;
   a.eps = j.eps;
   constexpr Form other = G == 1 ? kSmall : kRagged;
-  if (j.cols == 8 * CH * lanes)
-    hipLaunchKernelGGL((k_norm_forward<T, RES, G, CH, kExact, HOIST>), dim3(grid), dim3(nt), 0, st, a);
-  else
-    hipLaunchKernelGGL((k_norm_forward<T, RES, G, CH, other, HOIST>), dim3(grid), dim3(nt), 0, st, a);
+  const bool exact = j.cols == 8 * CH * lanes;
+  if constexpr (can_store_early<T>(G * CH)) {
+    if (stores_early<T>(j.rows, j.cols, RES && j.s.p ? 2 : 1)) {
+      if (exact) hipLaunchKernelGGL((k_norm_forward<T, RES, G, CH, kExact, HOIST, true>), dim3(grid), dim3(nt), 0, st, a);
+      else hipLaunchKernelGGL((k_norm_forward<T, RES, G, CH, other, HOIST, true>), dim3(grid), dim3(nt), 0, st, a);
+      return hipGetLastError();
+    }
+  }
+  if (exact) hipLaunchKernelGGL((k_norm_forward<T, RES, G, CH, kExact, HOIST, false>), dim3(grid), dim3(nt), 0, st, a);
+  else hipLaunchKernelGGL((k_norm_forward<T, RES, G, CH, other, HOIST, false>), dim3(grid), dim3(nt), 0, st, a);
   return hipGetLastError();
 }
 
@@ -937,10 +973,15 @@ hipError_t backward_with(const NormJob& j, const BackwardPlan& p, hipStream_t st
     if (p.parts > 0) {
       a.grid = p.parts;
       const dim3 threads(p.threads * p.groups);
-      if (exact)
-        hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, kExact>), dim3(p.parts), threads, 0, st, a);
-      else
-        hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, other>), dim3(p.parts), threads, 0, st, a);
+      if constexpr (can_store_early<T>(G * CH)) {
+        if (stores_early<T>(j.rows, j.cols, RES && j.dr.p && j.dx.p ? 2 : 1)) {
+          if (exact) hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, kExact, true>), dim3(p.parts), threads, 0, st, a);
+          else hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, other, true>), dim3(p.parts), threads, 0, st, a);
+          return hipGetLastError();
+        }
+      }
+      if (exact) hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, kExact, false>), dim3(p.parts), threads, 0, st, a);
+      else hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, other, false>), dim3(p.parts), threads, 0, st, a);
       return hipGetLastError();
     }
   }
