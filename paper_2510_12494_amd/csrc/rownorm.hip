@@ -796,22 +796,25 @@ int wide_threads(int per, int CH) { return (per + 64 * CH - 1) / (64 * CH) * 64;
 // chunks fit, and the first half of a lane's are whole.
 bool chunks_fit(int per, int lanes, int CH) { return per <= lanes * CH && (CH == 1 || per > lanes * (CH / 2)); }
 
-// Whether the results of a call over many rows leave the L2s early.  These hold up
-// to 32 MB that a kernel's end has to write back; written early, that overlaps
-// with the rows' work, but what reads a large result next no longer finds a part
-// of it in a cache.  The time of the call, and of the call and a layer norm of
-// its result, us, late and early: layer norm of 8 MB (4194 x 1000 bf16) 5.5, 4.8
-// and 10.2, 9.2; 16 MB (4096 x 1024 float32) 7.6, 6.2 and 15.7, 12.6; 32 MB 12.0,
+// Whether the results of a call (of a backward pass: over many rows) leave the
+// L2s early.  These hold up to 32 MB that a kernel's end has to write back;
+// written early, that overlaps with the rows' work, but what reads a large result
+// next no longer finds a part of it in a cache.  The time of the call, and of the
+// call and a layer norm of its result, us, late and early: layer norm of 8 MB
+// (4194 x 1000 bf16) 5.5, 4.8 and 10.2, 9.2; 16 MB (4096 x 1024 float32) 7.6, 6.2 and 15.7, 12.6; 32 MB 12.0,
 // 11.2 and 25.8, 26.9; residual join of 12 MB each (6144 x 1024 bf16) 8.9, 6.2 and
-// 14.5, 13.8, its backward 14.9, 14.4 and 20.5, 19.9; of 24 MB each 24.9, 26.6
-// and 35.2, 37.7 (float32).  Rows of few bytes, whose stores end inside a line,
-// take longer (layer norm 262144 x 13 float32 10.2, 11.8).
-constexpr int64_t kEarlyOne = 16 << 20, kEarlyTwo = 12 << 20, kEarlyRow = 256;
+// 14.5, 13.8; of 24 MB each (float32) 16.4, 19.1 and 27.3, 29.8; its backward of 8
+// MB each (2048 x 1024 float32) 12.0, 10.2 and 18.3, 16.6, of 24 MB each 24.9, 26.6
+// and 35.2, 37.7; a layer norm's backward of 16 MB (7813 x 500 float32) 12.0, 12.7.
+// Rows of few bytes, whose stores end inside a line, take longer (layer norm
+// 262144 x 13 float32 10.2, 11.8).
+constexpr int64_t kEarlyNorm = 16 << 20, kEarlyJoin = 12 << 20, kEarlyBackward = 8 << 20;   // bytes of a result
+constexpr int64_t kEarlyRow = 256;
 template <typename T>
 constexpr bool can_store_early(int chunks) { return chunks * 8 * (int)sizeof(T) >= kEarlyRow; }
 template <typename T>
-bool stores_early(int64_t rows, int cols, int results) {
-  const int64_t row = (int64_t)cols * (int64_t)sizeof(T), most = results > 1 ? kEarlyTwo : kEarlyOne;
+bool stores_early(int64_t rows, int cols, int64_t most) {
+  const int64_t row = (int64_t)cols * (int64_t)sizeof(T);
   return row >= kEarlyRow && rows <= most / row;
 }
 
@@ -844,7 +847,7 @@ hipError_t forward_with(const NormJob& j, hipStream_t st) {
   constexpr Form other = G == 1 ? kSmall : kRagged;
   const bool exact = j.cols == 8 * CH * lanes;
   if constexpr (can_store_early<T>(G * CH)) {
-    if (stores_early<T>(j.rows, j.cols, RES && j.s.p ? 2 : 1)) {
+    if (stores_early<T>(j.rows, j.cols, RES && j.s.p ? kEarlyJoin : kEarlyNorm)) {
       if (exact) hipLaunchKernelGGL((k_norm_forward<T, RES, G, CH, kExact, HOIST, true>), dim3(grid), dim3(nt), 0, st, a);
       else hipLaunchKernelGGL((k_norm_forward<T, RES, G, CH, other, HOIST, true>), dim3(grid), dim3(nt), 0, st, a);
       return hipGetLastError();
@@ -974,7 +977,7 @@ hipError_t backward_with(const NormJob& j, const BackwardPlan& p, hipStream_t st
       a.grid = p.parts;
       const dim3 threads(p.threads * p.groups);
       if constexpr (can_store_early<T>(G * CH)) {
-        if (stores_early<T>(j.rows, j.cols, RES && j.dr.p && j.dx.p ? 2 : 1)) {
+        if (stores_early<T>(j.rows, j.cols, kEarlyBackward)) {
           if (exact) hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, kExact, true>), dim3(p.parts), threads, 0, st, a);
           else hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, other, true>), dim3(p.parts), threads, 0, st, a);
           return hipGetLastError();
