@@ -848,14 +848,12 @@ hipError_t forward_with(const NormJob& j, hipStream_t st) {
   const bool exact = j.cols == 8 * CH * lanes;
   if constexpr (can_store_early<T>(G * CH)) {
     if (stores_early<T>(j.rows, j.cols, RES && j.s.p ? kEarlyJoin : kEarlyNorm)) {
-      if (exact) hipLaunchKernelGGL((k_norm_forward<T, RES, G, CH, kExact, HOIST, true>), dim3(grid), dim3(nt), 0, st, a);
-      else hipLaunchKernelGGL((k_norm_forward<T, RES, G, CH, other, HOIST, true>), dim3(grid), dim3(nt), 0, st, a);
-      return hipGetLastError();
+      return enqueue(exact ? k_norm_forward<T, RES, G, CH, kExact, HOIST, true>
+                           : k_norm_forward<T, RES, G, CH, other, HOIST, true>, grid, nt, a, st);
     }
   }
-  if (exact) hipLaunchKernelGGL((k_norm_forward<T, RES, G, CH, kExact, HOIST, false>), dim3(grid), dim3(nt), 0, st, a);
-  else hipLaunchKernelGGL((k_norm_forward<T, RES, G, CH, other, HOIST, false>), dim3(grid), dim3(nt), 0, st, a);
-  return hipGetLastError();
+  return enqueue(exact ? k_norm_forward<T, RES, G, CH, kExact, HOIST, false>
+                       : k_norm_forward<T, RES, G, CH, other, HOIST, false>, grid, nt, a, st);
 }
 
 // Rows of several wavefronts: where a round of workgroups takes them all, gamma
@@ -975,17 +973,15 @@ hipError_t backward_with(const NormJob& j, const BackwardPlan& p, hipStream_t st
   if constexpr (CH <= 2) {
     if (p.parts > 0) {
       a.grid = p.parts;
-      const dim3 threads(p.threads * p.groups);
+      const int threads = p.threads * p.groups;
       if constexpr (can_store_early<T>(G * CH)) {
         if (stores_early<T>(j.rows, j.cols, kEarlyBackward)) {
-          if (exact) hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, kExact, true>), dim3(p.parts), threads, 0, st, a);
-          else hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, other, true>), dim3(p.parts), threads, 0, st, a);
-          return hipGetLastError();
+          return enqueue(exact ? k_norm_backward<T, RES, G, CH, nt, kExact, true>
+                               : k_norm_backward<T, RES, G, CH, nt, other, true>, p.parts, threads, a, st);
         }
       }
-      if (exact) hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, kExact, false>), dim3(p.parts), threads, 0, st, a);
-      else hipLaunchKernelGGL((k_norm_backward<T, RES, G, CH, nt, other, false>), dim3(p.parts), threads, 0, st, a);
-      return hipGetLastError();
+      return enqueue(exact ? k_norm_backward<T, RES, G, CH, nt, kExact, false>
+                           : k_norm_backward<T, RES, G, CH, nt, other, false>, p.parts, threads, a, st);
     }
   }
   if constexpr (G == 256 || (G == 1024 && CH == 1)) {   // many rows only
@@ -994,21 +990,17 @@ hipError_t backward_with(const NormJob& j, const BackwardPlan& p, hipStream_t st
     auto run = [&](int col_blocks, int row_blocks) {
       a.col_blocks = col_blocks;
       a.grid = col_blocks + row_blocks;
-      if (a.grid == 0) return;
-      if (exact)
-        hipLaunchKernelGGL((k_norm_backward_split<T, RES, G, CH, nt, kExact>), dim3(a.grid), dim3(nt), 0, st, a);
-      else
-        hipLaunchKernelGGL((k_norm_backward_split<T, RES, G, CH, nt, other>), dim3(a.grid), dim3(nt), 0, st, a);
+      if (a.grid == 0) return hipSuccess;
+      return enqueue(exact ? k_norm_backward_split<T, RES, G, CH, nt, kExact>
+                           : k_norm_backward_split<T, RES, G, CH, nt, other>, a.grid, nt, a, st);
     };
     const int row_blocks = j.dr.p || j.dx.p ? p.row_blocks : 0;
     auto over = [&](const Mat& m) { return m.p && (m.p == j.dy.p || m.p == j.v.p); };
     if (row_blocks > 0 && (over(j.dr) || over(j.dx))) {   // in place: the columns first
-      run(p.col_blocks, 0);
-      run(0, row_blocks);
-    } else {
-      run(p.col_blocks, row_blocks);
+      const hipError_t e = run(p.col_blocks, 0);
+      return e == hipSuccess ? run(0, row_blocks) : e;
     }
-    return hipGetLastError();
+    return run(p.col_blocks, row_blocks);
   }
 }
 
@@ -1062,10 +1054,8 @@ hipError_t dropout(const DropJob& j, hipStream_t st) {
   const int grid = (int)std::min<int64_t>((chunks + kThreads - 1) / kThreads, kMany);
   const int64_t stride = (int64_t)grid * kThreads;
   const DropArgs a{j.d, j.x, j.y, j.rows, stride / per, j.cols, (int)(stride % per)};
-  if (j.cols % 8 == 0) hipLaunchKernelGGL((k_dropout<T, kExact>), dim3(grid), dim3(kThreads), 0, st, a);
-  else if (j.cols > 8) hipLaunchKernelGGL((k_dropout<T, kRagged>), dim3(grid), dim3(kThreads), 0, st, a);
-  else hipLaunchKernelGGL((k_dropout<T, kSmall>), dim3(grid), dim3(kThreads), 0, st, a);
-  return hipGetLastError();
+  return enqueue(j.cols % 8 == 0 ? k_dropout<T, kExact> : j.cols > 8 ? k_dropout<T, kRagged> : k_dropout<T, kSmall>,
+                 grid, kThreads, a, st);
 }
 
 hipError_t launch_dropout(Elt e, const DropJob& j, hipStream_t st) {
@@ -1086,11 +1076,8 @@ hipError_t launch_norm_backward(Elt e, const NormJob& j, hipStream_t st) {
   if (err != hipSuccess || p.parts <= 1) return err;
   const ReduceArgs a{j.part, j.dgamma, j.dbeta, j.cols, p.parts};
   // 64 columns a workgroup once they fill the CUs, else 16
-  if (2 * j.cols > 256 * 16)
-    hipLaunchKernelGGL((k_norm_reduce<64>), dim3((2 * j.cols + 63) / 64), dim3(kReduceThreads), 0, st, a);
-  else
-    hipLaunchKernelGGL((k_norm_reduce<16>), dim3((2 * j.cols + 15) / 16), dim3(kReduceThreads), 0, st, a);
-  return hipGetLastError();
+  if (2 * j.cols > 256 * 16) return enqueue(k_norm_reduce<64>, (2 * j.cols + 63) / 64, kReduceThreads, a, st);
+  return enqueue(k_norm_reduce<16>, (2 * j.cols + 15) / 16, kReduceThreads, a, st);
 }
 
 }  // namespace vfl

@@ -741,3 +741,33 @@ def test_narrow_rows_by_either_way_of_the_weights_gradients(V, dt, rows, cols):
     c.backward()
     c.check_backward()
     c.guards()
+
+
+@pytest.mark.parametrize("rows,cols", [(5, 40), (2100, 40)])
+def test_an_earlier_error_of_the_caller_is_not_this_calls(V, rows, cols):
+    """A failure that the caller has not asked for yet is neither reported by a
+    call that succeeds nor taken from the caller."""
+    lib = V.library()
+    c = Call(V, "residual", "f32", rows, cols, p=0.2)
+    n = Call(V, "norm", "f32", rows, cols)
+    y = Mat("f32", rows, cols)
+    d = V.vfl_dropout_args()
+    d.dtype, d.rows, d.cols = V.VFL_F32, rows, cols
+    key(d.drop, 0.5)
+    c.x.put(d.x)
+    y.put(d.y)
+    torch.cuda.synchronize()
+    try:
+        assert lib.hipSetDevice(-1) != 0             # refused on the host
+        before = lib.hipPeekAtLastError()
+        assert before != 0
+        for call in (lambda: V.vfl_dropout(d), c.forward, c.backward, n.forward, n.backward):
+            call()
+            assert lib.hipPeekAtLastError() == before
+    finally:
+        lib.hipGetLastError()
+    torch.cuda.synchronize()
+    assert ((y.np() != 0) == (keep(0.5, rows, cols) & (c.x.np() != 0))).all()
+    for m in (c, n):
+        m.check_forward()
+        m.check_backward()

@@ -163,3 +163,19 @@ def test_a_workspace_serves_every_smaller_batch(V, cols):
         n = V.vfl_norm_workspace_size(rows, cols)
         assert n >= last
         last = n
+
+
+def test_an_earlier_error_of_the_caller_is_not_this_calls(V):
+    """A backward pass of no rows without weights launches nothing: it succeeds
+    whatever the thread's last error is, and leaves that to the caller."""
+    lib = V.library()
+    assert lib.hipSetDevice(-1) != 0
+    before = lib.hipPeekAtLastError()
+    assert before != 0
+    for call in ("vfl_layernorm_backward", "vfl_residual_backward"):
+        a = _args(V, CALLS[call])
+        a.rows, a.dgamma, a.dbeta = 0, None, None
+        getattr(V, call)(a)
+        assert V.vfl_last_error(None) == ""
+        assert lib.hipPeekAtLastError() == before
+    lib.hipGetLastError()
