@@ -1372,7 +1372,7 @@ bool capture_record(vfl_ctx* c, hipEvent_t ev, hipStream_t st, int cls, int end)
     he = hipStreamUpdateCaptureDependencies(st, &node, 1, hipStreamSetCaptureDependencies);
   }
   if (he == hipSuccess) return true;
-  (void)hipGetLastError();   // do not leave it to the next launch's check
+  (void)hipGetLastError();   // reported below, not left to the caller
   if (c->tm_err == hipSuccess) {
     c->tm_err = he;
     c->tm_err_what = std::string(what) + (end ? " (end" : " (begin") + ", class " + std::to_string(cls) +

@@ -1324,11 +1324,11 @@ hipError_t raise_lds(K kernel) {
 
 #define VFL_CHAIN_RT(K, T, rt, ...)                                                         \
   do {                                                                                     \
-    if (rt == 1) hipLaunchKernelGGL((K<T, 1>), __VA_ARGS__);                               \
-    else if (rt == 2) hipLaunchKernelGGL((K<T, 2>), __VA_ARGS__);                          \
-    else if (rt == 3) hipLaunchKernelGGL((K<T, 3>), __VA_ARGS__);                          \
-    else if (rt == 4) hipLaunchKernelGGL((K<T, 4>), __VA_ARGS__);                          \
-    else return hipErrorInvalidValue;                                                      \
+    if (rt == 1) return enqueue(K<T, 1>, __VA_ARGS__);                                     \
+    if (rt == 2) return enqueue(K<T, 2>, __VA_ARGS__);                                     \
+    if (rt == 3) return enqueue(K<T, 3>, __VA_ARGS__);                                     \
+    if (rt == 4) return enqueue(K<T, 4>, __VA_ARGS__);                                     \
+    return hipErrorInvalidValue;                                                           \
   } while (0)
 #define VFL_CHAIN(K, e, rt, ...)                                                            \
   do {                                                                                     \
@@ -1341,19 +1341,16 @@ hipError_t raise_lds(K kernel) {
 hipError_t launch_fwd(Elt e, int rt, const FwdJob* job, int lds, int blocks, const ChainCall& c,
                       TickRef tr, hipStream_t st) {
   VFL_CHAIN(k_fwd, e, rt, lds, st, job, c, tr);
-  return hipGetLastError();
 }
 
 hipError_t launch_active(Elt e, int rt, const ActiveJob* job, int lds, int blocks,
                          const ChainCall& c, TickRef tr, hipStream_t st) {
   VFL_CHAIN(k_active, e, rt, lds, st, job, c, tr);
-  return hipGetLastError();
 }
 
 hipError_t launch_bwd(Elt e, int rt, const BwdJob* job, int lds, int blocks, const ChainCall& c,
                       TickRef tr, hipStream_t st) {
   VFL_CHAIN(k_bwd, e, rt, lds, st, job, c, tr);
-  return hipGetLastError();
 }
 
 namespace {

@@ -845,9 +845,7 @@ hipError_t launch_dw(Elt e, const DwJob* job, int blocks, int R, float scale, Ti
                      hipStream_t st) {
   if (blocks < 1) return hipErrorInvalidValue;
   const int grid = (blocks + 7) / 8 * 8;       // see dw_item
-  if (e == BF16) hipLaunchKernelGGL(k_dw<uint16_t>, dim3(grid), dim3(256), 0, st, job, R, scale, tr);
-  else hipLaunchKernelGGL(k_dw<float>, dim3(grid), dim3(256), 0, st, job, R, scale, tr);
-  return hipGetLastError();
+  return enqueue(e == BF16 ? k_dw<uint16_t> : k_dw<float>, dim3(grid), dim3(256), 0, st, job, R, scale, tr);
 }
 
 hipError_t dwt_init() {
@@ -856,34 +854,23 @@ hipError_t dwt_init() {
 
 hipError_t launch_dwt(const DwJob* job, int blocks, hipStream_t st) {
   if (blocks < 1) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(k_dwt, dim3((blocks + 7) / 8 * 8), dim3(256), kDwtLds, st, job);   // see dw_item
-  return hipGetLastError();
+  return enqueue(k_dwt, dim3((blocks + 7) / 8 * 8), dim3(256), kDwtLds, st, job);   // see dw_item
 }
 
 hipError_t launch_dw32(Elt e, const DwJob* job, int blocks, int R, float scale, float* loss_out,
                       TickRef tr, float* loss_base, hipStream_t st) {
   if (blocks < 1) return hipErrorInvalidValue;
-#define VFL_DW32(T, W) \
-  hipLaunchKernelGGL((k_dw32<T, W>), dim3(blocks), dim3(64 * W), 0, st, job, R, scale, loss_out, tr, loss_base)
   const bool wide = blocks <= kDwuTiles;
-  if (e == BF16 && wide) VFL_DW32(uint16_t, 16);
-  else if (e == BF16) VFL_DW32(uint16_t, 4);
-  else if (wide) VFL_DW32(float, 16);
-  else VFL_DW32(float, 4);
-#undef VFL_DW32
-  return hipGetLastError();
+  const auto kernel = e == BF16 ? (wide ? k_dw32<uint16_t, 16> : k_dw32<uint16_t, 4>)
+                                : (wide ? k_dw32<float, 16> : k_dw32<float, 4>);
+  return enqueue(kernel, dim3(blocks), dim3(64 * (wide ? 16 : 4)), 0, st, job, R, scale, loss_out, tr, loss_base);
 }
 
 hipError_t launch_dw_reduce(Elt e, const DwJob* job, int blocks, int R, float scale,
                             float* loss_out, TickRef tr, float* loss_base, hipStream_t st) {
   if (blocks < 1) return hipErrorInvalidValue;
-  if (e == BF16)
-    hipLaunchKernelGGL(k_dw_reduce<uint16_t>, dim3(blocks), dim3(256), 0, st, job, R, scale, loss_out,
-                       tr, loss_base);
-  else
-    hipLaunchKernelGGL(k_dw_reduce<float>, dim3(blocks), dim3(256), 0, st, job, R, scale, loss_out, tr,
-                       loss_base);
-  return hipGetLastError();
+  return enqueue(e == BF16 ? k_dw_reduce<uint16_t> : k_dw_reduce<float>, dim3(blocks), dim3(256), 0, st, job, R,
+                 scale, loss_out, tr, loss_base);
 }
 
 }  // namespace vfl

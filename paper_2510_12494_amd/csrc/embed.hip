@@ -536,8 +536,7 @@ __global__ __launch_bounds__(kThreads, 3) void k_embed_sgd(ScatterJob j) {
 
 hipError_t launch_scatter_sgd(const ScatterJob& j, hipStream_t st) {
   if (j.E > kMaxEmbDim || j.E % 4 || j.ldg % 4 || j.V > (1 << (32 - kRowBits))) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(k_embed_sgd, dim3(j.n_cat * kBlocksPerField), dim3(kThreads), 0, st, j);
-  return hipGetLastError();
+  return enqueue(k_embed_sgd, dim3(j.n_cat * kBlocksPerField), dim3(kThreads), 0, st, j);
 }
 
 }  // namespace vfl

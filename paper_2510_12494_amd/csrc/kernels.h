@@ -37,6 +37,19 @@ enum Elt { F32 = 0, BF16 = 1 };
 
 inline int elt_size(Elt e) { return e == F32 ? 4 : 2; }
 
+// Enqueues a kernel with its arguments.  The status is that of this launch: the
+// thread's last error, which may be an earlier one of the caller, is neither
+// asked for nor cleared, and a launch that fails leaves none of its own there.
+template <typename T> struct Param { typedef T type; };   // takes no part in deduction
+template <typename... P>
+hipError_t enqueue(void (*kernel)(P...), dim3 grid, dim3 threads, int lds, hipStream_t st,
+                   const typename Param<P>::type&... args) {
+  void* params[] = {(void*)&args...};
+  const hipError_t e = hipLaunchKernel((const void*)kernel, grid, threads, params, (size_t)lds, st);
+  if (e != hipSuccess) (void)hipGetLastError();
+  return e;
+}
+
 constexpr int kMaxChain = 16;         // layers per chain (bottom or top)
 constexpr int kMaxDw = 16;            // weight-gradient problems per launch
 constexpr int kMaxLogitCols = 512;    // widest last hidden layer of the top model

@@ -299,8 +299,7 @@ int lin_blocks(int rows_pad, int N) {
 
 hipError_t launch_lin(const LinJob* job, int blocks, int rows, TickRef tr, hipStream_t st) {
   if (blocks < 1) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(k_lin, dim3(blocks), dim3(256), kLinLds, st, job, rows, tr);
-  return hipGetLastError();
+  return enqueue(k_lin, dim3(blocks), dim3(256), kLinLds, st, job, rows, tr);
 }
 
 }  // namespace vfl

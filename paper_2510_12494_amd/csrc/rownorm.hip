@@ -849,11 +849,11 @@ hipError_t forward_with(const NormJob& j, hipStream_t st) {
   if constexpr (can_store_early<T>(G * CH)) {
     if (stores_early<T>(j.rows, j.cols, RES && j.s.p ? kEarlyJoin : kEarlyNorm)) {
       return enqueue(exact ? k_norm_forward<T, RES, G, CH, kExact, HOIST, true>
-                           : k_norm_forward<T, RES, G, CH, other, HOIST, true>, grid, nt, a, st);
+                           : k_norm_forward<T, RES, G, CH, other, HOIST, true>, grid, nt, 0, st, a);
     }
   }
   return enqueue(exact ? k_norm_forward<T, RES, G, CH, kExact, HOIST, false>
-                       : k_norm_forward<T, RES, G, CH, other, HOIST, false>, grid, nt, a, st);
+                       : k_norm_forward<T, RES, G, CH, other, HOIST, false>, grid, nt, 0, st, a);
 }
 
 // Rows of several wavefronts: where a round of workgroups takes them all, gamma
@@ -977,11 +977,11 @@ hipError_t backward_with(const NormJob& j, const BackwardPlan& p, hipStream_t st
       if constexpr (can_store_early<T>(G * CH)) {
         if (stores_early<T>(j.rows, j.cols, kEarlyBackward)) {
           return enqueue(exact ? k_norm_backward<T, RES, G, CH, nt, kExact, true>
-                               : k_norm_backward<T, RES, G, CH, nt, other, true>, p.parts, threads, a, st);
+                               : k_norm_backward<T, RES, G, CH, nt, other, true>, p.parts, threads, 0, st, a);
         }
       }
       return enqueue(exact ? k_norm_backward<T, RES, G, CH, nt, kExact, false>
-                           : k_norm_backward<T, RES, G, CH, nt, other, false>, p.parts, threads, a, st);
+                           : k_norm_backward<T, RES, G, CH, nt, other, false>, p.parts, threads, 0, st, a);
     }
   }
   if constexpr (G == 256 || (G == 1024 && CH == 1)) {   // many rows only
@@ -992,7 +992,7 @@ hipError_t backward_with(const NormJob& j, const BackwardPlan& p, hipStream_t st
       a.grid = col_blocks + row_blocks;
       if (a.grid == 0) return hipSuccess;
       return enqueue(exact ? k_norm_backward_split<T, RES, G, CH, nt, kExact>
-                           : k_norm_backward_split<T, RES, G, CH, nt, other>, a.grid, nt, a, st);
+                           : k_norm_backward_split<T, RES, G, CH, nt, other>, a.grid, nt, 0, st, a);
     };
     const int row_blocks = j.dr.p || j.dx.p ? p.row_blocks : 0;
     auto over = [&](const Mat& m) { return m.p && (m.p == j.dy.p || m.p == j.v.p); };
@@ -1055,7 +1055,7 @@ hipError_t dropout(const DropJob& j, hipStream_t st) {
   const int64_t stride = (int64_t)grid * kThreads;
   const DropArgs a{j.d, j.x, j.y, j.rows, stride / per, j.cols, (int)(stride % per)};
   return enqueue(j.cols % 8 == 0 ? k_dropout<T, kExact> : j.cols > 8 ? k_dropout<T, kRagged> : k_dropout<T, kSmall>,
-                 grid, kThreads, a, st);
+                 grid, kThreads, 0, st, a);
 }
 
 hipError_t launch_dropout(Elt e, const DropJob& j, hipStream_t st) {
@@ -1076,8 +1076,8 @@ hipError_t launch_norm_backward(Elt e, const NormJob& j, hipStream_t st) {
   if (err != hipSuccess || p.parts <= 1) return err;
   const ReduceArgs a{j.part, j.dgamma, j.dbeta, j.cols, p.parts};
   // 64 columns a workgroup once they fill the CUs, else 16
-  if (2 * j.cols > 256 * 16) return enqueue(k_norm_reduce<64>, (2 * j.cols + 63) / 64, kReduceThreads, a, st);
-  return enqueue(k_norm_reduce<16>, (2 * j.cols + 15) / 16, kReduceThreads, a, st);
+  if (2 * j.cols > 256 * 16) return enqueue(k_norm_reduce<64>, (2 * j.cols + 63) / 64, kReduceThreads, 0, st, a);
+  return enqueue(k_norm_reduce<16>, (2 * j.cols + 15) / 16, kReduceThreads, 0, st, a);
 }
 
 }  // namespace vfl

@@ -36,17 +36,6 @@ struct NormJob {
   int64_t rows;
 };
 
-// Enqueues a kernel whose parameter is `a`.  The status is that of this launch:
-// the thread's last error, which may be an earlier one of the caller, is neither
-// asked for nor cleared, and a launch that fails leaves none of its own there.
-template <typename Args>
-hipError_t enqueue(void (*kernel)(Args), int grid, int threads, const Args& a, hipStream_t st) {
-  void* params[] = {const_cast<Args*>(&a)};
-  const hipError_t e = hipLaunchKernel((const void*)kernel, dim3(grid), dim3(threads), params, 0, st);
-  if (e != hipSuccess) (void)hipGetLastError();
-  return e;
-}
-
 // the most partial pairs (2 x cols floats each) of weights' gradients that a
 // backward pass over rows x cols, or fewer rows, leaves in its workspace,
 // whatever its element type (1: none, the result is written at once)

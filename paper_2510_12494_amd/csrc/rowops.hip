@@ -95,8 +95,8 @@ __global__ __launch_bounds__(256) void k_avg(AvgJob j) {
 }
 
 template <int N>
-void launch_avg_n(const AvgJob& j, int grid, hipStream_t st) {
-  hipLaunchKernelGGL(k_avg<N>, dim3(grid), dim3(256), 0, st, j);
+hipError_t launch_avg_n(const AvgJob& j, int grid, hipStream_t st) {
+  return enqueue(k_avg<N>, dim3(grid), dim3(256), 0, st, j);
 }
 
 int grid_for(int64_t work, int per_block, int cap) {
@@ -106,21 +106,18 @@ int grid_for(int64_t work, int per_block, int cap) {
 }  // namespace
 
 hipError_t launch_tick_base(TickSrc* src, int cyc, hipStream_t st) {
-  hipLaunchKernelGGL(k_tick_base, dim3(1), dim3(64), 0, st, src, cyc);
-  return hipGetLastError();
+  return enqueue(k_tick_base, dim3(1), dim3(64), 0, st, src, cyc);
 }
 
 hipError_t launch_tick_set(TickSrc* dst, const TickSrc& v, hipStream_t st) {
-  hipLaunchKernelGGL(k_tick_set, dim3(1), dim3(64), 0, st, dst, v);
-  return hipGetLastError();
+  return enqueue(k_tick_set, dim3(1), dim3(64), 0, st, dst, v);
 }
 
 hipError_t launch_philox_words(uint64_t seed, uint32_t step, uint32_t tag, uint32_t row0,
                                int rows, int groups, uint32_t* out, hipStream_t st) {
   const int64_t total = (int64_t)rows * groups;
-  hipLaunchKernelGGL(k_philox_words, dim3(grid_for(total, 256, 4096)), dim3(256), 0, st, seed,
-                     step, tag, row0, rows, groups, out);
-  return hipGetLastError();
+  return enqueue(k_philox_words, dim3(grid_for(total, 256, 4096)), dim3(256), 0, st, seed, step, tag, row0, rows,
+                 groups, out);
 }
 
 hipError_t launch_avg(const AvgJob& j, hipStream_t st) {
@@ -129,24 +126,23 @@ hipError_t launch_avg(const AvgJob& j, hipStream_t st) {
   if (total == 0) return hipSuccess;
   const int g = grid_for(total, 256, 4096);
   switch (j.n) {
-    case 1: launch_avg_n<1>(j, g, st); break;
-    case 2: launch_avg_n<2>(j, g, st); break;
-    case 3: launch_avg_n<3>(j, g, st); break;
-    case 4: launch_avg_n<4>(j, g, st); break;
-    case 5: launch_avg_n<5>(j, g, st); break;
-    case 6: launch_avg_n<6>(j, g, st); break;
-    case 7: launch_avg_n<7>(j, g, st); break;
-    case 8: launch_avg_n<8>(j, g, st); break;
-    case 9: launch_avg_n<9>(j, g, st); break;
-    case 10: launch_avg_n<10>(j, g, st); break;
-    case 11: launch_avg_n<11>(j, g, st); break;
-    case 12: launch_avg_n<12>(j, g, st); break;
-    case 13: launch_avg_n<13>(j, g, st); break;
-    case 14: launch_avg_n<14>(j, g, st); break;
-    case 15: launch_avg_n<15>(j, g, st); break;
-    default: launch_avg_n<16>(j, g, st); break;
+    case 1: return launch_avg_n<1>(j, g, st);
+    case 2: return launch_avg_n<2>(j, g, st);
+    case 3: return launch_avg_n<3>(j, g, st);
+    case 4: return launch_avg_n<4>(j, g, st);
+    case 5: return launch_avg_n<5>(j, g, st);
+    case 6: return launch_avg_n<6>(j, g, st);
+    case 7: return launch_avg_n<7>(j, g, st);
+    case 8: return launch_avg_n<8>(j, g, st);
+    case 9: return launch_avg_n<9>(j, g, st);
+    case 10: return launch_avg_n<10>(j, g, st);
+    case 11: return launch_avg_n<11>(j, g, st);
+    case 12: return launch_avg_n<12>(j, g, st);
+    case 13: return launch_avg_n<13>(j, g, st);
+    case 14: return launch_avg_n<14>(j, g, st);
+    case 15: return launch_avg_n<15>(j, g, st);
+    default: return launch_avg_n<16>(j, g, st);
   }
-  return hipGetLastError();
 }
 
 hipError_t launch_cast(Elt e, const CastJob* jobs, int n_jobs, hipStream_t st) {
@@ -160,9 +156,7 @@ hipError_t launch_cast(Elt e, const CastJob* jobs, int n_jobs, hipStream_t st) {
   }
   js.n = n_jobs;
   dim3 grid(grid_for(maxw, 256, 1024), n_jobs);
-  if (e == BF16) hipLaunchKernelGGL(k_cast<uint16_t>, grid, dim3(256), 0, st, js);
-  else hipLaunchKernelGGL(k_cast<float>, grid, dim3(256), 0, st, js);
-  return hipGetLastError();
+  return enqueue(e == BF16 ? k_cast<uint16_t> : k_cast<float>, grid, dim3(256), 0, st, js);
 }
 
 }  // namespace vfl

@@ -168,3 +168,38 @@ def test_discard_protocol():
         V.vfl_bottom_forward(sess.ctx, V.VFL_PARTY_B, g, sess.batches("B", g))
     finally:
         sess.close()
+
+
+@pytest.mark.parametrize("name", ["dense_tabular", "ctr", "hetero"])
+def test_an_earlier_error_of_the_caller_does_not_fail_a_tick(name):
+    """A failure that the calling thread has not asked for yet belongs to the
+    caller: ticks, replayed graphs and vfl_philox
+    work beside it and give the same parameters and losses."""
+    import torch
+    from paper_2510_12494_amd import vfl as V
+    lib = V.library()
+    got = []
+    for failed in (False, True):
+        w, sess, p = _session(name, groups=6)
+        out = torch.zeros(4 * 5 * 3, dtype=torch.int32, device="cuda")
+        ticks = 2 * (w.staleness + 1)
+        torch.cuda.synchronize()
+        try:
+            if failed:
+                assert lib.hipSetDevice(-1) != 0 and lib.hipPeekAtLastError() != 0   # refused on the host
+            try:
+                for t in range(ticks):
+                    sess.step(t)
+                sess.bind()
+                sess.run(ticks, 4)
+                V.vfl_philox(5, 1, 2, 3, 5, 3, out.data_ptr())
+            finally:
+                lib.hipGetLastError()
+            torch.cuda.synchronize()
+            got.append((sess.params({k: v.shape for k, v in p.items()}), sess.losses(range(ticks + 4 - w.staleness)),
+                        out.cpu().numpy()))
+        finally:
+            sess.close()
+    (pa, la, oa), (pb, lb, ob) = got
+    assert all(np.array_equal(pa[k], pb[k]) for k in pa)
+    assert np.array_equal(la, lb) and np.array_equal(oa, ob) and ob.any()
