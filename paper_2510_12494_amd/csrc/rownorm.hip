@@ -127,11 +127,11 @@ __device__ __forceinline__ Raw<T> load_chunk(const T* row, int q, const Cols& k,
   return load_at(row + min(8 * q, edge ? k.n - 8 : 8 * k.per - 8));
 }
 
-// Its values: zero at and past the row's end (on an edge row, those of a
+// Its values: `past` at and past the row's end (on an edge row, those of a
 // partial chunk moved to their places).
 template <Form F, typename T>
 __device__ __forceinline__ void chunk_values(const Raw<T>& r, int q, const Cols& k, bool edge, float (&v)[8],
-                                             bool whole = false) {
+                                             bool whole = false, float past = 0.f) {
   unpack(r, v);
   if (F == kExact || whole) return;
   if (edge && k.n >= 8 && q == k.per - 1) {
@@ -151,7 +151,7 @@ __device__ __forceinline__ void chunk_values(const Raw<T>& r, int q, const Cols&
   }
   const int left = k.n - 8 * q;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = i < left ? v[i] : 0.f;
+  for (int i = 0; i < 8; ++i) v[i] = i < left ? v[i] : past;
 }
 
 // Those of a row of its own (gamma, beta).
@@ -541,7 +541,9 @@ __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_
       for (int c = 0; c < CH; ++c) {
         const int q = c * lanes + lane;
         if constexpr (!HOIST) weights(c, 0);
-        chunk_values<F>(xr[c], q, k, edge, h[c], c < CH / 2);
+        // past the row's end x is its mean: h is 0 there, and not mean * rs,
+        // which may be infinite and would make the sums of g * h NaN
+        chunk_values<F>(xr[c], q, k, edge, h[c], c < CH / 2, mean);
         chunk_values<F>(yr[c], q, k, edge, g[c], c < CH / 2);
         if constexpr (RES && OUT) sc[c] = sr[c];
 #pragma unroll

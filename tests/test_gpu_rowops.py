@@ -771,3 +771,20 @@ def test_an_earlier_error_of_the_caller_is_not_this_calls(V, rows, cols):
     for m in (c, n):
         m.check_forward()
         m.check_backward()
+
+
+@pytest.mark.parametrize("dt", DTS)
+@pytest.mark.parametrize("rows", [9, 2100])
+@pytest.mark.parametrize("cols", [1, 4, 8, 13, 100, 1001, 1500])
+def test_backward_of_huge_constant_rows(V, dt, rows, cols):
+    """Rows without variance far from zero: (x - mean) * k is 0 at every column,
+    and what lies past a row's end must not enter its sums as mean * k, which is
+    infinite in float32."""
+    c = Call(V, "residual", dt, rows, cols, p=0.2)
+    c.forward()
+    c.s.t[[0, rows // 2, rows - 1]] = 2.0 ** 121
+    stats = R.layer_norm(c.s.np(), 1.0, 0.0, EPS)[1]
+    c.stats[:2 * rows] = torch.from_numpy(stats.reshape(-1)).float()
+    c.backward()
+    c.check_backward()
+    assert bool(c.dr.t.isfinite().all()) and bool(c.dgamma[:cols].isfinite().all())
