@@ -42,6 +42,7 @@ class ResidualTower:
         dev = torch.device(device)
         self.dev = dev if dev.index is not None else torch.device(dev.type, torch.cuda.current_device())
         self.bf16, self.trained = dtype == "bf16", 0        # rows whose training forward the buffers hold
+        self.next_step = 0                                  # of a training forward that names none
         self.tdt = torch.bfloat16 if self.bf16 else torch.float32
         g = torch.Generator().manual_seed(seed)
 
@@ -117,15 +118,19 @@ class ResidualTower:
         return torch.cuda.current_stream(self.dev).cuda_stream
 
     @torch.no_grad()
-    def forward(self, x: torch.Tensor, row0: int = 0, step: int = 0, train: bool = True) -> torch.Tensor:
+    def forward(self, x: torch.Tensor, row0: int = 0, step: int | None = None, train: bool = True) -> torch.Tensor:
         """The embedding of rows ``x`` (global sample ids from ``row0``), a view of
         the tower's buffer that the next forward overwrites; without ``train``
-        nothing is dropped (scoring)."""
+        nothing is dropped (scoring).  ``step`` keys the masks: towers that have to
+        make the same ones (replicas, a replay, a batch in parts) name it; without
+        it a training forward takes the step after the last one's, from 0."""
         if (x.dim() != 2 or not 1 <= x.shape[0] <= self.max_rows or x.shape[1] != self.d_in or x.dtype != self.tdt
                 or x.device != self.dev):
             raise ValueError(f"x must be [1..{self.max_rows} x {self.d_in}] of {self.tdt} on {self.dev}")
         rows, c = x.shape[0], self.copies
         self.trained = 0
+        if step is None:
+            step = self.next_step
         with torch.cuda.device(self.dev):
             st = self._call(rows, row0, step, self.p if train else 0.0)
             self.x = x
@@ -139,7 +144,7 @@ class ResidualTower:
                 torch.matmul(a, c[f"W2.{l}"].T, out=self.branch[:rows])
                 V.vfl_residual_forward(self.joins[l], st)
         if train:
-            self.trained = rows
+            self.trained, self.next_step = rows, step + 1
         return self.y[self.blocks][:rows]
 
     @torch.no_grad()

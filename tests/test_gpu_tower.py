@@ -124,3 +124,19 @@ def test_gradient_of_one_row_in_any_layout():
     t.backward(dz.T.reshape(-1).reshape(1, 32).clone())
     assert all(torch.equal(got[k], v) for k, v in t.grads.items())
     assert t.grads["gamma.0"].abs().max() > 0
+
+
+def test_training_forwards_without_a_step_differ_in_their_masks():
+    """Each takes the step after the last one's; scoring takes none."""
+    from paper_2510_12494_amd.tower import ResidualTower
+    x = torch.randn(40, 16, generator=torch.Generator().manual_seed(4)).cuda()
+    named = ResidualTower(16, 64, 64, 1, 64, "f32", p=0.3, seed=8)
+    want = [named.forward(x, step=i).clone() for i in range(3)]
+    t = ResidualTower(16, 64, 64, 1, 64, "f32", p=0.3, seed=8)
+    for i in range(2):
+        assert torch.equal(t.forward(x), want[i])
+        t.forward(x, train=False)
+    assert (want[0] - want[1]).abs().max() > 0.1
+    assert torch.equal(t.forward(x, step=0), want[0])         # named: that one, and the next counts from it
+    assert torch.equal(t.forward(x), want[1])
+    assert torch.equal(t.forward(x), want[2])
