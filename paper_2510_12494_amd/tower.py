@@ -8,8 +8,8 @@ that train their own party model.
 
 and the embedding is the last y.  The dropouts, norms and joins run in the
 library's kernels (vfl_dropout, vfl_layernorm_*, vfl_residual_*), the products
-in torch's matmul, whose results have the tower's dtype (a weight gradient is
-rounded to it once, as the gradients it is a product of are).  Parameters are float32 masters with operand copies in the
+in torch's matmul, whose results have the tower's dtype; weight gradients are
+float32, unrounded.  Parameters are float32 masters with operand copies in the
 tower's dtype, as in the library's own models; buffers and call descriptors are
 made once, for at most ``max_rows`` rows.  A dropout mask follows from (seed,
 step, layer, sample id), so the backward pass stores none and a sample's mask
@@ -147,6 +147,12 @@ class ResidualTower:
             self.trained, self.next_step = rows, step + 1
         return self.y[self.blocks][:rows]
 
+    def _weight_grad(self, d: torch.Tensor, x: torch.Tensor, out: torch.Tensor):
+        if self.bf16:
+            torch.mm(d.T, x, out_dtype=torch.float32, out=out)
+        else:
+            torch.mm(d.T, x, out=out)
+
     @torch.no_grad()
     def backward(self, dz: torch.Tensor):
         """Gradients of every parameter into ``grads`` for the gradient ``dz`` of
@@ -163,11 +169,11 @@ class ResidualTower:
                 _set(j.dy, dy)
                 V.vfl_residual_backward(j, st)
                 db, dh = self.dbranch[:rows], self.dh[:rows]
-                G[f"W2.{l}"].copy_(torch.matmul(db.T, self.a[l][:rows]))
+                self._weight_grad(db, self.a[l][:rows], G[f"W2.{l}"])
                 torch.matmul(db, c[f"W2.{l}"], out=dh)
                 V.vfl_dropout(self.undrops[l], st)
                 dh.mul_(self.h[l][:rows] > 0)
-                G[f"W1.{l}"].copy_(torch.matmul(dh.T, self.y[l][:rows]))
+                self._weight_grad(dh, self.y[l][:rows], G[f"W1.{l}"])
                 torch.sum(dh, 0, dtype=torch.float32, out=G[f"b.{l}"])
                 dy = torch.matmul(dh, c[f"W1.{l}"])
             n = self.norm0
@@ -175,7 +181,7 @@ class ResidualTower:
             _set(n.dx, self.dbranch)
             V.vfl_layernorm_backward(n, st)
             ds += self.dbranch[:rows]
-            G["W_in"].copy_(torch.matmul(ds.T, self.x))
+            self._weight_grad(ds, self.x, G["W_in"])
 
     @torch.no_grad()
     def sgd(self, lr: float):

@@ -140,3 +140,26 @@ def test_training_forwards_without_a_step_differ_in_their_masks():
     assert torch.equal(t.forward(x, step=0), want[0])         # named: that one, and the next counts from it
     assert torch.equal(t.forward(x), want[1])
     assert torch.equal(t.forward(x), want[2])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_weight_gradients_are_float32_sums(dtype):
+    """Not rounded to the tower's type on their way to the float32 masters: within
+    a float32 sum's bound of the float64 product of the buffers they come from."""
+    from paper_2510_12494_amd.tower import ResidualTower
+    rows = 60
+    tdt = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    t = ResidualTower(24, 64, 96, 1, 64, dtype, p=0.2, seed=6)
+    g = torch.Generator().manual_seed(7)
+    wide = torch.randn(rows, 30, generator=g).cuda().to(tdt)
+    x, dz = wide[:, 3:27], torch.randn(rows, 64, generator=g).cuda()
+    t.forward(x, row0=5, step=2)
+    t.backward(dz)
+    for name, d, v in (("W_in", t.ds, x), ("W1.0", t.dh, t.y[0])):
+        d, v = d[:rows].double(), v[:rows].double()
+        assert t.grads[name].dtype == torch.float32
+        err = (t.grads[name].double() - d.T @ v).abs()
+        assert bool((err <= (rows + 2) * 2.0 ** -24 * (d.abs().T @ v.abs()) + 1e-30).all()), name
+    for name in ("W_in", "W1.0", "W2.0"):
+        w = t.grads[name]
+        assert bool((w != w.bfloat16().float()).any()), name
