@@ -58,7 +58,7 @@ class ResidualTower:
             P[f"beta.{l}"] = torch.zeros(width, device=self.dev)
         self.params = P
         self.grads = {k: torch.zeros_like(v) for k, v in P.items()}
-        self.copies = {k: torch.empty_like(v, dtype=self.tdt) for k, v in P.items() if k[0] in "Wb"}
+        self.copies = {k: torch.empty_like(v, dtype=self.tdt) for k, v in P.items() if k.startswith(("W", "b."))}
         self.refresh()
 
         new = lambda n: torch.empty((max_rows, n), dtype=self.tdt, device=self.dev)  # noqa: E731

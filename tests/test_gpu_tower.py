@@ -163,3 +163,9 @@ def test_weight_gradients_are_float32_sums(dtype):
     for name in ("W_in", "W1.0", "W2.0"):
         w = t.grads[name]
         assert bool((w != w.bfloat16().float()).any()), name
+
+
+def test_operand_copies_are_of_what_the_products_read():
+    from paper_2510_12494_amd.tower import ResidualTower
+    t = ResidualTower(16, 32, 32, 2, 64)
+    assert set(t.copies) == {"W_in"} | {f"{k}.{l}" for k in ("W1", "W2", "b") for l in range(2)}
