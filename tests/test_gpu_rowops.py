@@ -788,3 +788,193 @@ def test_backward_of_huge_constant_rows(V, dt, rows, cols):
     c.backward()
     c.check_backward()
     assert bool(c.dr.t.isfinite().all()) and bool(c.dgamma[:cols].isfinite().all())
+
+
+# ------------------------------------------------------------- large batches
+class Large(Call):
+    """Inputs made on the device; checked at sampled rows (results of a row
+    depend on that row alone) and, for the weights' gradients, in float64 on the
+    device."""
+
+    def __init__(self, V, kind, dt, rows, cols, ld=0, p=0.0):
+        self.V, self.kind, self.dt, self.rows, self.cols, self.p = V, kind, dt, rows, cols, p
+        g = torch.Generator(device="cuda").manual_seed(rows * 31 + cols)
+        rnd = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+        self.a = a = V.vfl_layernorm_args() if kind == "norm" else V.vfl_residual_args()
+        a.dtype, a.rows, a.cols, a.eps = (V.VFL_F32, V.VFL_BF16)[dt == "bf16"], rows, cols, EPS
+
+        def new(values=None):
+            m = Mat(dt, rows, cols, ld)
+            if values is not None:
+                m.t.copy_(values)
+            return m
+
+        act = lambda: rnd(rows, cols) * torch.exp(0.5 * rnd(cols)) + 0.5 * rnd(rows, 1)  # noqa: E731
+        self.x, self.y, self.dx, self.dy = new(act()), new(), new(), new(rnd(rows, cols) * 1e-2)
+        self.m = {"x": self.x, "y": self.y, "dy": self.dy, "dx": self.dx}
+        if kind == "residual":
+            self.r, self.s, self.dr, self.ds = new(act()), new(), new(), new(rnd(rows, cols) * 1e-2)
+            self.m.update(r=self.r, s=self.s, dr=self.dr, ds=self.ds)
+            key(a.drop, p)
+        self.gamma, self.beta = f32(cols), f32(cols)
+        self.gamma[:cols], self.beta[:cols] = 1 + 0.1 * rnd(cols), 0.1 * rnd(cols)
+        self.g64, self.b64 = stored(self.gamma, cols), stored(self.beta, cols)
+        a.gamma, a.beta = self.gamma.data_ptr(), self.beta.data_ptr()
+        self.stats, self.dgamma, self.dbeta = f32(2 * rows), f32(cols), f32(cols)
+        a.stats, a.dgamma, a.dbeta = (t.data_ptr() for t in (self.stats, self.dgamma, self.dbeta))
+        self.nws = V.vfl_norm_workspace_size(rows, cols)
+        self.ws = torch.full((self.nws + 64,), 0xFF, dtype=torch.uint8, device="cuda")
+        a.workspace, a.workspace_bytes = self.ws.data_ptr(), self.nws
+        for name, m in self.m.items():
+            m.put(getattr(a, name))
+        # the first and the last rows, and some between
+        n = min(rows, 40)
+        between = np.random.default_rng(rows).integers(0, rows, 60)
+        self.sel = np.unique(np.concatenate([np.arange(n), between, np.arange(rows - n, rows)]))
+
+    def at(self, m):
+        return m.t[torch.from_numpy(self.sel).cuda()].double().cpu().numpy()
+
+    def keep(self):
+        return R.keep_mask(self.p, KEY["seed"], KEY["step"], KEY["tag"], KEY["row0"] + self.sel, self.cols)
+
+    def check_forward(self):
+        v = self.at(self.x)
+        ev = np.zeros_like(v)
+        if self.kind == "residual":
+            xd = R.dropout(v, self.p, self.keep())
+            v = self.at(self.r) + xd
+            ev = 2 * U * np.abs(xd) * (self.p > 0) + U * np.abs(v)
+            close(self.at(self.s), v, SLACK * ev, "s", self.dt)
+        y, stats = R.layer_norm(v, self.g64, self.b64, EPS)
+        e_y, e_st = norm_bounds(v, ev, self.g64, self.b64)
+        close(self.at(self.y), y, e_y, "y", self.dt)
+        close(self.st()[self.sel], stats, e_st, "stats")
+
+    def check_backward(self):
+        v = self.x if self.kind == "norm" else self.s
+        vs, dy, st = self.at(v), self.at(self.dy), self.st()[self.sel]
+        e, _, _ = grad_bounds(vs, st, self.g64, dy)
+        d, _, _ = R.layer_norm_backward(vs, st, self.g64, dy)
+        if self.kind == "residual":
+            if self.a.ds.data:
+                d = d + self.at(self.ds)
+            e = e + SLACK * U * np.abs(d)
+            if self.a.dr.data:
+                close(self.at(self.dr), d, e, "dr", self.dt)
+            k = self.keep()
+            d, e = R.dropout(d, self.p, k), R.dropout(e, self.p, k)
+            e = e + 2 * U * np.abs(d) * (self.p > 0)
+        if self.a.dx.data:
+            close(self.at(self.dx), d, e, "dx", self.dt)
+        # as in grad_bounds, over all rows
+        st = self.stats[:2 * self.rows].double().view(-1, 2)
+        dy = self.dy.t.double()
+        t = (v.t.double() - st[:, :1]) * st[:, 1:] * dy
+        chain = min(self.rows, 512) + 32
+        for name, terms, roundings in (("dgamma", t, chain + 4), ("dbeta", dy, chain)):
+            if getattr(self.a, name):
+                want, bound = terms.sum(0), SLACK * roundings * U * terms.abs().sum(0) + 1e-37
+                close(stored(getattr(self, name), self.cols), want.cpu().numpy(), bound.cpu().numpy(), name)
+
+
+# more rows than a round of forward workgroups takes, so that they go on to a next
+# row (1 to 64 lanes a row, one and two chunks a lane, several wavefronts a row),
+# with whole and partial last chunks; results too large to leave the L2s early
+LARGE = [(1_050_001, 5), (1_050_001, 8), (530_001, 13), (270_001, 30), (140_001, 64), (70_001, 100), (70_001, 128),
+         (35_001, 200), (44_001, 200), (33_001, 256), (17_001, 500), (17_001, 512), (8_501, 1000), (9_001, 1024),
+         (66_001, 520), (33_001, 1032), (4_201, 2048), (3_001, 1536), (14_001, 4104), (9_001, 4096), (3_001, 5001),
+         (1_501, 8192)]
+
+
+@pytest.mark.parametrize("dt", DTS)
+@pytest.mark.parametrize("kind", ["norm", "residual"])
+@pytest.mark.parametrize("rows,cols", LARGE)
+def test_large_batches(V, kind, dt, rows, cols):
+    c = Large(V, kind, dt, rows, cols, p=0.3 if kind == "residual" else 0.0)
+    c.forward()
+    c.check_forward()
+    c.backward()
+    c.check_backward()
+    c.guards()
+
+
+@pytest.mark.parametrize("dt", DTS)
+@pytest.mark.parametrize("rows,cols", [(210_001, 167), (70_001, 512), (4_300_001, 7)])
+def test_dropout_of_more_chunks_than_threads(V, dt, rows, cols):
+    """Threads step on to further (row, chunk) pairs."""
+    p = 0.25
+    x = Mat(dt, rows, cols)
+    x.t.copy_(torch.rand((rows, cols), generator=torch.Generator(device="cuda").manual_seed(cols), device="cuda") + 0.5)
+    y = Mat(dt, rows, cols)
+    a = V.vfl_dropout_args()
+    a.dtype, a.rows, a.cols = (V.VFL_F32, V.VFL_BF16)[dt == "bf16"], rows, cols
+    key(a.drop, p)
+    x.put(a.x)
+    y.put(a.y)
+    V.vfl_dropout(a)
+    # everywhere: 0, or the element times the scale, rounded once to float32 and
+    # once to the type
+    want = (x.t.float() * float(np.float32(R.scale(p)))).to(DT[dt])
+    kept = y.t != 0
+    assert torch.equal(y.t, torch.where(kept, want, torch.zeros_like(want)))
+    assert abs(kept.float().mean().item() - (1 - p)) < 0.002      # 30 million numbers: a deviation is 1e-4
+    sel = np.unique(np.concatenate([np.arange(60), np.arange(rows - 60, rows), np.arange(0, rows, rows // 300)]))
+    mask = R.keep_mask(p, KEY["seed"], KEY["step"], KEY["tag"], KEY["row0"] + sel, cols)
+    assert (kept[torch.from_numpy(sel).cuda()].cpu().numpy() == mask).all()
+    y.assert_guard()
+
+
+@pytest.mark.parametrize("dt", DTS)
+@pytest.mark.parametrize("rows,cols", [(2100, 50), (1300, 640), (1300, 1500), (800, 5001), (4300, 1000)])
+@pytest.mark.parametrize("kind", ["norm", "residual"])
+def test_optional_operands_of_many_rows(V, kind, dt, rows, cols):
+    """Absent operands where partial weight gradients are summed in a second
+    launch: neither read nor written, the others as the formulas say."""
+    for names in {"norm": ["dx", "dgamma", "dbeta", "dgamma dbeta"],
+                  "residual": ["ds", "dr", "dx", "dr dx", "ds dx", "ds dr", "dgamma", "dbeta", "ds dgamma", "dr dbeta",
+                               "dgamma dbeta"]}[kind]:
+        c = Large(V, kind, dt, rows, cols, cols + 3, p=0.25)
+        c.forward()
+        for n in names.split():
+            f = getattr(c.a, n)
+            if isinstance(f, V.vfl_matrix):
+                f.data = None
+            else:
+                setattr(c.a, n, None)
+        c.backward()
+        c.check_backward()
+        c.guards()
+        for n in set(names.split()) - {"ds"}:
+            buf = getattr(c, n)
+            assert bool(((buf.t if isinstance(buf, Mat) else buf) == Mat.GUARD).all()), (names, n)
+
+
+@pytest.mark.parametrize("rows,cols", [(60, 72), (2100, 72), (40, 1100)])
+def test_residual_join_with_the_step_on_the_device_in_a_replayed_graph(V, rows, cols):
+    """Both directions make the masks of step + *step_dev, at each replay anew."""
+    p = 0.3
+    c = Call(V, "residual", "f32", rows, cols, p=p)
+    step = torch.zeros(1, dtype=torch.int32, device="cuda")
+    c.a.drop.step_dev = step.data_ptr()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        s = torch.cuda.current_stream().cuda_stream
+        c.forward(s)
+        c.backward(s)
+        step.add_(1)
+    xs = c.x.np()
+    assert (xs != 0).mean() > 0.9
+    for i in range(4):
+        for t in (c.s.t, c.dx.t, c.y.t):
+            t.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        k = keep(p, rows, cols, step=KEY["step"] + i)
+        want = c.r.np() + R.dropout(xs, p, k)
+        close(c.s.np(), want, SLACK * (2 * U * np.abs(R.dropout(xs, p, k)) + U * np.abs(want)), "s")
+        dx, dr = c.dx.np(), c.dr.np()
+        assert (dx[~k] == 0).all()
+        close(dx, R.dropout(dr, p, k), 2.5 * U * np.abs(R.dropout(dr, p, k)), "dx")
+        assert (dx[k & (dr != 0)] != 0).all()
