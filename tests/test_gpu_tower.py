@@ -169,3 +169,90 @@ def test_operand_copies_are_of_what_the_products_read():
     from paper_2510_12494_amd.tower import ResidualTower
     t = ResidualTower(16, 32, 32, 2, 64)
     assert set(t.copies) == {"W_in"} | {f"{k}.{l}" for k in ("W1", "W2", "b") for l in range(2)}
+
+
+def _reference_of_the_same_relus(t, x, dz, row0, step):
+    """_reference with the tower's operand copies (the weights as its products
+    read them) and the ReLU pattern of its own forward."""
+    P = {k: (t.copies[k] if k in t.copies else v).double().cpu().requires_grad_() for k, v in t.params.items()}
+    ids = np.arange(row0, row0 + len(x))
+
+    def drop(v, tag):
+        k = torch.from_numpy(R.keep_mask(t.p, t.seed, step, tag, ids, v.shape[1]))
+        return torch.where(k, v * R.scale(t.p), 0.0)
+
+    def norm(s, l):
+        return torch.nn.functional.layer_norm(s, (t.width,), P[f"gamma.{l}"], P[f"beta.{l}"], 1e-5)
+
+    s = x.double().cpu() @ P["W_in"].T
+    y = norm(s, 0)
+    for l in range(t.blocks):
+        on = (t.h[l][:len(x)] > 0).cpu()
+        h = torch.where(on, y @ P[f"W1.{l}"].T + P[f"b.{l}"], 0.0)
+        s = s + drop(drop(h, 2 * l) @ P[f"W2.{l}"].T, 2 * l + 1)
+        y = norm(s, l + 1)
+    y.backward(dz.double().cpu())
+    return y.detach(), {k: v.grad for k, v in P.items()}
+
+
+def _rel(a, b):
+    return float((a.double().cpu() - b).norm() / b.norm())
+
+
+# A stored bf16 value is off by at most 2^-9 of itself, so a stored tensor by at
+# most 2^-9 of its L2 norm; norms, random products and joins hand a relative error
+# on about as it is.  The longest path stores, in a block, y, the ReLU's input and
+# output, a, the branch and s going forward and dbranch, dh (three times), dy and
+# ds going back: 12, and two more at either end, all added up as if they agreed.
+def _bf16_bound(blocks):
+    return (12 * blocks + 4) * 2.0 ** -9
+
+
+@pytest.mark.parametrize("width,hidden,blocks,rows", [(64, 96, 2, 300), (40, 33, 1, 77), (256, 256, 2, 1500)])
+def test_bf16_gradients_equal_float64_autograd(width, hidden, blocks, rows):
+    from paper_2510_12494_amd.tower import ResidualTower
+    t = ResidualTower(24, width, hidden, blocks, rows + 50, "bf16", p=0.25, seed=5)
+    g = torch.Generator().manual_seed(rows)
+    x, dz = torch.randn(rows, 24, generator=g).bfloat16(), torch.randn(rows, width, generator=g) / rows
+    for l in range(blocks + 1):                               # values that show a factor left out
+        t.params[f"gamma.{l}"].copy_(1 + 0.3 * torch.randn(width, generator=g))
+        t.params[f"beta.{l}"].copy_(0.3 * torch.randn(width, generator=g))
+    z = t.forward(x.cuda(), row0=900, step=4)
+    want, grads = _reference_of_the_same_relus(t, x, dz, 900, 4)
+    assert _rel(z, want) <= _bf16_bound(blocks)
+    t.backward(dz.cuda())
+    for k, v in grads.items():
+        assert _rel(t.grads[k], v) <= _bf16_bound(blocks), (k, _rel(t.grads[k], v))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_trained_towers_score_single_samples_as_batches(dtype):
+    """Two towers and a linear head learn a linear teacher of both parties'
+    features; held-out samples scored one by one give the batch's scores, and
+    are right far more often than by chance."""
+    from paper_2510_12494_amd.tower import ResidualTower
+    tdt = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    g = torch.Generator().manual_seed(12)
+    x = torch.randn(2400, 20, generator=g)
+    label = (x @ torch.randn(20, generator=g) > 0).float().cuda()
+    xa, xb = x[:, :8].to("cuda", tdt), x[:, 8:].to("cuda", tdt)
+    A, B = ResidualTower(8, 64, 64, 2, 2048, dtype, 0.1, 1), ResidualTower(12, 64, 64, 2, 2048, dtype, 0.1, 2)
+    head = torch.zeros(128, device="cuda")
+    for _ in range(150):
+        z = torch.cat([A.forward(xa[:2000]), B.forward(xb[:2000])], 1).float()
+        d = (torch.sigmoid(z @ head) - label[:2000]) / 2000
+        dz = d[:, None] * head
+        head -= 0.1 * (z.T @ d)
+        for t, part in ((A, dz[:, :64]), (B, dz[:, 64:])):
+            t.backward(part)
+            t.sgd(0.1)
+
+    def score(rows):
+        return torch.cat([A.forward(xa[rows], train=False), B.forward(xb[rows], train=False)], 1).float() @ head
+
+    batch = score(slice(2000, 2400))
+    one = torch.cat([score(slice(i, i + 1)) for i in range(2000, 2400)])
+    # a batch's products may add up in another order: each stored value may be rounded the other way
+    assert _rel(one, batch.double().cpu()) <= (_bf16_bound(2) if dtype == "bf16" else 1e-4)
+    right = float(((one > 0) == (label[2000:] > 0.5)).float().mean())
+    assert right >= 0.7                                       # chance: 0.5, with a deviation of 0.025
