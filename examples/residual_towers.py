@@ -3,8 +3,10 @@
 Each party runs a tower of residual blocks (layer norm, dropout, residual join:
 the library's row operators) on its own features; party B's embedding goes to
 party A, which holds the labels, a linear head on both embeddings and the
-binary cross-entropy, and sends back the gradient of B's embedding.  Synthetic
-data (the seeded teacher of vfl_synth), plain SGD.
+binary cross-entropy, and sends back the gradient of B's embedding.  Both run in
+one process and hand these over as tensors, in step (the library's channels,
+with their bounded staleness, clipping and noise, carry the messages of its own
+bottom models).  Synthetic data (the seeded teacher of vfl_synth), plain SGD.
 
     python examples/residual_towers.py [--steps 200] [--rows 20000] [--dtype bf16]
 """

@@ -40,6 +40,8 @@
  * vfl_last_error() gives a text for the last failure on a context; with a
  * NULL context, the text of the calling thread's last vfl_workspace_size,
  * vfl_create or row operator failure (empty after a success of one of them).
+ * An earlier HIP error that the calling thread has not asked for yet is not
+ * taken for a call's own.
  */
 #ifndef VFL_H
 #define VFL_H
@@ -408,8 +410,10 @@ vfl_status vfl_philox(uint64_t seed, uint32_t step, uint32_t tag, uint32_t row0,
 
 /* Row operators of residual towers: dropout, layer norm and the residual
  * join of the two, forward and backward.  They need no context: a program
- * that trains its own tower in front of the exchange (residual blocks instead
- * of the bottom model's plain layers) calls them on its own buffers.  Each
+ * that trains a party model of its own (residual blocks instead of the bottom
+ * model's plain layers) calls them on its own buffers, and hands its embeddings
+ * and gradients over itself (the channels of a context carry those of its
+ * bottom models only).  Each
  * call enqueues its work on `stream` (a hipStream_t, NULL: the null stream) of
  * the current device and returns; nothing is allocated, and every result is
  * the same from run to run.  Activations and their gradients have the

@@ -246,7 +246,7 @@ __device__ __forceinline__ T* out_row(const Mat& m, int64_t r) { return (T*)m.p 
 // The matrix's chunks dealt to the threads in order, so that a wavefront's are
 // consecutive whatever the width; a thread steps its (row, chunk) pair by
 // (drow, dq), a whole grid, without a division.  HBM bounds it (32768 x 1024
-// bf16: 23.7 us, 5.7 TB/s; the Philox block of a chunk costs 10 rounds of two
+// bf16: 23.6 us, 5.7 TB/s; the Philox block of a chunk costs 10 rounds of two
 // multiplications beside 32 bytes moved), and the launch below about 10 MB
 // (4099 x 333 float32: 4.2 us).
 template <typename T, Form F>
@@ -321,7 +321,7 @@ __device__ __forceinline__ int group_of_wave(int lanes) {
 // row's sum of squares is the sum of M_w + n_w (m_w - mean)^2, which takes one
 // barrier a row (the slots alternate) and loses nothing to cancellation.  HOIST:
 // a thread's gamma and beta are loaded before its first row and kept.  HBM
-// bounds it: residual 32768 x 1024 bf16 46.3 us (5.8 TB/s), layer norm 32768 x
+// bounds it: residual 32768 x 1024 bf16 45.9 us (5.8 TB/s), layer norm 32768 x
 // 512 bf16 11.1 us (6.1 TB/s, partly from the last-level cache); one row takes
 // 2.1 us, a kernel's launch.
 template <typename T, bool RES, int G, int CH, Form F, bool HOIST, bool EARLY>
@@ -603,8 +603,8 @@ __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_
 // and leave one partial pair of float32 rows (2 x cols at j.part), or the result
 // itself where the grid is one workgroup.  A workgroup a CU keeps the partial
 // pairs few; HBM bounds it, and beside that the start, the end and the second
-// launch, about 8 us in all: residual 32768 x 1024 bf16 67.0 us (5.0 TB/s),
-// 1537 x 5001 float32 38.7 (4.0 TB/s), layer norm 262144 x 64 bf16 22.8 (4.5
+// launch, about 8 us in all: residual 32768 x 1024 bf16 66.8 us (5.0 TB/s),
+// 1537 x 5001 float32 38.5 (4.0 TB/s), layer norm 262144 x 64 bf16 22.7 (4.5
 // TB/s; 24.2 with two workgroups a CU).
 template <typename T, bool RES, int G, int CH, int NT, Form F, bool EARLY>
 __global__ __launch_bounds__(NT) void k_norm_backward(BackwardArgs<RES> j) {
@@ -670,11 +670,11 @@ __global__ __launch_bounds__(NT) void k_norm_backward(BackwardArgs<RES> j) {
 // Chunks of the columns that a workgroup of backward_columns takes.
 constexpr int column_lanes(int G) { return G > 64 ? 8 : 4; }
 
-// Few rows: the first workgroups take 32 columns of the weights' gradients each
-// over all rows (64 of wide rows), the others the rows; x and dy are read twice
-// (the second time from a cache), but nothing has to meet between workgroups.
-// The columns' chain of loads bounds it: 256 x 16 float32 3.0 us, 1024 x 2048
-// bf16 9.9.
+// Few rows (and any number of more than 16384 columns): the first workgroups take
+// 32 columns of the weights' gradients each over all rows (64 of wide rows), the
+// others the rows; x and dy are read twice (few rows the second time from a
+// cache), but nothing has to meet between workgroups.  The columns' chain of loads
+// bounds it: layer norm 512 x 16 float32 3.6 us, 1024 x 2048 bf16 10.2.
 template <typename T, bool RES, int NT, int LC, Form F>
 __device__ __forceinline__ void backward_columns(const BackwardArgs<RES>& j, int block) {
   constexpr int NW = NT / 64, SL = NT / LC, U = sizeof(T) == 2 && LC == 4 ? 8 : 4;
@@ -874,14 +874,16 @@ hipError_t forward_wide(const NormJob& j, hipStream_t st) {
 // threads of a workgroup of the backward
 constexpr int backward_threads(int G) { return G > 512 ? G : 512; }
 
-// Rows up to which a backward pass reads x and dy twice in one launch instead of
-// leaving partial sums to a second one.  The columns' workgroups take a time
-// that grows with the rows, and with their bytes once these no longer come from
-// one cache; the second launch costs 2 to 4 us.  One launch against two, us:
-// 1536 x 64 6.6, 7.9, 2048 x 64 7.7, 8.0; 1280 x 256 float32 8.1, 7.9; bf16
-// layer norm 1024 x 500 7.9, 7.9, 1024 x 2048 9.9, 9.9, 768 x 5001 14.7, 13.8,
-// residual 1536 x 1500 13.8, 14.5; float32 layer norm 768 x 500 7.9, 7.9,
-// 768 x 1500 11.8, 9.8, residual 768 x 3000 17.5, 18.1, 1024 x 5001 34.4, 28.8.
+// Rows up to which (these included) a backward pass reads x and dy twice in one
+// launch instead of leaving partial sums to a second one.  The columns' workgroups
+// take a time that grows with the rows, and with their bytes once these no longer
+// come from one cache; the second launch costs 2 to 4 us.  One launch against two,
+// us: 1536 x 64 6.6, 7.9; bf16 layer norm 1024 x 500 7.9, 7.9, 1024 x 2048 9.9,
+// 9.9; float32 layer norm 768 x 500 7.9, 7.9, residual 768 x 3000 17.5, 18.1,
+// 1024 x 5001 34.4, 28.8.  One limit serves both operators, so it is too high for
+// some layer norms that lie on it (1280 x 256 float32 8.1, 7.9; 768 x 5001 bf16
+// 14.7, 13.8; 768 x 1500 float32 11.8, 9.8) and too low for others (2048 x 64
+// 7.7, 8.0) and for some joins (1536 x 1500 bf16 13.8, 14.5).
 int64_t few_rows(int per, Elt e) {
   if (per <= 16) return 1920;
   if (per <= 32) return 1280;
@@ -901,6 +903,12 @@ struct BackwardPlan {
 BackwardPlan backward_plan(int64_t rows, int cols, Elt e, bool weights) {
   const int per = (cols + 7) / 8;
   const bool wide = per > 128;
+  // More than 16384 columns are four chunks a lane, which leave no registers for
+  // the weights' gradients: one launch reads x and dy twice whatever the rows, and
+  // a residual join keeps up to 54 registers a lane in scratch memory (its float32
+  // pass over 8193 to 16384 columns up to 7).  1000 x 20000 layer norm float32 82
+  // us, bf16 46 (47 and 23 for the bytes at a copy's rate), residual join 189 and
+  // 123 (78 and 39).
   BackwardPlan p{};
   for (p.lanes = 1; p.lanes < 64 && p.lanes < per; p.lanes *= 2) {}
   if (wide) p.lanes = per <= 1024 ? 512 : 1024;
@@ -951,8 +959,9 @@ hipError_t backward_with(const NormJob& j, const BackwardPlan& p, hipStream_t st
   if (!chunks_fit((j.cols + 7) / 8, lanes, CH)) return hipErrorInvalidConfiguration;
   BackwardArgs<RES> a;
   if constexpr (RES) {
-    // an absent operand becomes one that changes nothing: ds is read from v and
-    // not added, dr goes where dx is written after it, dx where dr is, undropped
+    // an absent operand becomes one that changes nothing, at the price of a load
+    // that is not used or of a second store to the same place: ds is read from v
+    // and not added, dr goes where dx is written after it, dx where dr is, undropped
     a.d = j.d;
     a.add = j.ds.p != nullptr;
     a.ds = j.ds.p ? j.ds : j.v;

@@ -1,6 +1,6 @@
-"""A residual tower in front of the exchange, built from the library's row
-operators: an alternative to the plain bottom MLP of ``session`` for programs
-that train their own party model.
+"""A residual tower, built from the library's row operators: an alternative to
+the plain bottom MLP of ``session`` for programs that train a party model of
+their own and hand its embeddings and their gradients over themselves.
 
     s_0 = x W_in^T                       y_0 = layer norm(s_0)
     a_l = dropout(relu(y_l W1_l^T + b_l))
