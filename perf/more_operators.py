@@ -30,7 +30,7 @@ import torch
 
 own = False
 
-EPS = 1e-5
+EPS = 2.0 ** -17
 BLOCK, TOP = 128, 448.0
 NAMES = {"f32": torch.float32, "bf16": torch.bfloat16}
 
