@@ -528,6 +528,141 @@ typedef struct {
 vfl_status vfl_residual_forward(const vfl_residual_args* a, void* stream);
 vfl_status vfl_residual_backward(const vfl_residual_args* a, void* stream);
 
+/* The root-mean-square norm of a residual join, with its result in the storage
+ * type, in 8 bits, or both: the row operator of towers whose products take
+ * matrices in 8 bits (vfl_matmul8, below). */
+
+/* A matrix in 8 bits: e4m3 values (1 sign, 4 exponent and 3 fraction bits,
+ * largest value 448, no infinities) with one power of two for each block of
+ * VFL_Q8_BLOCK consecutive columns of a row.  Element (r, c) is
+ * e4m3(data[r * ld + c]) * 2^(scale[(c / 128) * scale_ld + r] - 127).
+ * data: 16-byte aligned; ld: bytes from row to row, a multiple of 128 and at
+ * least the columns rounded up to one (0: that).  scale: 16-byte aligned;
+ * scale_ld: a multiple of 16, at least the rows (0: the rows rounded up to one).
+ * What an operator makes has the smallest power, 2^-127 or more, that keeps the
+ * block's magnitudes within 448, values rounded to nearest even, zeros in the
+ * columns past the last one up to the next multiple of 128 (an operator that
+ * reads one takes these for granted), and any bytes among the exponents past the
+ * last row, up to the next multiple of 16.  A value that is infinite or NaN
+ * becomes NaN and takes no part in its block's power. */
+#define VFL_Q8_BLOCK 128
+typedef struct {
+  void* data;
+  int64_t ld;
+  uint8_t* scale;
+  int64_t scale_ld;
+} vfl_q8;
+
+/* s = r + x (in float32; r.data NULL: s = x),
+ *   k = 1 / sqrt(sum_c s^2 / cols + eps),  y = (s * k) * gamma,
+ * 1 <= cols <= VFL_NORM_MAX_COLS, eps > 0; gamma float32 [cols] (NULL: 1).  The
+ * sum is taken in 64 bits and k rounded to float32 once, so that neither k nor y
+ * nor its 8-bit form depends on how a batch is laid out or split.  The forward reads x and
+ * r and writes s, y, q (y in 8 bits, from its float32 values) and stats (float32
+ * [rows] of k), each where it is not NULL (one at least).  The backward reads s,
+ * stats, dy and ds (the gradient that reaches s past the norm; NULL data: none)
+ * and writes, with h = s * k and g = dy * gamma,
+ *   dx = ds + k * (g - h * sum_c (g h) / cols)      (the gradient of x and of r),
+ *   dgamma = sum_r dy * h      (float32 [cols]),
+ * each where it is not NULL (one at least); dgamma needs a workspace of
+ * vfl_norm_workspace_size() bytes.  Fields that a direction does not use are
+ * ignored. */
+typedef struct {
+  vfl_dtype dtype;
+  int32_t cols;
+  int64_t rows;
+  float eps;
+  const float* gamma;
+  vfl_matrix x, r, s, y, dy, ds, dx;
+  vfl_q8 q;
+  float* stats;
+  float* dgamma;
+  void* workspace;
+  size_t workspace_bytes;
+} vfl_rmsnorm_args;
+vfl_status vfl_rmsnorm_forward(const vfl_rmsnorm_args* a, void* stream);
+vfl_status vfl_rmsnorm_backward(const vfl_rmsnorm_args* a, void* stream);
+
+/* A matrix [rows x cols] of `dtype` in 8 bits: q, and qt, its transpose
+ * [cols x rows] (whose blocks run down the columns of x), each where its data is
+ * not NULL (one at least).  A layer's products take x and its weight as they are
+ * (forward), the gradient and the weight's transpose (input gradient), and the
+ * transposes of the gradient and of x (weight gradient). */
+typedef struct {
+  vfl_dtype dtype;
+  int32_t cols;
+  int64_t rows;
+  vfl_matrix x;
+  vfl_q8 q, qt;
+} vfl_quantize_args;
+vfl_status vfl_quantize(const vfl_quantize_args* a, void* stream);
+
+/* c = a b^T + bias, negative results 0 where relu is not 0: a [m x k] and b
+ * [n x k] in 8 bits, bias float32 [n] (NULL: none), c [m x n] of `dtype`, rounded
+ * once from float32 sums.  m, n <= 2^30, m n <= 2^38, 1 <= k <= VFL_MATMUL8_MAX_DEPTH, and rows
+ * of a and b are below 2^24 bytes apart.  No element of c may be one of a, b or
+ * bias.  The workspace (16-byte aligned, vfl_matmul8_workspace_size() bytes, 0 for
+ * many sizes) holds partial sums during the call; calls that may run at the same
+ * time need one each.  vfl_matmul8_workspace_size is host-only. */
+#define VFL_MATMUL8_MAX_DEPTH 8388608
+typedef struct {
+  vfl_dtype dtype;
+  int32_t relu;
+  int64_t m, n, k;
+  vfl_q8 a, b;
+  const float* bias;
+  vfl_matrix c;
+  void* workspace;
+  size_t workspace_bytes;
+} vfl_matmul8_args;
+vfl_status vfl_matmul8_workspace_size(int64_t m, int64_t n, int64_t k, size_t* bytes);
+vfl_status vfl_matmul8(const vfl_matmul8_args* a, void* stream);
+
+/* The softmax cross-entropy of a linear head over many classes, without its
+ * logits in memory (the label party's loss where a label is one of many items):
+ *   z = x w^T + bias,  lse = log(sum_c exp z_c),  loss = lse - z[label],
+ * x [rows x dim], w [classes x dim] of `dtype`, bias float32 [classes] (NULL: 0),
+ * labels int32 [rows], loss and lse float32 [rows]; rows <= VFL_LOSS_MAX_ROWS, 1 <=
+ * dim <= VFL_LOSS_MAX_DIM, 1 <= classes <= VFL_LOSS_MAX_CLASSES.  A label outside
+ * [0, classes) marks a row without one: its loss is 0 and it takes no part in any
+ * gradient, whatever its x holds (its lse is that of its x).  A bias of -inf takes
+ * a class out of every sum, whatever its weights hold; a label of such a class has
+ * a loss of +inf.
+ *   The forward writes loss and lse, each where it is not NULL (one at least;
+ * labels may be NULL where loss is).  The backward reads lse as the forward left
+ * it and, with G = dloss_r (exp(z - lse) - onehot(label)), writes
+ *   dx = G w,  dw = G^T x  (of `dtype`),  dbias = sum_r G  (float32 [classes]),
+ * each where it is not NULL (one at least).  dloss: float32 [rows], the gradient
+ * of each row's loss (NULL: `scale` for every row).  A class taken out has a
+ * gradient of 0.  G is rounded to `dtype` once, as the operand of its products;
+ * their sums are float32.
+ *   The workspace (16-byte aligned, vfl_softmax_loss_workspace_size() bytes: copies
+ * of x and w in the products' layout and pieces of G of 64 MB or one piece of 256
+ * classes) means nothing between calls; calls that may run at the same time need
+ * one each.  Fields that a direction does not use are ignored. */
+#define VFL_LOSS_MAX_ROWS 2097152
+#define VFL_LOSS_MAX_CLASSES 2097152
+#define VFL_LOSS_MAX_DIM 32768
+typedef struct {
+  vfl_dtype dtype;
+  int32_t dim;
+  int64_t rows, classes;
+  vfl_matrix x, w;
+  const float* bias;
+  const int32_t* labels;
+  float *loss, *lse;
+  const float* dloss;
+  float scale;
+  vfl_matrix dx, dw;
+  float* dbias;
+  void* workspace;
+  size_t workspace_bytes;
+} vfl_softmax_loss_args;
+vfl_status vfl_softmax_loss_workspace_size(vfl_dtype dtype, int64_t rows, int32_t dim, int64_t classes,
+                                           size_t* bytes);
+vfl_status vfl_softmax_loss_forward(const vfl_softmax_loss_args* a, void* stream);
+vfl_status vfl_softmax_loss_backward(const vfl_softmax_loss_args* a, void* stream);
+
 /* Kernel classes for vfl_timing_* (bit i of a mask selects class i). */
 typedef enum {
   VFL_K_FWD = 0,        /* party B: bottom forward + published embedding */

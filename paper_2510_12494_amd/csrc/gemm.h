@@ -1,0 +1,303 @@
+// The matrix-product core of the class head and of products in 8 bits on
+// gfx950: C = A B^T of two operands whose rows are contiguous along the sum.
+//
+// A workgroup of WR x WC wavefronts owns a BM x BN tile.  The sum runs in steps
+// of KB bytes of every row: a step's (BM + BN) * KB bytes are copied from
+// global memory straight into one of NST buffers in LDS (16 bytes a lane), NST - 1
+// steps ahead, with one barrier a step.  What a step holds depends on the type
+// alone (128 bytes: 128 e4m3 values, 64 bf16 or 32 float32), so all types share
+// the tile, its copies and its reads.
+//
+// A fragment is 16 rows of an operand; lane l holds 16-byte chunks l / 16 and
+// l / 16 + 4 of row l % 16.  The sum may be taken in any order as long as A and
+// B agree, so a chunk's elements go to one MFMA (bf16: 16x16x32), to four
+// (float32: 16x16x4, an element each), or both chunks to one (e4m3: 16x16x128
+// with a power of two for each block of 128).  That instruction sums its 128
+// products with about 16 bits: results are 1.5e-5 of their norm off whatever the
+// length of the sum (256 and 4096 squared, 128 to 8192 long), 1 / 100 of what
+// rounding them to bf16 adds.  kE4m3Wide makes bf16 of the values, powers and all,
+// which loses nothing, and takes the bf16 instruction at half the rate, whose sums
+// are float32 ones.
+//
+// LDS holds a fragment's rows together, chunk c of its row i at place
+// c ^ swizzle(i): 16 lanes read 256 consecutive bytes in some order, without bank
+// conflicts, while a copy writes lane after lane.  Which rows of the tile make
+// up a fragment is free: columns are dealt to groups of DN = 4 fragments (fewer
+// where a wavefront has fewer) in turn (fragment f, row i: DN i + f), so a lane's
+// results of a group are DN consecutive columns and are stored at once; rows
+// likewise (kDealt), or in blocks of 4 DM with four consecutive ones from each
+// fragment (kBlocks), so that a lane has 4 DM consecutive rows of a column and can
+// also store the transpose.
+#pragma once
+#include <utility>
+
+#include "device.h"
+
+namespace vfl {
+namespace gemm {
+
+using namespace dev;
+
+enum Type { kE4m3, kE4m3Wide, kBf16, kF32 };
+__host__ __device__ constexpr bool is_e4m3(Type t) { return t == kE4m3 || t == kE4m3Wide; }
+enum Rows { kDealt, kBlocks };
+
+typedef __attribute__((ext_vector_type(8))) int i32x8;
+typedef __attribute__((address_space(3))) void lds_t;
+
+// wait until at most n of this wavefront's vector-memory operations and none
+// of its LDS operations are outstanding
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+  static_assert(N >= 0 && N < 64);
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));
+}
+
+// An operand: rows of ld bytes, `last` the last row's index; rows past it are
+// read as that row (their results are not kept).  8-bit operands: the exponent
+// bytes of step s at scale + s * scale_ld + row, in dwords of four rows.
+struct Operand {
+  const char* p;
+  int64_t ld;
+  int64_t last;
+  const uint8_t* scale;
+  int64_t scale_ld;
+};
+
+template <Type TY, int BM_, int BN_, int WR, int WC, int KB_, int NST_, Rows ROWS = kDealt>
+struct Tile {
+  static constexpr int BM = BM_, BN = BN_, KB = KB_, NST = NST_;
+  static constexpr int kWaves = WR * WC, kThreads = 64 * kWaves;
+  static constexpr int WM = BM / WR, WN = BN / WC, MF = WM / 16, NF = WN / 16;
+  static constexpr int kStage = (BM + BN) * KB, kLds = NST * kStage;
+  static constexpr int kRowsPerCopy = 1024 / KB, kChunks = KB / 16;
+  static constexpr int kCopies = kStage / 1024 / kWaves;      // a wavefront's copies of a step
+  static constexpr int kHalves = KB / 64;                     // 16-byte chunks a lane reads of a row
+  static constexpr int kScales = is_e4m3(TY) ? (MF + NF) / 4 : 0;
+  static constexpr int kBytes = is_e4m3(TY) ? 1 : TY == kBf16 ? 2 : 4, kElements = KB / kBytes;
+  static_assert(KB == 64 || KB == 128);
+  static_assert(!is_e4m3(TY) || KB == 128, "a step of e4m3 is one block of its scales");
+  static_assert(kStage % (1024 * kWaves) == 0 && BM * KB % 1024 == 0);
+  static constexpr int DM = MF < 4 ? MF : 4, DN = NF < 4 ? NF : 4;      // fragments of a group
+  static_assert(MF % DM == 0 && NF % DN == 0);
+  static_assert(!is_e4m3(TY) || (DM == 4 && DN == 4), "a dword of exponents is four rows");
+  static_assert((NST - 2) * (kCopies + kScales) < 64);
+
+  typedef f32x4 Acc[MF][NF];
+
+  // the row within its group of row i of the group's fragment f
+  __device__ static int row_of(int f, int i) {
+    return ROWS == kDealt ? DM * i + f : 4 * DM * (i >> 2) + 4 * f + (i & 3);
+  }
+  __device__ static int col_of(int f, int i) { return DN * i + f; }
+
+  // where in the tile this wavefront's results lie
+  int lane, wm, wn;
+  __device__ Tile() {
+    lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    wm = wave / WC * WM;
+    wn = wave % WC * WN;
+  }
+  // tile row of result r (0..3) of row fragment f; first of the DN tile columns of
+  // column fragments DN q .. DN q + DN - 1
+  __device__ int row(int f, int r) const {
+    return wm + 16 * DM * (f / DM) + row_of(f % DM, 4 * (lane >> 4) + r);
+  }
+  __device__ int col(int q) const { return wn + 16 * DN * q + DN * (lane & 15); }
+
+  // acc += the sum over steps [s0, s1) of A's rows from m0 and B's from n0; s0 < s1
+  __device__ void run(const Operand& A, const Operand& B, int64_t m0, int64_t n0, int s0, int s1, char* lds,
+                      Acc& acc) const {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // this lane's source of each of the wavefront's copies: the offset from
+    // the tile's first row (below 2^31: the host bounds ld), or the row that
+    // stands for those past the end
+    const VFL_GLOBAL char* a0 = glb(A.p) + min(m0, A.last) * A.ld + (int64_t)s0 * KB;
+    const VFL_GLOBAL char* b0 = glb(B.p) + min(n0, B.last) * B.ld + (int64_t)s0 * KB;
+    uint32_t off[kCopies];
+#pragma unroll
+    for (int c = 0; c < kCopies; ++c) {
+      const int R = (wave + c * kWaves) * kRowsPerCopy + lane / kChunks;      // its LDS row
+      const bool of_a = (wave + c * kWaves) * kRowsPerCopy < BM;              // uniform
+      const int rr = of_a ? R : R - BM;
+      const int f = rr >> 4, i = rr & 15;
+      const int row = of_a ? f / DM * (16 * DM) + row_of(f % DM, i) : f / DN * (16 * DN) + col_of(f % DN, i);
+      const int64_t top = of_a ? A.last - min(m0, A.last) : B.last - min(n0, B.last);
+      const int swz = KB == 128 ? (i >> 1) & 7 : (i >> 2) & 3;
+      off[c] = (uint32_t)(min((int64_t)row, top) * (of_a ? A.ld : B.ld)) + (uint32_t)(((lane % kChunks) ^ swz) * 16);
+    }
+    auto copy = [&](int s) {                         // step s0 + s
+      char* dst = lds + (NST == 2 ? s & 1 : s % NST) * kStage;
+#pragma unroll
+      for (int c = 0; c < kCopies; ++c) {
+        const int blk = wave + c * kWaves;
+        const VFL_GLOBAL char* src = (blk * kRowsPerCopy < BM ? a0 : b0) + (int64_t)s * KB;
+        __builtin_amdgcn_global_load_lds((VFL_GLOBAL void*)(src + off[c]), (lds_t*)(dst + blk * 1024), 16, 0, 0);
+      }
+    };
+    // e4m3: the exponents of this lane's rows, a dword for four fragments
+    uint32_t sa[kScales ? MF / 4 : 1], sb[kScales ? NF / 4 : 1], na[kScales ? MF / 4 : 1], nb[kScales ? NF / 4 : 1];
+    const VFL_GLOBAL uint8_t *sa0 = nullptr, *sb0 = nullptr;
+    uint32_t soa[kScales ? MF / 4 : 1], sob[kScales ? NF / 4 : 1];
+    if constexpr (is_e4m3(TY)) {
+      static_assert(ROWS == kDealt, "a dword of exponents is four consecutive rows");
+      sa0 = glb(A.scale);
+      sb0 = glb(B.scale);
+#pragma unroll
+      for (int q = 0; q < MF / 4; ++q)
+        soa[q] = (uint32_t)min(m0 + wm + 64 * q + 4 * (lane & 15), A.last & ~(int64_t)3);
+#pragma unroll
+      for (int q = 0; q < NF / 4; ++q)
+        sob[q] = (uint32_t)min(n0 + wn + 64 * q + 4 * (lane & 15), B.last & ~(int64_t)3);
+    }
+    auto scales = [&](int s, uint32_t* da, uint32_t* db) {
+      const VFL_GLOBAL uint8_t* pa = sa0 + (int64_t)(s0 + s) * A.scale_ld;
+      const VFL_GLOBAL uint8_t* pb = sb0 + (int64_t)(s0 + s) * B.scale_ld;
+#pragma unroll
+      for (int q = 0; q < MF / 4; ++q) da[q] = *(const VFL_GLOBAL uint32_t*)(pa + soa[q]);
+#pragma unroll
+      for (int q = 0; q < NF / 4; ++q) db[q] = *(const VFL_GLOBAL uint32_t*)(pb + sob[q]);
+    };
+
+    const int n = s1 - s0;
+    const int fi = lane & 15, g = lane >> 4;
+    const int swz = KB == 128 ? (fi >> 1) & 7 : (fi >> 2) & 3;
+    int place[kHalves];
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) place[h] = fi * KB + ((g + 4 * h) ^ swz) * 16;
+
+#pragma unroll
+    for (int s = 0; s < NST - 1; ++s)
+      if (s < n) copy(s);
+    if constexpr (is_e4m3(TY)) scales(0, na, nb);
+    for (int s = 0; s < n; ++s) {
+      // this wavefront's copies of step s have landed, and after the barrier
+      // everyone's; everyone has also read step s - 1, whose buffer is next
+      if (NST > 2 && s + NST - 2 < n) wait_copies<(NST - 2) * kCopies>();
+      else wait_copies<0>();
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (is_e4m3(TY)) {
+#pragma unroll
+        for (int q = 0; q < MF / 4; ++q) sa[q] = na[q];
+#pragma unroll
+        for (int q = 0; q < NF / 4; ++q) sb[q] = nb[q];
+        if (s + 1 < n) scales(s + 1, na, nb);
+      }
+      if (s + NST - 1 < n) copy(s + NST - 1);
+      __builtin_amdgcn_sched_barrier(0);
+      const char* S = lds + (NST == 2 ? s & 1 : s % NST) * kStage;
+      const char* SA = S + wm * KB;
+      const char* SB = S + (BM + wn) * KB;
+      if constexpr (TY == kE4m3) {
+        u32x4 b[NF][2];
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) b[f][h] = *(const u32x4*)(SB + f * 16 * KB + place[h]);
+#pragma unroll
+        for (int f = 0; f < MF; ++f) {
+          u32x4 a[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) a[h] = *(const u32x4*)(SA + f * 16 * KB + place[h]);
+          mma8(a, b, sa[f / 4], sb, f & 3, acc[f], std::make_integer_sequence<int, NF>{});
+        }
+      } else if constexpr (TY == kE4m3Wide) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          bf16x8 b[NF][2];
+#pragma unroll
+          for (int f = 0; f < NF; ++f) widen(*(const u32x4*)(SB + f * 16 * KB + place[h]), sb[f / 4], f & 3, b[f]);
+#pragma unroll
+          for (int f = 0; f < MF; ++f) {
+            bf16x8 a[2];
+            widen(*(const u32x4*)(SA + f * 16 * KB + place[h]), sa[f / 4], f & 3, a);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+              for (int c = 0; c < NF; ++c)
+                acc[f][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[t], b[c][t], acc[f][c], 0, 0, 0);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) {
+          u32x4 b[NF];
+#pragma unroll
+          for (int f = 0; f < NF; ++f) b[f] = *(const u32x4*)(SB + f * 16 * KB + place[h]);
+#pragma unroll
+          for (int f = 0; f < MF; ++f) {
+            const u32x4 a = *(const u32x4*)(SA + f * 16 * KB + place[h]);
+            if constexpr (TY == kBf16) {
+#pragma unroll
+              for (int c = 0; c < NF; ++c)
+                acc[f][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                                    __builtin_bit_cast(bf16x8, b[c]), acc[f][c], 0, 0, 0);
+            } else {
+#pragma unroll
+              for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int c = 0; c < NF; ++c)
+                  acc[f][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[t]), __uint_as_float(b[c][t]),
+                                                                   acc[f][c], 0, 0, 0);
+            }
+          }
+        }
+      }
+    }
+  }
+
+  // sixteen e4m3 values times their power of two as bf16 (byte f of s: its exponent,
+  // moved to where a float32 has it)
+  __device__ static __forceinline__ void widen(const u32x4& v, uint32_t s, int f, bf16x8 (&out)[2]) {
+    const float power = __uint_as_float(((s >> (8 * f)) & 255u) << 23);
+    u32x4 w[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      w[i / 2][2 * (i % 2)] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[i], power, false));
+      w[i / 2][2 * (i % 2) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[i], power, true));
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) out[t] = __builtin_bit_cast(bf16x8, w[t]);
+  }
+
+  // one row fragment of e4m3 times every column fragment; the exponent byte of a
+  // fragment is its number's within four (an immediate of the instruction)
+  template <int... C>
+  __device__ static __forceinline__ void mma8(const u32x4 (&a)[2], const u32x4 (&b)[NF][2], uint32_t sa,
+                                              const uint32_t* sb, int fa, f32x4 (&acc)[NF],
+                                              std::integer_sequence<int, C...>) {
+    struct Pair { u32x4 x, y; };
+    const i32x8 va = __builtin_bit_cast(i32x8, (Pair{a[0], a[1]}));
+    switch (fa) {
+#define VFL_ROW_FRAGMENT(F)                                                                                   \
+  case F:                                                                                                     \
+    ((acc[C] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(                                              \
+          va, __builtin_bit_cast(i32x8, (Pair{b[C][0], b[C][1]})), acc[C], 0, 0, F, (int)sa, C & 3,           \
+          (int)sb[C / 4])),                                                                                   \
+     ...);                                                                                                    \
+    break
+      VFL_ROW_FRAGMENT(0);
+      VFL_ROW_FRAGMENT(1);
+      VFL_ROW_FRAGMENT(2);
+      VFL_ROW_FRAGMENT(3);
+#undef VFL_ROW_FRAGMENT
+    }
+  }
+};
+
+// Tile t of tm x tn: workgroups are dealt to the eight XCDs in turn, so each XCD
+// takes a contiguous range of an order that walks bands of eight tile rows column
+// by column: the tiles of a range share rows of both operands in one L2.
+__device__ __forceinline__ void tile_of(uint32_t block, uint32_t tm, uint32_t tn, uint32_t* m, uint32_t* n) {
+  const uint32_t total = tm * tn, per = total / 8, more = total % 8;
+  const uint32_t x = block % 8;
+  const uint32_t t = x * per + min(x, more) + block / 8;
+  const uint32_t band = t / (8 * tn), in = t - band * 8 * tn, rows = min(8u, tm - 8 * band);
+  *m = 8 * band + in % rows;
+  *n = in / rows;
+}
+
+}  // namespace gemm
+}  // namespace vfl

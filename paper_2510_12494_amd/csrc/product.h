@@ -1,0 +1,140 @@
+// Kernels of a matrix product over the core of gemm.h: a tile a workgroup, the
+// sum cut into parts where there are few tiles, the parts joined in order.
+#pragma once
+#include "gemm.h"
+#include "rowchunk.h"
+
+namespace vfl {
+namespace {
+
+using namespace dev;
+using namespace gemm;
+
+struct ProductArgs {
+  Operand a, b;
+  void* c;
+  int64_t ldc;
+  const float* bias;
+  uint32_t tm, tn;
+  int n, steps, per;                   // per: steps of a part
+  int64_t m;
+  int relu, add;
+};
+
+__device__ __forceinline__ f32x4 finish(f32x4 v, const f32x4& bias, int relu) {
+  v += bias;
+  // a NaN passes, as through a comparison
+  if (relu) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];
+  }
+  return v;
+}
+
+__device__ __forceinline__ f32x4 bias4(const float* bias, int col, int n) {
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (bias) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (col + i < n) v[i] = bias[col + i];
+  }
+  return v;
+}
+
+// the first `left` of W values (all: at once)
+template <int W = 4, typename T>
+__device__ __forceinline__ void store_to(T* p, const f32x4& v, int left) {
+  if constexpr (W == 4) {
+    if (left >= 4) {
+      const float w[4] = {v[0], v[1], v[2], v[3]};
+      store4(p, w);
+      return;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < W; ++i)
+    if (i < left) st1<T>(p + i, v[i]);
+}
+
+// One tile of the product, or (gridDim.y > 1) of part blockIdx.y of its sum, as
+// float32 partial sums [part][m][n]; add: on top of what C holds.
+template <class TL, typename T>
+__global__ __launch_bounds__(TL::kThreads) void k_product(ProductArgs j) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  uint32_t tm, tn;
+  tile_of(blockIdx.x, j.tm, j.tn, &tm, &tn);
+  const TL tile;
+  typename TL::Acc acc;
+#pragma unroll
+  for (int f = 0; f < TL::MF; ++f)
+#pragma unroll
+    for (int c = 0; c < TL::NF; ++c) acc[f][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int s0 = blockIdx.y * j.per, s1 = min(s0 + j.per, j.steps);
+  const int64_t m0 = (int64_t)tm * TL::BM;
+  const int n0 = (int)tn * TL::BN;
+  tile.run(j.a, j.b, m0, n0, s0, s1, smem, acc);
+#pragma unroll
+  for (int q = 0; q < TL::NF / TL::DN; ++q) {
+    const int col = n0 + tile.col(q), left = j.n - col;
+    const f32x4 bias = bias4(j.bias, col, j.n);
+#pragma unroll
+    for (int f = 0; f < TL::MF; ++f)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int64_t row = m0 + tile.row(f, r);
+        if (row >= j.m || left <= 0) continue;
+        T* p = (T*)j.c + ((int64_t)blockIdx.y * j.m + row) * j.ldc + col;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < TL::DN; ++c) {
+          v[c] = acc[f][TL::DN * q + c][r];
+          if (j.add && c < left) v[c] += ld1<T>(p + c);
+        }
+        store_to<TL::DN>(p, finish(v, bias, j.relu), left);
+      }
+  }
+}
+
+constexpr int kJoinThreads = 256;
+struct JoinArgs {
+  const float* part;
+  const float* bias;
+  void* c;
+  int64_t ldc, m, items, ld;           // ld: of the partial sums
+  int n, quads, parts, relu;
+};
+
+// The parts of a split product, summed in order.
+template <typename T>
+__global__ __launch_bounds__(kJoinThreads) void k_product_join(JoinArgs j) {
+  const int64_t at = (int64_t)blockIdx.x * kJoinThreads + threadIdx.x;
+  if (at >= j.items) return;
+  const int64_t row = at / j.quads;
+  const int col = 4 * (int)(at - row * j.quads);
+  const float* p = j.part + row * j.ld + col;
+  f32x4 v = *(const f32x4*)p;
+  for (int i = 1; i < j.parts; ++i) v += *(const f32x4*)(p + (int64_t)i * j.m * j.ld);
+  store_to((T*)j.c + row * j.ldc + col, finish(v, bias4(j.bias, col, j.n), j.relu), j.n - col);
+}
+
+int64_t tiles_of(int64_t v, int by) { return (v + by - 1) / by; }
+// elements of a row of partial sums over n columns
+int64_t part_ld(int64_t n) { return (n + 3) & ~(int64_t)3; }
+
+template <class TL, typename T>
+hipError_t product(const ProductArgs& a, int parts, hipStream_t st) {
+  return enqueue(k_product<TL, T>, dim3(a.tm * a.tn, (unsigned)parts), dim3(TL::kThreads), TL::kLds, st, a);
+}
+
+// parts [parts][m][part_ld(n)] -> c
+template <typename T>
+hipError_t join(const float* part, int parts, int64_t m, int64_t n, const float* bias, int relu, const Mat& c,
+                hipStream_t st) {
+  const int64_t ld = part_ld(n), items = m * (ld / 4);
+  const JoinArgs a{part, bias, c.p, c.ld, m, items, ld, (int)n, (int)(ld / 4), parts, relu};
+  return enqueue(k_product_join<T>, dim3((unsigned)((items + kJoinThreads - 1) / kJoinThreads)), dim3(kJoinThreads), 0, st,
+                 a);
+}
+
+}  // namespace
+}  // namespace vfl

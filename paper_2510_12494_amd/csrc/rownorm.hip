@@ -10,8 +10,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "device.h"
-#include "rowops.h"
+#include "rowchunk.h"
 
 namespace vfl {
 namespace {
@@ -41,9 +40,14 @@ struct ForwardArgs : std::conditional_t<RES, ForwardResidual, NoResidual> {
   int cols, grid, threads;
   float eps;
 };
-struct BackwardResidual { DropKey d; Mat ds, dx; int add; };
-template <bool RES>
-struct BackwardArgs : std::conditional_t<RES, BackwardResidual, NoResidual> {
+struct BackwardJoin { DropKey d; Mat ds, dx; int add; };
+struct BackwardRms { Mat ds; int add; };
+// kRms: the root-mean-square norm of a join (its forward is in rms.hip); the
+// layer norm's formulas with a mean of 0, no mean of g and no dbeta
+enum Op { kNorm, kJoin, kRms };
+template <Op OP>
+struct BackwardArgs
+    : std::conditional_t<OP == kJoin, BackwardJoin, std::conditional_t<OP == kRms, BackwardRms, NoResidual>> {
   Mat v, dy, dr;
   const float *gamma, *stats;
   float *dgamma, *dbeta, *part;
@@ -55,161 +59,6 @@ struct ReduceArgs {
   float *dgamma, *dbeta;
   int cols, parts;
 };
-
-// ------------------------------------------------------------------- chunks
-// Vectors at element alignment: gfx950 loads and stores 16 bytes at any
-// address, so rows of an odd stride take the same path as aligned ones.
-typedef u32x4 __attribute__((aligned(2))) u32x4_a2;
-typedef u32x2 __attribute__((aligned(2))) u32x2_a2;
-typedef uint32_t __attribute__((aligned(2))) u32_a2;
-typedef f32x4 __attribute__((aligned(4))) f32x4_a4;
-typedef f32x2 __attribute__((aligned(4))) f32x2_a4;
-
-template <typename T> struct Raw;                 // a chunk as it is stored
-template <> struct Raw<uint16_t> { u32x4 a; };
-template <> struct Raw<float> { f32x4 a, b; };
-
-__device__ __forceinline__ Raw<uint16_t> load_at(const uint16_t* p) { return {*(const u32x4_a2*)p}; }
-__device__ __forceinline__ Raw<float> load_at(const float* p) {
-  return {*(const f32x4_a4*)p, *(const f32x4_a4*)(p + 4)};
-}
-__device__ __forceinline__ void unpack(const Raw<uint16_t>& r, float (&v)[8]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __uint_as_float(r.a[i] << 16);
-    v[2 * i + 1] = __uint_as_float(r.a[i] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ void unpack(const Raw<float>& r, float (&v)[8]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[i] = r.a[i];
-    v[4 + i] = r.b[i];
-  }
-}
-
-// The columns of a row (kernel-uniform): n of them in `per` chunks, the last
-// one `part` columns wide when that is not 0.  Rows from `edge` on are so near
-// the matrix's end that a whole last chunk would pass it.
-struct Cols {
-  int n, per, part;
-  int64_t edge;
-  __device__ explicit Cols(int cols, int64_t rows) : n(cols), per((cols + 7) >> 3), part(cols & 7) {
-    const int past = 8 * per - n;                    // rows of n columns and more hold these
-    edge = past ? rows - (past + n - 1) / n : INT64_MAX;
-  }
-};
-
-// How the columns of a kernel's rows lie: kExact: each lane's chunks are all
-// whole; kRagged: a row may end inside a chunk, and lanes may have none of it
-// (rows of eight columns and more); kSmall: rows of one chunk of any width.
-// `whole`: this chunk is whole whatever the form.
-enum Form { kExact, kRagged, kSmall };
-
-// Chunk q of a row, loaded without a branch.  A row's last chunk is read whole:
-// past the row's end lie the next row or what is between the two.  Lanes
-// without a chunk read the last one.  On the matrix's edge rows the last eight
-// columns are read instead (rows of fewer are gathered), so that no access
-// passes the matrix.
-template <Form F, typename T>
-__device__ __forceinline__ Raw<T> load_chunk(const T* row, int q, const Cols& k, bool edge, bool whole = false) {
-  if (F == kExact || whole) return load_at(row + 8 * q);
-  if constexpr (F == kSmall) {
-    if (k.n < 8) {
-      if (!edge) return load_at(row);
-      T e[8] = {};
-#pragma unroll
-      for (int i = 0; i < 7; ++i)
-        if (i < k.n) e[i] = row[i];
-      return __builtin_bit_cast(Raw<T>, e);
-    }
-  }
-  return load_at(row + min(8 * q, edge ? k.n - 8 : 8 * k.per - 8));
-}
-
-// Its values: `past` at and past the row's end (on an edge row, those of a
-// partial chunk moved to their places).
-template <Form F, typename T>
-__device__ __forceinline__ void chunk_values(const Raw<T>& r, int q, const Cols& k, bool edge, float (&v)[8],
-                                             bool whole = false, float past = 0.f) {
-  unpack(r, v);
-  if (F == kExact || whole) return;
-  if (edge && k.n >= 8 && q == k.per - 1) {
-    const int by = 8 - k.part;                       // uniform
-    if (by & 4) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = v[i + 4];
-    }
-    if (by & 2) {
-#pragma unroll
-      for (int i = 0; i < 6; ++i) v[i] = v[i + 2];
-    }
-    if (by & 1) {
-#pragma unroll
-      for (int i = 0; i < 7; ++i) v[i] = v[i + 1];
-    }
-  }
-  const int left = k.n - 8 * q;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = i < left ? v[i] : past;
-}
-
-// Those of a row of its own (gamma, beta).
-template <Form F>
-__device__ __forceinline__ void vector_values(const float* p, int q, const Cols& k, float (&v)[8], bool whole) {
-  chunk_values<F>(load_chunk<F>(p, q, k, true, whole), q, k, true, v, whole);
-}
-
-__device__ __forceinline__ void store4(uint16_t* p, const float* v) {
-  *(u32x2_a2*)p = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-}
-__device__ __forceinline__ void store4(float* p, const float* v) { *(f32x4_a4*)p = f32x4{v[0], v[1], v[2], v[3]}; }
-__device__ __forceinline__ void store2(uint16_t* p, const float* v) { *(u32_a2*)p = pack_bf16(v[0], v[1]); }
-__device__ __forceinline__ void store2(float* p, const float* v) { *(f32x2_a4*)p = f32x2{v[0], v[1]}; }
-// EARLY: the lines leave the L2 as they are written (a non-temporal store)
-// instead of all at the kernel's end.
-template <bool EARLY>
-__device__ __forceinline__ void store8(uint16_t* p, const float* v) {
-  const u32x4_a2 w{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
-  if constexpr (EARLY) __builtin_nontemporal_store(w, (u32x4_a2*)p);
-  else *(u32x4_a2*)p = w;
-}
-template <bool EARLY>
-__device__ __forceinline__ void store8(float* p, const float* v) {
-  if constexpr (EARLY) {
-    __builtin_nontemporal_store(f32x4_a4{v[0], v[1], v[2], v[3]}, (f32x4_a4*)p);
-    __builtin_nontemporal_store(f32x4_a4{v[4], v[5], v[6], v[7]}, (f32x4_a4*)(p + 4));
-  } else {
-    store4(p, v);
-    store4(p + 4, v + 4);
-  }
-}
-
-// Stores chunk q of a row: whole, or the columns that the row has of it, in
-// pieces of four, two and one.
-template <Form F, bool EARLY = false, typename T>
-__device__ __forceinline__ void store_chunk(T* row, int q, const Cols& k, const float (&v)[8], bool whole = false) {
-  T* p = row + 8 * q;
-  if (F == kExact || whole || 8 * q + 8 <= k.n) {
-    store8<EARLY>(p, v);
-  } else if (q < k.per) {
-    const int m = k.part;                          // uniform
-    if (m & 4) {
-      store4(p, v);
-      if (m & 2) {
-        store2(p + 4, v + 4);
-        if (m & 1) st1<T>(p + 6, v[6]);
-      } else if (m & 1) {
-        st1<T>(p + 4, v[4]);
-      }
-    } else if (m & 2) {
-      store2(p, v);
-      if (m & 1) st1<T>(p + 2, v[2]);
-    } else {
-      st1<T>(p, v[0]);
-    }
-  }
-}
 
 // ------------------------------------------------------------------ dropout
 __device__ __forceinline__ uint32_t step_of(const DropKey& d) {
@@ -237,11 +86,6 @@ __device__ __forceinline__ void drop_values(const DropKey& d, const Numbers& n, 
     v[2 * i + 1] = n.w[i] > last ? v[2 * i + 1] * d.scale : 0.f;
   }
 }
-
-template <typename T>
-__device__ __forceinline__ const T* row_of(const Mat& m, int64_t r) { return (const T*)m.p + r * m.ld; }
-template <typename T>
-__device__ __forceinline__ T* out_row(const Mat& m, int64_t r) { return (T*)m.p + r * m.ld; }
 
 // The matrix's chunks dealt to the threads in order, so that a wavefront's are
 // consecutive whatever the width; a thread steps its (row, chunk) pair by
@@ -272,43 +116,6 @@ __global__ __launch_bounds__(kThreads) void k_dropout(DropArgs j) {
       ++r;
     }
   }
-}
-
-// --------------------------------------------------------------------- sums
-template <int CTRL>
-__device__ __forceinline__ float dpp(float x) {
-  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xf, 0xf, true));
-}
-
-// The sum over each group of G lanes, in every lane of it (the same bits: each
-// step adds the same two values, in either order).
-template <int G>
-__device__ __forceinline__ float group_sum(float v) {
-  if constexpr (G >= 2) v += dpp<0xB1>(v);          // lane ^ 1
-  if constexpr (G >= 4) v += dpp<0x4E>(v);          // lane ^ 2
-  if constexpr (G >= 8) v += dpp<0x141>(v);         // mirrored in 8 lanes
-  if constexpr (G >= 16) v += dpp<0x140>(v);        // mirrored in 16 lanes
-  if constexpr (G >= 32) {
-    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
-  }
-  if constexpr (G >= 64) {
-    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
-  }
-  return v;
-}
-
-// The row group of a thread: a scalar where a wavefront holds one row only.
-template <int G>
-__device__ __forceinline__ int group_of_thread() {
-  const int g = threadIdx.x / G;
-  return G >= 64 ? __builtin_amdgcn_readfirstlane(g) : g;
-}
-
-// That of a wavefront where `lanes` threads hold a row.
-__device__ __forceinline__ int group_of_wave(int lanes) {
-  return __builtin_amdgcn_readfirstlane(threadIdx.x / 64) / (lanes / 64);
 }
 
 // ------------------------------------------------------------------ forward
@@ -449,22 +256,11 @@ __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_norm_forward(Fo
 }
 
 // ----------------------------------------------------------------- backward
-// The sum over the lanes of a wavefront that share lane % G, in lanes 0 .. G-1.
-template <int G>
-__device__ __forceinline__ float stride_sum(float v) {
-  if constexpr (G <= 8) v += dpp<0x128>(v);          // rotated by 8 in 16 lanes
-  if constexpr (G <= 4) v += dpp<0x124>(v);          // by 4
-  if constexpr (G <= 2) v += dpp<0x122>(v);          // by 2
-  if constexpr (G <= 1) v += dpp<0x121>(v);          // by 1
-  if constexpr (G <= 16) {
-    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
-  }
-  if constexpr (G <= 32) {
-    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
-  }
-  return v;
+// mean and k of row r as the forward left them (kRms: k alone)
+template <Op OP>
+__device__ __forceinline__ f32x2 row_stats(const float* stats, int64_t r) {
+  if constexpr (OP == kRms) return f32x2{0.f, stats[r]};
+  else return *(const f32x2*)(stats + 2 * r);
 }
 
 // Rows first, first + stride, ... as in the forward, one pass.  G = 256: a
@@ -472,8 +268,8 @@ __device__ __forceinline__ float stride_sum(float v) {
 // those without a row left go along.  ACC: a thread also adds its columns' terms
 // of the weights' gradients to ag and ab (not with four chunks a lane, which
 // leave no registers for those).
-template <typename T, bool RES, int G, int CH, Form F, bool ACC, bool OUT, bool EARLY>
-__device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_t r, int64_t stride, float (&ag)[CH][8],
+template <typename T, Op OP, int G, int CH, Form F, bool ACC, bool OUT, bool EARLY>
+__device__ __forceinline__ void backward_rows(const BackwardArgs<OP>& j, int64_t r, int64_t stride, float (&ag)[CH][8],
                                               float (&ab)[CH][8]) {
   constexpr bool WIDE = G > 64;
   constexpr int GL = G < 64 ? G : 64;
@@ -487,28 +283,26 @@ __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_
   const int lane = WIDE ? (int)threadIdx.x - group * lanes : threadIdx.x % G;
   const float inv = 1.f / (float)k.n;
   bool add = false, drop = false;
-  if constexpr (RES) {
-    add = j.add;
-    drop = j.d.thr;
-  }
+  if constexpr (OP != kNorm) add = j.add;
+  if constexpr (OP == kJoin) drop = j.d.thr;
 
   Raw<T> xr[CH], yr[CH], sr[CH];
   f32x2 st = {0.f, 0.f};
   auto fetch = [&](int64_t r) {
-    st = *(const f32x2*)(j.stats + 2 * r);
+    st = row_stats<OP>(j.stats, r);
     const bool edge = r >= k.edge;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const int q = c * lanes + lane;
       xr[c] = load_chunk<F>(row_of<T>(j.v, r), q, k, edge, c < CH / 2);
       yr[c] = load_chunk<F>(row_of<T>(j.dy, r), q, k, edge, c < CH / 2);
-      if constexpr (RES && OUT) sr[c] = load_chunk<F>(row_of<T>(j.ds, r), q, k, edge, c < CH / 2);
+      if constexpr (OP != kNorm && OUT) sr[c] = load_chunk<F>(row_of<T>(j.ds, r), q, k, edge, c < CH / 2);
     }
   };
   if constexpr (GROUPS) fetch(min(r, j.rows - 1));
   else if (AHEAD && r < j.rows) fetch(r);
   uint32_t step = 0;
-  if constexpr (RES) step = step_of(j.d);
+  if constexpr (OP == kJoin) step = step_of(j.d);
 
   float gm[HOIST ? CH : 1][8];
   auto weights = [&](int c, int slot) {
@@ -525,7 +319,7 @@ __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_
     const bool live = !GROUPS || r < j.rows;
     if constexpr (!AHEAD) fetch(r);
     Numbers n[CH];
-    if constexpr (RES && AHEAD && OUT) {
+    if constexpr (OP == kJoin && AHEAD && OUT) {
       if (drop) {                                    // beside the row's loads
 #pragma unroll
         for (int c = 0; c < CH; ++c) n[c] = chunk_numbers(j.d, step, j.d.row0 + r, c * lanes + lane);
@@ -545,30 +339,30 @@ __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_
         // which may be infinite and would make the sums of g * h NaN
         chunk_values<F>(xr[c], q, k, edge, h[c], c < CH / 2, mean);
         chunk_values<F>(yr[c], q, k, edge, g[c], c < CH / 2);
-        if constexpr (RES && OUT) sc[c] = sr[c];
+        if constexpr (OP != kNorm && OUT) sc[c] = sr[c];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           h[c][i] = (h[c][i] - mean) * rs;
           if constexpr (ACC) {
             ag[c][i] = fmaf(g[c][i], h[c][i], ag[c][i]);
-            ab[c][i] += g[c][i];
+            if constexpr (OP != kRms) ab[c][i] += g[c][i];
           }
           g[c][i] *= gm[HOIST ? c : 0][i];
-          sg += g[c][i];
+          if constexpr (OP != kRms) sg += g[c][i];
           sgh = fmaf(g[c][i], h[c][i], sgh);
         }
       }
     }
     if (AHEAD) fetch(r + stride < j.rows ? r + stride : GROUPS ? min(r, j.rows - 1) : r);
     if constexpr (!OUT) continue;
-    sg = group_sum<GL>(sg);
+    if constexpr (OP != kRms) sg = group_sum<GL>(sg);
     sgh = group_sum<GL>(sgh);
     if constexpr (WIDE) {
       if (threadIdx.x % 64 == 0) slots[flip][threadIdx.x / 64] = f32x2{sg, sgh};
       __syncthreads();
       const int w = threadIdx.x % 16;
       const f32x2 s = 64 * w < lanes ? slots[flip][group * (lanes / 64) + w] : f32x2{0.f, 0.f};
-      sg = group_sum<16>(s[0]);
+      if constexpr (OP != kRms) sg = group_sum<16>(s[0]);
       sgh = group_sum<16>(s[1]);
       flip ^= 1;
     }
@@ -580,7 +374,7 @@ __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_
       float d[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) d[i] = rs * (g[c][i] - mg - h[c][i] * mgh);
-      if constexpr (RES) {
+      if constexpr (OP != kNorm) {
         if (add) {
           float t[8];
           chunk_values<F>(sc[c], q, k, edge, t, c < CH / 2);
@@ -589,7 +383,7 @@ __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_
         }
       }
       store_chunk<F, EARLY>(out_row<T>(j.dr, r), q, k, d, c < CH / 2);
-      if constexpr (RES) {
+      if constexpr (OP == kJoin) {
         if (!AHEAD && drop) n[c] = chunk_numbers(j.d, step, j.d.row0 + r, q);
         if (drop) drop_values(j.d, n[c], d);
         store_chunk<F, EARLY>(out_row<T>(j.dx, r), q, k, d, c < CH / 2);
@@ -606,8 +400,8 @@ __device__ __forceinline__ void backward_rows(const BackwardArgs<RES>& j, int64_
 // launch, about 8 us in all: residual 32768 x 1024 bf16 66.8 us (5.0 TB/s),
 // 1537 x 5001 float32 38.5 (4.0 TB/s), layer norm 262144 x 64 bf16 22.7 (4.5
 // TB/s; 24.2 with two workgroups a CU).
-template <typename T, bool RES, int G, int CH, int NT, Form F, bool EARLY>
-__global__ __launch_bounds__(NT) void k_norm_backward(BackwardArgs<RES> j) {
+template <typename T, Op OP, int G, int CH, int NT, Form F, bool EARLY>
+__global__ __launch_bounds__(NT) void k_norm_backward(BackwardArgs<OP> j) {
   constexpr int NW = NT / 64;
   constexpr int GL = G < 64 ? G : 64;
   constexpr bool GROUPS = G == 256;
@@ -616,8 +410,8 @@ __global__ __launch_bounds__(NT) void k_norm_backward(BackwardArgs<RES> j) {
   const int group = GROUPS ? group_of_wave(j.lanes) : G > 64 ? 0 : group_of_thread<G>();
   const int rpb = GROUPS ? j.groups : G > 64 ? 1 : NT / G;
   const int64_t first = (int64_t)blockIdx.x * rpb + group, stride = (int64_t)j.grid * rpb;
-  if (j.dr.p) backward_rows<T, RES, G, CH, F, true, true, EARLY>(j, first, stride, ag, ab);
-  else backward_rows<T, RES, G, CH, F, true, false, false>(j, first, stride, ag, ab);
+  if (j.dr.p) backward_rows<T, OP, G, CH, F, true, true, EARLY>(j, first, stride, ag, ab);
+  else backward_rows<T, OP, G, CH, F, true, false, false>(j, first, stride, ag, ab);
   const Cols k(j.cols, j.rows);
   const int lane = G > 64 ? (int)threadIdx.x - group * j.lanes : threadIdx.x % G, wave = threadIdx.x / 64;
   float* const out[2] = {j.grid == 1 ? j.dgamma : j.part + (int64_t)(2 * blockIdx.x) * k.n,
@@ -625,7 +419,7 @@ __global__ __launch_bounds__(NT) void k_norm_backward(BackwardArgs<RES> j) {
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
 #pragma unroll
-    for (int a = 0; a < 2; ++a) {
+    for (int a = 0; a < (OP == kRms ? 1 : 2); ++a) {
       float* const dst = out[a];
       float(&acc)[8] = a == 0 ? ag[c] : ab[c];
       if constexpr (G > 64) {
@@ -675,8 +469,8 @@ constexpr int column_lanes(int G) { return G > 64 ? 8 : 4; }
 // others the rows; x and dy are read twice (few rows the second time from a
 // cache), but nothing has to meet between workgroups.  The columns' chain of loads
 // bounds it: layer norm 512 x 16 float32 3.6 us, 1024 x 2048 bf16 10.2.
-template <typename T, bool RES, int NT, int LC, Form F>
-__device__ __forceinline__ void backward_columns(const BackwardArgs<RES>& j, int block) {
+template <typename T, Op OP, int NT, int LC, Form F>
+__device__ __forceinline__ void backward_columns(const BackwardArgs<OP>& j, int block) {
   constexpr int NW = NT / 64, SL = NT / LC, U = sizeof(T) == 2 && LC == 4 ? 8 : 4;
   __shared__ float sums[NW][2][8 * LC];
   const Cols k(j.cols, j.rows);
@@ -689,7 +483,7 @@ __device__ __forceinline__ void backward_columns(const BackwardArgs<RES>& j, int
     for (int u = 0; u < U; ++u) {
       const int64_t ru = r + u * SL;
       if (ru < j.rows) {
-        st[u] = *(const f32x2*)(j.stats + 2 * ru);
+        st[u] = row_stats<OP>(j.stats, ru);
         x[u] = load_chunk<F>(row_of<T>(j.v, ru), q, k, ru >= k.edge);
         y[u] = load_chunk<F>(row_of<T>(j.dy, ru), q, k, ru >= k.edge);
       }
@@ -710,7 +504,7 @@ __device__ __forceinline__ void backward_columns(const BackwardArgs<RES>& j, int
     }
   }
 #pragma unroll
-  for (int a = 0; a < 2; ++a) {
+  for (int a = 0; a < (OP == kRms ? 1 : 2); ++a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[a][i] = stride_sum<LC>(acc[a][i]);
     if (threadIdx.x % 64 < LC) {
@@ -720,7 +514,7 @@ __device__ __forceinline__ void backward_columns(const BackwardArgs<RES>& j, int
   }
   __syncthreads();
   const int a = threadIdx.x / (8 * LC), i = threadIdx.x % (8 * LC), col = block * 8 * LC + i;
-  if (a < 2 && col < k.n) {
+  if (a < (OP == kRms ? 1 : 2) && col < k.n) {
     float* const dst = a == 0 ? j.dgamma : j.dbeta;
     float t = 0.f;
 #pragma unroll
@@ -729,16 +523,16 @@ __device__ __forceinline__ void backward_columns(const BackwardArgs<RES>& j, int
   }
 }
 
-template <typename T, bool RES, int G, int CH, int NT, Form F>
-__global__ __launch_bounds__(NT) void k_norm_backward_split(BackwardArgs<RES> j) {
+template <typename T, Op OP, int G, int CH, int NT, Form F>
+__global__ __launch_bounds__(NT) void k_norm_backward_split(BackwardArgs<OP> j) {
   constexpr int RPB = G > 64 ? 1 : NT / G;
   constexpr int LC = column_lanes(G);
   constexpr Form FC = F == kExact && G * CH % LC != 0 ? (G == 1 ? kSmall : kRagged) : F;
   if ((int)blockIdx.x < j.col_blocks) {
-    backward_columns<T, RES, NT, LC, FC>(j, blockIdx.x);
+    backward_columns<T, OP, NT, LC, FC>(j, blockIdx.x);
   } else {
     float none[CH][8];
-    backward_rows<T, RES, G, CH, F, false, true, false>(j, (int64_t)(blockIdx.x - j.col_blocks) * RPB + group_of_thread<G>(),
+    backward_rows<T, OP, G, CH, F, false, true, false>(j, (int64_t)(blockIdx.x - j.col_blocks) * RPB + group_of_thread<G>(),
                                            (int64_t)(j.grid - j.col_blocks) * RPB, none, none);
   }
 }
@@ -950,15 +744,19 @@ BackwardPlan backward_plan(int64_t rows, int cols, Elt e, bool weights) {
   return p;
 }
 
-template <typename T, bool RES, int G, int CH>
+template <typename T, Op OP, int G, int CH>
 hipError_t backward_with(const NormJob& j, const BackwardPlan& p, hipStream_t st) {
   constexpr int nt = backward_threads(G);
   constexpr Form other = G == 1 ? kSmall : kRagged;
   const int lanes = G > 64 ? p.threads : G;
   const bool exact = j.cols == 8 * CH * lanes;
   if (!chunks_fit((j.cols + 7) / 8, lanes, CH)) return hipErrorInvalidConfiguration;
-  BackwardArgs<RES> a;
-  if constexpr (RES) {
+  BackwardArgs<OP> a;
+  if constexpr (OP == kRms) {
+    a.add = j.ds.p != nullptr;
+    a.ds = j.ds.p ? j.ds : j.v;
+  }
+  if constexpr (OP == kJoin) {
     // an absent operand becomes one that changes nothing, at the price of a load
     // that is not used or of a second store to the same place: ds is read from v
     // and not added, dr goes where dx is written after it, dx where dr is, undropped
@@ -987,12 +785,12 @@ hipError_t backward_with(const NormJob& j, const BackwardPlan& p, hipStream_t st
       const int threads = p.threads * p.groups;
       if constexpr (can_store_early<T>(G * CH)) {
         if (stores_early<T>(j.rows, j.cols, kEarlyBackward)) {
-          return enqueue(exact ? k_norm_backward<T, RES, G, CH, nt, kExact, true>
-                               : k_norm_backward<T, RES, G, CH, nt, other, true>, p.parts, threads, 0, st, a);
+          return enqueue(exact ? k_norm_backward<T, OP, G, CH, nt, kExact, true>
+                               : k_norm_backward<T, OP, G, CH, nt, other, true>, p.parts, threads, 0, st, a);
         }
       }
-      return enqueue(exact ? k_norm_backward<T, RES, G, CH, nt, kExact, false>
-                           : k_norm_backward<T, RES, G, CH, nt, other, false>, p.parts, threads, 0, st, a);
+      return enqueue(exact ? k_norm_backward<T, OP, G, CH, nt, kExact, false>
+                           : k_norm_backward<T, OP, G, CH, nt, other, false>, p.parts, threads, 0, st, a);
     }
   }
   if constexpr (G == 256 || (G == 1024 && CH == 1)) {   // many rows only
@@ -1002,8 +800,8 @@ hipError_t backward_with(const NormJob& j, const BackwardPlan& p, hipStream_t st
       a.col_blocks = col_blocks;
       a.grid = col_blocks + row_blocks;
       if (a.grid == 0) return hipSuccess;
-      return enqueue(exact ? k_norm_backward_split<T, RES, G, CH, nt, kExact>
-                           : k_norm_backward_split<T, RES, G, CH, nt, other>, a.grid, nt, 0, st, a);
+      return enqueue(exact ? k_norm_backward_split<T, OP, G, CH, nt, kExact>
+                           : k_norm_backward_split<T, OP, G, CH, nt, other>, a.grid, nt, 0, st, a);
     };
     const int row_blocks = j.dr.p || j.dx.p ? p.row_blocks : 0;
     auto over = [&](const Mat& m) { return m.p && (m.p == j.dy.p || m.p == j.v.p); };
@@ -1015,22 +813,30 @@ hipError_t backward_with(const NormJob& j, const BackwardPlan& p, hipStream_t st
   }
 }
 
-template <typename T, bool RES>
+template <typename T, Op OP>
 hipError_t backward(const NormJob& j, const BackwardPlan& p, hipStream_t st) {
   switch (p.lanes) {
-    case 1: return backward_with<T, RES, 1, 1>(j, p, st);
-    case 2: return backward_with<T, RES, 2, 1>(j, p, st);
-    case 4: return backward_with<T, RES, 4, 1>(j, p, st);
-    case 8: return backward_with<T, RES, 8, 1>(j, p, st);
-    case 16: return backward_with<T, RES, 16, 1>(j, p, st);
-    case 32: return backward_with<T, RES, 32, 1>(j, p, st);
-    case 64: return p.chunks == 1 ? backward_with<T, RES, 64, 1>(j, p, st) : backward_with<T, RES, 64, 2>(j, p, st);
-    case 256: return backward_with<T, RES, 256, sizeof(T) == 2 ? 2 : 1>(j, p, st);
-    case 512: return p.chunks == 1 ? backward_with<T, RES, 512, 1>(j, p, st) : backward_with<T, RES, 512, 2>(j, p, st);
+    case 1: return backward_with<T, OP, 1, 1>(j, p, st);
+    case 2: return backward_with<T, OP, 2, 1>(j, p, st);
+    case 4: return backward_with<T, OP, 4, 1>(j, p, st);
+    case 8: return backward_with<T, OP, 8, 1>(j, p, st);
+    case 16: return backward_with<T, OP, 16, 1>(j, p, st);
+    case 32: return backward_with<T, OP, 32, 1>(j, p, st);
+    case 64: return p.chunks == 1 ? backward_with<T, OP, 64, 1>(j, p, st) : backward_with<T, OP, 64, 2>(j, p, st);
+    case 256: return backward_with<T, OP, 256, sizeof(T) == 2 ? 2 : 1>(j, p, st);
+    case 512: return p.chunks == 1 ? backward_with<T, OP, 512, 1>(j, p, st) : backward_with<T, OP, 512, 2>(j, p, st);
     default:
-      if (p.chunks == 1) return backward_with<T, RES, 1024, 1>(j, p, st);
-      return p.chunks == 2 ? backward_with<T, RES, 1024, 2>(j, p, st) : backward_with<T, RES, 1024, 4>(j, p, st);
+      if (p.chunks == 1) return backward_with<T, OP, 1024, 1>(j, p, st);
+      return p.chunks == 2 ? backward_with<T, OP, 1024, 2>(j, p, st) : backward_with<T, OP, 1024, 4>(j, p, st);
   }
+}
+
+// the first `cols` of a partial pair's 2 x j.cols columns
+hipError_t reduce(const NormJob& j, int parts, int cols, hipStream_t st) {
+  const ReduceArgs a{j.part, j.dgamma, j.dbeta, j.cols, parts};
+  // 64 columns a workgroup once they fill the CUs, else 16
+  if (cols > 256 * 16) return enqueue(k_norm_reduce<64>, (cols + 63) / 64, kReduceThreads, 0, st, a);
+  return enqueue(k_norm_reduce<16>, (cols + 15) / 16, kReduceThreads, 0, st, a);
 }
 
 template <typename T, bool RES>
@@ -1082,13 +888,15 @@ hipError_t launch_norm_backward(Elt e, const NormJob& j, hipStream_t st) {
   const bool weights = j.dgamma || j.dbeta, residual = j.ds.p || j.dx.p;
   const BackwardPlan p = backward_plan(j.rows, j.cols, e, weights);
   hipError_t err;
-  if (e == BF16) err = residual ? backward<uint16_t, true>(j, p, st) : backward<uint16_t, false>(j, p, st);
-  else err = residual ? backward<float, true>(j, p, st) : backward<float, false>(j, p, st);
-  if (err != hipSuccess || p.parts <= 1) return err;
-  const ReduceArgs a{j.part, j.dgamma, j.dbeta, j.cols, p.parts};
-  // 64 columns a workgroup once they fill the CUs, else 16
-  if (2 * j.cols > 256 * 16) return enqueue(k_norm_reduce<64>, (2 * j.cols + 63) / 64, kReduceThreads, 0, st, a);
-  return enqueue(k_norm_reduce<16>, (2 * j.cols + 15) / 16, kReduceThreads, 0, st, a);
+  if (e == BF16) err = residual ? backward<uint16_t, kJoin>(j, p, st) : backward<uint16_t, kNorm>(j, p, st);
+  else err = residual ? backward<float, kJoin>(j, p, st) : backward<float, kNorm>(j, p, st);
+  return err != hipSuccess || p.parts <= 1 ? err : reduce(j, p.parts, 2 * j.cols, st);
+}
+
+hipError_t launch_rms_backward(Elt e, const NormJob& j, hipStream_t st) {
+  const BackwardPlan p = backward_plan(j.rows, j.cols, e, j.dgamma != nullptr);
+  const hipError_t err = e == BF16 ? backward<uint16_t, kRms>(j, p, st) : backward<float, kRms>(j, p, st);
+  return err != hipSuccess || p.parts <= 1 ? err : reduce(j, p.parts, j.cols, st);
 }
 
 }  // namespace vfl

@@ -43,6 +43,8 @@ int norm_parts(int64_t rows, int cols);
 hipError_t launch_dropout(Elt e, const DropJob& j, hipStream_t st);
 hipError_t launch_norm_forward(Elt e, const NormJob& j, hipStream_t st);
 hipError_t launch_norm_backward(Elt e, const NormJob& j, hipStream_t st);
+// the root-mean-square norm's: of v, dy, ds, stats (k of each row) into dr and dgamma
+hipError_t launch_rms_backward(Elt e, const NormJob& j, hipStream_t st);
 // text that vfl_last_error(NULL) returns on the calling thread
 void set_call_error(const char* why) noexcept;
 

@@ -23,6 +23,10 @@ VFL_MAX_LAYERS = 16
 VFL_GRAPH_CYCLES = 4
 VFL_STATIC_WORKSPACE_BYTES = 64 << 20
 VFL_NORM_MAX_COLS = 32768
+VFL_Q8_BLOCK = 128
+VFL_MATMUL8_MAX_DEPTH = 8388608
+VFL_LOSS_MAX_ROWS = VFL_LOSS_MAX_CLASSES = 2097152
+VFL_LOSS_MAX_DIM = 32768
 VFL_TIMED_EVERY = 4       # vfl_run times the launches of every 4th tick of a captured cycle
 STATUS_NAMES = {0: "VFL_OK", 1: "VFL_E_INVALID", 2: "VFL_E_NOMEM", 3: "VFL_E_HIP",
                 4: "VFL_E_NOT_READY", 5: "VFL_E_STALE", 6: "VFL_E_STATE"}
@@ -34,7 +38,9 @@ EXPORTS = ("vfl_workspace_size", "vfl_create", "vfl_create_static", "vfl_set_par
            "vfl_state_size", "vfl_get_state", "vfl_set_state", "vfl_discard", "vfl_plan", "vfl_fit_delay",
            "vfl_sync_interval", "vfl_replica_average", "vfl_dropout", "vfl_norm_workspace_size",
            "vfl_layernorm_forward", "vfl_layernorm_backward", "vfl_residual_forward",
-           "vfl_residual_backward",
+           "vfl_residual_backward", "vfl_rmsnorm_forward", "vfl_rmsnorm_backward", "vfl_quantize",
+           "vfl_matmul8_workspace_size", "vfl_matmul8", "vfl_softmax_loss_workspace_size",
+           "vfl_softmax_loss_forward", "vfl_softmax_loss_backward",
            "vfl_last_error", "vfl_destroy")
 KERNEL_CLASSES = ("fwd", "active", "bwd", "dw", "reduce", "cast", "emb_sgd", "gemm", "dwt", "avg")
 
@@ -109,6 +115,37 @@ class vfl_residual_args(C.Structure):
                 ("workspace_bytes", C.c_size_t)]
 
 
+class vfl_q8(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("ld", C.c_int64), ("scale", C.c_void_p), ("scale_ld", C.c_int64)]
+
+
+class vfl_rmsnorm_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("cols", C.c_int32), ("rows", C.c_int64), ("eps", C.c_float),
+                ("gamma", C.c_void_p), ("x", vfl_matrix), ("r", vfl_matrix), ("s", vfl_matrix),
+                ("y", vfl_matrix), ("dy", vfl_matrix), ("ds", vfl_matrix), ("dx", vfl_matrix), ("q", vfl_q8),
+                ("stats", C.c_void_p), ("dgamma", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t)]
+
+
+class vfl_quantize_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("cols", C.c_int32), ("rows", C.c_int64), ("x", vfl_matrix),
+                ("q", vfl_q8), ("qt", vfl_q8)]
+
+
+class vfl_matmul8_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("relu", C.c_int32), ("m", C.c_int64), ("n", C.c_int64), ("k", C.c_int64),
+                ("a", vfl_q8), ("b", vfl_q8), ("bias", C.c_void_p), ("c", vfl_matrix),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class vfl_softmax_loss_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("dim", C.c_int32), ("rows", C.c_int64), ("classes", C.c_int64),
+                ("x", vfl_matrix), ("w", vfl_matrix), ("bias", C.c_void_p), ("labels", C.c_void_p),
+                ("loss", C.c_void_p), ("lse", C.c_void_p), ("dloss", C.c_void_p), ("scale", C.c_float),
+                ("dx", vfl_matrix), ("dw", vfl_matrix), ("dbias", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t)]
+
+
 class VflError(RuntimeError):
     def __init__(self, status: int, where: str, text: str = ""):
         self.status = status
@@ -160,6 +197,14 @@ def _load():
         "vfl_layernorm_backward": [C.POINTER(vfl_layernorm_args), P],
         "vfl_residual_forward": [C.POINTER(vfl_residual_args), P],
         "vfl_residual_backward": [C.POINTER(vfl_residual_args), P],
+        "vfl_rmsnorm_forward": [C.POINTER(vfl_rmsnorm_args), P],
+        "vfl_rmsnorm_backward": [C.POINTER(vfl_rmsnorm_args), P],
+        "vfl_quantize": [C.POINTER(vfl_quantize_args), P],
+        "vfl_matmul8_workspace_size": [C.c_int64, C.c_int64, C.c_int64, C.POINTER(C.c_size_t)],
+        "vfl_matmul8": [C.POINTER(vfl_matmul8_args), P],
+        "vfl_softmax_loss_workspace_size": [C.c_int, C.c_int64, C.c_int32, C.c_int64, C.POINTER(C.c_size_t)],
+        "vfl_softmax_loss_forward": [C.POINTER(vfl_softmax_loss_args), P],
+        "vfl_softmax_loss_backward": [C.POINTER(vfl_softmax_loss_args), P],
     }
     for name, args in sig.items():
         f = getattr(lib, name)
@@ -318,6 +363,42 @@ def vfl_residual_forward(a: vfl_residual_args, stream: int = 0):
 
 def vfl_residual_backward(a: vfl_residual_args, stream: int = 0):
     _chk(_lib.vfl_residual_backward(a, stream), "vfl_residual_backward")
+
+
+def vfl_rmsnorm_forward(a: vfl_rmsnorm_args, stream: int = 0):
+    _chk(_lib.vfl_rmsnorm_forward(a, stream), "vfl_rmsnorm_forward")
+
+
+def vfl_rmsnorm_backward(a: vfl_rmsnorm_args, stream: int = 0):
+    _chk(_lib.vfl_rmsnorm_backward(a, stream), "vfl_rmsnorm_backward")
+
+
+def vfl_quantize(a: vfl_quantize_args, stream: int = 0):
+    _chk(_lib.vfl_quantize(a, stream), "vfl_quantize")
+
+
+def vfl_matmul8_workspace_size(m: int, n: int, k: int) -> int:
+    size = C.c_size_t(0)
+    _chk(_lib.vfl_matmul8_workspace_size(m, n, k, C.byref(size)), "vfl_matmul8_workspace_size")
+    return size.value
+
+
+def vfl_matmul8(a: vfl_matmul8_args, stream: int = 0):
+    _chk(_lib.vfl_matmul8(a, stream), "vfl_matmul8")
+
+
+def vfl_softmax_loss_workspace_size(dtype: int, rows: int, dim: int, classes: int) -> int:
+    n = C.c_size_t(0)
+    _chk(_lib.vfl_softmax_loss_workspace_size(dtype, rows, dim, classes, C.byref(n)), "vfl_softmax_loss_workspace_size")
+    return n.value
+
+
+def vfl_softmax_loss_forward(a: vfl_softmax_loss_args, stream: int = 0):
+    _chk(_lib.vfl_softmax_loss_forward(a, stream), "vfl_softmax_loss_forward")
+
+
+def vfl_softmax_loss_backward(a: vfl_softmax_loss_args, stream: int = 0):
+    _chk(_lib.vfl_softmax_loss_backward(a, stream), "vfl_softmax_loss_backward")
 
 
 def vfl_timing_enable(ctx, mask: int):

@@ -1,0 +1,678 @@
+"""GPU tests of the root-mean-square norm, matrices in 8 bits, their product and
+the softmax loss against their float64 definitions in oracle/eight.py.
+
+Matrices in 8 bits are compared for equality: their definition has one rounding
+of float32 values.  The other tolerances are bounds of float32 arithmetic (u =
+2^-24), computed element by element from float64 values and fixed before the
+first run:
+* a sum over a row passes at most SUM = 96 roundings per term, a sum over rows at
+  most min(rows, 512) + 32, and a sum of k products in the matrix cores k / 4 + 16
+  (the instructions add 4 to 32 products to an accumulator; the parts of a split
+  sum add fewer than 16);
+* every other operation adds its own rounding;
+* a product of matrices in 8 bits with a bf16 result adds 128 products at once
+  with 15 bits below the largest magnitude among them: 2^-14 of the magnitudes'
+  sum bounds what is lost;
+* G is rounded to the operands' type, half a step: 2^-8 relative for bf16;
+* a stored value must be the rounding of a value within the bound;
+* first-order bounds are multiplied by 1.1 for the terms of second order.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import eight as E
+
+pytestmark = pytest.mark.gpu
+
+U, SUM, SLACK = 2.0 ** -24, 96, 1.1
+EPS = 2.0 ** -17
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+GUARD = 77.0
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("needs an MI355X")
+
+
+@pytest.fixture(scope="module")
+def V():
+    from paper_2510_12494_amd import vfl
+    return vfl
+
+
+def rounded(a, dt):
+    if dt == "f32":
+        return a
+    m, e = np.frexp(a)
+    return np.ldexp(np.rint(m * 256.0), e - 8)
+
+
+class Mat:
+    """A [rows x cols] device matrix inside a guarded buffer."""
+
+    def __init__(self, dt, rows, cols, ld=0, lead=0, values=None):
+        self.rows, self.cols, self.ld, self.lead = rows, cols, ld or cols, lead
+        self.buf = torch.full((lead + rows * self.ld + 64,), GUARD, dtype=DT[dt], device="cuda")
+        self.t = self.buf[lead:lead + rows * self.ld].view(rows, self.ld)[:, :cols]
+        if values is not None:
+            self.t.copy_(torch.from_numpy(np.asarray(values, np.float64)))
+
+    def np(self):
+        return self.t.double().cpu().numpy()
+
+    def put(self, m):
+        m.data, m.ld = self.t.data_ptr(), self.ld
+        return self
+
+    def assert_guard(self):
+        b = self.buf.clone()
+        if self.rows:
+            b[self.lead:self.lead + self.rows * self.ld].view(self.rows, self.ld)[:, :self.cols] = GUARD
+        assert bool((b == GUARD).all())
+
+
+class Eight:
+    """A matrix in 8 bits inside guarded buffers, ld and scale_ld above the least."""
+
+    def __init__(self, rows, cols, more=0, values=None):
+        self.rows, self.cols = rows, cols
+        self.wide, self.tall = -(-cols // 128) * 128, -(-rows // 16) * 16
+        self.ld, self.sld, self.nb = self.wide + 128 * more, self.tall + 16 * more, self.wide // 128
+        self.data = torch.full((rows * self.ld + 256,), 0x55, dtype=torch.uint8, device="cuda")
+        self.scale = torch.full((self.nb * self.sld + 256,), 0x55, dtype=torch.uint8, device="cuda")
+        if values is not None:
+            q, p = E.quantize(values)
+            self._bytes().copy_(torch.from_numpy(q).float().cuda().to(torch.float8_e4m3fn).view(torch.uint8))
+            self._powers().copy_(torch.from_numpy((p + 127).astype(np.uint8)))
+
+    def _bytes(self):
+        return self.data[:self.rows * self.ld].view(self.rows, self.ld)[:, :self.wide]
+
+    def _powers(self):
+        return self.scale[:self.nb * self.sld].view(self.nb, self.sld)[:, :self.rows]
+
+    def put(self, m):
+        m.data, m.ld, m.scale, m.scale_ld = self.data.data_ptr(), self.ld, self.scale.data_ptr(), self.sld
+        return self
+
+    def np(self):
+        """(values, power)"""
+        v = self._bytes().contiguous().view(torch.float8_e4m3fn).double().cpu().numpy()
+        return v, self._powers().cpu().numpy().astype(int) - 127
+
+    def values(self):
+        return E.dequantize(*self.np())[:, :self.cols]
+
+    def assert_guard(self):
+        d, s = self.data.clone(), self.scale.clone()
+        d[:self.rows * self.ld].view(self.rows, self.ld)[:, :self.wide] = 0x55
+        s[:self.nb * self.sld].view(self.nb, self.sld)[:, :self.tall] = 0x55
+        assert bool((d == 0x55).all()) and bool((s == 0x55).all())
+
+    def assert_equal(self, values):
+        q, p = E.quantize(values)
+        gq, gp = self.np()
+        assert np.array_equal(gp, p), f"powers differ at {np.argwhere(gp != p)[:3]}"
+        assert np.array_equal(gq, q, equal_nan=True), f"values differ at {np.argwhere(~((gq == q) | np.isnan(q)))[:3]}"
+
+
+def vec(n, values=None, dtype=torch.float32):
+    t = torch.full((n + 8,), GUARD, dtype=dtype, device="cuda")
+    if values is not None:
+        t[:n] = torch.from_numpy(np.asarray(values)).to(dtype)
+    return t
+
+
+def stored(t, n):
+    assert bool((t[n:] == GUARD).all())
+    return t[:n].double().cpu().numpy()
+
+
+def close(got, want, bound, what, dt="f32"):
+    bad = ~((got >= rounded(want - bound, dt)) & (got <= rounded(want + bound, dt)))
+    assert not bad.any(), (f"{what}: {int(bad.sum())} of {bad.size} elements past their bound, worst "
+                           f"{np.nanmax(np.where(bad, np.abs(got - want) / np.maximum(bound, 1e-300), 0)):.3g} times it, "
+                           f"first at {np.argwhere(bad)[0]}")
+
+
+def activations(rng, rows, cols):
+    a = rng.normal(size=(rows, cols)) * np.exp(0.5 * rng.normal(size=cols))
+    if rows > 2:
+        a[rows // 2] = 0.0
+    return a
+
+
+def gradients(rng, rows, cols):
+    return rng.normal(size=(rows, cols)) * np.exp(2 * rng.normal(size=(rows, 1))) * 1e-3
+
+
+def ptr(t):
+    return 0 if t is None else t.data_ptr()
+
+
+# ----------------------------------------------------------------- rms norm
+def rms(V, dt, rows, cols, x=None, r=None, gamma=None, s=None, y=None, q=None, stats=None, call=True):
+    a = V.vfl_rmsnorm_args()
+    a.dtype, a.rows, a.cols, a.eps, a.gamma, a.stats = (V.VFL_BF16 if dt == "bf16" else V.VFL_F32, rows, cols, EPS,
+                                                        ptr(gamma), ptr(stats))
+    for k, m in (("x", x), ("r", r), ("s", s), ("y", y), ("q", q)):
+        if m is not None:
+            m.put(getattr(a, k))
+    if call:
+        V.vfl_rmsnorm_forward(a)
+        torch.cuda.synchronize()
+    return a
+
+
+def expected_y(v, k, gamma):
+    """The two float32 products of the definition, from the kernel's own k."""
+    return (v.astype(np.float32) * k.astype(np.float32)[:, None] * gamma.astype(np.float32)).astype(np.float64)
+
+
+WIDTHS = [1, 5, 8, 64, 127, 128, 129, 256, 500, 512, 1000, 1024, 1030, 2048, 3500, 4104, 8192, 8200, 16384, 20001, 32768]
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", WIDTHS)
+def test_rms_forward(V, dt, cols):
+    rng = np.random.default_rng(cols)
+    rows = 37 if cols <= 2048 else 5
+    x = Mat(dt, rows, cols, cols + 3, 1, activations(rng, rows, cols))
+    r = Mat(dt, rows, cols, cols, 0, activations(rng, rows, cols))
+    gamma = vec(cols, 1 + 0.1 * rng.normal(size=cols))
+    s, y, q, stats = Mat(dt, rows, cols, cols + 1, 3), Mat(dt, rows, cols, cols + 9), Eight(rows, cols, 1), vec(rows)
+    rms(V, dt, rows, cols, x, r, gamma, s, y, q, stats)
+    g = stored(gamma, cols)
+    v = (x.np().astype(np.float32) + r.np().astype(np.float32)).astype(np.float64)
+    k = stored(stats, rows)
+    want = E.rms_stats(v, EPS)
+    assert (np.abs(k - want) <= want * U * (1 + 2.0 ** -20)).all()
+    yv = expected_y(v, k, g)
+    assert np.array_equal(s.np(), rounded(v, dt)) and np.array_equal(y.np(), rounded(yv, dt))
+    q.assert_equal(yv)
+    for m in (x, r, s, y, q):
+        m.assert_guard()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(1, 1024), (1, 130), (5000, 64), (3001, 200), (20000, 9), (300, 1024), (400, 9000)])
+def test_rms_forward_without_what_may_be_absent(V, dt, rows, cols):
+    rng = np.random.default_rng(rows + cols)
+    x = Mat(dt, rows, cols, 0, 0, activations(rng, rows, cols))
+    q, q2, y, stats = Eight(rows, cols), Eight(rows, cols), Mat(dt, rows, cols), vec(rows)
+    rms(V, dt, rows, cols, x, q=q)
+    rms(V, dt, rows, cols, x, y=y)
+    rms(V, dt, rows, cols, x, stats=stats)
+    v, k = x.np(), stored(stats, rows)
+    yv = expected_y(v, k, np.ones(cols))
+    q.assert_equal(yv)
+    assert np.array_equal(y.np(), rounded(yv, dt))
+    # a row's results do not depend on the batch that it is in
+    half = rows // 2
+    if half:
+        part = Mat(dt, rows - half, cols, 0, 0, v[half:])
+        q3 = Eight(rows - half, cols)
+        rms(V, dt, rows - half, cols, part, q=q3)
+        assert np.array_equal(q3.np()[0], q.np()[0][half:], equal_nan=True)
+    # the join in place of its inputs
+    r = Mat(dt, rows, cols, 0, 0, v)
+    rms(V, dt, rows, cols, x, r, s=r, y=x, q=q2, stats=stats)
+    assert np.array_equal(r.np(), rounded(2 * v, dt))
+    q2.assert_equal(expected_y(2 * v, stored(stats, rows), np.ones(cols)))
+
+
+def test_rms_rows_of_no_numbers_and_extreme_ones(V):
+    rows, cols = 8, 300
+    rng = np.random.default_rng(5)
+    a = rng.normal(size=(rows, cols))
+    a[1, 7], a[2, 200], a[4], a[5], a[6] = np.nan, np.inf, 0.0, a[5] * 1e-30, a[6] * 1e30
+    x = Mat("f32", rows, cols, 0, 0, a)
+    q, y, stats = Eight(rows, cols), Mat("f32", rows, cols), vec(rows)
+    rms(V, "f32", rows, cols, x, y=y, q=q, stats=stats)
+    k = stats[:rows].double().cpu().numpy()
+    assert np.isnan(k[1]) and k[2] == 0.0 and np.isclose(k[4], EPS ** -0.5)
+    ok = [0, 3, 4, 5, 6, 7]
+    with np.errstate(invalid="ignore"):
+        yv = expected_y(x.np(), k, np.ones(cols))
+    assert np.array_equal(y.np(), yv, equal_nan=True)
+    q.assert_equal(yv)
+    assert np.isfinite(y.np()[ok]).all() and np.isfinite(q.values()[ok]).all()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 1024), (3, 7), (40, 500), (700, 64), (3000, 24), (5000, 130), (2100, 1024),
+                                       (1200, 2000), (900, 5001), (300, 9000), (40, 20000)])
+def test_rms_backward(V, dt, rows, cols):
+    rng = np.random.default_rng(rows * 7 + cols)
+    s = Mat(dt, rows, cols, cols + 2, 0, activations(rng, rows, cols))
+    dy, ds = (Mat(dt, rows, cols, cols + i, i, gradients(rng, rows, cols)) for i in (1, 5))
+    gamma = vec(cols, 1 + 0.1 * rng.normal(size=cols))
+    sv, dyv, dsv, g = s.np(), dy.np(), ds.np(), stored(gamma, cols)
+    stats = vec(rows, E.rms_stats(sv, EPS))
+    k = stored(stats, rows)
+    size = V.vfl_norm_workspace_size(rows, cols)
+    ws = torch.empty(size + 16, dtype=torch.uint8, device="cuda")
+    for with_ds, with_gamma, outs in ((True, True, "both"), (False, False, "both"), (True, True, "dx"), (True, True, "dgamma")):
+        dx, dgamma = Mat(dt, rows, cols, cols + 4), vec(cols)
+        a = V.vfl_rmsnorm_args()
+        a.dtype, a.rows, a.cols, a.stats = V.VFL_BF16 if dt == "bf16" else V.VFL_F32, rows, cols, ptr(stats)
+        s.put(a.s)
+        dy.put(a.dy)
+        if with_ds:
+            ds.put(a.ds)
+        if with_gamma:
+            a.gamma = ptr(gamma)
+        if outs != "dgamma":
+            dx.put(a.dx)
+        if outs != "dx":
+            a.dgamma = ptr(dgamma)
+        a.workspace, a.workspace_bytes = ptr(ws), size
+        V.vfl_rmsnorm_backward(a)
+        torch.cuda.synchronize()
+        gv, dv = g if with_gamma else np.ones(cols), dsv if with_ds else np.zeros_like(dsv)
+        want, wgamma = E.rms_backward(sv, k, dyv, dv, gv)
+        h, gg = sv * k[:, None], dyv * gv
+        A = np.abs(gg * h).mean(1, keepdims=True)
+        c = np.abs((gg * h).mean(1, keepdims=True))
+        bound = SLACK * U * (np.abs(k)[:, None] * ((SUM + 6) * np.abs(h) * A + 6 * (np.abs(gg) + np.abs(h) * c))
+                             + 2 * np.abs(want) + np.abs(dv)) + 1e-40
+        if outs != "dgamma":
+            close(dx.np(), want, bound, "dx", dt)
+            dx.assert_guard()
+        if outs != "dx":
+            close(stored(dgamma, cols), wgamma, SLACK * U * (min(rows, 512) + 34) * np.abs(dyv * h).sum(0) + 1e-40, "dgamma")
+
+
+def test_rms_backward_of_no_rows(V):
+    a = V.vfl_rmsnorm_args()
+    dgamma = vec(40)
+    a.cols, a.dgamma = 40, ptr(dgamma)
+    V.vfl_rmsnorm_backward(a)
+    torch.cuda.synchronize()
+    assert not stored(dgamma, 40).any()
+
+
+# ----------------------------------------------------------------- quantize
+def quantize(V, dt, x, q=None, qt=None, stream=0):
+    a = V.vfl_quantize_args()
+    a.dtype, a.rows, a.cols = V.VFL_BF16 if dt == "bf16" else V.VFL_F32, x.rows, x.cols
+    x.put(a.x)
+    if q is not None:
+        q.put(a.q)
+    if qt is not None:
+        qt.put(a.qt)
+    V.vfl_quantize(a, stream)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 1024), (3, 5), (7, 8), (127, 129), (128, 128), (129, 127), (200, 1030),
+                                       (1030, 40), (2000, 3), (300, 4096)])
+def test_quantize(V, dt, rows, cols):
+    rng = np.random.default_rng(rows + 3 * cols)
+    x = Mat(dt, rows, cols, cols + 5, 3, gradients(rng, rows, cols))
+    q, qt, q1, t1 = Eight(rows, cols, 1), Eight(cols, rows, 2), Eight(rows, cols), Eight(cols, rows)
+    quantize(V, dt, x, q, qt)
+    quantize(V, dt, x, q1)
+    quantize(V, dt, x, None, t1)
+    v = x.np()
+    for m in (q, q1):
+        m.assert_equal(v)
+    for m in (qt, t1):
+        m.assert_equal(v.T)
+    for m in (x, q, qt, q1, t1):
+        m.assert_guard()
+
+
+def test_quantize_values_at_every_border(V):
+    table = np.sort(E.e4m3_table()[:127])
+    mid = (table[1:] + table[:-1]) / 2
+    vals = np.concatenate([table, mid, mid * (1 + 2.0 ** -20), mid * (1 - 2.0 ** -20)])
+    vals = np.concatenate([vals, -vals])
+    rows, cols = -(-vals.size // 127), 128
+    a = np.zeros((rows, cols))
+    a[:, 0] = 448.0
+    a[:, 1:].flat[:vals.size] = vals
+    a = np.concatenate([a, a * 2.0 ** -30, a * 2.0 ** 60, a * 2.0 ** -140, a * 2.0 ** -120])
+    edge = np.zeros((9, cols))
+    edge[0, 3], edge[1, 3], edge[2, 3], edge[3, 3] = 3.4e38, 1e-45, np.nextafter(np.float32(448), np.float32(449)), -448.0
+    edge[4, :4] = np.nan, 1.0, np.inf, -np.inf
+    edge[5] = np.nan
+    edge[6] = np.inf
+    edge[7, ::2] = -0.0
+    edge[8, :2] = 448.0, 448.0 * 2.0 ** -18
+    a = np.concatenate([a, edge])
+    x = Mat("f32", a.shape[0], cols, 0, 0, a)
+    q, qt = Eight(a.shape[0], cols), Eight(cols, a.shape[0])
+    quantize(V, "f32", x, q, qt)
+    q.assert_equal(x.np())
+    qt.assert_equal(x.np().T)
+
+
+# ------------------------------------------------------------------- matmul
+def matmul8(V, dt, a, b, c, k, bias=None, relu=0, stream=0, ws=None):
+    d = V.vfl_matmul8_args()
+    d.dtype, d.relu, d.m, d.n, d.k = V.VFL_BF16 if dt == "bf16" else V.VFL_F32, relu, a.rows, b.rows, k
+    a.put(d.a)
+    b.put(d.b)
+    c.put(d.c)
+    d.bias = ptr(bias)
+    size = V.vfl_matmul8_workspace_size(a.rows, b.rows, k)
+    ws = torch.empty(size + 16, dtype=torch.uint8, device="cuda") if ws is None else ws
+    d.workspace, d.workspace_bytes = ptr(ws), size
+    V.vfl_matmul8(d, stream)
+    return d, ws
+
+
+def product_bound(av, bv, dt):
+    k = av.shape[1]
+    mags = np.abs(av) @ np.abs(bv).T
+    return SLACK * (k / 4 + 16) * U * mags + (2.0 ** -14 * mags if dt == "bf16" else 0)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n,k", [(1, 1, 1), (1, 1024, 1024), (1, 37, 130), (3, 8, 128), (16, 100, 300), (17, 513, 1024),
+                                   (48, 250, 512), (64, 64, 4096), (65, 129, 129), (130, 70, 1000), (300, 300, 96),
+                                   (257, 1025, 640), (520, 129, 5000), (4099, 264, 264), (2048, 2048, 128), (1, 4000, 9000)])
+def test_matmul8(V, dt, m, n, k):
+    rng = np.random.default_rng(m + n + k)
+    a, b = Eight(m, k, 1, activations(rng, m, k)), Eight(n, k, 0, gradients(rng, n, k))
+    bias = vec(n, 1e-3 * rng.normal(size=n))
+    av, bv, biasv = a.values(), b.values(), stored(bias, n)
+    want, bound = av @ bv.T, product_bound(av, bv, dt)
+    c = Mat(dt, m, n, n + 3, 1)
+    matmul8(V, dt, a, b, c, k)
+    torch.cuda.synchronize()
+    close(c.np(), want, bound + 1e-40, "c", dt)
+    c.assert_guard()
+    first = c.t.clone()
+    matmul8(V, dt, a, b, c, k, bias, 1)
+    torch.cuda.synchronize()
+    z = want + biasv
+    bound = bound + SLACK * U * (np.abs(z) + np.abs(biasv)) + 1e-40
+    close(c.np(), np.maximum(z, 0), bound, "relu(c + bias)", dt)
+    c.assert_guard()
+    matmul8(V, dt, a, b, c, k)
+    torch.cuda.synchronize()
+    assert torch.equal(c.t, first)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_matmul8_powers_and_numbers_that_are_none(V, dt):
+    # blocks of very different powers in one row, whose products meet again
+    m, n, k = 70, 90, 512
+    rng = np.random.default_rng(9)
+    av, bv = rng.normal(size=(m, k)), rng.normal(size=(n, k))
+    for i, e in enumerate((-60, 0, 40, 20)):
+        av[:, 128 * i:128 * i + 128] *= 2.0 ** e
+        bv[:, 128 * i:128 * i + 128] *= 2.0 ** -e
+    av[5, 300], bv[7, 9] = np.nan, np.inf
+    a, b = Eight(m, k, 0, av), Eight(n, k, 0, bv)
+    c = Mat(dt, m, n)
+    matmul8(V, dt, a, b, c, k)
+    torch.cuda.synchronize()
+    av, bv, got = a.values(), b.values(), c.np()
+    assert np.isnan(got[5]).all() and np.isnan(got[:, 7]).all()
+    av, bv, got = np.delete(av, 5, 0), np.delete(bv, 7, 0), np.delete(np.delete(got, 5, 0), 7, 1)
+    close(got, av @ bv.T, product_bound(av, bv, dt), "c", dt)
+
+
+# ------------------------------------------------------------- softmax loss
+class Loss:
+    """One call's data on the device and in float64."""
+
+    def __init__(self, V, dt, rows, dim, classes, seed=0, bias=True, dloss=True, ld=0, lead=0, x=None, w=None, labels=None):
+        rng = np.random.default_rng(seed + rows + dim + classes)
+        self.V, self.dt, self.rows, self.dim, self.classes = V, dt, rows, dim, classes
+        w = rng.normal(size=(classes, dim)) * 1.5 / np.sqrt(dim) if w is None else w
+        if labels is None:
+            labels = rng.integers(0, classes, rows)
+        self.labels = labels
+        x = rng.normal(size=(rows, dim)) + 2 * rng.uniform(size=(rows, 1)) * w[np.clip(labels, 0, classes - 1)] if x is None else x
+        self.x, self.w = Mat(dt, rows, dim, ld or dim, lead, x), Mat(dt, classes, dim, ld or dim, lead, w)
+        b = 0.5 * rng.normal(size=classes)
+        self.bias = vec(classes, b) if bias is True else None if bias is None else vec(classes, bias)
+        self.lab = vec(rows, labels, torch.int32)
+        self.dl = vec(rows, rng.uniform(0.5, 1.5, rows) / rows) if dloss else None
+        self.scale = 0.25
+        self.loss, self.lse = vec(rows), vec(rows)
+        self.dx, self.dw, self.db = Mat(dt, rows, dim, dim + 1), Mat(dt, classes, dim, dim + 3, 1), vec(classes)
+        code = V.VFL_BF16 if dt == "bf16" else V.VFL_F32
+        size = V.vfl_softmax_loss_workspace_size(code, rows, dim, classes)
+        self.ws = torch.full((size + 256,), 0xFF, dtype=torch.uint8, device="cuda")   # NaN in every type
+        a = self.a = V.vfl_softmax_loss_args()
+        a.dtype, a.dim, a.rows, a.classes, a.scale = code, dim, rows, classes, self.scale
+        for k in ("x", "w", "dx", "dw"):
+            getattr(self, k).put(getattr(a, k))
+        a.bias, a.labels, a.loss, a.lse, a.dloss, a.dbias = (ptr(t) for t in (self.bias, self.lab, self.loss, self.lse,
+                                                                             self.dl, self.db))
+        a.workspace, a.workspace_bytes = ptr(self.ws), size
+
+    def run(self, stream=0):
+        self.V.vfl_softmax_loss_forward(self.a, stream)
+        self.V.vfl_softmax_loss_backward(self.a, stream)
+
+    def results(self):
+        return [t.clone() for t in (self.loss, self.lse, self.dx.t, self.dw.t, self.db)]
+
+    def check(self):
+        torch.cuda.synchronize()
+        dt, x, w = self.dt, self.x.np(), self.w.np()
+        b = stored(self.bias, self.classes) if self.bias is not None else np.zeros(self.classes)
+        has = (self.labels >= 0) & (self.labels < self.classes)
+        xz = np.where(np.isfinite(x), x, 0.0)                  # rows of no numbers are compared apart
+        wz = np.where(np.isneginf(b)[:, None], 0.0, w)
+        fine = np.isfinite(x).all(1)
+        loss, lse = E.softmax_loss(xz, wz, b, self.labels)
+        bz = np.where(np.isneginf(b), 0.0, b)
+        ez = (self.dim / 4 + 16) * U * (np.abs(xz) @ np.abs(wz).T) + 3 * U * np.abs(bz)
+        z = np.abs(xz @ wz.T + bz)
+        ez += 4 * U * z                                        # to base 2 and back
+        top = ez.max(1) + (SUM + 64) * U + 6 * U * np.abs(np.where(np.isfinite(lse), lse, 0))
+        got_lse, got_loss = stored(self.lse, self.rows), stored(self.loss, self.rows)
+        on = fine & np.isfinite(lse)
+        close(got_lse[on], lse[on], SLACK * top[on], "lse")
+        assert np.isneginf(got_lse[fine & np.isneginf(lse)]).all()
+        on = fine & np.isfinite(loss)
+        zl = z[np.arange(self.rows), np.where(has, self.labels, 0)]
+        close(got_loss[on], loss[on], SLACK * (2 * top + 4 * U * zl)[on] * has[on], "loss")
+        assert np.isposinf(got_loss[fine & np.isposinf(loss)]).all() and not got_loss[~has].any()
+        # G from the lse that the forward left, as the backward's definition has it
+        d = stored(self.dl, self.rows) if self.dl is not None else np.full(self.rows, self.scale)
+        has = has & fine
+        used = np.where(has, self.labels, -1)
+        G = E.softmax_grad(xz, wz, b, used, np.where(has, got_lse, 0.0), d)
+        p = np.abs(G)
+        p[np.nonzero(has)[0], self.labels[has]] += np.where(np.isneginf(b[self.labels[has]]), 0, np.abs(d[has]))
+        lz = np.where(np.isfinite(got_lse), np.abs(got_lse), 0)[:, None]
+        # below float32's smallest normal number an exponential, and G, may be taken as 0
+        eg = p * (ez + 4 * U * lz + 10 * U) + 2.0 ** -126 * (np.abs(d[:, None]) + 1) * has[:, None]
+        half = 2.0 ** -8 if dt == "bf16" else 0.0
+        e = eg + half * np.abs(G)
+        sums = lambda n: (n / 4 + 32) * U  # noqa: E731
+        close(self.dx.np(), G @ wz, SLACK * (e @ np.abs(wz) + sums(self.classes) * (np.abs(G) @ np.abs(wz))) + 1e-40, "dx", dt)
+        close(self.dw.np(), G.T @ xz, SLACK * (e.T @ np.abs(xz) + sums(self.rows) * (np.abs(G).T @ np.abs(xz))) + 1e-40, "dw", dt)
+        close(stored(self.db, self.classes), G.sum(0), SLACK * (eg.sum(0) + (min(self.rows, 512) + 64) * U * np.abs(G).sum(0)) + 1e-40,
+              "dbias")
+        for m in (self.x, self.w, self.dx, self.dw):
+            m.assert_guard()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,dim,classes", [(1, 1, 1), (1, 64, 1000), (2, 8, 2), (5, 3, 7), (48, 250, 1000), (63, 64, 65),
+                                              (129, 128, 257), (300, 40, 2000), (1000, 7, 300), (260, 520, 777), (3, 1030, 400),
+                                              (2100, 64, 600), (70, 33, 9001), (1500, 128, 5003)])
+def test_softmax_loss(V, dt, rows, dim, classes):
+    t = Loss(V, dt, rows, dim, classes)
+    t.run()
+    t.check()
+    first = t.results()
+    t.ws.fill_(0x7F)
+    t.run()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(first, t.results()))
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_softmax_loss_without_what_may_be_absent(V, dt):
+    t = Loss(V, dt, 130, 70, 300, bias=None, dloss=False, ld=75, lead=1)
+    t.run()
+    t.check()
+    whole = t.results()
+    for keep in ("dx", "dw", "dbias"):
+        u = Loss(V, dt, 130, 70, 300, bias=None, dloss=False, ld=75, lead=1)
+        V.vfl_softmax_loss_forward(u.a)
+        for k in ("dx", "dw"):
+            if k != keep:
+                getattr(u.a, k).data = None
+        if keep != "dbias":
+            u.a.dbias = None
+        V.vfl_softmax_loss_backward(u.a)
+        torch.cuda.synchronize()
+        i = {"dx": 2, "dw": 3, "dbias": 4}[keep]
+        assert torch.equal(whole[i], u.results()[i])
+    u = Loss(V, dt, 130, 70, 300, bias=None, dloss=False, ld=75, lead=1)
+    u.a.labels = u.a.loss = None
+    V.vfl_softmax_loss_forward(u.a)
+    torch.cuda.synchronize()
+    assert torch.equal(whole[1], u.lse) and not torch.equal(whole[0], u.loss)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_softmax_loss_rows_without_a_label_and_classes_taken_out(V, dt):
+    rows, dim, classes = 140, 64, 500
+    rng = np.random.default_rng(11)
+    labels = rng.integers(0, classes, rows)
+    labels[::5], labels[7], labels[8], labels[9] = -1, classes, 2 ** 31 - 1, -2 ** 31
+    x, w = rng.normal(size=(rows, dim)), rng.normal(size=(classes, dim)) * 0.2
+    x[5], x[10, 3], x[7] = np.nan, np.inf, np.nan              # rows without a label
+    bias = rng.normal(size=classes)
+    bias[100:140] = bias[labels[1]] = -np.inf
+    w[110], w[111, 3], w[499] = np.nan, np.inf, w[499] * 5
+    t = Loss(V, dt, rows, dim, classes, bias=bias, x=x, w=w, labels=labels)
+    t.run()
+    t.check()
+    assert not t.dw.np()[100:140].any() and not t.dx.np()[~((labels >= 0) & (labels < classes))].any()
+
+
+def test_softmax_loss_of_no_class_at_all(V):
+    t = Loss(V, "f32", 20, 16, 40, bias=np.full(40, -np.inf), labels=np.arange(20) % 3 - 1)
+    t.run()
+    t.check()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_softmax_loss_of_far_logits(V, dt):
+    rows, dim, classes = 64, 128, 300
+    rng = np.random.default_rng(12)
+    x, w = rng.normal(size=(rows, dim)) * 10, rng.normal(size=(classes, dim)) * 3
+    t = Loss(V, dt, rows, dim, classes, x=x, w=w)
+    t.run()
+    t.check()
+
+
+@pytest.mark.parametrize("dt,rows,classes", [("bf16", 8192, 9000), ("f32", 8192, 4500)])
+def test_softmax_loss_in_pieces(V, dt, rows, classes):
+    """More classes than one piece of the gradient holds."""
+    t = Loss(V, dt, rows, 24, classes)
+    assert rows * classes * (2 if dt == "bf16" else 4) > 2 * 64 << 20
+    t.run()
+    t.check()
+
+
+def test_softmax_loss_backward_of_no_rows(V):
+    t = Loss(V, "bf16", 0, 24, 300)
+    t.run()
+    torch.cuda.synchronize()
+    assert not t.dw.np().any() and not stored(t.db, 300).any()
+    t.dw.assert_guard()
+
+
+def test_gradients_against_differences(V):
+    """The loss's own differences along random directions, float32."""
+    t = Loss(V, "f32", 40, 24, 90)
+    t.run()
+    torch.cuda.synchronize()
+    d = t.dl[:40].double()
+    grads = {"x": t.dx.t.double(), "w": t.dw.t.double(), "bias": t.db[:90].double()}
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for k, p in (("x", t.x.t), ("w", t.w.t), ("bias", t.bias[:90])):
+        u = torch.randn(p.shape, generator=g, device="cuda")
+        start, h, f = p.clone(), 2.0 ** -7, []
+        for sign in (1, -1):
+            p.copy_(start + sign * h * u)
+            step = (p.double() - start.double())
+            t.V.vfl_softmax_loss_forward(t.a)
+            torch.cuda.synchronize()
+            f.append(((t.loss[:40].double() * d).sum(), step))
+        p.copy_(start)
+        diff, along = f[0][0] - f[1][0], ((f[0][1] - f[1][1]) * grads[k]).sum()
+        # third order: h^3 times a few; the losses' rounding: 40 rows of 2^-22 / 40
+        assert abs(diff - along) <= 20 * h ** 3 + 2.0 ** -20, (k, float(diff), float(along))
+
+
+# -------------------------------------------------------- streams and graphs
+def test_on_another_stream_and_in_a_replayed_graph(V):
+    """A run of the operators as a layer and a head use them, enqueued on a stream,
+    captured, and replayed with other inputs between eager calls."""
+    rows, cols, hidden, classes = 300, 256, 192, 1000
+    rng = np.random.default_rng(21)
+    x, r = (Mat("bf16", rows, cols, 0, 0, activations(rng, rows, cols)) for _ in range(2))
+    w = Mat("bf16", hidden, cols, 0, 0, rng.normal(size=(hidden, cols)) / 16)
+    s, q, wq, wt, h, stats = Mat("bf16", rows, cols), Eight(rows, cols), Eight(hidden, cols), Eight(cols, hidden), Mat("bf16", rows, hidden), vec(rows)
+    a = rms(V, "bf16", rows, cols, x, r, None, s, None, q, stats, call=False)
+    quantize(V, "bf16", w, wq, wt)
+    t = Loss(V, "bf16", rows, hidden, classes)
+    h.put(t.a.x)
+    wsize = max(V.vfl_matmul8_workspace_size(rows, hidden, cols), V.vfl_matmul8_workspace_size(rows, cols, hidden))
+    ws = torch.empty(wsize + 16, dtype=torch.uint8, device="cuda")
+    dq, dy = Eight(rows, hidden), Mat("bf16", rows, cols)
+    dx, dgamma = Mat("bf16", rows, cols), vec(cols)
+    nws = torch.empty(V.vfl_norm_workspace_size(rows, cols) + 16, dtype=torch.uint8, device="cuda")
+    back = V.vfl_rmsnorm_args()
+    back.dtype, back.rows, back.cols, back.stats, back.dgamma = V.VFL_BF16, rows, cols, ptr(stats), ptr(dgamma)
+    s.put(back.s)
+    dy.put(back.dy)
+    dx.put(back.dx)
+    back.workspace, back.workspace_bytes = ptr(nws), nws.numel() - 16
+    qa = V.vfl_quantize_args()
+    qa.dtype, qa.rows, qa.cols = V.VFL_BF16, rows, hidden
+    t.dx.put(qa.x)
+    dq.put(qa.q)
+
+    def step(stream):
+        V.vfl_rmsnorm_forward(a, stream)
+        matmul8(V, "bf16", q, wq, h, cols, None, 1, stream, ws)
+        t.run(stream)
+        V.vfl_quantize(qa, stream)
+        matmul8(V, "bf16", dq, wt, dy, hidden, None, 0, stream, ws)
+        V.vfl_rmsnorm_backward(back, stream)
+
+    def results():
+        torch.cuda.synchronize()
+        return t.results() + [h.t.clone(), dx.t.clone(), dgamma.clone(), s.t.clone()]
+
+    side = torch.cuda.Stream()
+    step(0)
+    first = results()
+    assert all(torch.isfinite(v.float()).all() for v in first)
+    with torch.cuda.stream(side):
+        step(side.cuda_stream)
+    assert all(torch.equal(u, v) for u, v in zip(first, results()))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(torch.cuda.current_stream().cuda_stream)
+    for i in range(4):
+        x.t.copy_(torch.from_numpy(activations(rng, rows, cols)))
+        step(0)
+        want = results()
+        for m in (h, dx, s):
+            m.t.zero_()
+        t.ws.fill_(i)
+        torch.cuda.synchronize()
+        graph.replay()
+        assert all(torch.equal(u, v) for u, v in zip(want, results()))
+    assert not torch.equal(first[2], want[2])
