@@ -623,7 +623,8 @@ vfl_status vfl_matmul8(const vfl_matmul8_args* a, void* stream);
  *   z = x w^T + bias,  lse = log(sum_c exp z_c),  loss = lse - z[label],
  * x [rows x dim], w [classes x dim] of `dtype`, bias float32 [classes] (NULL: 0),
  * labels int32 [rows], loss and lse float32 [rows]; rows <= VFL_LOSS_MAX_ROWS, 1 <=
- * dim <= VFL_LOSS_MAX_DIM, 1 <= classes <= VFL_LOSS_MAX_CLASSES.  A label outside
+ * dim <= VFL_LOSS_MAX_DIM, 1 <= classes <= VFL_LOSS_MAX_CLASSES, rows classes <=
+ * 2^37.  A label outside
  * [0, classes) marks a row without one: its loss is 0 and it takes no part in any
  * gradient, whatever its x holds (its lse is that of its x).  A bias of -inf takes
  * a class out of every sum, whatever its weights hold; a label of such a class has
@@ -637,7 +638,7 @@ vfl_status vfl_matmul8(const vfl_matmul8_args* a, void* stream);
  * gradient of 0.  G is rounded to `dtype` once, as the operand of its products;
  * their sums are float32.
  *   The workspace (16-byte aligned, vfl_softmax_loss_workspace_size() bytes: copies
- * of x and w in the products' layout and pieces of G of 64 MB or one piece of 256
+ * of x and w in the products' layout and pieces of G of 256 MB or one piece of 256
  * classes) means nothing between calls; calls that may run at the same time need
  * one each.  Fields that a direction does not use are ignored. */
 #define VFL_LOSS_MAX_ROWS 2097152

@@ -287,6 +287,185 @@ struct Tile {
   }
 };
 
+// A matrix [sum x columns] whose rows are single terms of the sum: `chunks` 16-byte
+// chunks a row, `last` the last row; what lies past either is read as the last one.
+struct SumMajor {
+  const char* p;
+  int64_t ld;
+  int64_t last;
+  int chunks;
+};
+
+// C^T = A^T B (BOTH) or A^T B^T over the sum: A [sum x m], B [sum x n] or, as
+// an Operand, [n x sum].  LDS holds what it is given, 16-byte chunk c of row k at
+// place c ^ swizzle(k).  bf16 fragments of a sum-major operand come from transposing
+// reads (ds_read_b64_tr_b16: 16 lanes give the addresses of four columns of
+// four rows each, and lane i gets column i of the four rows), two for the eight
+// terms that a lane of the MFMA holds; float32 ones are read element by element.
+// Columns are dealt to D fragments by fours (fragment f, lane i: 4 D (i / 4) + 4 f +
+// i % 4), which is what those reads can gather, and leaves a lane 4 D consecutive
+// columns of A for each column of B: they are stored at once.
+template <Type TY, int BM_, int BN_, int WR, int WC, int KB_, int NST_, bool BOTH>
+struct SumTile {
+  static constexpr int BM = BM_, BN = BN_, KB = KB_, NST = NST_;
+  static constexpr int kWaves = WR * WC, kThreads = 64 * kWaves;
+  static constexpr int WM = BM / WR, WN = BN / WC, MF = WM / 16, NF = WN / 16;
+  static constexpr int kStage = (BM + BN) * KB, kLds = NST * kStage;
+  static constexpr int kBytes = TY == kBf16 ? 2 : 4, kElements = KB / kBytes;   // terms of a step
+  static constexpr int kCopies = kStage / 1024 / kWaves, kCopiesA = BM * KB / 1024;
+  static constexpr int kHalves = KB / 64;
+  static constexpr int D = MF < 4 ? MF : 4, DN = NF < 4 ? NF : 4;
+  static_assert(TY == kBf16 || TY == kF32);
+  static_assert(TY == kF32 ? D >= 2 && DN >= 2 : D == 4 && DN == 4, "the swizzles below");
+  static_assert(MF % D == 0 && NF % DN == 0 && kStage % (1024 * kWaves) == 0 && BM * KB % 1024 == 0);
+  static_assert(BM * kBytes >= 256 && BN * kBytes >= 256);
+  static_assert((NST - 2) * kCopies < 64);
+  typedef f32x4 Acc[MF][NF];
+
+  int lane, wm, wn;
+  __device__ SumTile() {
+    lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    wm = wave / WC * WM;
+    wn = wave % WC * WN;
+  }
+  // the first of the 4 D consecutive columns of A that a lane's fragments D q .. hold
+  __device__ int a_col(int q) const { return wm + 16 * D * q + 4 * D * (lane >> 4); }
+  // the column of B of its fragment f
+  __device__ int b_col(int f) const {
+    return wn + 16 * DN * (f / DN) + 4 * DN * ((lane & 15) >> 2) + 4 * (f % DN) + (lane & 3);
+  }
+
+  // Four rows that are read at once (bf16: consecutive; float32: four apart) lie in
+  // different banks: the fragment's place among its D flips with the low bits, the
+  // half of 256 bytes with the high one.
+  __device__ static int swizzle(int k, int deal) {
+    if constexpr (TY == kBf16) return (k & 1) | (k & 2) << 2;
+    else return deal == 4 ? (k >> 2) & 3 : (k >> 2 & 1) | (k >> 3 & 1) << 3;
+  }
+
+  __device__ void run(const SumMajor& A, const SumMajor& Bs, const Operand& B, int64_t m0, int64_t n0, int s0, int s1,
+                      char* lds, Acc& acc) const {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // a copy's lane: row `row[c]` of the step (of a sum-major operand) at byte col[c]
+    // of it, or the offset of its chunk from the tile's first row
+    int row[kCopies];
+    int64_t at[kCopies];
+    const int64_t b_first = BOTH ? 0 : min(n0, B.last);
+#pragma unroll
+    for (int c = 0; c < kCopies; ++c) {
+      const int blk = wave + c * kWaves;
+      const bool of_a = blk < kCopiesA;                                  // uniform
+      if (of_a || BOTH) {
+        const int per = (of_a ? BM : BN) * kBytes / 16;                  // chunks of a row
+        const int u = (of_a ? blk : blk - kCopiesA) * 64 + lane;         // chunk of the operand's step
+        const int k = u / per;
+        const int ch = (u % per) ^ swizzle(k, of_a ? D : DN);
+        const SumMajor& o = of_a ? A : Bs;
+        const int64_t chunk = min((of_a ? m0 : n0) * kBytes / 16 + ch, (int64_t)o.chunks - 1);
+        row[c] = k;
+        at[c] = chunk * 16;
+      } else {
+        const int R = (blk - kCopiesA) * (1024 / KB) + lane / (KB / 16);
+        const int f = R >> 4, i = R & 15;
+        const int r = f / DN * (16 * DN) + 4 * DN * (i >> 2) + 4 * (f % DN) + (i & 3);
+        const int swz = KB == 128 ? (i >> 1) & 7 : (i >> 2) & 3;
+        row[c] = 0;
+        at[c] = min((int64_t)r, B.last - b_first) * B.ld + ((lane % (KB / 16)) ^ swz) * 16;
+      }
+    }
+    const VFL_GLOBAL char* const b0 = BOTH ? nullptr : glb(B.p) + b_first * B.ld;
+    auto copy = [&](int s) {
+      char* dst = lds + (NST == 2 ? s & 1 : s % NST) * kStage;
+#pragma unroll
+      for (int c = 0; c < kCopies; ++c) {
+        const int blk = wave + c * kWaves;
+        const bool of_a = blk < kCopiesA;
+        const VFL_GLOBAL char* src;
+        if (of_a || BOTH) {
+          const SumMajor& o = of_a ? A : Bs;
+          src = glb(o.p) + min((int64_t)(s0 + s) * kElements + row[c], o.last) * o.ld + at[c];
+        } else {
+          src = b0 + (int64_t)(s0 + s) * KB + at[c];
+        }
+        __builtin_amdgcn_global_load_lds((VFL_GLOBAL void*)src, (lds_t*)(dst + blk * 1024), 16, 0, 0);
+      }
+    };
+    const int n = s1 - s0, i = lane & 15, g = lane >> 4;
+
+    // this lane's byte in the sum-major operand of WIDTH columns: fragment f of the
+    // wavefront's columns from w; bf16: rows k .. k + 3 by transposing reads
+    auto transposed = [&](const char* S, int width, int deal, int w, int f, int k) {
+      typedef __attribute__((ext_vector_type(4))) short s16x4;
+      const int kk = k + (i >> 2);
+      const int col = w + 16 * deal * (f / deal) + 4 * deal * (i & 3) + 4 * (f % deal);
+      const int ch = (col / 8) ^ swizzle(kk, deal);
+      const char* p = S + kk * width * 2 + ch * 16 + (col % 8) * 2;
+      return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                           (__attribute__((address_space(3))) s16x4*)p));
+    };
+    auto element = [&](const char* S, int width, int deal, int w, int f, int k) {
+      const int col = w + 16 * deal * (f / deal) + 4 * deal * (i >> 2) + 4 * (f % deal) + (i & 3);
+      const int ch = (col / 4) ^ swizzle(k, deal);
+      return *(const float*)(S + k * width * 4 + ch * 16 + (col % 4) * 4);
+    };
+    // the 16 bytes of the sum that lane (i, g) holds of a fragment: terms 8 (g + 4 h)
+    // of bf16, 4 (g + 4 h) of float32
+    auto fragment = [&](const char* S, int width, int deal, int w, int f, int h) {
+      u32x4 v;
+      if constexpr (TY == kBf16) {
+        const u32x2 lo = transposed(S, width, deal, w, f, 8 * (g + 4 * h));
+        const u32x2 hi = transposed(S, width, deal, w, f, 8 * (g + 4 * h) + 4);
+        v = u32x4{lo[0], lo[1], hi[0], hi[1]};
+      } else {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) v[t] = __float_as_uint(element(S, width, deal, w, f, 4 * (g + 4 * h) + t));
+      }
+      return v;
+    };
+
+#pragma unroll
+    for (int s = 0; s < NST - 1; ++s)
+      if (s < n) copy(s);
+    for (int s = 0; s < n; ++s) {
+      if (NST > 2 && s + NST - 2 < n) wait_copies<(NST - 2) * kCopies>();
+      else wait_copies<0>();
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+      if (s + NST - 1 < n) copy(s + NST - 1);
+      __builtin_amdgcn_sched_barrier(0);
+      const char* S = lds + (NST == 2 ? s & 1 : s % NST) * kStage;
+      const char* SB = S + BM * KB;
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) {
+        u32x4 b[NF];
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+          if constexpr (BOTH) b[f] = fragment(SB, BN, DN, wn, f, h);
+          else b[f] = *(const u32x4*)(SB + (wn + 16 * f + i) * KB + ((g + 4 * h) ^ (KB == 128 ? (i >> 1) & 7 : (i >> 2) & 3)) * 16);
+        }
+#pragma unroll
+        for (int f = 0; f < MF; ++f) {
+          const u32x4 a = fragment(S, BM, D, wm, f, h);
+          if constexpr (TY == kBf16) {
+#pragma unroll
+            for (int c = 0; c < NF; ++c)
+              acc[f][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                                  __builtin_bit_cast(bf16x8, b[c]), acc[f][c], 0, 0, 0);
+          } else {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+              for (int c = 0; c < NF; ++c)
+                acc[f][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[t]), __uint_as_float(b[c][t]),
+                                                                 acc[f][c], 0, 0, 0);
+          }
+        }
+      }
+    }
+  }
+};
+
 // Tile t of tm x tn: workgroups are dealt to the eight XCDs in turn, so each XCD
 // takes a contiguous range of an order that walks bands of eight tile rows column
 // by column: the tiles of a range share rows of both operands in one L2.

@@ -12,6 +12,7 @@ namespace {
 
 constexpr int64_t kMaxSide8 = (int64_t)1 << 30;      // rows of an operand of a product, results' columns
 constexpr int64_t kMaxResults = (int64_t)1 << 38;    // of a product: its grid is below 2^32 threads
+constexpr int64_t kMaxLogits = (int64_t)1 << 37;
 constexpr int64_t kMaxDepth = VFL_MATMUL8_MAX_DEPTH;
 
 int64_t round_up(int64_t v, int64_t by) { return (v + by - 1) / by * by; }
@@ -54,6 +55,7 @@ Checks loss_checks(const char* call, const vfl_softmax_loss_args& a) {
   Checks c = begin(call, dtype_of(a.dtype), a.rows, a.dim, VFL_LOSS_MAX_DIM);
   c.need(a.rows <= VFL_LOSS_MAX_ROWS, "rows above the operator's limit");
   c.need(a.classes >= 1 && a.classes <= VFL_LOSS_MAX_CLASSES, "classes out of range");
+  c.need(c.why || a.rows <= kMaxLogits / a.classes, "rows x classes out of range");
   return c;
 }
 
@@ -198,6 +200,7 @@ vfl_status vfl_softmax_loss_workspace_size(vfl_dtype dtype, int64_t rows, int32_
   Checks c = begin(call, dtype_of(dtype), rows, dim, VFL_LOSS_MAX_DIM);
   c.need(rows <= VFL_LOSS_MAX_ROWS, "rows above the operator's limit");
   c.need(classes >= 1 && classes <= VFL_LOSS_MAX_CLASSES, "classes out of range");
+  c.need(c.why || rows <= kMaxLogits / classes, "rows x classes out of range");
   c.need(bytes != nullptr, "bytes must not be NULL");
   if (c.why) return refuse(call, c.why);
   *bytes = rows == 0 ? 0 : loss_workspace(elt(c.dtype), rows, dim, classes);

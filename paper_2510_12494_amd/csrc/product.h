@@ -95,6 +95,61 @@ __global__ __launch_bounds__(TL::kThreads) void k_product(ProductArgs j) {
   }
 }
 
+// A tile of C^T, C [n x m]: results of sum-major operands (gemm.h), or partial sums
+// of them [part][n][m].
+struct SumArgs {
+  SumMajor a, bs;
+  Operand b;
+  void* c;
+  int64_t ldc, n;
+  uint32_t tm, tn;
+  int m, steps, per, add;
+};
+template <class TL, typename T>
+__global__ __launch_bounds__(TL::kThreads) void k_sum_product(SumArgs j) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  uint32_t tm, tn;
+  tile_of(blockIdx.x, j.tm, j.tn, &tm, &tn);
+  const TL tile;
+  typename TL::Acc acc;
+#pragma unroll
+  for (int f = 0; f < TL::MF; ++f)
+#pragma unroll
+    for (int c = 0; c < TL::NF; ++c) acc[f][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int s0 = blockIdx.y * j.per, s1 = min(s0 + j.per, j.steps);
+  const int m0 = (int)tm * TL::BM;
+  const int64_t n0 = (int64_t)tn * TL::BN;
+  tile.run(j.a, j.bs, j.b, m0, n0, s0, s1, smem, acc);
+#pragma unroll
+  for (int f = 0; f < TL::NF; ++f) {
+    const int64_t row = n0 + tile.b_col(f);
+    if (row >= j.n) continue;
+    T* const out = (T*)j.c + ((int64_t)blockIdx.y * j.n + row) * j.ldc;
+#pragma unroll
+    for (int q = 0; q < TL::MF / TL::D; ++q)
+#pragma unroll
+      for (int d = 0; d < TL::D; d += 2) {
+        const int col = m0 + tile.a_col(q) + 4 * d, left = j.m - col;
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = acc[q * TL::D + d + i / 4][f][i % 4];
+        if (left >= 8) {
+          if (j.add) {
+            float o[8];
+            unpack(load_at(out + col), o);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += o[i];
+          }
+          store8<false>(out + col, v);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 7; ++i)
+            if (i < left) st1<T>(out + col + i, j.add ? v[i] + ld1<T>(out + col + i) : v[i]);
+        }
+      }
+  }
+}
+
 constexpr int kJoinThreads = 256;
 struct JoinArgs {
   const float* part;
@@ -120,6 +175,11 @@ __global__ __launch_bounds__(kJoinThreads) void k_product_join(JoinArgs j) {
 int64_t tiles_of(int64_t v, int by) { return (v + by - 1) / by; }
 // elements of a row of partial sums over n columns
 int64_t part_ld(int64_t n) { return (n + 3) & ~(int64_t)3; }
+
+template <class TL, typename T>
+hipError_t sum_product(const SumArgs& a, int parts, hipStream_t st) {
+  return enqueue(k_sum_product<TL, T>, dim3(a.tm * a.tn, (unsigned)parts), dim3(TL::kThreads), TL::kLds, st, a);
+}
 
 template <class TL, typename T>
 hipError_t product(const ProductArgs& a, int parts, hipStream_t st) {

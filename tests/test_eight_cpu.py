@@ -162,7 +162,7 @@ def test_workspace_sizes_check_their_sizes(V):
     for bad in ((-1, 1, 1), (1, -1, 1), (1, 1, 0), (2**31, 1, 1), (2**25, 2**25, 1), (1, 1, 2**24)):
         with pytest.raises(V.VflError):
             V.vfl_matmul8_workspace_size(*bad)
-    for bad in ((2, 1, 1, 1), (0, -1, 1, 1), (0, 1, 0, 1), (0, 1, 1, 0), (0, 2**22, 1, 1), (0, 1, 1, 2**22)):
+    for bad in ((2, 1, 1, 1), (0, -1, 1, 1), (0, 1, 0, 1), (0, 1, 1, 0), (0, 2**22, 1, 1), (0, 1, 1, 2**22), (0, 2**20, 1, 2**18)):
         with pytest.raises(V.VflError):
             V.vfl_softmax_loss_workspace_size(*bad)
     assert V.vfl_matmul8_workspace_size(0, 8, 8) == 0

@@ -574,11 +574,11 @@ def test_softmax_loss_of_far_logits(V, dt):
     t.check()
 
 
-@pytest.mark.parametrize("dt,rows,classes", [("bf16", 8192, 9000), ("f32", 8192, 4500)])
+@pytest.mark.parametrize("dt,rows,classes", [("bf16", 30000, 9000), ("f32", 20000, 6800)])
 def test_softmax_loss_in_pieces(V, dt, rows, classes):
     """More classes than one piece of the gradient holds."""
     t = Loss(V, dt, rows, 24, classes)
-    assert rows * classes * (2 if dt == "bf16" else 4) > 2 * 64 << 20
+    assert rows * classes * (2 if dt == "bf16" else 4) > 2 * 256 << 20
     t.run()
     t.check()
 
