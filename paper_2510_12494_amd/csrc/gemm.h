@@ -53,6 +53,20 @@ __device__ __forceinline__ void wait_copies() {
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));
 }
 
+// Sixteen e4m3 values times their power of two, whose exponent is s's low byte, as bf16:
+// the conversion takes the power as a float32, whose exponent lies 23 bits up.
+__device__ __forceinline__ void widen_e4m3(const u32x4& v, uint32_t s, bf16x8 (&out)[2]) {
+  const float power = __uint_as_float((s & 255u) << 23);
+  u32x4 w[2];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    w[i / 2][2 * (i % 2)] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[i], power, false));
+    w[i / 2][2 * (i % 2) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[i], power, true));
+  }
+#pragma unroll
+  for (int t = 0; t < 2; ++t) out[t] = __builtin_bit_cast(bf16x8, w[t]);
+}
+
 // An operand: rows of ld bytes, `last` the last row's index; rows past it are
 // read as that row (their results are not kept).  8-bit operands: the exponent
 // bytes of step s at scale + s * scale_ld + row, in dwords of four rows.
@@ -208,11 +222,11 @@ struct Tile {
         for (int h = 0; h < 2; ++h) {
           bf16x8 b[NF][2];
 #pragma unroll
-          for (int f = 0; f < NF; ++f) widen(*(const u32x4*)(SB + f * 16 * KB + place[h]), sb[f / 4], f & 3, b[f]);
+          for (int f = 0; f < NF; ++f) widen_e4m3(*(const u32x4*)(SB + f * 16 * KB + place[h]), sb[f / 4] >> (8 * (f & 3)), b[f]);
 #pragma unroll
           for (int f = 0; f < MF; ++f) {
             bf16x8 a[2];
-            widen(*(const u32x4*)(SA + f * 16 * KB + place[h]), sa[f / 4], f & 3, a);
+            widen_e4m3(*(const u32x4*)(SA + f * 16 * KB + place[h]), sa[f / 4] >> (8 * (f & 3)), a);
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -246,20 +260,6 @@ struct Tile {
         }
       }
     }
-  }
-
-  // sixteen e4m3 values times their power of two as bf16 (byte f of s: its exponent,
-  // moved to where a float32 has it)
-  __device__ static __forceinline__ void widen(const u32x4& v, uint32_t s, int f, bf16x8 (&out)[2]) {
-    const float power = __uint_as_float(((s >> (8 * f)) & 255u) << 23);
-    u32x4 w[2];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      w[i / 2][2 * (i % 2)] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[i], power, false));
-      w[i / 2][2 * (i % 2) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[i], power, true));
-    }
-#pragma unroll
-    for (int t = 0; t < 2; ++t) out[t] = __builtin_bit_cast(bf16x8, w[t]);
   }
 
   // one row fragment of e4m3 times every column fragment; the exponent byte of a

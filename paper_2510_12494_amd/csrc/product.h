@@ -168,7 +168,14 @@ __global__ __launch_bounds__(kJoinThreads) void k_product_join(JoinArgs j) {
   const int col = 4 * (int)(at - row * j.quads);
   const float* p = j.part + row * j.ld + col;
   f32x4 v = *(const f32x4*)p;
-  for (int i = 1; i < j.parts; ++i) v += *(const f32x4*)(p + (int64_t)i * j.m * j.ld);
+  const int64_t pitch = j.m * j.ld;
+  for (int i = 1; i < j.parts; i += 8) {             // eight loads in flight
+    f32x4 o[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) o[u] = i + u < j.parts ? *(const f32x4*)(p + (i + u) * pitch) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v += o[u];
+  }
   store_to((T*)j.c + row * j.ldc + col, finish(v, bias4(j.bias, col, j.n), j.relu), j.n - col);
 }
 

@@ -264,12 +264,31 @@ struct FinishArgs {
   int dim;
 };
 
-// A row a group of 16 lanes: the tiles' pairs joined, and the label's logit.
-template <typename T>
+// A row a group of 16 lanes: the tiles' pairs joined, and the label's logit (whose
+// operands are asked for first: latency bounds this).
+template <typename T, Form F>
 __global__ __launch_bounds__(kThreads) void k_loss(FinishArgs j) {
   const int lane = threadIdx.x & 15;
   const int64_t row = (int64_t)blockIdx.x * (kThreads / 16) + (threadIdx.x >> 4);
   if (row >= j.rows) return;
+  const int label = j.loss ? j.labels[row] : -1;
+  const bool has = label >= 0 && label < j.classes;
+  float z = 0.f, b = 0.f;
+  if (has) {
+    const Cols kx(j.dim, j.rows), kw(j.dim, j.classes);
+    const T* const x = row_of<T>(j.x, row);
+    const T* const w = row_of<T>(j.w, label);
+    b = j.bias ? j.bias[label] : 0.f;
+#pragma unroll 2
+    for (int q = lane; q < kx.per; q += 16) {
+      float u[8], v[8];
+      const Raw<T> xr = load_chunk<F>(x, q, kx, row >= kx.edge), wr = load_chunk<F>(w, q, kw, label >= kw.edge);
+      chunk_values<F>(xr, q, kx, row >= kx.edge, u);
+      chunk_values<F>(wr, q, kw, label >= kw.edge, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) z = fmaf(u[i], v[i], z);
+    }
+  }
   float top = -__builtin_inff(), sum = 0.f;
 #pragma unroll 4
   for (int64_t t = lane; t < j.tiles; t += 16) {
@@ -288,18 +307,8 @@ __global__ __launch_bounds__(kThreads) void k_loss(FinishArgs j) {
   const float lse = (all + __builtin_amdgcn_logf(sum)) * kLn2;
   if (j.lse && lane == 0) j.lse[row] = lse;
   if (!j.loss) return;
-  const int label = j.labels[row];
-  float loss = 0.f;
-  if (label >= 0 && label < j.classes) {
-    const T* const x = row_of<T>(j.x, row);
-    const T* const w = row_of<T>(j.w, label);
-    float z = 0.f;
-    for (int c = lane; c < j.dim; c += 16) z = fmaf(ld1<T>(x + c), ld1<T>(w + c), z);
-    z = group_sum<16>(z);
-    const float b = j.bias ? j.bias[label] : 0.f;
-    loss = b == -__builtin_inff() ? __builtin_inff() : lse - (z + b);
-  }
-  if (lane == 0) j.loss[row] = loss;
+  z = group_sum<16>(z);
+  if (lane == 0) j.loss[row] = !has ? 0.f : b == -__builtin_inff() ? __builtin_inff() : lse - (z + b);
 }
 
 // the gradients of no rows
@@ -328,16 +337,16 @@ template <typename T> struct Tiles;
 template <> struct Tiles<uint16_t> {
   typedef Tile<kBf16, 256, 256, 4, 4, 128, 2, kBlocks> Long;    // many columns of x
   typedef Tile<kBf16, 256, 128, 4, 2, 64, 3, kBlocks> Short;   // few: two workgroups a CU
-  typedef Tile<kBf16, 256, 64, 4, 1, 64, 2, kBlocks> Few;       // few rows
+  typedef Tile<kBf16, 256, 64, 4, 1, 64, 4, kBlocks> Few;       // few rows
   template <bool BOTH> using Large = SumTile<kBf16, 256, 256, 4, 4, 128, 2, BOTH>;
   template <bool BOTH> using Small = SumTile<kBf16, 128, 128, 2, 2, 128, 2, BOTH>;
 };
 template <> struct Tiles<float> {
   typedef Tile<kF32, 128, 128, 2, 2, 64, 2, kBlocks> Long;
   typedef Tile<kF32, 128, 128, 2, 2, 64, 2, kBlocks> Short;
-  typedef Tile<kF32, 64, 64, 2, 2, 64, 2, kBlocks> Few;
+  typedef Tile<kF32, 64, 64, 2, 2, 64, 4, kBlocks> Few;
   template <bool BOTH> using Large = SumTile<kF32, 128, 128, 2, 2, 64, 2, BOTH>;
-  template <bool BOTH> using Small = SumTile<kF32, 64, 64, 2, 2, 64, 2, BOTH>;
+  template <bool BOTH> using Small = SumTile<kF32, 64, 64, 2, 2, 64, 4, BOTH>;
 };
 
 enum Kind { kLong, kShort, kFew };
@@ -361,11 +370,12 @@ Pass pass(int64_t m, int64_t n, int64_t depth) {
   typedef typename Tiles<T>::template Small<true> S;
   Pass p;
   p.large = m > S::BM && n > S::BN;
+  if (sizeof(T) == 4) p.large = tiles_of(m, L::BM) * tiles_of(n, L::BN) >= 1024;
   const int bm = p.large ? L::BM : S::BM, bn = p.large ? L::BN : S::BN;
   p.steps = (int)tiles_of(depth, p.large ? L::kElements : S::kElements);
   p.tm = tiles_of(m, bm);
   p.tn = tiles_of(n, bn);
-  const int64_t tiles = p.tm * p.tn, room = p.large && sizeof(T) == 2 ? 256 : 512;
+  const int64_t tiles = p.tm * p.tn, room = sizeof(T) == 4 ? 1024 : p.large ? 256 : 512;
   const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(room / tiles, p.steps / 4));
   p.per = (int)((p.steps + parts - 1) / parts);
   p.parts = (p.steps + p.per - 1) / p.per;
@@ -393,7 +403,7 @@ Plan plan(int64_t rows, int dim, int64_t classes) {
     at += ((size_t)elements * size + 255) & ~(size_t)255;
     return here;
   };
-  p.kind = rows <= 64 || (sizeof(T) == 4 && tiles_of(rows, 128) * tiles_of(classes, 128) < 256) ? kFew
+  p.kind = rows <= 64 || (sizeof(T) == 4 && tiles_of(rows, 128) * tiles_of(classes, 128) < 1024) ? kFew
            : dim * (int)sizeof(T) > 512                                                        ? kLong
                                                                                                 : kShort;
   with_tile<T>(p.kind, [&](auto* tile) {
@@ -477,7 +487,7 @@ hipError_t forward(const LossJob& j, hipStream_t st) {
   e = logits<T, false>(a, p, j.classes, st);
   if (e != hipSuccess) return e;
   const FinishArgs f{a.part, j.x, j.w, j.bias, j.labels, j.loss, j.lse, j.rows, j.classes, a.tm, j.dim};
-  return enqueue(k_loss<T>, dim3((unsigned)tiles_of(j.rows, kThreads / 16)), dim3(kThreads), 0, st, f);
+  return enqueue(j.dim % 8 == 0 ? k_loss<T, kExact> : j.dim > 8 ? k_loss<T, kRagged> : k_loss<T, kSmall>, dim3((unsigned)tiles_of(j.rows, kThreads / 16)), dim3(kThreads), 0, st, f);
 }
 
 template <typename T>
