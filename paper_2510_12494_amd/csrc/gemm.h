@@ -466,16 +466,23 @@ struct SumTile {
   }
 };
 
-// Tile t of tm x tn: workgroups are dealt to the eight XCDs in turn, so each XCD
-// takes a contiguous range of an order that walks bands of eight tile rows column
-// by column: the tiles of a range share rows of both operands in one L2.
-__device__ __forceinline__ void tile_of(uint32_t block, uint32_t tm, uint32_t tn, uint32_t* m, uint32_t* n) {
-  const uint32_t total = tm * tn, per = total / 8, more = total % 8;
+// What workgroup `block` of tm x tn tiles and `parts` parts of the sum takes.
+// Workgroups are dealt to the eight XCDs in turn, so each XCD takes a contiguous
+// range of an order that goes part by part and, in a part, walks bands of eight tile
+// rows column by column: what a range reads of both operands meets in one L2
+// (1024 x 500 x 32768 in 16 parts: 38 us with the tiles of a part on all XCDs).
+struct Place { uint32_t m, n, part; };
+__device__ __forceinline__ Place place_of(uint32_t block, uint32_t tm, uint32_t tn, uint32_t parts) {
+  const uint32_t tiles = tm * tn, total = tiles * parts, per = total / 8, more = total % 8;
   const uint32_t x = block % 8;
-  const uint32_t t = x * per + min(x, more) + block / 8;
+  uint32_t t = x * per + min(x, more) + block / 8;
+  Place p;
+  p.part = t / tiles;
+  t -= p.part * tiles;
   const uint32_t band = t / (8 * tn), in = t - band * 8 * tn, rows = min(8u, tm - 8 * band);
-  *m = 8 * band + in % rows;
-  *n = in / rows;
+  p.m = 8 * band + in % rows;
+  p.n = in / rows;
+  return p;
 }
 
 }  // namespace gemm

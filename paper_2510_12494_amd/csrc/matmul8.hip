@@ -166,16 +166,17 @@ hipError_t matmul8(const Matmul8Job& j, const Cut& c, hipStream_t st) {
   a.tn = (uint32_t)c.tn;
   a.steps = c.steps;
   a.per = c.per;
+  a.parts = (uint32_t)c.parts;
   if (c.parts == 1) {
     a.c = j.c.p;
     a.ldc = j.c.ld;
     a.bias = j.bias;
     a.relu = j.relu;
-    return product<TL, T>(a, 1, st);
+    return product<TL, T>(a, st);
   }
   a.c = j.part;
   a.ldc = part_ld(j.n);
-  const hipError_t e = product<TL, float>(a, c.parts, st);
+  const hipError_t e = product<TL, float>(a, st);
   return e != hipSuccess ? e : join<T>(j.part, c.parts, j.m, j.n, j.bias, j.relu, j.c, st);
 }
 

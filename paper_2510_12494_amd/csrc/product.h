@@ -15,7 +15,7 @@ struct ProductArgs {
   void* c;
   int64_t ldc;
   const float* bias;
-  uint32_t tm, tn;
+  uint32_t tm, tn, parts;
   int n, steps, per;                   // per: steps of a part
   int64_t m;
   int relu, add;
@@ -56,22 +56,21 @@ __device__ __forceinline__ void store_to(T* p, const f32x4& v, int left) {
     if (i < left) st1<T>(p + i, v[i]);
 }
 
-// One tile of the product, or (gridDim.y > 1) of part blockIdx.y of its sum, as
+// One tile of the product, or (parts > 1) of a part of its sum, as
 // float32 partial sums [part][m][n]; add: on top of what C holds.
 template <class TL, typename T>
 __global__ __launch_bounds__(TL::kThreads) void k_product(ProductArgs j) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  uint32_t tm, tn;
-  tile_of(blockIdx.x, j.tm, j.tn, &tm, &tn);
+  const Place at = place_of(blockIdx.x, j.tm, j.tn, j.parts);
   const TL tile;
   typename TL::Acc acc;
 #pragma unroll
   for (int f = 0; f < TL::MF; ++f)
 #pragma unroll
     for (int c = 0; c < TL::NF; ++c) acc[f][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int s0 = blockIdx.y * j.per, s1 = min(s0 + j.per, j.steps);
-  const int64_t m0 = (int64_t)tm * TL::BM;
-  const int n0 = (int)tn * TL::BN;
+  const int s0 = (int)at.part * j.per, s1 = min(s0 + j.per, j.steps);
+  const int64_t m0 = (int64_t)at.m * TL::BM;
+  const int n0 = (int)at.n * TL::BN;
   tile.run(j.a, j.b, m0, n0, s0, s1, smem, acc);
 #pragma unroll
   for (int q = 0; q < TL::NF / TL::DN; ++q) {
@@ -83,7 +82,7 @@ __global__ __launch_bounds__(TL::kThreads) void k_product(ProductArgs j) {
       for (int r = 0; r < 4; ++r) {
         const int64_t row = m0 + tile.row(f, r);
         if (row >= j.m || left <= 0) continue;
-        T* p = (T*)j.c + ((int64_t)blockIdx.y * j.m + row) * j.ldc + col;
+        T* p = (T*)j.c + ((int64_t)at.part * j.m + row) * j.ldc + col;
         f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < TL::DN; ++c) {
@@ -102,29 +101,28 @@ struct SumArgs {
   Operand b;
   void* c;
   int64_t ldc, n;
-  uint32_t tm, tn;
+  uint32_t tm, tn, parts;
   int m, steps, per, add;
 };
 template <class TL, typename T>
 __global__ __launch_bounds__(TL::kThreads) void k_sum_product(SumArgs j) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  uint32_t tm, tn;
-  tile_of(blockIdx.x, j.tm, j.tn, &tm, &tn);
+  const Place at = place_of(blockIdx.x, j.tm, j.tn, j.parts);
   const TL tile;
   typename TL::Acc acc;
 #pragma unroll
   for (int f = 0; f < TL::MF; ++f)
 #pragma unroll
     for (int c = 0; c < TL::NF; ++c) acc[f][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int s0 = blockIdx.y * j.per, s1 = min(s0 + j.per, j.steps);
-  const int m0 = (int)tm * TL::BM;
-  const int64_t n0 = (int64_t)tn * TL::BN;
+  const int s0 = (int)at.part * j.per, s1 = min(s0 + j.per, j.steps);
+  const int m0 = (int)at.m * TL::BM;
+  const int64_t n0 = (int64_t)at.n * TL::BN;
   tile.run(j.a, j.bs, j.b, m0, n0, s0, s1, smem, acc);
 #pragma unroll
   for (int f = 0; f < TL::NF; ++f) {
     const int64_t row = n0 + tile.b_col(f);
     if (row >= j.n) continue;
-    T* const out = (T*)j.c + ((int64_t)blockIdx.y * j.n + row) * j.ldc;
+    T* const out = (T*)j.c + ((int64_t)at.part * j.n + row) * j.ldc;
 #pragma unroll
     for (int q = 0; q < TL::MF / TL::D; ++q)
 #pragma unroll
@@ -184,13 +182,13 @@ int64_t tiles_of(int64_t v, int by) { return (v + by - 1) / by; }
 int64_t part_ld(int64_t n) { return (n + 3) & ~(int64_t)3; }
 
 template <class TL, typename T>
-hipError_t sum_product(const SumArgs& a, int parts, hipStream_t st) {
-  return enqueue(k_sum_product<TL, T>, dim3(a.tm * a.tn, (unsigned)parts), dim3(TL::kThreads), TL::kLds, st, a);
+hipError_t sum_product(const SumArgs& a, hipStream_t st) {
+  return enqueue(k_sum_product<TL, T>, dim3(a.tm * a.tn * a.parts), dim3(TL::kThreads), TL::kLds, st, a);
 }
 
 template <class TL, typename T>
-hipError_t product(const ProductArgs& a, int parts, hipStream_t st) {
-  return enqueue(k_product<TL, T>, dim3(a.tm * a.tn, (unsigned)parts), dim3(TL::kThreads), TL::kLds, st, a);
+hipError_t product(const ProductArgs& a, hipStream_t st) {
+  return enqueue(k_product<TL, T>, dim3(a.tm * a.tn * a.parts), dim3(TL::kThreads), TL::kLds, st, a);
 }
 
 // parts [parts][m][part_ld(n)] -> c

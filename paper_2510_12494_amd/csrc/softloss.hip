@@ -112,8 +112,8 @@ __global__ __launch_bounds__(TL::kThreads) void k_logits(LogitArgs j) {
   constexpr int WC = TL::BN / TL::WN, WR = TL::BM / TL::WM, RUN = 4 * TL::DM;
   static_assert(TL::MF == TL::DM, "a lane's classes are one run");
   static_assert(WR * TL::BN * 8 <= TL::kLds && WC * TL::BM * 4 <= TL::kLds);
-  uint32_t tm, tn;
-  tile_of(blockIdx.x, j.tm, j.tn, &tm, &tn);
+  const Place at = place_of(blockIdx.x, j.tm, j.tn, 1);
+  const uint32_t tm = at.m, tn = at.n;
   const TL tile;
   const int64_t c0 = (int64_t)tm * TL::BM, r0 = (int64_t)tn * TL::BN;
   const int64_t mine = c0 + tile.row(0, 0);
@@ -469,7 +469,8 @@ hipError_t times(SumArgs& a, const Pass& p, hipStream_t st) {
   a.per = p.per;
   a.tm = (uint32_t)p.tm;
   a.tn = (uint32_t)p.tn;
-  return p.large ? sum_product<L, O>(a, p.parts, st) : sum_product<S, O>(a, p.parts, st);
+  a.parts = (uint32_t)p.parts;
+  return p.large ? sum_product<L, O>(a, st) : sum_product<S, O>(a, st);
 }
 
 template <typename T>
