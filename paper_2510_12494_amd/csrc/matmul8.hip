@@ -144,8 +144,7 @@ Cut cut(Elt e, int64_t m, int64_t n, int64_t k) {
   c.tm = tiles_of(m, by);
   c.tn = tiles_of(n, by);
   const int64_t all = c.tm * c.tn;
-  int64_t parts = 1;
-  if (all < 256) parts = std::max<int64_t>(1, std::min<int64_t>(512 / all, c.steps / 4));
+  const int64_t parts = all < 256 ? parts_of(all, 512, c.steps, 4, m, n, 5e5) : 1;
   c.per = (int)((c.steps + parts - 1) / parts);
   c.parts = (c.steps + c.per - 1) / c.per;
   return c;

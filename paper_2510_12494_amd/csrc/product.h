@@ -1,6 +1,9 @@
 // Kernels of a matrix product over the core of gemm.h: a tile a workgroup, the
 // sum cut into parts where there are few tiles, the parts joined in order.
 #pragma once
+#include <algorithm>
+#include <cmath>
+
 #include "gemm.h"
 #include "rowchunk.h"
 
@@ -157,29 +160,51 @@ struct JoinArgs {
   int n, quads, parts, relu;
 };
 
-// The parts of a split product, summed in order.
-template <typename T>
+// The parts of a split product, summed in a fixed order: SL threads take every SL-th
+// part of the same four columns each and meet in LDS (many parts of few results: one
+// row of 256 columns in 512 parts 15 us with a thread for all parts).
+template <typename T, int SL>
 __global__ __launch_bounds__(kJoinThreads) void k_product_join(JoinArgs j) {
-  const int64_t at = (int64_t)blockIdx.x * kJoinThreads + threadIdx.x;
-  if (at >= j.items) return;
-  const int64_t row = at / j.quads;
-  const int col = 4 * (int)(at - row * j.quads);
+  constexpr int Q = kJoinThreads / SL;
+  __shared__ f32x4 sums[SL > 1 ? SL : 1][Q];
+  const int q = threadIdx.x % Q, slice = threadIdx.x / Q;
+  const int64_t at = (int64_t)blockIdx.x * Q + q;
+  const bool live = at < j.items;
+  const int64_t row = live ? at / j.quads : 0;
+  const int col = live ? 4 * (int)(at - row * j.quads) : 0;
   const float* p = j.part + row * j.ld + col;
-  f32x4 v = *(const f32x4*)p;
   const int64_t pitch = j.m * j.ld;
-  for (int i = 1; i < j.parts; i += 8) {             // eight loads in flight
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  for (int i = slice; i < j.parts; i += 8 * SL) {    // eight loads in flight
     f32x4 o[8];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) o[u] = i + u < j.parts ? *(const f32x4*)(p + (i + u) * pitch) : f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int u = 0; u < 8; ++u)
+      o[u] = i + u * SL < j.parts ? *(const f32x4*)(p + (i + u * SL) * pitch) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int u = 0; u < 8; ++u) v += o[u];
   }
-  store_to((T*)j.c + row * j.ldc + col, finish(v, bias4(j.bias, col, j.n), j.relu), j.n - col);
+  if constexpr (SL > 1) {
+    sums[slice][q] = v;
+    __syncthreads();
+    if (slice > 0) return;
+#pragma unroll
+    for (int i = 1; i < SL; ++i) v += sums[i][q];
+  }
+  if (live) store_to((T*)j.c + row * j.ldc + col, finish(v, bias4(j.bias, col, j.n), j.relu), j.n - col);
 }
 
 int64_t tiles_of(int64_t v, int by) { return (v + by - 1) / by; }
 // elements of a row of partial sums over n columns
 int64_t part_ld(int64_t n) { return (n + 3) & ~(int64_t)3; }
+
+// Parts of a sum of `steps` steps over m x n results in `tiles` tiles: as many as
+// fill `room` workgroups, each with `least` steps or more, and no more than balance
+// the steps that a part saves with the partial sums that it writes and reads
+// (`weight`: results that move in the time of a step, both ways).
+inline int64_t parts_of(int64_t tiles, int64_t room, int64_t steps, int64_t least, int64_t m, int64_t n, double weight) {
+  const int64_t balance = (int64_t)std::sqrt((double)steps * weight / ((double)m * (double)n));
+  return std::max<int64_t>(1, std::min({room / tiles, steps / least, std::max<int64_t>(balance, 1)}));
+}
 
 template <class TL, typename T>
 hipError_t sum_product(const SumArgs& a, hipStream_t st) {
@@ -197,8 +222,9 @@ hipError_t join(const float* part, int parts, int64_t m, int64_t n, const float*
                 hipStream_t st) {
   const int64_t ld = part_ld(n), items = m * (ld / 4);
   const JoinArgs a{part, bias, c.p, c.ld, m, items, ld, (int)n, (int)(ld / 4), parts, relu};
-  return enqueue(k_product_join<T>, dim3((unsigned)((items + kJoinThreads - 1) / kJoinThreads)), dim3(kJoinThreads), 0, st,
-                 a);
+  if (parts >= 16 && items <= 65536)
+    return enqueue(k_product_join<T, 16>, dim3((unsigned)tiles_of(items, kJoinThreads / 16)), dim3(kJoinThreads), 0, st, a);
+  return enqueue(k_product_join<T, 1>, dim3((unsigned)tiles_of(items, kJoinThreads)), dim3(kJoinThreads), 0, st, a);
 }
 
 }  // namespace

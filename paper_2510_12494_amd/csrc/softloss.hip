@@ -376,7 +376,7 @@ Pass pass(int64_t m, int64_t n, int64_t depth) {
   p.tm = tiles_of(m, bm);
   p.tn = tiles_of(n, bn);
   const int64_t tiles = p.tm * p.tn, room = sizeof(T) == 4 ? 1024 : p.large ? 256 : 512;
-  const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(room / tiles, p.steps / 4));
+  const int64_t parts = parts_of(tiles, room, p.steps, 4, m, n, sizeof(T) == 4 ? 2e5 : p.large ? 6e5 : 3e5);
   p.per = (int)((p.steps + parts - 1) / parts);
   p.parts = (p.steps + p.per - 1) / p.per;
   return p;
