@@ -369,7 +369,7 @@ Pass pass(int64_t m, int64_t n, int64_t depth) {
   typedef typename Tiles<T>::template Large<true> L;
   typedef typename Tiles<T>::template Small<true> S;
   Pass p;
-  p.large = m > S::BM && n > S::BN;
+  p.large = m > S::BM && n > S::BN && tiles_of(m, L::BM) * tiles_of(n, L::BN) * tiles_of(depth, L::kElements) >= 2048;
   if (sizeof(T) == 4) p.large = tiles_of(m, L::BM) * tiles_of(n, L::BN) >= 1024;
   const int bm = p.large ? L::BM : S::BM, bn = p.large ? L::BN : S::BN;
   p.steps = (int)tiles_of(depth, p.large ? L::kElements : S::kElements);
