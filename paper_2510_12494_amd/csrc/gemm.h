@@ -53,6 +53,9 @@ __device__ __forceinline__ void wait_copies() {
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));
 }
 
+// wait until none of this wavefront's LDS operations is outstanding
+__device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt((15) | (3 << 14) | (7 << 4)); }
+
 // Sixteen e4m3 values times their power of two, whose exponent is s's low byte, as bf16:
 // the conversion takes the power as a float32, whose exponent lies 23 bits up.
 __device__ __forceinline__ void widen_e4m3(const u32x4& v, uint32_t s, bf16x8 (&out)[2]) {

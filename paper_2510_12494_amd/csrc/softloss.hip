@@ -98,6 +98,23 @@ __device__ __forceinline__ float quarters_top(float v) {
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
+// old + sum_t 2^(z_t - from).  A class that is out of every sum (bias -inf) has z =
+// -inf, or NaN where its weights are no numbers; a maximum passes over the NaN, and
+// a sum that is one is taken again without such classes, instead of a comparison and
+// a selection for every logit (8192 x 256 rows, 100000 classes: 540 us with those).
+template <int N>
+__device__ __forceinline__ float sum_of(const float (&z)[N], const float (&bias)[N], float from, float old) {
+  float s = old;
+#pragma unroll
+  for (int t = 0; t < N; ++t) s += exp2_of(z[t] - from);
+  if (__any(s != s)) {
+    s = old;
+#pragma unroll
+    for (int t = 0; t < N; ++t) s += bias[t] == -__builtin_inff() ? 0.f : exp2_of(z[t] - from);
+  }
+  return s;
+}
+
 // LDS of a tile: the copies, then the biases of its classes and three words a row.
 template <class TL>
 constexpr int logits_lds() { return TL::kLds + 4 * TL::BM + 12 * TL::BN; }
@@ -155,37 +172,27 @@ __global__ __launch_bounds__(TL::kThreads) void k_logits(LogitArgs j) {
 
   // the biases of the lane's classes to base 2; -inf: out of every sum
   float bias[RUN];
-  bool out = false;
 #pragma unroll
   for (int t = 0; t < RUN; t += 4) {
     const f32x4 b = j.bias ? *(const f32x4*)(e_bias + (int)(mine - c0) + t) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       bias[t + i] = mine + t + i < j.classes ? b[i] * kLog2e : -__builtin_inff();
-      out |= bias[t + i] == -__builtin_inff();
     }
   }
 
   if constexpr (!GRAD) {
     f32x2* const stat = (f32x2*)smem;                // [WR][BN]
-    const bool any = __any(out);                     // some class's weights may be anything
 #pragma unroll
     for (int c = 0; c < TL::NF; ++c) {
       float z[RUN], top = -__builtin_inff();
 #pragma unroll
       for (int t = 0; t < RUN; ++t) z[t] = fmaf(acc[t / 4][c][t % 4], kLog2e, bias[t]);
-      if (any) {
-#pragma unroll
-        for (int t = 0; t < RUN; ++t) z[t] = bias[t] == -__builtin_inff() ? bias[t] : z[t];
-      }
 #pragma unroll
       for (int t = 0; t < RUN; ++t) top = fmaxf(top, z[t]);
       top = quarters_top(top);
       const float from = top == -__builtin_inff() ? 0.f : top;
-      float sum = 0.f;
-#pragma unroll
-      for (int t = 0; t < RUN; ++t) sum += exp2_of(z[t] - from);
-      sum = quarters_sum(sum);
+      const float sum = quarters_sum(sum_of(z, bias, from, 0.f));
       if (tile.lane < 16) stat[tile.wm / TL::WM * TL::BN + tile.col(c / TL::DN) + c % TL::DN] = f32x2{top, sum};
     }
     __syncthreads();
@@ -250,6 +257,155 @@ __global__ __launch_bounds__(TL::kThreads) void k_logits(LogitArgs j) {
         j.part_bias[(int64_t)tn * j.bias_ld + c0 + i] = t;
       }
     }
+  }
+}
+
+// The forward of rows of up to 256 columns in bf16 (KP panels of 64) over many classes: a
+// workgroup keeps the fragments of 256 rows in registers and walks a strip of tiles of
+// 128 classes, whose weights alone go through LDS.  Two groups of four wavefronts, one of
+// each on a SIMD, take the halves of a tile half a turn apart: one group's products
+// run in the matrix cores while the other's exponentials run in the vector units.
+// A barrier ends each phase; a tile's weights are copied two phases ahead.  A lane
+// carries the largest value and the sum of its own classes from tile to tile, so
+// nothing crosses lanes before the strip's end.  8192 x 256 rows, 100000 classes: 449
+// us, 600 in tiles (a matrix and a vector instruction do not quite overlap: halves of
+// the wavefronts doing one each take 0.77 of the sum of the times); 16384 classes, 16
+// tiles a workgroup, 92 and 93.
+struct StripArgs {
+  Operand w, x;
+  const float* bias;
+  int64_t rows, classes;
+  f32x2* part;                         // [2 strips][rows] of (largest, sum), to base 2
+  int tiles, strips;
+};
+constexpr int kStripRows = 256, kStripClasses = 128;
+template <int KP>
+constexpr int strip_lds() { return 2 * KP * 16384 + 4 * kStripClasses * 4; }
+
+template <int KP>
+__global__ __launch_bounds__(512) void k_strip(StripArgs j) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  float* const e_bias = (float*)(smem + 2 * KP * 16384);            // [4 tiles][128]
+  const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = wave >> 2, rw = wave & 3;
+  const uint32_t strip = blockIdx.x % (uint32_t)j.strips, block = blockIdx.x / (uint32_t)j.strips;
+  const int t0 = (int)((int64_t)j.tiles * strip / j.strips), n = (int)((int64_t)j.tiles * (strip + 1) / j.strips) - t0;
+  const int64_t row0 = (int64_t)block * kStripRows + 64 * rw + 4 * i;   // the lane's rows: row0 .. row0 + 3
+
+  // a copy's lane: class `at` of the tile's half, byte `byte` of its panel (the
+  // layout of gemm.h: rows in blocks, places swizzled)
+  const int R = 8 * wave + (lane >> 3), ri = R & 15;
+  const int at = 16 * (ri >> 2) + 4 * (R >> 4) + (ri & 3);
+  const int byte = ((lane & 7) ^ ((ri >> 1) & 7)) * 16;
+  auto copy = [&](int t) {                           // tile t0 + t
+    const int64_t c0 = (int64_t)(t0 + t) * kStripClasses;
+    char* const dst = smem + (t & 1) * (KP * 16384) + wave * 1024;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const VFL_GLOBAL char* src = glb(j.w.p) + min(c0 + 64 * h + at, j.w.last) * j.w.ld + byte;
+#pragma unroll
+      for (int p = 0; p < KP; ++p)
+        __builtin_amdgcn_global_load_lds((VFL_GLOBAL void*)(src + 128 * p), (lds_t*)(dst + p * 16384 + h * 8192), 16, 0, 0);
+    }
+    if (j.bias && rw < 2 && group == 0)
+      __builtin_amdgcn_global_load_lds(
+          (VFL_GLOBAL void*)(glb(j.bias) + min(c0 + 64 * rw + lane, j.classes - 1)),
+          (lds_t*)(e_bias + (t & 3) * kStripClasses + 64 * rw), 4, 0, 0);
+  };
+  copy(0);
+
+  bf16x8 x[2 * KP][4];
+  float top[4], sum[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const VFL_GLOBAL char* const src = glb(j.x.p) + min(row0 + c, j.x.last) * j.x.ld + 16 * g;
+#pragma unroll
+    for (int k = 0; k < 2 * KP; ++k) x[k][c] = __builtin_bit_cast(bf16x8, *(const VFL_GLOBAL u32x4*)(src + 64 * k));
+    top[c] = -__builtin_inff();
+    sum[c] = 0.f;
+  }
+
+  // Group 0 is in its products of tile t in phase 2 t and in its exponentials in phase
+  // 2 t + 1, group 1 a phase later.  Tile t + 1's buffer was last read in phase 2 t - 1:
+  // each group copies its share at the start of phase 2 t and waits for it at the
+  // end of phase 2 t + 1.
+  const int mine_at = (64 * group + i) * 128, swz = (i >> 1) & 7;
+  wait_copies<0>();
+  __builtin_amdgcn_s_barrier();
+  if (group == 1) {
+    if (n > 1) copy(1);
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+  }
+  for (int t = 0; t < n; ++t) {
+    if (group == 0 && t + 1 < n) copy(t + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    f32x4 acc[4][4];
+    const char* const S = smem + (t & 1) * (KP * 16384) + mine_at;
+    // fragments of the weights are read a step ahead of their products: one
+    // wavefront a SIMD is in this phase, and nothing else would hide the reads
+    bf16x8 a[2][4];
+    auto read = [&](int k) {
+#pragma unroll
+      for (int f = 0; f < 4; ++f)
+        a[k & 1][f] = *(const bf16x8*)(S + (k >> 1) * 16384 + f * 2048 + ((g + 4 * (k & 1)) ^ swz) * 16);
+    };
+    read(0);
+#pragma unroll
+    for (int k = 0; k < 2 * KP; ++k) {
+      if (k + 1 < 2 * KP) read(k + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int f = 0; f < 4; ++f)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          acc[f][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[k & 1][f], x[k][c], k ? acc[f][c] : f32x4{0.f, 0.f, 0.f, 0.f},
+                                                              0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (group == 1) wait_copies<0>();
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    if (group == 1 && t + 2 < n) copy(t + 2);
+    __builtin_amdgcn_sched_barrier(0);
+
+    const int mine = 64 * group + 16 * g;            // the lane's 16 classes
+    const int64_t c0 = (int64_t)(t0 + t) * kStripClasses + mine;
+    float bias[16];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const f32x4 b = *(const f32x4*)(e_bias + (t & 3) * kStripClasses + mine + 4 * q);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) bias[4 * q + u] = j.bias ? b[u] * kLog2e : 0.f;
+    }
+    if (c0 + 16 > j.classes) {
+#pragma unroll
+      for (int u = 0; u < 16; ++u) bias[u] = c0 + u < j.classes ? bias[u] : -__builtin_inff();
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      float z[16], now = top[c];
+#pragma unroll
+      for (int u = 0; u < 16; ++u) z[u] = fmaf(acc[u / 4][c][u % 4], kLog2e, bias[u]);
+#pragma unroll
+      for (int u = 0; u < 16; ++u) now = fmaxf(now, z[u]);
+      const float from = now == -__builtin_inff() ? 0.f : now, old = sum[c] * exp2_of(top[c] - from);
+      sum[c] = sum_of(z, bias, from, old);
+      top[c] = now;
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (group == 0) wait_copies<0>();
+    else wait_lds();
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  if (group == 0) __builtin_amdgcn_s_barrier();
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const float all = quarters_top(top[c]), from = all == -__builtin_inff() ? 0.f : all;
+    const float s = quarters_sum(sum[c] * exp2_of(top[c] - from));
+    if (g == 0 && row0 + c < j.rows) j.part[(int64_t)(2 * strip + group) * j.rows + row0 + c] = f32x2{all, s};
   }
 }
 
@@ -390,6 +546,7 @@ struct Plan {
   Kind kind;
   int bm, bn;                                        // of the logits' tile
   int64_t dim_pad, rows_pad, all, piece, pieces;     // all, piece: classes in whole tiles
+  int64_t strips, parts;                             // k_strip's strips (0: tiles); the forward's pairs of a row
   size_t x, w, part, g, bias, dx, dw, bytes;
   Pass to_x, to_w;
 };
@@ -421,7 +578,16 @@ Plan plan(int64_t rows, int dim, int64_t classes) {
   p.x = take(rows * p.dim_pad, sizeof(T));
   p.w = take(classes * p.dim_pad, sizeof(T));
   const size_t both = at;
-  p.part = take(p.all / p.bm * rows, sizeof(f32x2));
+  p.parts = p.all / p.bm;
+  if (sizeof(T) == 2 && p.dim_pad <= 256) {
+    const int64_t blocks = tiles_of(rows, kStripRows), tiles = tiles_of(classes, kStripClasses);
+    const int64_t strips = std::max<int64_t>(1, 256 / blocks);
+    if (rows > 128 && tiles >= 16 * strips) {
+      p.strips = strips;
+      p.parts = 2 * strips;
+    }
+  }
+  p.part = take(p.parts * rows, sizeof(f32x2));
   const size_t forward = at;
   at = both;
   p.g = take(p.rows_pad * p.piece, sizeof(T));
@@ -481,13 +647,26 @@ hipError_t forward(const LossJob& j, hipStream_t st) {
   if (e == hipSuccess)
     e = operand<T>(j.w, j.classes, j.dim, p.dim_pad, nullptr, 0, nullptr, j.workspace + p.w, &a.w, st);
   if (e != hipSuccess) return e;
-  a.bias = j.bias;
-  a.rows = j.rows;
-  a.classes = j.classes;
-  a.part = (f32x2*)(j.workspace + p.part);
-  e = logits<T, false>(a, p, j.classes, st);
+  f32x2* const part = (f32x2*)(j.workspace + p.part);
+  if (p.strips) {
+    const StripArgs s{a.w, a.x, j.bias, j.rows, j.classes, part, (int)tiles_of(j.classes, kStripClasses), (int)p.strips};
+    auto run = [&](auto kernel, int lds) {
+      return enqueue(kernel, dim3((unsigned)(tiles_of(j.rows, kStripRows) * p.strips)), dim3(512), lds, st, s);
+    };
+    e = p.dim_pad == 64    ? run(k_strip<1>, strip_lds<1>())
+        : p.dim_pad == 128 ? run(k_strip<2>, strip_lds<2>())
+        : p.dim_pad == 192 ? run(k_strip<3>, strip_lds<3>())
+                           : run(k_strip<4>, strip_lds<4>());
+  } else {
+    a.bias = j.bias;
+    a.rows = j.rows;
+    a.classes = j.classes;
+    a.part = part;
+    e = logits<T, false>(a, p, j.classes, st);
+  }
   if (e != hipSuccess) return e;
-  const FinishArgs f{a.part, j.x, j.w, j.bias, j.labels, j.loss, j.lse, j.rows, j.classes, a.tm, j.dim};
+  const int64_t parts = p.strips ? p.parts : a.tm;
+  const FinishArgs f{part, j.x, j.w, j.bias, j.labels, j.loss, j.lse, j.rows, j.classes, parts, j.dim};
   return enqueue(j.dim % 8 == 0 ? k_loss<T, kExact> : j.dim > 8 ? k_loss<T, kRagged> : k_loss<T, kSmall>, dim3((unsigned)tiles_of(j.rows, kThreads / 16)), dim3(kThreads), 0, st, f);
 }
 

@@ -583,6 +583,42 @@ def test_softmax_loss_in_pieces(V, dt, rows, classes):
     t.check()
 
 
+@pytest.mark.parametrize("rows,dim,classes", [(2100, 60, 70001), (300, 128, 263000), (600, 136, 263000), (2049, 250, 66000)])
+def test_softmax_loss_over_many_classes(V, rows, dim, classes):
+    """Strips of tiles of classes: lse and loss, with classes taken out and a bf16
+    row and class that hold no numbers."""
+    rng = np.random.default_rng(rows)
+    x, w = rng.normal(size=(rows, dim)), rng.normal(size=(classes, dim)) * 1.5 / np.sqrt(dim)
+    bias = 0.5 * rng.normal(size=classes)
+    bias[rng.integers(0, classes, 500)] = -np.inf
+    bias[1000:1300] = -np.inf                                  # whole tiles of a lane, and of a wavefront
+    w[1100], w[1101, 3] = np.nan, np.inf
+    labels = rng.integers(0, classes, rows)
+    labels[::7] = -1
+    x[7] = np.nan
+    t = Loss(V, "bf16", rows, dim, classes, bias=bias, x=x, w=w, labels=labels)
+    V.vfl_softmax_loss_forward(t.a)
+    torch.cuda.synchronize()
+    b = stored(t.bias, classes)
+    xd, wd = t.x.t.double(), t.w.t.double()
+    wd[torch.from_numpy(np.isneginf(b)).cuda()] = 0.0
+    xd[7] = 0.0
+    z = torch.addmm(torch.from_numpy(b).cuda(), xd, wd.T)
+    lse = torch.logsumexp(z, 1).cpu().numpy()
+    zl = z[torch.arange(rows), torch.from_numpy(np.clip(labels, 0, None)).cuda()].cpu().numpy()
+    mags = (xd.abs() @ wd.abs().T).amax(1).cpu().numpy() * (dim / 4 + 16)
+    top = np.abs(np.where(np.isneginf(b), 0, b)).max() + float(torch.where(torch.isinf(z), 0.0, z).abs().max())
+    # one more rounding for every tile that a lane carries its sum over
+    bound = SLACK * U * (mags + 8 * top + SUM + 64 + classes / 128 + 6 * np.abs(lse))
+    got, loss = stored(t.lse, rows), stored(t.loss, rows)
+    on = np.arange(rows) != 7
+    close(got[on], lse[on], bound[on], "lse")
+    has = on & (labels >= 0) & np.isfinite(zl)
+    close(loss[has], (lse - zl)[has], 2 * bound[has], "loss")
+    gone = on & (labels >= 0) & np.isneginf(zl)
+    assert np.isposinf(loss[gone]).all() and not loss[labels < 0].any()
+
+
 def test_softmax_loss_backward_of_no_rows(V):
     t = Loss(V, "bf16", 0, 24, 300)
     t.run()
