@@ -132,7 +132,7 @@ def test_workspaces_that_are_too_small(V):
     a.rows = 100_000
     sizes = {"vfl_rmsnorm_backward": (a, V.vfl_norm_workspace_size(a.rows, a.cols))}
     a = _args(V, "vfl_matmul8")
-    a.k = 100_000
+    a.m, a.k = 100, 100_000                   # a sum that is cut into parts
     a.a.ld = a.b.ld = 0
     sizes["vfl_matmul8"] = (a, V.vfl_matmul8_workspace_size(a.m, a.n, a.k))
     for call in ("vfl_softmax_loss_forward", "vfl_softmax_loss_backward"):
@@ -167,3 +167,22 @@ def test_workspace_sizes_check_their_sizes(V):
             V.vfl_softmax_loss_workspace_size(*bad)
     assert V.vfl_matmul8_workspace_size(0, 8, 8) == 0
     assert V.vfl_softmax_loss_workspace_size(0, 0, 8, 8) == 0
+
+
+def test_workspaces_of_extreme_sizes(V):
+    """The plans' own arithmetic at the limits, and sizes that grow with the problem."""
+    w = V.vfl_softmax_loss_workspace_size
+    for dt in (V.VFL_F32, V.VFL_BF16):
+        for rows, dim, classes in ((1, 1, 1), (1, 1, 2**21), (2**21, 1, 1), (2**21, 32768, 2**16), (2**16, 32768, 2**21),
+                                   (1, 32768, 2**21), (2**21, 32768, 1), (64, 250, 100_000), (8192, 256, 100_000)):
+            size = w(dt, rows, dim, classes)
+            # the operands' copies and a piece of G are in it, and no whole G of the large ones
+            e = 4 if dt == V.VFL_F32 else 2
+            assert size >= (rows + classes) * dim * e
+            pairs = rows * max(classes // 64 + 2, 512) * 8                   # the forward's
+            piece = max(256 << 20, rows * 512 * e + (1 << 20)) * 1.01 + 2**20
+            sums = (64 * rows + 128 * 2**20 // max(dim, 1) + classes * 66) * (dim + 256) * 4
+            assert size <= 2 * ((rows + classes) * (dim + 64) * e) + pairs + piece + sums + 2**30
+    m = V.vfl_matmul8_workspace_size
+    assert m(2**30, 2**8, 2**23) == m(1, 2**30, 2**23) == m(16, 2**30, 1) == 0
+    assert 0 < m(128, 128, 2**23) <= 512 * 128 * 128 * 4
