@@ -40,7 +40,7 @@ Mat8 eight(Checks& c, const vfl_q8& m, int64_t rows, int64_t cols, bool required
   const int64_t long_ = round_up(rows, 16), sld = m.scale_ld == 0 ? long_ : m.scale_ld;
   if ((uintptr_t)m.data % 16 != 0 || ld % kBlock8 != 0 || ld < wide || ld > kMaxExtent / std::max<int64_t>(rows, 1) ||
       !m.scale || (uintptr_t)m.scale % 16 != 0 || sld % 16 != 0 || sld < long_ ||
-      sld > kMaxExtent / (wide / kBlock8)) {
+      sld > kMaxExtent / std::max<int64_t>(wide / kBlock8, 1)) {
     c.why = what;
     return out;
   }

@@ -158,6 +158,14 @@ def test_no_rows_enqueue_nothing(V, call):
     assert V.vfl_last_error(None) == ""
 
 
+def test_no_rows_with_outputs_present(V):
+    """A transpose of no rows has no blocks."""
+    a = _args(V, "vfl_quantize")
+    a.rows = 0
+    V.vfl_quantize(a)
+    assert V.vfl_last_error(None) == ""
+
+
 def test_workspace_sizes_check_their_sizes(V):
     for bad in ((-1, 1, 1), (1, -1, 1), (1, 1, 0), (2**31, 1, 1), (2**25, 2**25, 1), (1, 1, 2**24)):
         with pytest.raises(V.VflError):
