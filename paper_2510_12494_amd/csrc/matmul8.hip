@@ -139,7 +139,13 @@ Cut cut(Elt e, int64_t m, int64_t n, int64_t k) {
     c.parts = 1;
     return c;
   }
-  c.large = e == BF16 && tiles_of(m, 256) * tiles_of(n, 256) >= 192;
+// rounds of workgroups, a large tile's a CU each and a small one's two: a step of a
+  // round of large ones takes 1.4 to 1.85 us, of small ones 1.0 (large and small,
+  // us: 8192 x 8192 x 4096 237, 287; 2944 cubed 41, 47; 20000 x 1024 x 1024 36.3,
+  // 36.6; 1024 x 8192 x 8192 89, 64; 4096 x 2048 x 1024 19.8, 15.8)
+  const int64_t large = tiles_of(tiles_of(m, 256) * tiles_of(n, 256), 256);
+  const int64_t small = tiles_of(tiles_of(m, 128) * tiles_of(n, 128), 512);
+  c.large = e == BF16 && 8 * large < 5 * small;
   const int by = c.large ? 256 : 128;
   c.tm = tiles_of(m, by);
   c.tn = tiles_of(n, by);

@@ -214,26 +214,31 @@ __global__ __launch_bounds__(kThreads) void k_quantize(QuantArgs j) {
         for (int c = 0; c < 8; ++c) v[i][c] = 0.f;
       }
     }
+    // the rows' and the thread's largest magnitudes; what is no number shows in them
+    uint32_t top[8], most = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      top[i] = chunk_max(v[i]);
+      most = max(most, top[i]);
+    }
+    if (__any(most >= kInfinite)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        top[i] = 0;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          top[i] = max(top[i], number_magnitude(v[i][c]));
+          v[i][c] = number_or_nan(v[i][c]);
+        }
+      }
+    }
     if (j.q.p) {
       u32x2 bytes = {0u, 0u};
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        uint32_t m = block_max(chunk_max(v[i]));
-        float w[8];
-#pragma unroll
-        for (int c = 0; c < 8; ++c) w[c] = v[i][c];
-        if (m >= kInfinite) {
-          m = 0;
-#pragma unroll
-          for (int c = 0; c < 8; ++c) {
-            m = max(m, number_magnitude(w[c]));
-            w[c] = number_or_nan(w[c]);
-          }
-          m = block_max(m);
-        }
-        const uint32_t b = scale_byte(m);
+        const uint32_t b = scale_byte(block_max(top[i]));
         bytes[i / 4] |= b << (8 * (i % 4));
-        if (r0 + i < j.rows) *(u32x2*)(j.q.p + (r0 + i) * j.q.ld + 8 * (int64_t)q) = pack_e4m3(w, inverse_scale(b));
+        if (r0 + i < j.rows) *(u32x2*)(j.q.p + (r0 + i) * j.q.ld + 8 * (int64_t)q) = pack_e4m3(v[i], inverse_scale(b));
       }
       if (lane == 0 && r0 < j.rows) *(u32x2*)(j.q.scale + tn * j.q.scale_ld + r0) = bytes;
     }
@@ -242,8 +247,13 @@ __global__ __launch_bounds__(kThreads) void k_quantize(QuantArgs j) {
 #pragma unroll
       for (int c = 0; c < 8; ++c) {
         m[c] = 0;
+        if (most < kInfinite) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m[c] = max(m[c], number_magnitude(v[i][c]));
+          for (int i = 0; i < 8; ++i) m[c] = max(m[c], magnitude(v[i][c]));
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) m[c] = max(m[c], number_magnitude(v[i][c]));
+        }
         m[c] = quarters_max(m[c]);
       }
       if ((threadIdx.x & 63) < 16) {
@@ -268,7 +278,7 @@ __global__ __launch_bounds__(kThreads) void k_quantize(QuantArgs j) {
       for (int c = 0; c < 8; ++c) {
         float w[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = number_or_nan(v[i][c]);
+        for (int i = 0; i < 8; ++i) w[i] = v[i][c];
         const uint32_t b = (bytes[c / 4] >> (8 * (c % 4))) & 255u;
         const int64_t col = 8 * (int64_t)q + c;
         if (col < j.cols) *(u32x2*)(j.qt.p + col * j.qt.ld + r0) = pack_e4m3(w, inverse_scale(b));
