@@ -114,15 +114,6 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_rows(RowsArgs j) {
   }
 }
 
-// How a product is cut up: its tile and the parts of its sum.
-struct Cut {
-  int rows;                            // 16s of rows that k_rows takes, 0: tiles
-  bool large;
-  int64_t tm, tn;
-  int steps, parts, per;
-};
-
-
 // Products that k_rows takes: of few rows, and those of few workgroups and steps, to
 // which a tile's start and the joining of parts would come dearer (us, k_rows and
 // tiles, bf16: 64 x 1024 x 1024 7.1, 11.0; 256 x 1024 x 1024 6.9, 11.8; 1024 x 1024 x
@@ -130,30 +121,21 @@ struct Cut {
 // 32 x 8192 x 8192 24.6, 23.3; and where the tiles are many: 32768 x 64 x 500 15.8, 9.6).
 constexpr int kRowSteps = 32, kRowWork = 8192;
 
-Cut cut(Elt e, int64_t m, int64_t n, int64_t k) {
-  Cut c{};
-  c.steps = (int)((k + kBlock8 - 1) / kBlock8);
-  if (m <= 16 || (c.steps <= kRowSteps && tiles_of(m, 64) * tiles_of(n, 16) * c.steps <= kRowWork &&
-                  tiles_of(m, 128) * tiles_of(n, 128) < 128)) {
-    c.rows = m <= 16 ? 1 : m <= 32 ? 2 : 4;
-    c.parts = 1;
-    return c;
-  }
-// rounds of workgroups, a large tile's a CU each and a small one's two: a step of a
-  // round of large ones takes 1.4 to 1.85 us, of small ones 1.0 (large and small,
-  // us: 8192 x 8192 x 4096 237, 287; 2944 cubed 41, 47; 20000 x 1024 x 1024 36.3,
-  // 36.6; 1024 x 8192 x 8192 89, 64; 4096 x 2048 x 1024 19.8, 15.8)
-  const int64_t large = tiles_of(tiles_of(m, 256) * tiles_of(n, 256), 256);
-  const int64_t small = tiles_of(tiles_of(m, 128) * tiles_of(n, 128), 512);
-  c.large = e == BF16 && 8 * large < 5 * small;
-  const int by = c.large ? 256 : 128;
-  c.tm = tiles_of(m, by);
-  c.tn = tiles_of(n, by);
-  const int64_t all = c.tm * c.tn;
-  const int64_t parts = all < 256 ? parts_of(all, 512, c.steps, 4, m, n, 5e5) : 1;
-  c.per = (int)((c.steps + parts - 1) / parts);
-  c.parts = (c.steps + c.per - 1) / c.per;
-  return c;
+enum Kind { kRowsOne, kRowsTwo, kRowsFour, kLargeTile, kSmallTile };
+struct Choice : Cut { Kind kind; };
+
+// Steps timed over 8192 x 8192 x 4096.  The two kinds of tile, us: 8192 x 8192 x 4096
+// 237 large, 287 small; 2944 cubed 41, 47; 1024 x 8192 x 8192 89, 64; 4096 x 2048 x 1024
+// 19.8, 15.8.
+Choice choose(Elt e, int64_t m, int64_t n, int64_t k) {
+  const int steps = (int)tiles_of(k, kBlock8);
+  if (m <= 16 || (steps <= kRowSteps && tiles_of(m, 64) * tiles_of(n, 16) * steps <= kRowWork &&
+                  tiles_of(m, 128) * tiles_of(n, 128) < 128))
+    return {Cut{0, 0, steps, 1, steps, 0.0}, m <= 16 ? kRowsOne : m <= 32 ? kRowsTwo : kRowsFour};
+  const Cut small = cut_up(m, n, 128, 128, steps, e == F32 ? StepTime{0.98, 1.2, 2} : StepTime{0.5, 0.75, 2});
+  if (e == F32) return {small, kSmallTile};
+  const Cut large = cut_up(m, n, 256, 256, steps, StepTime{1.75, 1.75, 1});
+  return large.us < small.us ? Choice{large, kLargeTile} : Choice{small, kSmallTile};
 }
 
 Operand operand(const Mat8& m, int64_t rows) {
@@ -161,7 +143,7 @@ Operand operand(const Mat8& m, int64_t rows) {
 }
 
 template <class TL, typename T>
-hipError_t matmul8(const Matmul8Job& j, const Cut& c, hipStream_t st) {
+hipError_t tiles8(const Matmul8Job& j, const Cut& c, hipStream_t st) {
   ProductArgs a{};
   a.a = operand(j.a, j.m);
   a.b = operand(j.b, j.n);
@@ -185,11 +167,24 @@ hipError_t matmul8(const Matmul8Job& j, const Cut& c, hipStream_t st) {
   return e != hipSuccess ? e : join<T>(j.part, c.parts, j.m, j.n, j.bias, j.relu, j.c, st);
 }
 
-template <Type TY, typename T>
+template <Type TY, int MT, typename T>
 hipError_t rows8(const Matmul8Job& j, const Cut& c, hipStream_t st) {
   const RowsArgs a{operand(j.a, j.m), operand(j.b, j.n), j.c.p, j.c.ld, j.bias, (int)j.m, (int)j.n, c.steps, j.relu};
-  return enqueue(c.rows == 1 ? k_rows<TY, 1, T> : c.rows == 2 ? k_rows<TY, 2, T> : k_rows<TY, 4, T>,
-                 dim3((unsigned)tiles_of(j.n, 16), (unsigned)tiles_of(j.m, 16 * c.rows)), dim3(64 * kRowWaves), 0, st, a);
+  return enqueue(k_rows<TY, MT, T>, dim3((unsigned)tiles_of(j.n, 16), (unsigned)tiles_of(j.m, 16 * MT)),
+                 dim3(64 * kRowWaves), 0, st, a);
+}
+
+template <Type TY, class SMALL, typename T>
+hipError_t matmul8(const Matmul8Job& j, const Choice& c, hipStream_t st) {
+  switch (c.kind) {
+    case kRowsOne: return rows8<TY, 1, T>(j, c, st);
+    case kRowsTwo: return rows8<TY, 2, T>(j, c, st);
+    case kRowsFour: return rows8<TY, 4, T>(j, c, st);
+    case kLargeTile:
+      if constexpr (TY == kE4m3) return tiles8<Large, T>(j, c, st);
+      [[fallthrough]];
+    default: return tiles8<SMALL, T>(j, c, st);
+  }
 }
 
 }  // namespace
@@ -197,17 +192,15 @@ hipError_t rows8(const Matmul8Job& j, const Cut& c, hipStream_t st) {
 size_t matmul8_workspace(int64_t m, int64_t n, int64_t k) {
   size_t most = 0;
   for (Elt e : {F32, BF16}) {
-    const Cut c = cut(e, m, n, k);
+    const Cut c = choose(e, m, n, k);
     if (c.parts > 1) most = std::max(most, (size_t)c.parts * (size_t)m * (size_t)part_ld(n) * sizeof(float));
   }
   return most;
 }
 
 hipError_t launch_matmul8(Elt e, const Matmul8Job& j, hipStream_t st) {
-  const Cut c = cut(e, j.m, j.n, j.k);
-  if (c.rows) return e == F32 ? rows8<kE4m3Wide, float>(j, c, st) : rows8<kE4m3, uint16_t>(j, c, st);
-  if (e == F32) return matmul8<Wide, float>(j, c, st);
-  return c.large ? matmul8<Large, uint16_t>(j, c, st) : matmul8<Small, uint16_t>(j, c, st);
+  const Choice c = choose(e, j.m, j.n, j.k);
+  return e == F32 ? matmul8<kE4m3Wide, Wide, float>(j, c, st) : matmul8<kE4m3, Small, uint16_t>(j, c, st);
 }
 
 }  // namespace vfl

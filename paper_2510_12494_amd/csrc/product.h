@@ -2,7 +2,6 @@
 // sum cut into parts where there are few tiles, the parts joined in order.
 #pragma once
 #include <algorithm>
-#include <cmath>
 
 #include "gemm.h"
 #include "rowchunk.h"
@@ -197,13 +196,36 @@ int64_t tiles_of(int64_t v, int by) { return (v + by - 1) / by; }
 // elements of a row of partial sums over n columns
 int64_t part_ld(int64_t n) { return (n + 3) & ~(int64_t)3; }
 
-// Parts of a sum of `steps` steps over m x n results in `tiles` tiles: as many as
-// fill `room` workgroups, each with `least` steps or more, and no more than balance
-// the steps that a part saves with the partial sums that it writes and reads
-// (`weight`: results that move in the time of a step, both ways).
-inline int64_t parts_of(int64_t tiles, int64_t room, int64_t steps, int64_t least, int64_t m, int64_t n, double weight) {
-  const int64_t balance = (int64_t)std::sqrt((double)steps * weight / ((double)m * (double)n));
-  return std::max<int64_t>(1, std::min({room / tiles, steps / least, std::max<int64_t>(balance, 1)}));
+// What the steps of a kind of tile take, us: a step's share of a CU that is full, a
+// step of a workgroup that has a CU to itself, and the workgroups that a CU holds.
+struct StepTime { double share, alone; int room; };
+
+// How a product is cut up: its tiles, the parts of its sum, and what that should take.
+struct Cut {
+  int64_t tm, tn;
+  int steps, parts, per;
+  double us;
+};
+
+// A product of m x n results over `steps` steps in tiles of bm x bn: the number of parts
+// (of four steps or more) that should take the least time, full rounds of workgroups
+// and a last one, 2 us to start and end each, and for more than one part the partial
+// sums that are written and read, at a copy's rate, and a launch.
+inline Cut cut_up(int64_t m, int64_t n, int bm, int bn, int steps, const StepTime& t) {
+  Cut c{tiles_of(m, bm), tiles_of(n, bn), steps, 1, steps, 0.0};
+  const int64_t tiles = c.tm * c.tn, round = 256 * t.room;
+  const int most = (int)std::min<int64_t>(std::max<int64_t>(1, 4 * round / tiles), std::max(1, steps / 4));
+  for (int parts = 1; parts <= most; parts += parts < 16 ? 1 : parts / 8) {
+    const int64_t full = tiles * parts / round, rest = tiles * parts % round;
+    const double step = (double)full * std::max(t.room * t.share, t.alone) +
+                        (rest ? std::max((double)tiles_of(rest, 256) * t.share, t.alone) : 0.0);
+    const double us = (double)tiles_of(steps, parts) * step + 2.0 * (double)(full + (rest > 0)) +
+                      (parts > 1 ? 4.0 + (double)parts * (double)m * (double)n * (8.0 / 5e6) : 0.0);
+    if (parts == 1 || us < c.us) c.us = us, c.parts = parts;
+  }
+  c.per = (int)tiles_of(steps, c.parts);
+  c.parts = (int)tiles_of(steps, c.per);
+  return c;
 }
 
 template <class TL, typename T>
