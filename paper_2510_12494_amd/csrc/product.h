@@ -104,12 +104,27 @@ struct SumArgs {
   void* c;
   int64_t ldc, n;
   uint32_t tm, tn, parts;
-  int m, steps, per, add;
+  int m, steps, per, add, wide;        // wide: results in float32 whatever T
 };
+template <typename T>
+__device__ __forceinline__ void store_sums(T* out, float (&v)[8], int left, int add) {
+  if (left >= 8) {
+    if (add) {
+      float o[8];
+      unpack(load_at(out), o);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += o[i];
+    }
+    store8<false>(out, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 7; ++i)
+      if (i < left) st1<T>(out + i, add ? v[i] + ld1<T>(out + i) : v[i]);
+  }
+}
 template <class TL, typename T>
-__global__ __launch_bounds__(TL::kThreads) void k_sum_product(SumArgs j) {
-  extern __shared__ __attribute__((aligned(1024))) char smem[];
-  const Place at = place_of(blockIdx.x, j.tm, j.tn, j.parts);
+__device__ __forceinline__ void sum_tile(const SumArgs& j, uint32_t block, char* smem) {
+  const Place at = place_of(block, j.tm, j.tn, j.parts);
   const TL tile;
   typename TL::Acc acc;
 #pragma unroll
@@ -124,30 +139,32 @@ __global__ __launch_bounds__(TL::kThreads) void k_sum_product(SumArgs j) {
   for (int f = 0; f < TL::NF; ++f) {
     const int64_t row = n0 + tile.b_col(f);
     if (row >= j.n) continue;
-    T* const out = (T*)j.c + ((int64_t)at.part * j.n + row) * j.ldc;
+    const int64_t out = ((int64_t)at.part * j.n + row) * j.ldc;
 #pragma unroll
     for (int q = 0; q < TL::MF / TL::D; ++q)
 #pragma unroll
       for (int d = 0; d < TL::D; d += 2) {
-        const int col = m0 + tile.a_col(q) + 4 * d, left = j.m - col;
+        const int col = m0 + tile.a_col(q) + 4 * d;
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = acc[q * TL::D + d + i / 4][f][i % 4];
-        if (left >= 8) {
-          if (j.add) {
-            float o[8];
-            unpack(load_at(out + col), o);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += o[i];
-          }
-          store8<false>(out + col, v);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 7; ++i)
-            if (i < left) st1<T>(out + col + i, j.add ? v[i] + ld1<T>(out + col + i) : v[i]);
-        }
+        if (sizeof(T) == 4 || j.wide) store_sums((float*)j.c + out + col, v, j.m - col, j.add);
+        else store_sums((T*)j.c + out + col, v, j.m - col, j.add);
       }
   }
+}
+template <class TL, typename T>
+__global__ __launch_bounds__(TL::kThreads) void k_sum_product(SumArgs j) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  sum_tile<TL, T>(j, blockIdx.x, smem);
+}
+// Two products in one launch: the first `split` workgroups take the first one.
+template <class TA, class TB, typename T>
+__global__ __launch_bounds__(TA::kThreads) void k_sum_pair(SumArgs a, SumArgs b, uint32_t split) {
+  static_assert(TA::kThreads == TB::kThreads && TA::kLds == TB::kLds);
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  if (blockIdx.x < split) sum_tile<TA, T>(a, blockIdx.x, smem);
+  else sum_tile<TB, T>(b, blockIdx.x - split, smem);
 }
 
 constexpr int kJoinThreads = 256;
@@ -163,11 +180,11 @@ struct JoinArgs {
 // part of the same four columns each and meet in LDS (many parts of few results: one
 // row of 256 columns in 512 parts 15 us with a thread for all parts).
 template <typename T, int SL>
-__global__ __launch_bounds__(kJoinThreads) void k_product_join(JoinArgs j) {
+__device__ __forceinline__ void join_block(const JoinArgs& j, uint32_t block) {
   constexpr int Q = kJoinThreads / SL;
   __shared__ f32x4 sums[SL > 1 ? SL : 1][Q];
   const int q = threadIdx.x % Q, slice = threadIdx.x / Q;
-  const int64_t at = (int64_t)blockIdx.x * Q + q;
+  const int64_t at = (int64_t)block * Q + q;
   const bool live = at < j.items;
   const int64_t row = live ? at / j.quads : 0;
   const int col = live ? 4 * (int)(at - row * j.quads) : 0;
@@ -190,6 +207,11 @@ __global__ __launch_bounds__(kJoinThreads) void k_product_join(JoinArgs j) {
     for (int i = 1; i < SL; ++i) v += sums[i][q];
   }
   if (live) store_to((T*)j.c + row * j.ldc + col, finish(v, bias4(j.bias, col, j.n), j.relu), j.n - col);
+}
+
+template <typename T, int SL>
+__global__ __launch_bounds__(kJoinThreads) void k_product_join(JoinArgs j) {
+  join_block<T, SL>(j, blockIdx.x);
 }
 
 int64_t tiles_of(int64_t v, int by) { return (v + by - 1) / by; }
@@ -239,14 +261,18 @@ hipError_t product(const ProductArgs& a, hipStream_t st) {
 }
 
 // parts [parts][m][part_ld(n)] -> c
+JoinArgs join_args(const float* part, int parts, int64_t m, int64_t n, const float* bias, int relu, const Mat& c) {
+  const int64_t ld = part_ld(n), items = m * (ld / 4);
+  return {part, bias, c.p, c.ld, m, items, ld, (int)n, (int)(ld / 4), parts, relu};
+}
+bool joins_in_slices(const JoinArgs& a) { return a.parts >= 16 && a.items <= 65536; }
+int64_t join_blocks(const JoinArgs& a) { return tiles_of(a.items, joins_in_slices(a) ? kJoinThreads / 16 : kJoinThreads); }
 template <typename T>
 hipError_t join(const float* part, int parts, int64_t m, int64_t n, const float* bias, int relu, const Mat& c,
                 hipStream_t st) {
-  const int64_t ld = part_ld(n), items = m * (ld / 4);
-  const JoinArgs a{part, bias, c.p, c.ld, m, items, ld, (int)n, (int)(ld / 4), parts, relu};
-  if (parts >= 16 && items <= 65536)
-    return enqueue(k_product_join<T, 16>, dim3((unsigned)tiles_of(items, kJoinThreads / 16)), dim3(kJoinThreads), 0, st, a);
-  return enqueue(k_product_join<T, 1>, dim3((unsigned)tiles_of(items, kJoinThreads)), dim3(kJoinThreads), 0, st, a);
+  const JoinArgs a = join_args(part, parts, m, n, bias, relu, c);
+  return enqueue(joins_in_slices(a) ? k_product_join<T, 16> : k_product_join<T, 1>, dim3((unsigned)join_blocks(a)),
+                 dim3(kJoinThreads), 0, st, a);
 }
 
 }  // namespace

@@ -45,11 +45,11 @@ struct CopyArgs {
 // as zeros: eight columns a thread.
 constexpr int kPadGrid = 16384;
 template <typename T, Form F>
-__global__ __launch_bounds__(kThreads) void k_pad(CopyArgs j) {
+__device__ __forceinline__ void pad(const CopyArgs& j, uint32_t block) {
   const Cols k(j.cols, j.rows);
   const int per = (int)(j.dst_ld / 8);
   const int64_t chunks = j.rows * per;
-  for (int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x; at < chunks; at += (int64_t)kPadGrid * kThreads) {
+  for (int64_t at = (int64_t)block * kThreads + threadIdx.x; at < chunks; at += (int64_t)kPadGrid * kThreads) {
     const int64_t r = at / per;
     const int q = (int)(at - r * per);
     const bool edge = r >= k.edge;
@@ -63,6 +63,12 @@ __global__ __launch_bounds__(kThreads) void k_pad(CopyArgs j) {
     }
     store8<false>((T*)j.dst + r * j.dst_ld + 8 * q, v);
   }
+}
+// two matrices of as many columns: the first `split` workgroups take the first one
+template <typename T, Form F>
+__global__ __launch_bounds__(kThreads) void k_pad(CopyArgs a, CopyArgs b, uint32_t split) {
+  if (blockIdx.x < split) pad<T, F>(a, blockIdx.x);
+  else pad<T, F>(b, blockIdx.x - split);
 }
 
 // -------------------------------------------------------------------- logits
@@ -474,14 +480,36 @@ __global__ __launch_bounds__(kThreads) void k_zero(CopyArgs j) {
     for (int c = threadIdx.x; c < j.cols; c += kThreads) ((T*)j.dst)[r * j.dst_ld + c] = (T)0;
 }
 
+// What is summed at a backward pass's end, in one launch: the parts of dx, the parts
+// of dw, and dbias over the tiles' rows, as many workgroups as each has.
 struct BiasArgs { const float* part; float* dbias; int64_t ld, n; int parts; };
-__global__ __launch_bounds__(kThreads) void k_bias(BiasArgs j) {
-  const int64_t c = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+__device__ __forceinline__ void bias_block(const BiasArgs& j, uint32_t block) {
+  const int64_t c = (int64_t)block * kThreads + threadIdx.x;
   if (c >= j.n) return;
   float t = 0.f;
 #pragma unroll 8
   for (int i = 0; i < j.parts; ++i) t += j.part[i * j.ld + c];
   j.dbias[c] = t;
+}
+struct EndArgs {
+  JoinArgs x, w;
+  BiasArgs b;
+  uint32_t nx, nw;                     // workgroups of x and of w
+  int x_slices, w_slices;
+};
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_loss_end(EndArgs j) {
+  static_assert(kThreads == kJoinThreads);
+  const uint32_t b = blockIdx.x;
+  if (b < j.nx) {
+    if (j.x_slices) join_block<T, 16>(j.x, b);
+    else join_block<T, 1>(j.x, b);
+  } else if (b < j.nx + j.nw) {
+    if (j.w_slices) join_block<T, 16>(j.w, b - j.nx);
+    else join_block<T, 1>(j.w, b - j.nx);
+  } else {
+    bias_block(j.b, b - j.nx - j.nw);
+  }
 }
 
 // ---------------------------------------------------------------------- plan
@@ -589,20 +617,38 @@ Plan plan(int64_t rows, int dim, int64_t classes) {
   return p;
 }
 
-// An operand of whole steps whose rows can be copied 16 bytes at a time: the matrix
-// itself where it is one and all its rows may be read, else a copy.
+// Operands of whole steps whose rows can be copied 16 bytes at a time: the matrices
+// themselves where they are that and all their rows may be read, else copies.
 template <typename T>
-hipError_t operand(const Mat& m, int64_t rows, int dim, int64_t dim_pad, const int32_t* labels, int64_t classes,
-                   const float* bias, char* copy, Operand* out, hipStream_t st) {
-  *out = {(const char*)m.p, m.ld * (int64_t)sizeof(T), rows - 1, nullptr, 0};
-  if (!labels && !bias && dim == dim_pad && (uintptr_t)m.p % 16 == 0 && out->ld % 16 == 0 && out->ld < (int64_t)1 << 24)
-    return hipSuccess;
-  out->p = copy;
-  out->ld = dim_pad * (int64_t)sizeof(T);
-  const CopyArgs a{m, copy, dim_pad, rows, labels, bias, classes, dim};
-  const int64_t blocks = std::min<int64_t>((rows * dim_pad / 8 + kThreads - 1) / kThreads, kPadGrid);
-  return enqueue(dim % 8 == 0 && dim == dim_pad ? k_pad<T, kExact> : dim >= 8 ? k_pad<T, kRagged> : k_pad<T, kSmall>,
-                 dim3((unsigned)blocks), dim3(kThreads), 0, st, a);
+bool needs_copy(const Mat& m, int dim, int64_t dim_pad) {
+  const int64_t ld = m.ld * (int64_t)sizeof(T);
+  return dim != dim_pad || (uintptr_t)m.p % 16 != 0 || ld % 16 != 0 || ld >= (int64_t)1 << 24;
+}
+// labels: rows of x without one are zeros, bias: rows of w with -inf (null: as they are)
+template <typename T>
+hipError_t operands(const LossJob& j, int64_t dim_pad, const int32_t* labels, const float* bias, char* x_copy, char* w_copy,
+                    Operand* x, Operand* w, hipStream_t st) {
+  *x = {(const char*)j.x.p, j.x.ld * (int64_t)sizeof(T), j.rows - 1, nullptr, 0};
+  *w = {(const char*)j.w.p, j.w.ld * (int64_t)sizeof(T), j.classes - 1, nullptr, 0};
+  auto blocks = [&](int64_t rows) {
+    return (uint32_t)std::min<int64_t>((rows * dim_pad / 8 + kThreads - 1) / kThreads, kPadGrid);
+  };
+  uint32_t nx = 0, nw = 0;
+  if (labels || needs_copy<T>(j.x, j.dim, dim_pad)) {
+    nx = blocks(j.rows);
+    x->p = x_copy;
+    x->ld = dim_pad * (int64_t)sizeof(T);
+  }
+  if (bias || needs_copy<T>(j.w, j.dim, dim_pad)) {
+    nw = blocks(j.classes);
+    w->p = w_copy;
+    w->ld = dim_pad * (int64_t)sizeof(T);
+  }
+  if (nx + nw == 0) return hipSuccess;
+  const CopyArgs a{j.x, x_copy, dim_pad, j.rows, labels, nullptr, j.classes, j.dim};
+  const CopyArgs b{j.w, w_copy, dim_pad, j.classes, nullptr, bias, 0, j.dim};
+  return enqueue(j.dim == dim_pad ? k_pad<T, kExact> : j.dim >= 8 ? k_pad<T, kRagged> : k_pad<T, kSmall>,
+                 dim3(nx + nw), dim3(kThreads), 0, st, a, b, nx);
 }
 
 SumMajor terms(const Operand& o, int64_t row_bytes) { return {o.p, o.ld, o.last, (int)(row_bytes / 16)}; }
@@ -618,25 +664,38 @@ hipError_t logits(LogitArgs& a, const Plan& p, int64_t classes, hipStream_t st) 
   });
 }
 
-template <typename T, bool BOTH, typename O>
-hipError_t times(SumArgs& a, const Pass& p, hipStream_t st) {
-  typedef typename Tiles<T>::template Large<BOTH> L;
-  typedef typename Tiles<T>::template Small<BOTH> S;
-  a.steps = p.steps;
-  a.per = p.per;
-  a.tm = (uint32_t)p.tm;
-  a.tn = (uint32_t)p.tn;
-  a.parts = (uint32_t)p.parts;
-  return p.large ? sum_product<L, O>(a, st) : sum_product<S, O>(a, st);
+SumArgs& cut_as(SumArgs& a, const Cut& c) {
+  a.steps = c.steps;
+  a.per = c.per;
+  a.tm = (uint32_t)c.tm;
+  a.tn = (uint32_t)c.tn;
+  a.parts = (uint32_t)c.parts;
+  return a;
+}
+
+// dx's product, dw's, or both (tm 0: absent), in one launch where their tiles are of a kind
+template <typename T>
+hipError_t products(const SumArgs& x, bool x_large, const SumArgs& w, bool w_large, hipStream_t st) {
+  typedef typename Tiles<T>::template Large<false> LX;
+  typedef typename Tiles<T>::template Small<false> SX;
+  typedef typename Tiles<T>::template Large<true> LW;
+  typedef typename Tiles<T>::template Small<true> SW;
+  if (x.tm && w.tm && x_large == w_large) {
+    const uint32_t nx = x.tm * x.tn * x.parts, nw = w.tm * w.tn * w.parts;
+    return x_large ? enqueue(k_sum_pair<LX, LW, T>, dim3(nx + nw), dim3(LX::kThreads), LX::kLds, st, x, w, nx)
+                   : enqueue(k_sum_pair<SX, SW, T>, dim3(nx + nw), dim3(SX::kThreads), SX::kLds, st, x, w, nx);
+  }
+  hipError_t e = hipSuccess;
+  if (x.tm) e = x_large ? sum_product<LX, T>(x, st) : sum_product<SX, T>(x, st);
+  if (e == hipSuccess && w.tm) e = w_large ? sum_product<LW, T>(w, st) : sum_product<SW, T>(w, st);
+  return e;
 }
 
 template <typename T>
 hipError_t forward(const LossJob& j, hipStream_t st) {
   const Plan p = plan<T>(j.rows, j.dim, j.classes);
   LogitArgs a{};
-  hipError_t e = operand<T>(j.x, j.rows, j.dim, p.dim_pad, nullptr, 0, nullptr, j.workspace + p.x, &a.x, st);
-  if (e == hipSuccess)
-    e = operand<T>(j.w, j.classes, j.dim, p.dim_pad, nullptr, 0, nullptr, j.workspace + p.w, &a.w, st);
+  hipError_t e = operands<T>(j, p.dim_pad, nullptr, nullptr, j.workspace + p.x, j.workspace + p.w, &a.x, &a.w, st);
   if (e != hipSuccess) return e;
   f32x2* const part = (f32x2*)(j.workspace + p.part);
   if (p.strips) {
@@ -684,8 +743,7 @@ hipError_t backward(const LossJob& j, hipStream_t st) {
   LogitArgs a{};
   Operand w;
   // rows without a label and classes taken out may hold anything: they are zeros here
-  hipError_t e = operand<T>(j.x, j.rows, j.dim, p.dim_pad, j.labels, j.classes, nullptr, ws + p.x, &a.x, st);
-  if (e == hipSuccess) e = operand<T>(j.w, j.classes, j.dim, p.dim_pad, nullptr, 0, j.bias, ws + p.w, &w, st);
+  hipError_t e = operands<T>(j, p.dim_pad, j.labels, j.bias, ws + p.x, ws + p.w, &a.x, &w, st);
   a.rows = j.rows;
   a.lse = j.lse;
   a.dloss = j.dloss;
@@ -695,6 +753,8 @@ hipError_t backward(const LossJob& j, hipStream_t st) {
   a.g = ws + p.g;
   a.g_ld = p.piece;
   a.bias_ld = p.all;
+  // sums that are not the result yet
+  const bool dx_sums = p.pieces > 1 || p.to_x.parts > 1, dw_sums = p.to_w.parts > 1;
   for (int64_t i = 0; e == hipSuccess && i < p.pieces; ++i) {
     const int64_t first = i * p.piece, left = j.classes - first, mine = std::min(left, p.piece);
     const int64_t wide = round_up(mine, kClassPad);  // columns of G that are written
@@ -706,50 +766,58 @@ hipError_t backward(const LossJob& j, hipStream_t st) {
     a.first = first;
     a.part_bias = j.dbias ? (float*)(ws + p.bias) + first : nullptr;
     e = logits<T, true>(a, p, wide, st);
-    if (e == hipSuccess && j.dx.p) {
-      SumArgs b{};
-      b.a = terms(a.w, p.dim_pad * E);
-      b.b = {ws + p.g, p.piece * E, p.rows_pad - 1, nullptr, 0};
-      b.c = ws + p.dx;
-      b.ldc = part_ld(j.dim);
-      b.m = j.dim;
-      b.n = j.rows;
-      b.add = i > 0;
+    if (e != hipSuccess) return e;
+    SumArgs x{}, w{};
+    if (j.dx.p) {
+      x.a = terms(a.w, p.dim_pad * E);
+      x.b = {ws + p.g, p.piece * E, p.rows_pad - 1, nullptr, 0};
+      x.c = dx_sums ? (void*)(ws + p.dx) : j.dx.p;
+      x.ldc = dx_sums ? part_ld(j.dim) : j.dx.ld;
+      x.wide = dx_sums;
+      x.m = j.dim;
+      x.n = j.rows;
+      x.add = i > 0;
       Pass t = p.to_x;
       // the last piece may have fewer steps than parts: all parts hold sums by then
-      const int full = (int)(p.piece / t.steps);
-      t.steps = (int)(wide / full);
-      t.per = (t.steps + t.parts - 1) / t.parts;
-      if (i > 0) t.parts = (t.steps + t.per - 1) / t.per;
-      e = times<T, false, float>(b, t, st);
+      t.steps = (int)(wide / (p.piece / t.steps));
+      t.per = (int)tiles_of(t.steps, t.parts);
+      if (i > 0) t.parts = (int)tiles_of(t.steps, t.per);
+      cut_as(x, t);
     }
-    if (e == hipSuccess && j.dw.p) {
-      SumArgs b{};
-      b.a = terms(a.x, p.dim_pad * E);
-      b.bs = {ws + p.g, p.piece * E, p.rows_pad - 1, (int)(p.piece * E / 16)};
-      b.m = j.dim;
-      b.n = mine;
+    if (j.dw.p) {
+      w.a = terms(a.x, p.dim_pad * E);
+      w.bs = {ws + p.g, p.piece * E, p.rows_pad - 1, (int)(p.piece * E / 16)};
+      w.m = j.dim;
+      w.n = mine;
+      w.c = dw_sums ? (void*)(ws + p.dw) : (T*)j.dw.p + first * j.dw.ld;
+      w.ldc = dw_sums ? part_ld(j.dim) : j.dw.ld;
+      w.wide = dw_sums;
       Pass t = p.to_w;
       t.tn = tiles_of(mine, t.large ? Tiles<T>::template Large<true>::BN : Tiles<T>::template Small<true>::BN);
-      const Mat out = {(T*)j.dw.p + first * j.dw.ld, j.dw.ld};
-      if (t.parts == 1) {
-        b.c = out.p;
-        b.ldc = out.ld;
-        e = times<T, true, T>(b, t, st);
-      } else {
-        b.c = ws + p.dw;
-        b.ldc = part_ld(j.dim);
-        e = times<T, true, float>(b, t, st);
-        if (e == hipSuccess) e = join<T>((const float*)(ws + p.dw), t.parts, mine, j.dim, nullptr, 0, out, st);
-      }
+      cut_as(w, t);
     }
+    e = products<T>(x, p.to_x.large, w, p.to_w.large, st);
+    if (e != hipSuccess) return e;
+    const bool last = i + 1 == p.pieces;
+    EndArgs end{};
+    uint32_t nb = 0;
+    if (j.dw.p && dw_sums) {
+      const Mat out = {(T*)j.dw.p + first * j.dw.ld, j.dw.ld};
+      end.w = join_args((const float*)(ws + p.dw), p.to_w.parts, mine, j.dim, nullptr, 0, out);
+      end.nw = (uint32_t)join_blocks(end.w);
+      end.w_slices = joins_in_slices(end.w);
+    }
+    if (last && j.dx.p && dx_sums) {
+      end.x = join_args((const float*)(ws + p.dx), p.to_x.parts, j.rows, j.dim, nullptr, 0, j.dx);
+      end.nx = (uint32_t)join_blocks(end.x);
+      end.x_slices = joins_in_slices(end.x);
+    }
+    if (last && j.dbias) {
+      end.b = {(const float*)(ws + p.bias), j.dbias, p.all, j.classes, (int)(p.rows_pad / p.bn)};
+      nb = (uint32_t)tiles_of(j.classes, kThreads);
+    }
+    if (end.nx + end.nw + nb) e = enqueue(k_loss_end<T>, dim3(end.nx + end.nw + nb), dim3(kThreads), 0, st, end);
   }
-  if (e == hipSuccess && j.dbias) {
-    const BiasArgs b{(const float*)(ws + p.bias), j.dbias, p.all, j.classes, (int)(p.rows_pad / p.bn)};
-    e = enqueue(k_bias, dim3((unsigned)tiles_of(j.classes, kThreads)), dim3(kThreads), 0, st, b);
-  }
-  if (e == hipSuccess && j.dx.p)
-    e = join<T>((const float*)(ws + p.dx), p.to_x.parts, j.rows, j.dim, nullptr, 0, j.dx, st);
   return e;
 }
 
