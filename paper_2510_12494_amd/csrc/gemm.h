@@ -319,9 +319,9 @@ struct SumTile {
   static constexpr int kHalves = KB / 64;
   static constexpr int D = MF < 4 ? MF : 4, DN = NF < 4 ? NF : 4;
   static_assert(TY == kBf16 || TY == kF32);
-  static_assert(TY == kF32 ? D >= 2 && DN >= 2 : D == 4 && DN == 4, "the swizzles below");
+  static_assert(D >= 2 && DN >= 2, "the swizzles below");
   static_assert(MF % D == 0 && NF % DN == 0 && kStage % (1024 * kWaves) == 0 && BM * KB % 1024 == 0);
-  static_assert(BM * kBytes >= 256 && BN * kBytes >= 256);
+  static_assert(BM * kBytes >= 128 && BN * kBytes >= 128);
   static_assert((NST - 2) * kCopies < 64);
   typedef f32x4 Acc[MF][NF];
 
@@ -340,11 +340,13 @@ struct SumTile {
   }
 
   // Four rows that are read at once (bf16: consecutive; float32: four apart) lie in
-  // different banks: the fragment's place among its D flips with the low bits, the
-  // half of 256 bytes with the high one.
-  __device__ static int swizzle(int k, int deal) {
-    if constexpr (TY == kBf16) return (k & 1) | (k & 2) << 2;
-    else return deal == 4 ? (k >> 2) & 3 : (k >> 2 & 1) | (k >> 3 & 1) << 3;
+  // different banks: within what a fragment's reads leave free of a row, then in the
+  // other half of 256 bytes (a row of 128 has none: two rows meet).  `per`: a row's chunks.
+  __device__ static int swizzle(int k, int deal, int per) {
+    const int lo = TY == kBf16 ? k & 1 : k >> 2 & 1, hi = TY == kBf16 ? k >> 1 & 1 : k >> 3 & 1;
+    if (TY == kF32 && deal == 4) return lo | hi << 1;
+    const int at = TY == kBf16 && deal == 2 ? 2 : 0;  // the chunks that eight bytes of each lie in
+    return lo << at | (per >= 16 ? hi << 3 : 0);
   }
 
   __device__ void run(const SumMajor& A, const SumMajor& Bs, const Operand& B, int64_t m0, int64_t n0, int s0, int s1,
@@ -363,7 +365,7 @@ struct SumTile {
         const int per = (of_a ? BM : BN) * kBytes / 16;                  // chunks of a row
         const int u = (of_a ? blk : blk - kCopiesA) * 64 + lane;         // chunk of the operand's step
         const int k = u / per;
-        const int ch = (u % per) ^ swizzle(k, of_a ? D : DN);
+        const int ch = (u % per) ^ swizzle(k, of_a ? D : DN, per);
         const SumMajor& o = of_a ? A : Bs;
         const int64_t chunk = min((of_a ? m0 : n0) * kBytes / 16 + ch, (int64_t)o.chunks - 1);
         row[c] = k;
@@ -402,14 +404,14 @@ struct SumTile {
       typedef __attribute__((ext_vector_type(4))) short s16x4;
       const int kk = k + (i >> 2);
       const int col = w + 16 * deal * (f / deal) + 4 * deal * (i & 3) + 4 * (f % deal);
-      const int ch = (col / 8) ^ swizzle(kk, deal);
+      const int ch = (col / 8) ^ swizzle(kk, deal, width / 8);
       const char* p = S + kk * width * 2 + ch * 16 + (col % 8) * 2;
       return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                                            (__attribute__((address_space(3))) s16x4*)p));
     };
     auto element = [&](const char* S, int width, int deal, int w, int f, int k) {
       const int col = w + 16 * deal * (f / deal) + 4 * deal * (i >> 2) + 4 * (f % deal) + (i & 3);
-      const int ch = (col / 4) ^ swizzle(k, deal);
+      const int ch = (col / 4) ^ swizzle(k, deal, width / 4);
       return *(const float*)(S + k * width * 4 + ch * 16 + (col % 4) * 4);
     };
     // the 16 bytes of the sum that lane (i, g) holds of a fragment: terms 8 (g + 4 h)

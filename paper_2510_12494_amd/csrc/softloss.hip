@@ -522,42 +522,74 @@ template <> struct Tiles<uint16_t> {
   typedef Tile<kBf16, 256, 256, 4, 4, 128, 2, kBlocks> Long;    // many columns of x
   typedef Tile<kBf16, 256, 128, 4, 2, 64, 3, kBlocks> Short;   // few: two workgroups a CU
   typedef Tile<kBf16, 256, 64, 4, 1, 64, 4, kBlocks> Few;       // few rows
+  typedef Tile<kBf16, 64, 64, 2, 2, 128, 3, kBlocks> Tiny;      // few tiles of these
   template <bool BOTH> using Large = SumTile<kBf16, 256, 256, 4, 4, 128, 2, BOTH>;
   template <bool BOTH> using Small = SumTile<kBf16, 128, 128, 2, 2, 128, 2, BOTH>;
+  template <bool BOTH> using Least = SumTile<kBf16, 64, 64, 2, 2, 128, 3, BOTH>;
 };
 template <> struct Tiles<float> {
   typedef Tile<kF32, 128, 128, 2, 2, 64, 2, kBlocks> Long;
   typedef Tile<kF32, 128, 128, 2, 2, 64, 2, kBlocks> Short;
   typedef Tile<kF32, 64, 64, 2, 2, 64, 4, kBlocks> Few;
+  typedef Few Tiny;
   template <bool BOTH> using Large = SumTile<kF32, 128, 128, 2, 2, 64, 2, BOTH>;
   template <bool BOTH> using Small = SumTile<kF32, 64, 64, 2, 2, 64, 4, BOTH>;
+  template <bool BOTH> using Least = Small<BOTH>;
 };
 
-enum Kind { kLong, kShort, kFew };
+enum Kind { kLong, kShort, kFew, kTiny };
 // calls f(tile) with the kind's tile
 template <typename T, typename F>
 auto with_tile(Kind k, F f) {
   typedef Tiles<T> TS;
-  return k == kLong ? f((typename TS::Long*)nullptr) : k == kShort ? f((typename TS::Short*)nullptr)
-                                                                  : f((typename TS::Few*)nullptr);
+  return k == kLong    ? f((typename TS::Long*)nullptr)
+         : k == kShort ? f((typename TS::Short*)nullptr)
+         : k == kFew   ? f((typename TS::Few*)nullptr)
+                       : f((typename TS::Tiny*)nullptr);
+}
+
+// The logits' tile: the largest that fills the CUs.  float32 tiles of 64 x 64 until
+// those of 128 x 128 fill them four times: a last round of these that is not full
+// costs more (1537 rows over 5003 classes: 64 us, 87).
+template <typename T>
+Kind kind_of(int64_t rows, int dim, int64_t classes) {
+  if (sizeof(T) == 4) return tiles_of(rows, 128) * tiles_of(classes, 128) < 1024 ? kTiny : kLong;
+  if (rows <= 64) return tiles_of(classes, 256) >= 192 ? kFew : kTiny;
+  if (dim > 256 && tiles_of(rows, 256) * tiles_of(classes, 256) >= 192) return kLong;
+  return tiles_of(rows, 128) * tiles_of(classes, 256) >= 192 ? kShort : kTiny;
 }
 
 // A product of m columns and n rows over `depth` terms, in the tiles that should take
 // less time.  Steps timed over 8192 cubed (bf16) and 4096 cubed (float32).
-struct Pass : Cut { bool large; };
+enum Size { kLargeSum, kSmallSum, kLeastSum };
+struct Pass : Cut { Size size; };
 template <typename T>
 Pass pass(int64_t m, int64_t n, int64_t depth) {
   typedef typename Tiles<T>::template Large<true> L;
   typedef typename Tiles<T>::template Small<true> S;
-  constexpr bool wide = sizeof(T) == 2;
-  const Cut large = cut_up(m, n, L::BM, L::BN, (int)tiles_of(depth, L::kElements),
-                           wide ? StepTime{2.05, 2.05, 1} : StepTime{1.07, 1.3, 4});
-  const Cut small = cut_up(m, n, S::BM, S::BN, (int)tiles_of(depth, S::kElements),
-                           wide ? StepTime{0.67, 0.8, 2} : StepTime{0.29, 0.5, 4});
-  return large.us < small.us ? Pass{large, true} : Pass{small, false};
+  typedef typename Tiles<T>::template Least<true> E;
+  constexpr bool bf16 = sizeof(T) == 2;
+  auto cut = [&](int bm, int bn, int elements, const StepTime& t) {
+    return cut_up(m, n, bm, bn, (int)tiles_of(depth, elements), t);
+  };
+  Pass p{cut(L::BM, L::BN, L::kElements, bf16 ? StepTime{2.05, 2.05, 1} : StepTime{1.07, 1.3, 4}), kLargeSum};
+  const Cut s = cut(S::BM, S::BN, S::kElements, bf16 ? StepTime{0.67, 0.8, 2} : StepTime{0.29, 0.5, 4});
+  if (s.us < p.us) p = {s, kSmallSum};
+  if (bf16) {
+    const Cut e = cut(E::BM, E::BN, E::kElements, StepTime{0.22, 0.5, 3});
+    if (e.us < p.us) p = {e, kLeastSum};
+  }
+  return p;
+}
+// columns of B of a tile
+template <typename T>
+int rows_of(Size s) {
+  typedef Tiles<T> TS;
+  return s == kLargeSum   ? TS::template Large<true>::BN
+         : s == kSmallSum ? TS::template Small<true>::BN
+                          : TS::template Least<true>::BN;
 }
 
-constexpr int kClassPad = 256;         // classes of a piece: whole tiles of any kind
 constexpr int64_t kPiece = 256 << 20;  // bytes of G
 
 // Where things lie in the workspace, and how the classes are cut up.
@@ -579,18 +611,16 @@ Plan plan(int64_t rows, int dim, int64_t classes) {
     at += ((size_t)elements * size + 255) & ~(size_t)255;
     return here;
   };
-  p.kind = rows <= 64 || (sizeof(T) == 4 && tiles_of(rows, 128) * tiles_of(classes, 128) < 1024) ? kFew
-           : dim * (int)sizeof(T) > 512                                                        ? kLong
-                                                                                                : kShort;
+  p.kind = kind_of<T>(rows, dim, classes);
   with_tile<T>(p.kind, [&](auto* tile) {
     p.bm = std::remove_pointer_t<decltype(tile)>::BM;
     p.bn = std::remove_pointer_t<decltype(tile)>::BN;
   });
   p.dim_pad = round_up(dim, kRow<T>);
   p.rows_pad = round_up(rows, p.bn);
-  p.all = round_up(classes, kClassPad);
-  const int64_t most = kPiece / ((int64_t)sizeof(T) * p.rows_pad) / kClassPad * kClassPad;
-  p.piece = std::min<int64_t>(p.all, std::max<int64_t>(kClassPad, most));
+  p.all = round_up(classes, p.bm);                   // a step of every product divides a tile's classes
+  const int64_t most = kPiece / ((int64_t)sizeof(T) * p.rows_pad) / p.bm * p.bm;
+  p.piece = std::min<int64_t>(p.all, std::max<int64_t>(p.bm, most));
   p.pieces = (p.all + p.piece - 1) / p.piece;
   p.to_x = pass<T>(dim, rows, p.piece);
   p.to_w = pass<T>(dim, p.piece, rows);
@@ -673,22 +703,26 @@ SumArgs& cut_as(SumArgs& a, const Cut& c) {
   return a;
 }
 
-// dx's product, dw's, or both (tm 0: absent), in one launch where their tiles are of a kind
+// dx's product, dw's, or both (tm 0: absent), in one launch where their tiles are of a size
+template <typename T, template <bool> class TL>
+hipError_t products_of(const SumArgs& x, const SumArgs& w, hipStream_t st) {
+  if (!w.tm) return x.tm ? sum_product<TL<false>, T>(x, st) : hipSuccess;
+  if (!x.tm) return sum_product<TL<true>, T>(w, st);
+  const uint32_t nx = x.tm * x.tn * x.parts, nw = w.tm * w.tn * w.parts;
+  return enqueue(k_sum_pair<TL<false>, TL<true>, T>, dim3(nx + nw), dim3(TL<false>::kThreads), TL<false>::kLds, st, x, w, nx);
+}
 template <typename T>
-hipError_t products(const SumArgs& x, bool x_large, const SumArgs& w, bool w_large, hipStream_t st) {
-  typedef typename Tiles<T>::template Large<false> LX;
-  typedef typename Tiles<T>::template Small<false> SX;
-  typedef typename Tiles<T>::template Large<true> LW;
-  typedef typename Tiles<T>::template Small<true> SW;
-  if (x.tm && w.tm && x_large == w_large) {
-    const uint32_t nx = x.tm * x.tn * x.parts, nw = w.tm * w.tn * w.parts;
-    return x_large ? enqueue(k_sum_pair<LX, LW, T>, dim3(nx + nw), dim3(LX::kThreads), LX::kLds, st, x, w, nx)
-                   : enqueue(k_sum_pair<SX, SW, T>, dim3(nx + nw), dim3(SX::kThreads), SX::kLds, st, x, w, nx);
-  }
-  hipError_t e = hipSuccess;
-  if (x.tm) e = x_large ? sum_product<LX, T>(x, st) : sum_product<SX, T>(x, st);
-  if (e == hipSuccess && w.tm) e = w_large ? sum_product<LW, T>(w, st) : sum_product<SW, T>(w, st);
-  return e;
+hipError_t products_in(Size s, const SumArgs& x, const SumArgs& w, hipStream_t st) {
+  typedef Tiles<T> TS;
+  return s == kLargeSum   ? products_of<T, TS::template Large>(x, w, st)
+         : s == kSmallSum ? products_of<T, TS::template Small>(x, w, st)
+                          : products_of<T, TS::template Least>(x, w, st);
+}
+template <typename T>
+hipError_t products(const SumArgs& x, Size xs, const SumArgs& w, Size ws, hipStream_t st) {
+  if (xs == ws || !w.tm) return products_in<T>(xs, x, w, st);
+  const hipError_t e = products_in<T>(xs, x, SumArgs{}, st);
+  return e != hipSuccess ? e : products_in<T>(ws, SumArgs{}, w, st);
 }
 
 template <typename T>
@@ -757,7 +791,7 @@ hipError_t backward(const LossJob& j, hipStream_t st) {
   const bool dx_sums = p.pieces > 1 || p.to_x.parts > 1, dw_sums = p.to_w.parts > 1;
   for (int64_t i = 0; e == hipSuccess && i < p.pieces; ++i) {
     const int64_t first = i * p.piece, left = j.classes - first, mine = std::min(left, p.piece);
-    const int64_t wide = round_up(mine, kClassPad);  // columns of G that are written
+    const int64_t wide = round_up(mine, p.bm);       // columns of G that are written
     a.w = w;
     a.w.p = w.p + first * w.ld;
     a.w.last = left - 1;
@@ -793,10 +827,10 @@ hipError_t backward(const LossJob& j, hipStream_t st) {
       w.ldc = dw_sums ? part_ld(j.dim) : j.dw.ld;
       w.wide = dw_sums;
       Pass t = p.to_w;
-      t.tn = tiles_of(mine, t.large ? Tiles<T>::template Large<true>::BN : Tiles<T>::template Small<true>::BN);
+      t.tn = tiles_of(mine, rows_of<T>(t.size));
       cut_as(w, t);
     }
-    e = products<T>(x, p.to_x.large, w, p.to_w.large, st);
+    e = products<T>(x, p.to_x.size, w, p.to_w.size, st);
     if (e != hipSuccess) return e;
     const bool last = i + 1 == p.pieces;
     EndArgs end{};
