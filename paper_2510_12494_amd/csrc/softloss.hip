@@ -231,7 +231,11 @@ __global__ __launch_bounds__(TL::kThreads) void k_logits(LogitArgs j) {
       const int hit = has ? label - (int)(j.first + mine) : -1;
       float g[RUN];
 #pragma unroll
-      for (int t = 0; t < RUN; ++t) g[t] = d * exp2_of(fmaf(acc[t / 4][c][t % 4], kLog2e, bias[t]) - lse2);
+      for (int t = 0; t < RUN; ++t) g[t] = 0.f;
+      if (has) {                                     // whatever the weights hold
+#pragma unroll
+        for (int t = 0; t < RUN; ++t) g[t] = d * exp2_of(fmaf(acc[t / 4][c][t % 4], kLog2e, bias[t]) - lse2);
+      }
       if ((unsigned)hit < (unsigned)RUN) {
 #pragma unroll
         for (int t = 0; t < RUN; ++t) g[t] -= hit == t && !(bias[t] == -__builtin_inff()) ? d : 0.f;
