@@ -599,8 +599,8 @@ vfl_status vfl_quantize(const vfl_quantize_args* a, void* stream);
 
 /* c = a b^T + bias, negative results 0 where relu is not 0: a [m x k] and b
  * [n x k] in 8 bits, bias float32 [n] (NULL: none), c [m x n] of `dtype`, rounded
- * once from float32 sums.  m, n <= 2^30, m n <= 2^38, 1 <= k <= VFL_MATMUL8_MAX_DEPTH, and rows
- * of a and b are below 2^24 bytes apart.  No element of c may be one of a, b or
+ * once from float32 sums.  m, n <= 2^30, m n <= 2^36, 1 <= k <= VFL_MATMUL8_MAX_DEPTH, and
+ * rows of a and b are below 2^24 bytes apart.  No element of c may be one of a, b or
  * bias.  The workspace (16-byte aligned, vfl_matmul8_workspace_size() bytes, 0 for
  * many sizes) holds partial sums during the call; calls that may run at the same
  * time need one each.  vfl_matmul8_workspace_size is host-only. */

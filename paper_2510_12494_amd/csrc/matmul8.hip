@@ -120,6 +120,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_rows(RowsArgs j) {
 // 1024 12.7, 16.0; 64 x 4096 x 4096 12.3, 16.3; beyond: 64 x 1024 x 8192 20.6, 15.9;
 // 32 x 8192 x 8192 24.6, 23.3; and where the tiles are many: 32768 x 64 x 500 15.8, 9.6).
 constexpr int kRowSteps = 32, kRowWork = 8192;
+constexpr int64_t kRowColumns = (int64_t)1 << 26;    // its grid is below 2^32 threads
 
 enum Kind { kRowsOne, kRowsTwo, kRowsFour, kLargeTile, kSmallTile };
 struct Choice : Cut { Kind kind; };
@@ -129,8 +130,9 @@ struct Choice : Cut { Kind kind; };
 // 19.8, 15.8.
 Choice choose(Elt e, int64_t m, int64_t n, int64_t k) {
   const int steps = (int)tiles_of(k, kBlock8);
-  if (m <= 16 || (steps <= kRowSteps && tiles_of(m, 64) * tiles_of(n, 16) * steps <= kRowWork &&
-                  tiles_of(m, 128) * tiles_of(n, 128) < 128))
+  if ((m <= 16 && n <= kRowColumns) ||
+      (steps <= kRowSteps && tiles_of(m, 64) * tiles_of(n, 16) * steps <= kRowWork &&
+       tiles_of(m, 128) * tiles_of(n, 128) < 128))
     return {Cut{0, 0, steps, 1, steps, 0.0}, m <= 16 ? kRowsOne : m <= 32 ? kRowsTwo : kRowsFour};
   const Cut small = cut_up(m, n, 128, 128, steps, e == F32 ? StepTime{0.98, 1.2, 2} : StepTime{0.5, 0.75, 2});
   if (e == F32) return {small, kSmallTile};

@@ -11,7 +11,7 @@ using namespace vfl;
 namespace {
 
 constexpr int64_t kMaxSide8 = (int64_t)1 << 30;      // rows of an operand of a product, results' columns
-constexpr int64_t kMaxResults = (int64_t)1 << 38;    // of a product: its grid is below 2^32 threads
+constexpr int64_t kMaxResults = (int64_t)1 << 36;    // of a product: its grid is below 2^32 threads
 constexpr int64_t kMaxLogits = (int64_t)1 << 37;
 constexpr int64_t kMaxDepth = VFL_MATMUL8_MAX_DEPTH;
 

@@ -20,7 +20,7 @@ struct ProductArgs {
   uint32_t tm, tn, parts;
   int n, steps, per;                   // per: steps of a part
   int64_t m;
-  int relu, add;
+  int relu;
 };
 
 __device__ __forceinline__ f32x4 finish(f32x4 v, const f32x4& bias, int relu) {
@@ -43,27 +43,26 @@ __device__ __forceinline__ f32x4 bias4(const float* bias, int col, int n) {
   return v;
 }
 
-// the first `left` of W values (all: at once)
-template <int W = 4, typename T>
+// the first `left` of four values (all: at once)
+template <typename T>
 __device__ __forceinline__ void store_to(T* p, const f32x4& v, int left) {
-  if constexpr (W == 4) {
-    if (left >= 4) {
-      const float w[4] = {v[0], v[1], v[2], v[3]};
-      store4(p, w);
-      return;
-    }
+  if (left >= 4) {
+    const float w[4] = {v[0], v[1], v[2], v[3]};
+    store4(p, w);
+    return;
   }
 #pragma unroll
-  for (int i = 0; i < W; ++i)
+  for (int i = 0; i < 3; ++i)
     if (i < left) st1<T>(p + i, v[i]);
 }
 
-// One tile of the product, or (parts > 1) of a part of its sum, as
-// float32 partial sums [part][m][n]; add: on top of what C holds.
+// One tile of the product, or (parts > 1) of a part of its sum, as float32 partial
+// sums [part][m][n].
 template <class TL, typename T>
 __global__ __launch_bounds__(TL::kThreads) void k_product(ProductArgs j) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const Place at = place_of(blockIdx.x, j.tm, j.tn, j.parts);
+  static_assert(TL::DN == 4, "a lane stores four columns at once");
   const TL tile;
   typename TL::Acc acc;
 #pragma unroll
@@ -75,7 +74,7 @@ __global__ __launch_bounds__(TL::kThreads) void k_product(ProductArgs j) {
   const int n0 = (int)at.n * TL::BN;
   tile.run(j.a, j.b, m0, n0, s0, s1, smem, acc);
 #pragma unroll
-  for (int q = 0; q < TL::NF / TL::DN; ++q) {
+  for (int q = 0; q < TL::NF / 4; ++q) {
     const int col = n0 + tile.col(q), left = j.n - col;
     const f32x4 bias = bias4(j.bias, col, j.n);
 #pragma unroll
@@ -85,13 +84,10 @@ __global__ __launch_bounds__(TL::kThreads) void k_product(ProductArgs j) {
         const int64_t row = m0 + tile.row(f, r);
         if (row >= j.m || left <= 0) continue;
         T* p = (T*)j.c + ((int64_t)at.part * j.m + row) * j.ldc + col;
-        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        f32x4 v;
 #pragma unroll
-        for (int c = 0; c < TL::DN; ++c) {
-          v[c] = acc[f][TL::DN * q + c][r];
-          if (j.add && c < left) v[c] += ld1<T>(p + c);
-        }
-        store_to<TL::DN>(p, finish(v, bias, j.relu), left);
+        for (int c = 0; c < 4; ++c) v[c] = acc[f][4 * q + c][r];
+        store_to(p, finish(v, bias, j.relu), left);
       }
   }
 }
@@ -106,6 +102,7 @@ struct SumArgs {
   uint32_t tm, tn, parts;
   int m, steps, per, add, wide;        // wide: results in float32 whatever T
 };
+// add: on top of what is there (sums of an earlier piece, which are float32)
 template <typename T>
 __device__ __forceinline__ void store_sums(T* out, float (&v)[8], int left, int add) {
   if (left >= 8) {
@@ -149,7 +146,7 @@ __device__ __forceinline__ void sum_tile(const SumArgs& j, uint32_t block, char*
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = acc[q * TL::D + d + i / 4][f][i % 4];
         if (sizeof(T) == 4 || j.wide) store_sums((float*)j.c + out + col, v, j.m - col, j.add);
-        else store_sums((T*)j.c + out + col, v, j.m - col, j.add);
+        else store_sums((T*)j.c + out + col, v, j.m - col, 0);
       }
   }
 }
@@ -179,34 +176,38 @@ struct JoinArgs {
 // The parts of a split product, summed in a fixed order: SL threads take every SL-th
 // part of the same four columns each and meet in LDS (many parts of few results: one
 // row of 256 columns in 512 parts 15 us with a thread for all parts).
+constexpr int64_t kJoinGrid = 1 << 20;
 template <typename T, int SL>
 __device__ __forceinline__ void join_block(const JoinArgs& j, uint32_t block) {
   constexpr int Q = kJoinThreads / SL;
   __shared__ f32x4 sums[SL > 1 ? SL : 1][Q];
   const int q = threadIdx.x % Q, slice = threadIdx.x / Q;
-  const int64_t at = (int64_t)block * Q + q;
-  const bool live = at < j.items;
-  const int64_t row = live ? at / j.quads : 0;
-  const int col = live ? 4 * (int)(at - row * j.quads) : 0;
-  const float* p = j.part + row * j.ld + col;
   const int64_t pitch = j.m * j.ld;
-  f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  for (int i = slice; i < j.parts; i += 8 * SL) {    // eight loads in flight
-    f32x4 o[8];
+  int64_t at = (int64_t)block * Q + q;
+  do {
+    const bool live = at < j.items;
+    const int64_t row = live ? at / j.quads : 0;
+    const int col = live ? 4 * (int)(at - row * j.quads) : 0;
+    const float* p = j.part + row * j.ld + col;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    for (int i = slice; i < j.parts; i += 8 * SL) {  // eight loads in flight
+      f32x4 o[8];
 #pragma unroll
-    for (int u = 0; u < 8; ++u)
-      o[u] = i + u * SL < j.parts ? *(const f32x4*)(p + (i + u * SL) * pitch) : f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int u = 0; u < 8; ++u)
+        o[u] = i + u * SL < j.parts ? *(const f32x4*)(p + (i + u * SL) * pitch) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int u = 0; u < 8; ++u) v += o[u];
-  }
-  if constexpr (SL > 1) {
-    sums[slice][q] = v;
-    __syncthreads();
-    if (slice > 0) return;
+      for (int u = 0; u < 8; ++u) v += o[u];
+    }
+    if constexpr (SL > 1) {
+      sums[slice][q] = v;
+      __syncthreads();
+      if (slice > 0) return;
 #pragma unroll
-    for (int i = 1; i < SL; ++i) v += sums[i][q];
-  }
-  if (live) store_to((T*)j.c + row * j.ldc + col, finish(v, bias4(j.bias, col, j.n), j.relu), j.n - col);
+      for (int i = 1; i < SL; ++i) v += sums[i][q];
+    }
+    if (live) store_to((T*)j.c + row * j.ldc + col, finish(v, bias4(j.bias, col, j.n), j.relu), j.n - col);
+    at += kJoinGrid * Q;
+  } while (SL == 1 && at < j.items);   // in slices there are few results
 }
 
 template <typename T, int SL>
@@ -266,7 +267,9 @@ JoinArgs join_args(const float* part, int parts, int64_t m, int64_t n, const flo
   return {part, bias, c.p, c.ld, m, items, ld, (int)n, (int)(ld / 4), parts, relu};
 }
 bool joins_in_slices(const JoinArgs& a) { return a.parts >= 16 && a.items <= 65536; }
-int64_t join_blocks(const JoinArgs& a) { return tiles_of(a.items, joins_in_slices(a) ? kJoinThreads / 16 : kJoinThreads); }
+int64_t join_blocks(const JoinArgs& a) {
+  return std::min(tiles_of(a.items, joins_in_slices(a) ? kJoinThreads / 16 : kJoinThreads), kJoinGrid);
+}
 template <typename T>
 hipError_t join(const float* part, int parts, int64_t m, int64_t n, const float* bias, int relu, const Mat& c,
                 hipStream_t st) {

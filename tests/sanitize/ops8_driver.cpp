@@ -84,7 +84,7 @@ hipError_t launch_matmul8(Elt e, const Matmul8Job& j, hipStream_t) {
   check_8(j.b, j.n, j.k, true);
   check_mat(j.c, j.m, j.n, elt_size(e), true);
   expect(j.a.ld < (1 << 24) && j.b.ld < (1 << 24), "a tile's offsets fit 32 bits");
-  expect(j.m > 0 && j.n > 0 && j.k > 0 && j.m <= ((int64_t)1 << 38) / j.n && j.k <= VFL_MATMUL8_MAX_DEPTH, "sizes");
+  expect(j.m > 0 && j.n > 0 && j.k > 0 && j.m <= ((int64_t)1 << 36) / j.n && j.k <= VFL_MATMUL8_MAX_DEPTH, "sizes");
   const size_t need = matmul8_workspace(j.m, j.n, j.k);
   expect(need == 0 || (j.part && need <= ws_bytes), "the workspace holds the partial sums");
   return hipSuccess;

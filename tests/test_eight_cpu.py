@@ -167,7 +167,8 @@ def test_no_rows_with_outputs_present(V):
 
 
 def test_workspace_sizes_check_their_sizes(V):
-    for bad in ((-1, 1, 1), (1, -1, 1), (1, 1, 0), (2**31, 1, 1), (2**25, 2**25, 1), (1, 1, 2**24)):
+    for bad in ((-1, 1, 1), (1, -1, 1), (1, 1, 0), (2**31, 1, 1), (2**25, 2**25, 1), (2**30, 2**6 + 1, 1), (2**19, 2**18, 1),
+                (1, 1, 2**24)):
         with pytest.raises(V.VflError):
             V.vfl_matmul8_workspace_size(*bad)
     for bad in ((2, 1, 1, 1), (0, -1, 1, 1), (0, 1, 0, 1), (0, 1, 1, 0), (0, 2**22, 1, 1), (0, 1, 1, 2**22), (0, 2**20, 1, 2**18)):
@@ -192,5 +193,5 @@ def test_workspaces_of_extreme_sizes(V):
             sums = (64 * rows + 128 * 2**20 // max(dim, 1) + classes * 66) * (dim + 256) * 4
             assert size <= 2 * ((rows + classes) * (dim + 64) * e) + pairs + piece + sums + 2**30
     m = V.vfl_matmul8_workspace_size
-    assert m(2**30, 2**8, 2**23) == m(1, 2**30, 2**23) == m(16, 2**30, 1) == 0
+    assert m(2**30, 2**6, 2**23) == m(1, 2**30, 2**23) == m(16, 2**30, 1) == 0
     assert 0 < m(128, 128, 2**23) <= 512 * 128 * 128 * 4

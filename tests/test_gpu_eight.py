@@ -401,6 +401,45 @@ def test_matmul8(V, dt, m, n, k):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n,k", [(4099, 2051, 200), (260, 2000, 20000), (3000, 3000, 16000), (40, 70000, 260)])
+def test_matmul8_of_many_tiles(V, dt, m, n, k):
+    """Against float64 products of the same values on the device."""
+    g = torch.Generator(device="cuda").manual_seed(m)
+    e, vals = [], []
+    for rows in (m, n):
+        x = Mat("f32", rows, k)
+        x.t.copy_(torch.randn(rows, k, device="cuda", generator=g) * torch.exp(torch.randn(rows, 1, device="cuda", generator=g)))
+        e.append(Eight(rows, k, 1))
+        quantize(V, "f32", x, e[-1])
+        q = e[-1]._bytes().view(torch.float8_e4m3fn).double().view(rows, -1, 128)
+        vals.append((q * torch.exp2(e[-1]._powers().T.double() - 127)[:, :, None]).view(rows, -1))
+    c = Mat(dt, m, n, n + 5, 3)
+    matmul8(V, dt, *e, c, k)
+    want, mags = vals[0] @ vals[1].T, vals[0].abs() @ vals[1].abs().T
+    bound = SLACK * (k / 4 + 16) * U * mags + (2.0 ** -14 * mags if dt == "bf16" else 0)
+    # and the rounding of the stored value
+    off = (c.t.double() - want).abs() - bound - (2.0 ** -8 * (want.abs() + bound) if dt == "bf16" else U * want.abs())
+    assert float(off.max()) <= 0
+    c.assert_guard()
+
+
+def test_matmul8_of_one_row_and_very_many_columns(V):
+    n, k = 2 ** 27 + 3, 100
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GB of device memory")
+    b = Eight(0, k)
+    b.rows, b.ld, b.sld = n, 128, -(-n // 16) * 16
+    b.data, b.scale = (torch.full((s,), 0x38, dtype=torch.uint8, device="cuda") for s in (n * 128, b.sld))   # ones
+    power = (torch.arange(n, device="cuda", dtype=torch.int32) * 7919 >> 3) % 32
+    b.scale[:n] = (power + 110).to(torch.uint8)
+    a = Eight(1, k, 0, np.ones((1, k)))
+    c = Mat("f32", 1, n)
+    matmul8(V, "f32", a, b, c, k)
+    assert torch.equal(c.t[0], k * torch.exp2((power - 17).double()).float())
+    c.assert_guard()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_matmul8_powers_and_numbers_that_are_none(V, dt):
     # blocks of very different powers in one row, whose products meet again
     m, n, k = 70, 90, 512
@@ -504,7 +543,9 @@ class Loss:
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,dim,classes", [(1, 1, 1), (1, 64, 1000), (2, 8, 2), (5, 3, 7), (48, 250, 1000), (63, 64, 65),
                                               (129, 128, 257), (300, 40, 2000), (1000, 7, 300), (260, 520, 777), (3, 1030, 400),
-                                              (2100, 64, 600), (70, 33, 9001), (1500, 128, 5003)])
+                                              (2100, 64, 600), (70, 33, 9001), (1500, 128, 5003), (64, 100, 50000),
+                                              (33, 300, 60001), (3000, 300, 5000), (300, 5000, 2100), (600, 2000, 9000),
+                                              (4100, 1000, 4100)])
 def test_softmax_loss(V, dt, rows, dim, classes):
     t = Loss(V, dt, rows, dim, classes)
     t.run()
@@ -556,6 +597,32 @@ def test_softmax_loss_rows_without_a_label_and_classes_taken_out(V, dt):
     t.run()
     t.check()
     assert not t.dw.np()[100:140].any() and not t.dx.np()[~((labels >= 0) & (labels < classes))].any()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_softmax_loss_rows_without_a_label_and_infinite_weights(V, dt):
+    """A weight of -inf that takes its class to a logit of -inf in every row with a
+    label, and to none in one without: that row is in no gradient."""
+    rows, dim, classes = 150, 70, 200
+    rng = np.random.default_rng(13)
+    x, w = rng.normal(size=(rows, dim)), rng.normal(size=(classes, dim)) * 0.2
+    x[:, 0] = 0.5 + rng.uniform(size=rows)
+    labels = rng.integers(4, classes, rows)
+    labels[[3, 149]] = -1
+    x[3] = 0.0
+    bias = rng.normal(size=classes)
+    out = np.where(np.arange(classes) == 3, -np.inf, bias)     # the same, by the class's bias
+    t = Loss(V, dt, rows, dim, classes, bias=out, x=x, w=w, labels=labels)
+    t.run()
+    t.check()
+    w[3, 0] = -np.inf
+    u = Loss(V, dt, rows, dim, classes, bias=bias, x=x, w=w, labels=labels)
+    u.dl.copy_(t.dl)
+    u.run()
+    torch.cuda.synchronize()
+    has = torch.from_numpy(labels >= 0).cuda()
+    assert torch.equal(t.loss[:rows], u.loss[:rows]) and torch.equal(t.lse[:rows][has], u.lse[:rows][has])
+    assert torch.equal(t.dw.t, u.dw.t) and torch.equal(t.db, u.db)
 
 
 def test_softmax_loss_of_no_class_at_all(V):
