@@ -56,6 +56,24 @@ class Eight:
         return (v * torch.pow(2.0, e).repeat_interleave(V.VFL_Q8_BLOCK, 1))[:, :cols]
 
 
+def _rows_apart(t: torch.Tensor) -> bool:
+    # a stride of 0 would stand for contiguous rows
+    return t.stride(1) == 1 and (t.shape[0] == 1 or t.stride(0) >= t.shape[1])
+
+
+class _Room:
+    """Device memory that calls may use one after another.  What a size outgrows stays:
+    a captured graph may hold it."""
+
+    def __init__(self, size: int, device):
+        self.all = [torch.empty(max(size, 1), dtype=torch.uint8, device=device)]
+
+    def put(self, a, size: int):
+        if size > self.all[-1].numel():
+            self.all.append(torch.empty(size, dtype=torch.uint8, device=self.all[-1].device))
+        a.workspace, a.workspace_bytes = self.all[-1].data_ptr(), self.all[-1].numel()
+
+
 def _device(device):
     d = torch.device(device)
     return d if d.index is not None else torch.device(d.type, torch.cuda.current_device())
@@ -106,13 +124,10 @@ class EightTower:
         for m, n, k in sizes:
             for r in {max_rows} | {1 << i for i in range(max_rows.bit_length())}:
                 need.append(V.vfl_matmul8_workspace_size(r if m == max_rows else m, n, r if k == max_rows else k))
-        self.ws = torch.empty(max(max(need), 1), dtype=torch.uint8, device=self.dev)
+        need += [V.vfl_norm_workspace_size(max_rows, min(hidden, V.VFL_NORM_MAX_COLS))]
+        self.ws = _Room(max(need), self.dev)
+        self.no_stats = torch.zeros((max_rows, 2), device=self.dev)
         self.refresh()
-
-    def _workspace(self, a, size: int):
-        if size > self.ws.numel():
-            self.ws = torch.empty(size, dtype=torch.uint8, device=self.dev)
-        a.workspace, a.workspace_bytes = self.ws.data_ptr(), self.ws.numel()
 
     # --------------------------------------------------------------- the calls
     def _quantize(self, t: torch.Tensor, q: Eight | None, qt: Eight | None, st: int):
@@ -135,7 +150,7 @@ class EightTower:
         _set(a.c, c)
         if bias is not None:
             a.bias = bias.data_ptr()
-        self._workspace(a, V.vfl_matmul8_workspace_size(m, n, k))
+        self.ws.put(a, V.vfl_matmul8_workspace_size(m, n, k))
         V.vfl_matmul8(a, st)
 
     def _norm(self, l: int, rows: int, x: torch.Tensor, r: torch.Tensor | None, s: torch.Tensor | None, st: int):
@@ -160,7 +175,7 @@ class EightTower:
         if ds is not None:
             _set(a.ds, ds[:rows])
         _set(a.dx, dx[:rows])
-        self._workspace(a, V.vfl_norm_workspace_size(rows, self.width))
+        self.ws.put(a, V.vfl_norm_workspace_size(rows, self.width))
         V.vfl_rmsnorm_backward(a, st)
 
     def _weight_grad(self, d: torch.Tensor, x: torch.Tensor, name: str, st: int):
@@ -170,6 +185,19 @@ class EightTower:
         self._quantize(d, None, a8, st)
         self._quantize(x, None, b8, st)
         self._product(a8, b8, n, k, rows, self.grads[name], st)
+
+    def _column_sums(self, d: torch.Tensor, out: torch.Tensor, st: int):
+        """The sum of d over its rows: a layer norm's dbeta, in an order that the sizes
+        fix."""
+        for c in range(0, d.shape[1], V.VFL_NORM_MAX_COLS):
+            part = d[:, c:c + V.VFL_NORM_MAX_COLS]
+            a = V.vfl_layernorm_args()
+            a.dtype, (a.rows, a.cols), a.eps = V.VFL_BF16, part.shape, EPS
+            for m in (a.x, a.dy):
+                m.data, m.ld = part.data_ptr(), d.shape[1]
+            a.stats, a.dbeta = self.no_stats.data_ptr(), out[c:].data_ptr()
+            self.ws.put(a, V.vfl_norm_workspace_size(a.rows, a.cols))
+            V.vfl_layernorm_backward(a, st)
 
     def refresh(self):
         """Rewrite the copies in 8 bits from the masters."""
@@ -184,8 +212,8 @@ class EightTower:
         next forward overwrites.  Only a training forward can be followed by
         ``backward``."""
         if (x.dim() != 2 or not 1 <= x.shape[0] <= self.max_rows or x.shape[1] != self.d_in
-                or x.dtype != torch.bfloat16 or x.device != self.dev or x.stride(1) != 1):
-            raise ValueError(f"x must be [1..{self.max_rows} x {self.d_in}] of bfloat16 on {self.dev}")
+                or x.dtype != torch.bfloat16 or x.device != self.dev or not _rows_apart(x)):
+            raise ValueError(f"x must be [1..{self.max_rows} x {self.d_in}] of bfloat16 on {self.dev}, rows apart")
         rows, W = x.shape[0], self.W
         self.trained = 0
         with torch.cuda.device(self.dev):
@@ -222,7 +250,7 @@ class EightTower:
                 self._quantize(d, self.dq[self.width], None, st)
                 self._product(self.dq[self.width], self.WT[f"W2.{l}"], rows, self.hidden, self.width, dh, st)
                 dh.mul_(h > 0)
-                torch.sum(dh, 0, dtype=torch.float32, out=G[f"b.{l}"])
+                self._column_sums(dh, G[f"b.{l}"], st)
                 self._weight_grad(dh, self.y[l][:rows], f"W1.{l}", st)
                 self._quantize(dh, self.dq[self.hidden], None, st)
                 self._product(self.dq[self.hidden], self.WT[f"W1.{l}"], rows, self.width, self.hidden, self.dy[:rows], st)
@@ -252,7 +280,7 @@ class ClassHead:
         self.dbias = torch.empty_like(self.bias)
         self.losses, self.lse = (torch.empty(max_rows, device=self.dev) for _ in range(2))
         self.dz = torch.empty((max_rows, dim), dtype=torch.bfloat16, device=self.dev)
-        self.ws = torch.empty(0, dtype=torch.uint8, device=self.dev)
+        self.ws = _Room(V.vfl_softmax_loss_workspace_size(V.VFL_BF16, max_rows, dim, classes), self.dev)
 
     @torch.no_grad()
     def loss(self, z: torch.Tensor, labels: torch.Tensor, train: bool = True):
@@ -260,8 +288,8 @@ class ClassHead:
         the classes: a row without one), and the gradient of their mean over the
         rows with respect to z (None without ``train``): views that the next call overwrites."""
         if (z.dim() != 2 or not 1 <= z.shape[0] <= self.max_rows or z.shape[1] != self.dim or z.dtype != torch.bfloat16
-                or z.device != self.dev or z.stride(1) != 1):
-            raise ValueError(f"z must be [1..{self.max_rows} x {self.dim}] of bfloat16 on {self.dev}")
+                or z.device != self.dev or not _rows_apart(z)):
+            raise ValueError(f"z must be [1..{self.max_rows} x {self.dim}] of bfloat16 on {self.dev}, rows apart")
         rows = z.shape[0]
         if labels.shape != (rows,) or labels.dtype != torch.int32 or labels.device != self.dev or not labels.is_contiguous():
             raise ValueError(f"labels must be {rows} contiguous int32 values on {self.dev}")
@@ -273,10 +301,7 @@ class ClassHead:
                 _set(m, t)
             a.bias, a.labels, a.loss, a.lse, a.dbias = (t.data_ptr() for t in (self.bias, labels, self.losses, self.lse,
                                                                               self.dbias))
-            size = V.vfl_softmax_loss_workspace_size(V.VFL_BF16, rows, self.dim, self.classes)
-            if size > self.ws.numel():
-                self.ws = torch.empty(size, dtype=torch.uint8, device=self.dev)
-            a.workspace, a.workspace_bytes = self.ws.data_ptr(), self.ws.numel()
+            self.ws.put(a, V.vfl_softmax_loss_workspace_size(V.VFL_BF16, rows, self.dim, self.classes))
             V.vfl_softmax_loss_forward(a, st)
             if train:
                 V.vfl_softmax_loss_backward(a, st)

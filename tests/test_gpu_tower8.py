@@ -131,6 +131,57 @@ def test_refusals():
             head.loss(*args)
 
 
+def test_rows_that_are_one_row():
+    """An expanded row's stride of 0 is not a matrix of that many rows."""
+    from paper_2510_12494_amd.tower8 import ClassHead, EightTower
+    t, head = EightTower(16, 64, 64, 1, 32), ClassHead(64, 10, 32)
+    one = torch.zeros(1, 64, dtype=torch.bfloat16, device="cuda")
+    lab = torch.zeros(8, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        t.forward(one[:, :16].expand(8, 16))
+    with pytest.raises(ValueError):
+        head.loss(one.expand(8, 64), lab)
+    with pytest.raises(ValueError):
+        t.forward(torch.as_strided(torch.zeros(256, dtype=torch.bfloat16, device="cuda"), (8, 16), (8, 1)))
+
+
+def test_a_captured_step_is_the_eager_one():
+    """Forward, head and backward in a graph, replayed between eager steps of other
+    sizes, which use the same workspaces."""
+    from paper_2510_12494_amd.tower8 import ClassHead, EightTower
+    t, head = EightTower(40, 128, 320, 2, 3000, seed=6), ClassHead(128, 500, 3000, seed=7)
+    g = torch.Generator().manual_seed(9)
+    x = torch.zeros(2000, 40, dtype=torch.bfloat16, device="cuda")
+    lab = torch.zeros(2000, dtype=torch.int32, device="cuda")
+
+    def step(n):
+        loss, dz = head.loss(t.forward(x[:n]), lab[:n])
+        t.backward(dz)
+        return loss
+
+    def results(n):
+        torch.cuda.synchronize()
+        return [head.losses[:n].clone(), head.dW.clone(), head.dbias.clone()] + [v.clone() for v in t.grads.values()]
+
+    step(2000)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(2000)
+    for i in range(4):
+        x.copy_(torch.randn(2000, 40, generator=g))
+        lab.copy_(torch.randint(0, 500, (2000,), generator=g))
+        step(2000)
+        want = results(2000)
+        step(77 + 300 * i)
+        for v in t.grads.values():
+            v.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(want, results(2000)))
+        assert float(want[0].sum()) > 0 and all(float(v.abs().sum()) > 0 for v in want)
+
+
 def test_example_runs_and_learns_its_items(capsys):
     spec = importlib.util.spec_from_file_location("eight_bit_towers", os.path.join(ROOT, "examples", "eight_bit_towers.py"))
     m = importlib.util.module_from_spec(spec)
