@@ -188,12 +188,32 @@ __device__ __forceinline__ uint32_t quarters_max(uint32_t v) {
   return max((uint32_t)b[0], (uint32_t)b[1]);
 }
 
+// Chunks as they are stored: value i, and a chunk of values of the storage type.
+__device__ __forceinline__ float value(const Raw<uint16_t>& r, int i) {
+  return __uint_as_float(i & 1 ? r.a[i / 2] & 0xffff0000u : r.a[i / 2] << 16);
+}
+__device__ __forceinline__ float value(const Raw<float>& r, int i) { return i < 4 ? r.a[i] : r.b[i - 4]; }
+__device__ __forceinline__ void hold(Raw<uint16_t>& r, const float (&v)[8]) {
+  r.a = u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+}
+__device__ __forceinline__ void hold(Raw<float>& r, const float (&v)[8]) {
+  r.a = f32x4{v[0], v[1], v[2], v[3]};
+  r.b = f32x4{v[4], v[5], v[6], v[7]};
+}
+// What follows unpacks the chunk again instead of holding its values.
+__device__ __forceinline__ void again(Raw<uint16_t>& r) { asm volatile("" : "+v"(r.a)); }
+__device__ __forceinline__ void again(Raw<float>&) {}
+
 // A workgroup takes 128 x 128 values, a thread eight rows of a chunk of eight
 // columns: its rows' blocks are 16 lanes wide, its columns' blocks the workgroup's
 // 16 groups of them, which meet in LDS.  A thread's eight rows of a column are
-// eight consecutive bytes of the transpose.
+// eight consecutive bytes of the transpose.  HBM bounds it, and what keeps it busy is
+// the number of tiles in flight: a thread holds its values as they are stored and
+// unpacks them for each pass (four wavefronts a SIMD in bf16; two with 64 floats
+// held).  32768 x 1024 bf16, 64 MB in and 67 out, from memory: 33 us, 38 with floats
+// held (131072 x 200: 33, 47); without the transpose 22, 27.
 template <typename T, Form F>
-__global__ __launch_bounds__(kThreads) void k_quantize(QuantArgs j) {
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) void k_quantize(QuantArgs j) {
   __shared__ uint32_t tops[2][4][128];
   const Cols k(j.cols, j.rows);
   const int lane = threadIdx.x & 15, group = threadIdx.x >> 4, wave = threadIdx.x >> 6;
@@ -203,42 +223,52 @@ __global__ __launch_bounds__(kThreads) void k_quantize(QuantArgs j) {
     const int tn = (int)(t - tm * j.tn);
     const int64_t r0 = 128 * tm + 8 * group;
     const int q = 16 * tn + lane;
-    float v[8][8];
+    Raw<T> x[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int64_t r = min(r0 + i, j.rows - 1);
-      const bool edge = r >= k.edge;
-      chunk_values<F>(load_chunk<F>(row_of<T>(j.x, r), q, k, edge), q, k, edge, v[i]);
-      if (r0 + i >= j.rows) {
-#pragma unroll
-        for (int c = 0; c < 8; ++c) v[i][c] = 0.f;
-      }
+      x[i] = load_chunk<F>(row_of<T>(j.x, r), q, k, r >= k.edge);
     }
     // the rows' and the thread's largest magnitudes; what is no number shows in them
     uint32_t top[8], most = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      top[i] = chunk_max(v[i]);
+      const int64_t r = min(r0 + i, j.rows - 1);
+      float v[8];
+      chunk_values<F>(x[i], q, k, r >= k.edge, v);
+      if (F != kExact) hold(x[i], v);
+      top[i] = chunk_max(v);
+      if (r0 + i >= j.rows) {
+        x[i] = Raw<T>{};
+        top[i] = 0;
+      }
       most = max(most, top[i]);
+      again(x[i]);
     }
     if (__any(most >= kInfinite)) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
+        float v[8];
+        unpack(x[i], v);
         top[i] = 0;
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
-          top[i] = max(top[i], number_magnitude(v[i][c]));
-          v[i][c] = number_or_nan(v[i][c]);
+          top[i] = max(top[i], number_magnitude(v[c]));
+          v[c] = number_or_nan(v[c]);
         }
+        hold(x[i], v);
       }
     }
     if (j.q.p) {
       u32x2 bytes = {0u, 0u};
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
+        float v[8];
+        unpack(x[i], v);
         const uint32_t b = scale_byte(block_max(top[i]));
         bytes[i / 4] |= b << (8 * (i % 4));
-        if (r0 + i < j.rows) *(u32x2*)(j.q.p + (r0 + i) * j.q.ld + 8 * (int64_t)q) = pack_e4m3(v[i], inverse_scale(b));
+        if (r0 + i < j.rows) *(u32x2*)(j.q.p + (r0 + i) * j.q.ld + 8 * (int64_t)q) = pack_e4m3(v, inverse_scale(b));
+        again(x[i]);
       }
       if (lane == 0 && r0 < j.rows) *(u32x2*)(j.q.scale + tn * j.q.scale_ld + r0) = bytes;
     }
@@ -249,13 +279,15 @@ __global__ __launch_bounds__(kThreads) void k_quantize(QuantArgs j) {
         m[c] = 0;
         if (most < kInfinite) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) m[c] = max(m[c], magnitude(v[i][c]));
+          for (int i = 0; i < 8; ++i) m[c] = max(m[c], magnitude(value(x[i], c)));
         } else {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) m[c] = max(m[c], number_magnitude(v[i][c]));
+          for (int i = 0; i < 8; ++i) m[c] = max(m[c], number_magnitude(value(x[i], c)));
         }
         m[c] = quarters_max(m[c]);
       }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) again(x[i]);
       if ((threadIdx.x & 63) < 16) {
         *(u32x4*)&tops[flip][wave][8 * lane] = u32x4{m[0], m[1], m[2], m[3]};
         *(u32x4*)&tops[flip][wave][8 * lane + 4] = u32x4{m[4], m[5], m[6], m[7]};
@@ -278,7 +310,7 @@ __global__ __launch_bounds__(kThreads) void k_quantize(QuantArgs j) {
       for (int c = 0; c < 8; ++c) {
         float w[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = v[i][c];
+        for (int i = 0; i < 8; ++i) w[i] = value(x[i], c);
         const uint32_t b = (bytes[c / 4] >> (8 * (c % 4))) & 255u;
         const int64_t col = 8 * (int64_t)q + c;
         if (col < j.cols) *(u32x2*)(j.qt.p + col * j.qt.ld + r0) = pack_e4m3(w, inverse_scale(b));
