@@ -534,10 +534,10 @@ template <> struct Tiles<uint16_t> {
 template <> struct Tiles<float> {
   typedef Tile<kF32, 128, 128, 2, 2, 64, 2, kBlocks> Long;
   typedef Tile<kF32, 128, 128, 2, 2, 64, 2, kBlocks> Short;
-  typedef Tile<kF32, 64, 64, 2, 2, 128, 3, kBlocks> Few;
+  typedef Tile<kF32, 64, 64, 2, 2, 128, 2, kBlocks> Few;
   typedef Few Tiny;
   template <bool BOTH> using Large = SumTile<kF32, 128, 128, 2, 2, 64, 2, BOTH>;
-  template <bool BOTH> using Small = SumTile<kF32, 64, 64, 2, 2, 128, 3, BOTH>;
+  template <bool BOTH> using Small = SumTile<kF32, 64, 64, 2, 2, 128, 2, BOTH>;
   template <bool BOTH> using Least = Small<BOTH>;
 };
 
@@ -577,7 +577,7 @@ Pass pass(int64_t m, int64_t n, int64_t depth) {
     return cut_up(m, n, bm, bn, (int)tiles_of(depth, elements), t);
   };
   Pass p{cut(L::BM, L::BN, L::kElements, bf16 ? StepTime{2.05, 2.05, 1} : StepTime{1.07, 1.3, 4}), kLargeSum};
-  const Cut s = cut(S::BM, S::BN, S::kElements, bf16 ? StepTime{0.67, 0.8, 2} : StepTime{0.58, 0.8, 3});
+  const Cut s = cut(S::BM, S::BN, S::kElements, bf16 ? StepTime{0.67, 0.8, 2} : StepTime{0.58, 0.8, 4});
   if (s.us < p.us) p = {s, kSmallSum};
   if (bf16) {
     const Cut e = cut(E::BM, E::BN, E::kElements, StepTime{0.22, 0.5, 3});
