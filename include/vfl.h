@@ -638,9 +638,10 @@ vfl_status vfl_matmul8(const vfl_matmul8_args* a, void* stream);
  * gradient of 0.  G is rounded to `dtype` once, as the operand of its products;
  * their sums are float32.
  *   The workspace (16-byte aligned, vfl_softmax_loss_workspace_size() bytes: copies
- * of x and w in the products' layout and pieces of G of 256 MB or one piece of 256
- * classes) means nothing between calls; calls that may run at the same time need
- * one each.  Fields that a direction does not use are ignored. */
+ * of x and w in the products' layout, and G in pieces of all rows by as many classes as
+ * 1 GB holds, 256 at least) means nothing between calls; calls that may run at the
+ * same time need one each.  No element that is written may be one that is read.
+ * Fields that a direction does not use are ignored. */
 #define VFL_LOSS_MAX_ROWS 2097152
 #define VFL_LOSS_MAX_CLASSES 2097152
 #define VFL_LOSS_MAX_DIM 32768

@@ -594,7 +594,10 @@ int rows_of(Size s) {
                           : TS::template Least<true>::BN;
 }
 
-constexpr int64_t kPiece = 256 << 20;  // bytes of G
+// Bytes of G.  A piece's products cut their sums into parts where it has few classes, and
+// what the parts cost is paid for each piece (8192 x 256 rows, 100000 classes: 2.58 ms in
+// pieces of 256 MB, 2.51 of 512, 2.40 of 1 GB, 2.31 where those are of a size).
+constexpr int64_t kPiece = 1 << 30;
 
 // Where things lie in the workspace, and how the classes are cut up.
 struct Plan {
@@ -625,6 +628,8 @@ Plan plan(int64_t rows, int dim, int64_t classes) {
   p.all = round_up(classes, p.bm);                   // a step of every product divides a tile's classes
   const int64_t most = kPiece / ((int64_t)sizeof(T) * p.rows_pad) / p.bm * p.bm;
   p.piece = std::min<int64_t>(p.all, std::max<int64_t>(p.bm, most));
+  p.pieces = (p.all + p.piece - 1) / p.piece;
+  p.piece = round_up((p.all + p.pieces - 1) / p.pieces, p.bm);
   p.pieces = (p.all + p.piece - 1) / p.piece;
   p.to_x = pass<T>(dim, rows, p.piece);
   p.to_w = pass<T>(dim, p.piece, rows);

@@ -189,7 +189,7 @@ def test_workspaces_of_extreme_sizes(V):
             e = 4 if dt == V.VFL_F32 else 2
             assert size >= (rows + classes) * dim * e
             pairs = rows * max(classes // 64 + 2, 512) * 8                   # the forward's
-            piece = max(256 << 20, rows * 512 * e + (1 << 20)) * 1.01 + 2**20
+            piece = max(1 << 30, rows * 512 * e + (1 << 20)) * 1.01 + 2**20
             sums = (64 * rows + 128 * 2**20 // max(dim, 1) + classes * 66) * (dim + 256) * 4
             assert size <= 2 * ((rows + classes) * (dim + 64) * e) + pairs + piece + sums + 2**30
     m = V.vfl_matmul8_workspace_size

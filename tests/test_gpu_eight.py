@@ -641,13 +641,53 @@ def test_softmax_loss_of_far_logits(V, dt):
     t.check()
 
 
-@pytest.mark.parametrize("dt,rows,classes", [("bf16", 30000, 9000), ("f32", 20000, 6800)])
-def test_softmax_loss_in_pieces(V, dt, rows, classes):
-    """More classes than one piece of the gradient holds."""
-    t = Loss(V, dt, rows, 24, classes)
-    assert rows * classes * (2 if dt == "bf16" else 4) > 2 * 256 << 20
+@pytest.mark.parametrize("dt,rows,dim,classes", [("bf16", 131000, 24, 8300), ("f32", 53000, 20, 10300), ("bf16", 270, 40, 2090001)])
+def test_softmax_loss_in_pieces(V, dt, rows, dim, classes):
+    """More classes than one piece of the gradient holds, against float64 on the device,
+    rows at a time, with the bounds of Loss.check."""
+    assert rows * classes * (2 if dt == "bf16" else 4) > 1 << 30
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    t = Loss(V, dt, rows, dim, classes, x=np.zeros((rows, 1)), w=np.zeros((classes, 1)))
+    t.w.t.copy_(torch.randn(classes, dim, generator=g, device="cuda") * 1.5 / dim ** 0.5)
+    labels = torch.from_numpy(t.labels).cuda()
+    t.x.t.copy_(torch.randn(rows, dim, generator=g, device="cuda") + 2 * torch.rand(rows, 1, generator=g, device="cuda") * t.w.t[labels].float())
     t.run()
-    t.check()
+    torch.cuda.synchronize()
+    w, b, d = t.w.t.double(), t.bias[:classes].double(), t.dl[:rows].double()
+    half = 2.0 ** -8 if dt == "bf16" else 0.0
+    rounding = 2.0 ** -8 if dt == "bf16" else U
+    zero = lambda *s: torch.zeros(s, dtype=torch.float64, device="cuda")  # noqa: E731
+    dw, dw_bound, db, db_bound, all_dw = zero(classes, dim), zero(classes, dim), zero(classes), zero(classes), zero(classes, dim)
+    all_db = zero(classes)
+    step = max(1, (1 << 27) // classes)
+    for r in range(0, rows, step):
+        x, lab, lse, dd = t.x.t[r:r + step].double(), labels[r:r + step], t.lse[:rows][r:r + step].double(), d[r:r + step, None]
+        one = torch.arange(len(x), device="cuda")
+        z = torch.addmm(b, x, w.T)
+        ez = (dim / 4 + 16) * U * (x.abs() @ w.abs().T) + 3 * U * b.abs() + 4 * U * z.abs()
+        want = torch.logsumexp(z, 1)
+        top = ez.amax(1) + (SUM + 64 + classes / 128) * U + 6 * U * want.abs()
+        assert float(((lse - want).abs() - SLACK * top).max()) <= 0
+        G = dd * torch.exp(z - lse[:, None])
+        p = G.clone()
+        G[one, lab] -= dd[:, 0]
+        p[one, lab] += dd[:, 0]
+        eg = p * (ez + 4 * U * lse.abs()[:, None] + 10 * U) + 2.0 ** -126 * (dd + 1)
+        e = eg + half * G.abs()
+        dx, size = G @ w, G.abs() @ w.abs()
+        bound = SLACK * (e @ w.abs() + (classes / 4 + 32) * U * size)
+        assert float(((t.dx.t[r:r + step].double() - dx).abs() - bound - rounding * (dx.abs() + bound)).max()) <= 0
+        dw += G.T @ x
+        dw_bound += e.T @ x.abs()
+        all_dw += G.abs().T @ x.abs()
+        db += G.sum(0)
+        db_bound += eg.sum(0)
+        all_db += G.abs().sum(0)
+    bound = SLACK * (dw_bound + (rows / 4 + 32) * U * all_dw)
+    assert float(((t.dw.t.double() - dw).abs() - bound - rounding * (dw.abs() + bound)).max()) <= 0
+    assert float(((t.db[:classes].double() - db).abs() - SLACK * (db_bound + (rows / 64 + 128) * U * all_db)).max()) <= 0
+    for m in (t.x, t.w, t.dx, t.dw):
+        m.assert_guard()
 
 
 @pytest.mark.parametrize("rows,dim,classes", [(2100, 60, 70001), (300, 128, 263000), (600, 136, 263000), (2049, 250, 66000)])
