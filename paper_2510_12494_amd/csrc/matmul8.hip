@@ -18,10 +18,11 @@ typedef Tile<kE4m3, 256, 256, 4, 4, 128, 2> Large;
 typedef Tile<kE4m3, 128, 128, 2, 2, 128, 2> Small;
 typedef Tile<kE4m3Wide, 128, 128, 2, 2, 128, 2> Wide;     // of float32 results
 
-// Few rows (16 MT at most): a workgroup takes 16 columns, its wavefronts the blocks of
-// the sum in turn, straight from global memory into the MFMA's operands; their
-// results meet in LDS.  The rows of B are read once, 128 bytes of 16 of them a
-// wavefront, and that or the latency of one such step bounds it.
+// Few rows, or little work: a workgroup takes 16 columns of 16 MT rows, its wavefronts
+// the blocks of the sum in turn, straight from global memory into the MFMA's operands;
+// their results meet in LDS.  The rows of B are read once (for each 16 MT rows of A), 128
+// bytes of 16 of them a wavefront, and that or the latency of one such step bounds it: 1 x
+// 1024 x 1024 3.3 us (5.8 with the call, 9.1 in tiles); 16 x 8192 x 8192 18 us, 3.7 TB/s.
 struct RowsArgs {
   Operand a, b;
   void* c;

@@ -57,7 +57,10 @@ __device__ __forceinline__ void store_to(T* p, const f32x4& v, int left) {
 }
 
 // One tile of the product, or (parts > 1) of a part of its sum, as float32 partial
-// sums [part][m][n].
+// sums [part][m][n].  A lane stores four columns of a row at once, 16 lanes 128 bytes of
+// bf16.  The matrix cores bound long sums (8192 x 8192 x 4096 in 8 bits: 240 us, 2.3
+// PFLOP/s); where the sum is short a workgroup's first copies and its stores have
+// nothing beside them (32768 x 512 x 1024: 22 us, of which the products are 14).
 template <class TL, typename T>
 __global__ __launch_bounds__(TL::kThreads) void k_product(ProductArgs j) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -92,8 +95,36 @@ __global__ __launch_bounds__(TL::kThreads) void k_product(ProductArgs j) {
   }
 }
 
+// What a row's sum gets on top where its label's term was rounded: `rest` [rows], times
+// `factor` and the label's row of w (null: nothing).
+struct LabelTerm {
+  const float* rest;
+  const int32_t* labels;
+  const uint16_t* w;
+  int64_t ld, classes;                 // elements from row to row
+  float factor;
+};
+template <int N>
+__device__ __forceinline__ void add_label_term(const LabelTerm& j, int64_t row, int col, float* v) {
+  const int label = j.labels[row];
+  if (label < 0 || label >= j.classes) return;
+  const float rest = j.rest[row] * j.factor;
+  const uint16_t* const p = j.w + label * j.ld + col;
+#pragma unroll
+  for (int i = 0; i < N; i += 4) {
+    const u32x2 w = *(const u32x2*)(p + i);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      v[i + k] = fmaf(rest, __uint_as_float(k & 1 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16), v[i + k]);
+  }
+}
+
 // A tile of C^T, C [n x m]: results of sum-major operands (gemm.h), or partial sums
-// of them [part][n][m].
+// of them [part][n][m].  Each operand is read as it lies in memory, so neither G nor
+// the weights are ever transposed there; a lane stores 4 D consecutive columns of C.
+// bf16 over 50176 classes: dx of 8192 x 256 rows at 810 to 850 TFLOP/s, dw at 840 to 910,
+// G coming from HBM once for each; float32, 1537 x 333 rows over 5003 classes: both 144 us,
+// 71 TFLOP/s of 154 (333 columns fill 384 of tiles; two library products take 122).
 struct SumArgs {
   SumMajor a, bs;
   Operand b;
@@ -101,6 +132,8 @@ struct SumArgs {
   int64_t ldc, n;
   uint32_t tm, tn, parts;
   int m, steps, per, add, wide;        // wide: results in float32 whatever T
+  float factor;                        // of the sums
+  LabelTerm label;
 };
 // add: on top of what is there (sums of an earlier piece, which are float32)
 template <typename T>
@@ -144,7 +177,8 @@ __device__ __forceinline__ void sum_tile(const SumArgs& j, uint32_t block, char*
         const int col = m0 + tile.a_col(q) + 4 * d;
         float v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = acc[q * TL::D + d + i / 4][f][i % 4];
+        for (int i = 0; i < 8; ++i) v[i] = acc[q * TL::D + d + i / 4][f][i % 4] * j.factor;
+        if (sizeof(T) == 2 && j.label.rest && col < j.m) add_label_term<8>(j.label, row, col, v);
         if (sizeof(T) == 4 || j.wide) store_sums((float*)j.c + out + col, v, j.m - col, j.add);
         else store_sums((T*)j.c + out + col, v, j.m - col, 0);
       }
@@ -155,7 +189,9 @@ __global__ __launch_bounds__(TL::kThreads) void k_sum_product(SumArgs j) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   sum_tile<TL, T>(j, blockIdx.x, smem);
 }
-// Two products in one launch: the first `split` workgroups take the first one.
+// Two products in one launch: the first `split` workgroups take the first one.  Neither
+// fills the card alone where there are few results (8192 x 256 rows over 1000 classes: a
+// step 86 us in two launches, 64 in one); where both do, one launch takes what two take.
 template <class TA, class TB, typename T>
 __global__ __launch_bounds__(TA::kThreads) void k_sum_pair(SumArgs a, SumArgs b, uint32_t split) {
   static_assert(TA::kThreads == TB::kThreads && TA::kLds == TB::kLds);
@@ -171,6 +207,7 @@ struct JoinArgs {
   void* c;
   int64_t ldc, m, items, ld;           // ld: of the partial sums
   int n, quads, parts, relu;
+  LabelTerm label;
 };
 
 // The parts of a split product, summed in a fixed order: SL threads take every SL-th
@@ -204,6 +241,11 @@ __device__ __forceinline__ void join_block(const JoinArgs& j, uint32_t block) {
       if (slice > 0) return;
 #pragma unroll
       for (int i = 1; i < SL; ++i) v += sums[i][q];
+    }
+    if (j.label.rest && live) {
+      float w[4] = {v[0], v[1], v[2], v[3]};
+      add_label_term<4>(j.label, row, col, w);
+      v = f32x4{w[0], w[1], w[2], w[3]};
     }
     if (live) store_to((T*)j.c + row * j.ldc + col, finish(v, bias4(j.bias, col, j.n), j.relu), j.n - col);
     at += kJoinGrid * Q;
@@ -264,7 +306,7 @@ hipError_t product(const ProductArgs& a, hipStream_t st) {
 // parts [parts][m][part_ld(n)] -> c
 JoinArgs join_args(const float* part, int parts, int64_t m, int64_t n, const float* bias, int relu, const Mat& c) {
   const int64_t ld = part_ld(n), items = m * (ld / 4);
-  return {part, bias, c.p, c.ld, m, items, ld, (int)n, (int)(ld / 4), parts, relu};
+  return {part, bias, c.p, c.ld, m, items, ld, (int)n, (int)(ld / 4), parts, relu, LabelTerm{}};
 }
 bool joins_in_slices(const JoinArgs& a) { return a.parts >= 16 && a.items <= 65536; }
 int64_t join_blocks(const JoinArgs& a) {

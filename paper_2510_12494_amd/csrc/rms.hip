@@ -74,7 +74,9 @@ __device__ __forceinline__ double inverse_root(double v) {
 // block of 128 columns, so a block's largest magnitude is four exchanges away.
 // The sum of squares is taken in 64 bits: products of float32 values are exact
 // there, so k does not depend on the order of the sum and the same row gives the
-// same 8-bit values whatever the batch, the width's layout or the machine.
+// same 8-bit values whatever the batch, the width's layout or the machine.  HBM bounds
+// it: 32768 x 1024 bf16, x and r in, s, 8 bits and k out, 235 MB: 35 us beside the
+// last-level cache, 42 from memory (5.6 TB/s); one row 2.6 us, latency.
 template <typename T, int G, int CH, Form F>
 __global__ __launch_bounds__(G > kThreads ? G : kThreads) void k_rms_forward(RmsArgs j) {
   constexpr bool WIDE = G > 64;

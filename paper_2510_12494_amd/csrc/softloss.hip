@@ -11,10 +11,16 @@
 // type, and two products read it, one along its rows and one along its columns.
 //
 // Exponentials and sums are taken to base 2 (z log2 e is one multiplication-addition
-// with the bias, and the hardware's exponential is to base 2); one below 2^-126 is 0.  A class whose bias
-// is -inf, and a column past the last class, is out of every sum whatever its
-// weights hold; a row without a label has a gradient of 0 whatever its input holds.
+// with the bias, and the hardware's exponential is to base 2); one below 2^-126 is 0.
+// A class whose bias is -inf, and a column past the last class, is out of every sum
+// whatever its weights hold; a row without a label has a gradient of 0 whatever its
+// input holds.
+//
+// Of 8192 x 256 bf16 rows over 100000 classes (six products of 2 x 8192 x 256 x 100000,
+// 0.98 ms at a library product's rate) a step takes 2.31 ms: copies of the operands
+// 18 us, k_strip 440 to 480, G 2 x 360, both products 2 x 560, what is summed 20.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "ops8.h"
@@ -24,6 +30,9 @@ namespace vfl {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// what undoes the multiplication by kLog2e as float32 has it, in two parts
+constexpr double kUnit = 1.0 / (double)kLog2e;
+constexpr float kUnitHigh = (float)kUnit, kUnitLow = (float)(kUnit - (double)kUnitHigh);
 constexpr int kThreads = 256;
 
 template <typename T> constexpr int kRow = 128 / (int)sizeof(T);    // elements that operands' rows are padded to
@@ -35,6 +44,7 @@ struct CopyArgs {
   Mat src;
   void* dst;
   int64_t dst_ld, rows;                // elements from row to row
+  int64_t wrap;                        // rows of the copy, `rows` and zeros, that it holds twice (0: once, no zeros)
   const int32_t* labels;               // rows without a label are 0 (null: all are kept)
   const float* bias;                   // rows whose bias is -inf are 0
   int64_t classes;
@@ -42,26 +52,27 @@ struct CopyArgs {
 };
 
 // Rows padded with zeros to whole steps of a product, those that must not reach it
-// as zeros: eight columns a thread.
+// as zeros: eight columns a thread, both matrices in one launch (1537 and 5003 rows of
+// 333 float32: 7.3 us, of which the launch is 3; HBM bounds larger ones).
 constexpr int kPadGrid = 16384;
 template <typename T, Form F>
 __device__ __forceinline__ void pad(const CopyArgs& j, uint32_t block) {
   const Cols k(j.cols, j.rows);
   const int per = (int)(j.dst_ld / 8);
-  const int64_t chunks = j.rows * per;
+  const int64_t chunks = (j.wrap ? 2 * j.wrap : j.rows) * per;
   for (int64_t at = (int64_t)block * kThreads + threadIdx.x; at < chunks; at += (int64_t)kPadGrid * kThreads) {
-    const int64_t r = at / per;
-    const int q = (int)(at - r * per);
+    const int64_t to = at / per, from = j.wrap && to >= j.wrap ? to - j.wrap : to, r = min(from, j.rows - 1);
+    const int q = (int)(at - to * per);
     const bool edge = r >= k.edge;
     float v[8];
     chunk_values<F>(load_chunk<F>(row_of<T>(j.src, r), q, k, edge), q, k, edge, v);
-    const bool keep = (!j.labels || (j.labels[r] >= 0 && j.labels[r] < j.classes)) &&
+    const bool keep = from < j.rows && (!j.labels || (j.labels[r] >= 0 && j.labels[r] < j.classes)) &&
                       (!j.bias || !(j.bias[r] == -__builtin_inff()));
     if (!keep) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = 0.f;
     }
-    store8<false>((T*)j.dst + r * j.dst_ld + 8 * q, v);
+    store8<false>((T*)j.dst + to * j.dst_ld + 8 * q, v);
   }
 }
 // two matrices of as many columns: the first `split` workgroups take the first one
@@ -83,6 +94,8 @@ struct LogitArgs {
   const float *lse, *dloss;
   const int32_t* labels;
   float scale;
+  int64_t rest;                        // rows of G to that of what its rounding leaves (0: none)
+  float* label_rest;                   // [rows]: or what the label's rounding leaves (null: not kept)
   int64_t first, all_classes;          // the piece's first class
   void* g;
   int64_t g_ld;
@@ -128,7 +141,13 @@ constexpr int logits_lds() { return TL::kLds + 4 * TL::BM + 12 * TL::BN; }
 // A tile of classes x rows: with the classes as the MFMA's rows a lane holds 16
 // consecutive classes (4 DM in general) of each of its batch rows, so a row's
 // largest value and sum are mostly over a lane's own registers, what G needs of a
-// row is loaded once a lane, and G is stored 16 bytes at a time.
+// row is loaded once a lane, and G is stored 16 bytes at a time.  The matrix cores and
+// then the vector units bound it, which overlap only between workgroups: two a CU and
+// tiles of 256 x 128 where rows are short (G of 8192 x 256 rows and 50176 classes: 360
+// us, 585 TFLOP/s with an exponential a logit and 0.8 GB of G written), one of 256 x
+// 256 where they are long (8192 x 1024 rows over 16000 classes, forward: 1.11 PFLOP/s).  float32:
+// 1537 x 333 rows over 5003 classes 60 us, 85 TFLOP/s of 154; a library's product
+// alone takes 62 there.
 template <class TL, typename T, bool GRAD>
 __global__ __launch_bounds__(TL::kThreads) void k_logits(LogitArgs j) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -228,27 +247,49 @@ __global__ __launch_bounds__(TL::kThreads) void k_logits(LogitArgs j) {
       const bool has = row < j.rows && label >= 0 && label < j.all_classes;
       const float lse2 = has && !(lse == -__builtin_inff()) ? lse * kLog2e : __builtin_inff();
       const float d = has ? (j.dloss ? e_d[in] : j.scale) : 0.f;
+      // what rounding lse2 loses, as a factor of the row's exponentials
+      const float low = fabsf(lse2) < __builtin_inff() ? fmaf(lse, kLog2e, -lse2) : 0.f, dp = fmaf(-low * kLn2, d, d);
       const int hit = has ? label - (int)(j.first + mine) : -1;
       float g[RUN];
 #pragma unroll
       for (int t = 0; t < RUN; ++t) g[t] = 0.f;
       if (has) {                                     // whatever the weights hold
 #pragma unroll
-        for (int t = 0; t < RUN; ++t) g[t] = d * exp2_of(fmaf(acc[t / 4][c][t % 4], kLog2e, bias[t]) - lse2);
+        for (int t = 0; t < RUN; ++t) g[t] = dp * exp2_of(fmaf(acc[t / 4][c][t % 4], kLog2e, bias[t]) - lse2);
       }
       if ((unsigned)hit < (unsigned)RUN) {
 #pragma unroll
         for (int t = 0; t < RUN; ++t) g[t] -= hit == t && !(bias[t] == -__builtin_inff()) ? d : 0.f;
+        if constexpr (sizeof(T) == 2) {
+          if (j.label_rest) {
+            float at = 0.f;
+#pragma unroll
+            for (int t = 0; t < RUN; ++t) at = hit == t ? g[t] : at;
+            j.label_rest[row] = at - __uint_as_float(pack_bf16(at, 0.f) << 16);
+          }
+        }
       }
 #pragma unroll
       for (int t = 0; t < RUN; ++t) total[t] += g[t];
       T* const to = (T*)j.g + row * j.g_ld + mine;
+      if (sizeof(T) == 2 && j.rest && row >= j.rest) continue;   // where a second term lies
 #pragma unroll
       for (int t = 0; t < RUN; t += 8) {
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = g[t + i];
         store8<false>(to + t, v);
+        if constexpr (sizeof(T) == 2) {
+          if (j.rest) {
+            float w[8];
+            Raw<uint16_t> stored;
+            stored.a = u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+            unpack(stored, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = v[i] - w[i];
+            store8<false>(to + j.rest * j.g_ld + t, w);
+          }
+        }
       }
     }
     if (j.part_bias) {
@@ -431,7 +472,8 @@ struct FinishArgs {
 };
 
 // A row a group of 16 lanes: the tiles' pairs joined, and the label's logit (whose
-// operands are asked for first: latency bounds this).
+// operands are asked for first: latency bounds this; 3 to 5 us).  The logit is a sum of
+// float32 products of its own, so no tile has to find the row's label among its classes.
 template <typename T, Form F>
 __global__ __launch_bounds__(kThreads) void k_loss(FinishArgs j) {
   const int lane = threadIdx.x & 15;
@@ -470,7 +512,7 @@ __global__ __launch_bounds__(kThreads) void k_loss(FinishArgs j) {
   all = fmaxf(all, dpp<0x140>(all));
   const float from = all == -__builtin_inff() ? 0.f : all;
   sum = group_sum<16>(sum * exp2_of(top - from));
-  const float lse = (all + __builtin_amdgcn_logf(sum)) * kLn2;
+  const float lse = all == -__builtin_inff() ? all : fmaf(all, kUnitHigh, fmaf(all, kUnitLow, __builtin_amdgcn_logf(sum) * kUnitHigh));
   if (j.lse && lane == 0) j.lse[row] = lse;
   if (!j.loss) return;
   z = group_sum<16>(z);
@@ -485,15 +527,17 @@ __global__ __launch_bounds__(kThreads) void k_zero(CopyArgs j) {
 }
 
 // What is summed at a backward pass's end, in one launch: the parts of dx, the parts
-// of dw, and dbias over the tiles' rows, as many workgroups as each has.
-struct BiasArgs { const float* part; float* dbias; int64_t ld, n; int parts; };
+// of dw, and dbias over the tiles' rows, as many workgroups as each has (three launches
+// of 2 to 5 us each for small sizes; HBM bounds large ones: 8 parts of 8192 x 256 and 64
+// of dbias over 100000 classes 20 us).
+struct BiasArgs { const float* part; float* dbias; int64_t ld, n; int parts; float factor; };
 __device__ __forceinline__ void bias_block(const BiasArgs& j, uint32_t block) {
   const int64_t c = (int64_t)block * kThreads + threadIdx.x;
   if (c >= j.n) return;
   float t = 0.f;
 #pragma unroll 8
   for (int i = 0; i < j.parts; ++i) t += j.part[i * j.ld + c];
-  j.dbias[c] = t;
+  j.dbias[c] = t * j.factor;
 }
 struct EndArgs {
   JoinArgs x, w;
@@ -520,7 +564,9 @@ __global__ __launch_bounds__(kThreads) void k_loss_end(EndArgs j) {
 int64_t round_up(int64_t v, int64_t by) { return (v + by - 1) / by * by; }
 
 // The tiles of the logits (classes x rows) and of the products (columns x rows of
-// the result), by what the sizes fill.
+// the result), by what the sizes fill.  float32 64 x 64: two
+// steps of 128 bytes, 32 KB of LDS, let four workgroups on a CU (2048 rows x 512 over 2048 classes:
+// 177 us, 197 in three steps; steps of 64 bytes 180).
 template <typename T> struct Tiles;
 template <> struct Tiles<uint16_t> {
   typedef Tile<kBf16, 256, 256, 4, 4, 128, 2, kBlocks> Long;    // many columns of x
@@ -552,9 +598,11 @@ auto with_tile(Kind k, F f) {
                        : f((typename TS::Tiny*)nullptr);
 }
 
-// The logits' tile: the largest that fills the CUs.  float32 tiles of 64 x 64 until
-// those of 128 x 128 fill them four times: a last round of these that is not full
-// costs more (1537 rows over 5003 classes: 64 us, 87).
+// The logits' tile: the largest that fills the CUs (bf16, a step in the tiles of the
+// rule and in the next larger ones, us: 1000 rows x 1000 over 1000 classes 51, 94; 90 x
+// 90 over 450 26, 37).  float32 tiles of 64 x 64 until those of 128 x 128 fill the CUs four
+// times: a last round of these that is not full costs more (1537 rows over 5003 classes:
+// 60 us, 87).
 template <typename T>
 Kind kind_of(int64_t rows, int dim, int64_t classes) {
   if (sizeof(T) == 4) return tiles_of(rows, 128) * tiles_of(classes, 128) < 1024 ? kTiny : kLong;
@@ -599,13 +647,20 @@ int rows_of(Size s) {
 // pieces of 256 MB, 2.51 of 512, 2.40 of 1 GB, 2.31 where those are of a size).
 constexpr int64_t kPiece = 1 << 30;
 
+// bf16 gradients of at most so many rows take G as the sum of two: what is lost where a
+// row's largest term, its label's, is rounded is the same for the whole row, and only over
+// many rows does it average to what the result's own rounding loses.
+constexpr int64_t kTwoTerms = 256;
+
 // Where things lie in the workspace, and how the classes are cut up.
 struct Plan {
   Kind kind;
   int bm, bn;                                        // of the logits' tile
   int64_t dim_pad, rows_pad, all, piece, pieces;     // all, piece: classes in whole tiles
+  int64_t rest;                                      // rows of G to its second terms' (0: none)
+  int64_t g_rows;
   int64_t strips, parts;                             // k_strip's strips (0: tiles); the forward's pairs of a row
-  size_t x, w, part, g, bias, dx, dw, bytes;
+  size_t x, w, part, g, bias, dx, dw, label, bytes;
   Pass to_x, to_w;
 };
 
@@ -626,14 +681,17 @@ Plan plan(int64_t rows, int dim, int64_t classes) {
   p.dim_pad = round_up(dim, kRow<T>);
   p.rows_pad = round_up(rows, p.bn);
   p.all = round_up(classes, p.bm);                   // a step of every product divides a tile's classes
-  const int64_t most = kPiece / ((int64_t)sizeof(T) * p.rows_pad) / p.bm * p.bm;
+  p.rest = sizeof(T) == 4 || rows > kTwoTerms ? 0 : 2 * rows <= p.rows_pad ? p.rows_pad / 2 : p.rows_pad;
+  p.g_rows = std::max(p.rows_pad, 2 * p.rest);
+  const int64_t most = kPiece / ((int64_t)sizeof(T) * p.g_rows) / p.bm * p.bm;
   p.piece = std::min<int64_t>(p.all, std::max<int64_t>(p.bm, most));
   p.pieces = (p.all + p.piece - 1) / p.piece;
   p.piece = round_up((p.all + p.pieces - 1) / p.pieces, p.bm);
   p.pieces = (p.all + p.piece - 1) / p.piece;
-  p.to_x = pass<T>(dim, rows, p.piece);
-  p.to_w = pass<T>(dim, p.piece, rows);
-  p.x = take(rows * p.dim_pad, sizeof(T));
+  const int64_t terms = p.rest ? p.g_rows : rows;
+  p.to_x = pass<T>(dim, terms, p.piece);
+  p.to_w = pass<T>(dim, p.piece, terms);
+  p.x = take(terms * p.dim_pad, sizeof(T));
   p.w = take(classes * p.dim_pad, sizeof(T));
   const size_t both = at;
   p.parts = p.all / p.bm;
@@ -648,10 +706,11 @@ Plan plan(int64_t rows, int dim, int64_t classes) {
   p.part = take(p.parts * rows, sizeof(f32x2));
   const size_t forward = at;
   at = both;
-  p.g = take(p.rows_pad * p.piece, sizeof(T));
+  p.g = take(p.g_rows * p.piece, sizeof(T));
   p.bias = take(p.rows_pad / p.bn * p.all, sizeof(float));
-  p.dx = take(p.to_x.parts * rows * part_ld(dim), sizeof(float));
+  p.dx = take(p.to_x.parts * terms * part_ld(dim), sizeof(float));
   p.dw = take(p.to_w.parts * p.piece * part_ld(dim), sizeof(float));
+  p.label = take(sizeof(T) == 2 && !p.rest ? rows : 0, sizeof(float));
   p.bytes = std::max(at, forward);
   return p;
 }
@@ -663,10 +722,11 @@ bool needs_copy(const Mat& m, int dim, int64_t dim_pad) {
   const int64_t ld = m.ld * (int64_t)sizeof(T);
   return dim != dim_pad || (uintptr_t)m.p % 16 != 0 || ld % 16 != 0 || ld >= (int64_t)1 << 24;
 }
-// labels: rows of x without one are zeros, bias: rows of w with -inf (null: as they are)
+// labels: rows of x without one are zeros, bias: rows of w with -inf (null: as they are);
+// wrap: x twice, with zeros from its rows to `wrap`
 template <typename T>
-hipError_t operands(const LossJob& j, int64_t dim_pad, const int32_t* labels, const float* bias, char* x_copy, char* w_copy,
-                    Operand* x, Operand* w, hipStream_t st) {
+hipError_t operands(const LossJob& j, int64_t dim_pad, const int32_t* labels, const float* bias, int64_t wrap, char* x_copy,
+                    char* w_copy, Operand* x, Operand* w, hipStream_t st) {
   *x = {(const char*)j.x.p, j.x.ld * (int64_t)sizeof(T), j.rows - 1, nullptr, 0};
   *w = {(const char*)j.w.p, j.w.ld * (int64_t)sizeof(T), j.classes - 1, nullptr, 0};
   auto blocks = [&](int64_t rows) {
@@ -674,7 +734,7 @@ hipError_t operands(const LossJob& j, int64_t dim_pad, const int32_t* labels, co
   };
   uint32_t nx = 0, nw = 0;
   if (labels || needs_copy<T>(j.x, j.dim, dim_pad)) {
-    nx = blocks(j.rows);
+    nx = blocks(wrap ? 2 * wrap : j.rows);
     x->p = x_copy;
     x->ld = dim_pad * (int64_t)sizeof(T);
   }
@@ -684,8 +744,8 @@ hipError_t operands(const LossJob& j, int64_t dim_pad, const int32_t* labels, co
     w->ld = dim_pad * (int64_t)sizeof(T);
   }
   if (nx + nw == 0) return hipSuccess;
-  const CopyArgs a{j.x, x_copy, dim_pad, j.rows, labels, nullptr, j.classes, j.dim};
-  const CopyArgs b{j.w, w_copy, dim_pad, j.classes, nullptr, bias, 0, j.dim};
+  const CopyArgs a{j.x, x_copy, dim_pad, j.rows, wrap, labels, nullptr, j.classes, j.dim};
+  const CopyArgs b{j.w, w_copy, dim_pad, j.classes, 0, nullptr, bias, 0, j.dim};
   return enqueue(j.dim == dim_pad ? k_pad<T, kExact> : j.dim >= 8 ? k_pad<T, kRagged> : k_pad<T, kSmall>,
                  dim3(nx + nw), dim3(kThreads), 0, st, a, b, nx);
 }
@@ -738,7 +798,7 @@ template <typename T>
 hipError_t forward(const LossJob& j, hipStream_t st) {
   const Plan p = plan<T>(j.rows, j.dim, j.classes);
   LogitArgs a{};
-  hipError_t e = operands<T>(j, p.dim_pad, nullptr, nullptr, j.workspace + p.x, j.workspace + p.w, &a.x, &a.w, st);
+  hipError_t e = operands<T>(j, p.dim_pad, nullptr, nullptr, 0, j.workspace + p.x, j.workspace + p.w, &a.x, &a.w, st);
   if (e != hipSuccess) return e;
   f32x2* const part = (f32x2*)(j.workspace + p.part);
   if (p.strips) {
@@ -760,7 +820,8 @@ hipError_t forward(const LossJob& j, hipStream_t st) {
   if (e != hipSuccess) return e;
   const int64_t parts = p.strips ? p.parts : a.tm;
   const FinishArgs f{part, j.x, j.w, j.bias, j.labels, j.loss, j.lse, j.rows, j.classes, parts, j.dim};
-  return enqueue(j.dim % 8 == 0 ? k_loss<T, kExact> : j.dim > 8 ? k_loss<T, kRagged> : k_loss<T, kSmall>, dim3((unsigned)tiles_of(j.rows, kThreads / 16)), dim3(kThreads), 0, st, f);
+  return enqueue(j.dim % 8 == 0 ? k_loss<T, kExact> : j.dim > 8 ? k_loss<T, kRagged> : k_loss<T, kSmall>,
+                 dim3((unsigned)tiles_of(j.rows, kThreads / 16)), dim3(kThreads), 0, st, f);
 }
 
 template <typename T>
@@ -786,18 +847,23 @@ hipError_t backward(const LossJob& j, hipStream_t st) {
   LogitArgs a{};
   Operand w;
   // rows without a label and classes taken out may hold anything: they are zeros here
-  hipError_t e = operands<T>(j, p.dim_pad, j.labels, j.bias, ws + p.x, ws + p.w, &a.x, &w, st);
+  hipError_t e = operands<T>(j, p.dim_pad, j.labels, j.bias, p.rest, ws + p.x, ws + p.w, &a.x, &w, st);
   a.rows = j.rows;
   a.lse = j.lse;
   a.dloss = j.dloss;
   a.labels = j.labels;
-  a.scale = j.scale;
+  // one factor for all rows is left to the sums, so that no term is rounded for it
+  const bool factor = !j.dloss && std::isfinite(j.scale);
+  a.scale = factor ? 1.f : j.scale;
+  a.rest = p.rest;
+  if (sizeof(T) == 2 && j.dx.p && !p.rest) a.label_rest = (float*)(ws + p.label);
   a.all_classes = j.classes;
   a.g = ws + p.g;
   a.g_ld = p.piece;
   a.bias_ld = p.all;
+  const LabelTerm label{a.label_rest, j.labels, (const uint16_t*)w.p, w.ld / E, j.classes, factor ? j.scale : 1.f};
   // sums that are not the result yet
-  const bool dx_sums = p.pieces > 1 || p.to_x.parts > 1, dw_sums = p.to_w.parts > 1;
+  const bool dx_sums = p.pieces > 1 || p.to_x.parts > 1 || p.rest, dw_sums = p.to_w.parts > 1;
   for (int64_t i = 0; e == hipSuccess && i < p.pieces; ++i) {
     const int64_t first = i * p.piece, left = j.classes - first, mine = std::min(left, p.piece);
     const int64_t wide = round_up(mine, p.bm);       // columns of G that are written
@@ -811,15 +877,17 @@ hipError_t backward(const LossJob& j, hipStream_t st) {
     e = logits<T, true>(a, p, wide, st);
     if (e != hipSuccess) return e;
     SumArgs x{}, w{};
+    x.factor = w.factor = factor ? j.scale : 1.f;
     if (j.dx.p) {
       x.a = terms(a.w, p.dim_pad * E);
-      x.b = {ws + p.g, p.piece * E, p.rows_pad - 1, nullptr, 0};
+      x.b = {ws + p.g, p.piece * E, p.g_rows - 1, nullptr, 0};
       x.c = dx_sums ? (void*)(ws + p.dx) : j.dx.p;
       x.ldc = dx_sums ? part_ld(j.dim) : j.dx.ld;
       x.wide = dx_sums;
       x.m = j.dim;
-      x.n = j.rows;
+      x.n = p.rest ? p.g_rows : j.rows;
       x.add = i > 0;
+      if (!dx_sums) x.label = label;
       Pass t = p.to_x;
       // the last piece may have fewer steps than parts: all parts hold sums by then
       t.steps = (int)(wide / (p.piece / t.steps));
@@ -829,7 +897,8 @@ hipError_t backward(const LossJob& j, hipStream_t st) {
     }
     if (j.dw.p) {
       w.a = terms(a.x, p.dim_pad * E);
-      w.bs = {ws + p.g, p.piece * E, p.rows_pad - 1, (int)(p.piece * E / 16)};
+      if (p.rest) w.a.last = p.g_rows - 1;
+      w.bs = {ws + p.g, p.piece * E, p.g_rows - 1, (int)(p.piece * E / 16)};
       w.m = j.dim;
       w.n = mine;
       w.c = dw_sums ? (void*)(ws + p.dw) : (T*)j.dw.p + first * j.dw.ld;
@@ -852,11 +921,17 @@ hipError_t backward(const LossJob& j, hipStream_t st) {
     }
     if (last && j.dx.p && dx_sums) {
       end.x = join_args((const float*)(ws + p.dx), p.to_x.parts, j.rows, j.dim, nullptr, 0, j.dx);
+      if (p.rest) {                                  // the second terms' rows are parts too
+        end.x.parts = 2 * p.to_x.parts;
+        end.x.m = p.rest;
+      }
+      end.x.label = label;
       end.nx = (uint32_t)join_blocks(end.x);
       end.x_slices = joins_in_slices(end.x);
     }
     if (last && j.dbias) {
-      end.b = {(const float*)(ws + p.bias), j.dbias, p.all, j.classes, (int)(p.rows_pad / p.bn)};
+      end.b = {(const float*)(ws + p.bias), j.dbias, p.all, j.classes, (int)(p.rows_pad / p.bn),
+               factor ? j.scale : 1.f};
       nb = (uint32_t)tiles_of(j.classes, kThreads);
     }
     if (end.nx + end.nw + nb) e = enqueue(k_loss_end<T>, dim3(end.nx + end.nw + nb), dim3(kThreads), 0, st, end);

@@ -757,6 +757,102 @@ def test_gradients_against_differences(V):
         assert abs(diff - along) <= 20 * h ** 3 + 2.0 ** -20, (k, float(diff), float(along))
 
 
+# ------------------------------------------------------------- long offsets
+def test_rows_past_32_bits(V):
+    """9 GB of rows that repeat: each row's results are those of its first copy."""
+    if torch.cuda.mem_get_info()[0] < 48 << 30:
+        pytest.skip("needs 48 GB of device memory")
+    rows, cols, period = 140003, 32768, 1003
+    g = torch.Generator(device="cuda").manual_seed(1)
+    small = Mat("bf16", period, cols)
+    small.t.copy_(torch.randn(period, cols, generator=g, device="cuda") * torch.exp(torch.randn(period, 1, generator=g, device="cuda")))
+    x = Mat("bf16", rows, cols)
+    for r in range(0, rows, period):
+        x.t[r:r + period].copy_(small.t[:rows - r])
+    results = []
+    for m in (small, x):
+        q, qt, q2, s, st = Eight(m.rows, cols), Eight(cols, m.rows), Eight(m.rows, cols), Mat("bf16", m.rows, cols), vec(m.rows)
+        quantize(V, "bf16", m, q, qt)
+        rms(V, "bf16", m.rows, cols, m, m, None, s, None, q2, st)
+        results.append((q, qt, q2, s, st))
+    torch.cuda.synchronize()
+    (q, _, q2, s, st), (Q, QT, Q2, S, ST) = results
+    for r in range(0, rows, period):
+        n = min(period, rows - r)
+        for u, v in ((q, Q), (q2, Q2)):
+            assert torch.equal(v._bytes()[r:r + n], u._bytes()[:n]) and torch.equal(v._powers()[:, r:r + n], u._powers()[:, :n])
+        assert torch.equal(S.t[r:r + n], s.t[:n]) and torch.equal(ST[r:r + n], st[:n])
+    S.assert_guard()
+    # the transpose's last blocks, of rows by themselves
+    first = (rows - 500) // 128 * 128
+    end = Mat("bf16", rows - first, cols)
+    end.t.copy_(x.t[first:])
+    t = Eight(cols, rows - first)
+    quantize(V, "bf16", end, None, t)
+    assert torch.equal(QT._bytes()[:, first:], t._bytes()) and torch.equal(QT._powers()[first // 128:], t._powers())
+    del x, S, s, Q2, QT, results
+    # the product of all of them
+    b = Eight(40, cols)
+    y = Mat("f32", 40, cols)
+    y.t.copy_(torch.randn(40, cols, generator=g, device="cuda"))
+    quantize(V, "f32", y, b)
+    c, few = Mat("bf16", rows, 40), Mat("bf16", period, 40)
+    matmul8(V, "bf16", Q, b, c, cols)
+    matmul8(V, "bf16", q, b, few, cols)
+    torch.cuda.synchronize()
+    value = lambda e: (e._bytes().view(torch.float8_e4m3fn).float().view(e.rows, -1, 128) *  # noqa: E731
+                       torch.exp2(e._powers().T.float() - 127)[:, :, None]).view(e.rows, -1)
+    mags = value(q).double().abs() @ value(b).double().abs().T
+    # two ways to add up: each within the bound of its sum, and a stored value's rounding
+    bound = 2 * (SLACK * (cols / 4 + 16) * U + 2.0 ** -14) * mags
+    for r in range(0, rows, period):
+        n = min(period, rows - r)
+        want = few.t[:n].double()
+        off = (c.t[r:r + n].double() - want).abs() - bound[:n] - 2.0 ** -7 * (want.abs() + bound[:n])
+        assert float(off.max()) <= 0
+
+
+def test_classes_past_32_bits(V):
+    """A table of 4 GB: the gradients of its last classes, bias and all rows."""
+    if torch.cuda.mem_get_info()[0] < 48 << 30:
+        pytest.skip("needs 48 GB of device memory")
+    rows, dim, classes, n = 16, 1024, 2 ** 21, 5000
+    g = torch.Generator(device="cuda").manual_seed(2)
+    labels = np.array([classes - 1 - 300 * i for i in range(rows)])
+    t = Loss(V, "bf16", rows, dim, classes, x=np.zeros((rows, 1)), w=np.zeros((classes, 1)), labels=labels)
+    for c in range(0, classes, 1 << 18):
+        t.w.t[c:c + (1 << 18)].copy_(torch.randn(1 << 18, dim, generator=g, device="cuda") / 32)
+    t.x.t.copy_(t.w.t[torch.from_numpy(labels).cuda()] * 8 + torch.randn(rows, dim, generator=g, device="cuda"))
+    t.run()
+    torch.cuda.synchronize()
+    x, w, b = t.x.t.double(), t.w.t[-n:].double(), t.bias[classes - n:classes].double()
+    lse, d = t.lse[:rows].double()[:, None], t.dl[:rows].double()[:, None]
+    lab = torch.from_numpy(labels - (classes - n)).cuda()
+    one = torch.arange(rows, device="cuda")
+    z = torch.addmm(b, x, w.T)
+    ez = (dim / 4 + 16) * U * (x.abs() @ w.abs().T) + 3 * U * b.abs() + 4 * U * z.abs()
+    loss = lse[:, 0] - z[one, lab]
+    assert float(((t.loss[:rows].double() - loss).abs() - SLACK * (ez[one, lab] + 4 * U * (z[one, lab].abs() + lse[:, 0].abs()))).max()) <= 0
+    G = d * torch.exp(z - lse)
+    p = G.clone()
+    G[one, lab] -= d[:, 0]
+    p[one, lab] += d[:, 0]
+    eg = p * (ez + 4 * U * lse.abs() + 10 * U) + 2.0 ** -126 * (d + 1)
+    e = eg + 2.0 ** -8 * G.abs()
+    want, bound = G.T @ x, SLACK * (e.T @ x.abs() + (rows / 4 + 32) * U * (G.abs().T @ x.abs()))
+    assert float(((t.dw.t[-n:].double() - want).abs() - bound - 2.0 ** -8 * (want.abs() + bound)).max()) <= 0
+    off = (t.db[classes - n:classes].double() - G.sum(0)).abs() - SLACK * (eg.sum(0) + 96 * U * G.abs().sum(0))
+    assert float(off.max()) <= 0
+    # no class is left out: each row's probabilities add up to 1, within what lse and they
+    # are off by (a logit's magnitudes at most |x| |w|) and the sums' own roundings
+    reach = t.x.t.double().norm(dim=1) * max(float(t.w.t[c:c + (1 << 18)].float().norm(dim=1).max()) for c in range(0, classes, 1 << 18))
+    most = float(t.bias[:classes].abs().max())
+    eb = (dim / 4 + 16) * U * reach + 3 * U * most + 4 * U * (reach + most)
+    total = SLACK * (d[:, 0] * (2 * eb + (2 * SUM + 64 + classes / 128 + 10 + 10 * lse[:, 0].abs() + 2 * 96) * U)).sum()
+    assert abs(float(t.db[:classes].double().sum())) <= float(total)
+    t.dw.assert_guard()
+
+
 # -------------------------------------------------------- streams and graphs
 def test_on_another_stream_and_in_a_replayed_graph(V):
     """A run of the operators as a layer and a head use them, enqueued on a stream,
