@@ -89,10 +89,13 @@ struct LogitArgs {
   int steps;
   uint32_t tm, tn;                     // tiles of classes and of rows
   int64_t rows, classes;               // classes: left from the piece's first
-  f32x2* part;                         // forward: [tm][rows] of (largest, sum), to base 2
+  const int32_t* labels;
+  // forward: [tm][rows] of (largest, sum), and [rows] of the label's logit (null: not kept),
+  // to base 2
+  f32x2* part;
+  float* label_z;
   // backward
   const float *lse, *dloss;
-  const int32_t* labels;
   float scale;
   int64_t rest;                        // rows of G to that of what its rounding leaves (0: none)
   float* label_rest;                   // [rows]: or what the label's rounding leaves (null: not kept)
@@ -134,6 +137,16 @@ __device__ __forceinline__ float sum_of(const float (&z)[N], const float (&bias)
   return s;
 }
 
+// The logit of class `hit` of the lane's, where it has that.
+template <int N>
+__device__ __forceinline__ void keep_label(const float (&z)[N], const float (&bias)[N], uint32_t hit, float* to) {
+  if (hit >= (uint32_t)N) return;
+  float at = 0.f;
+#pragma unroll
+  for (int t = 0; t < N; ++t) at = hit == (uint32_t)t ? (bias[t] == -__builtin_inff() ? bias[t] : z[t]) : at;
+  *to = at;
+}
+
 // LDS of a tile: the copies, then the biases of its classes and three words a row.
 template <class TL>
 constexpr int logits_lds() { return TL::kLds + 4 * TL::BM + 12 * TL::BN; }
@@ -171,17 +184,18 @@ __global__ __launch_bounds__(TL::kThreads) void k_logits(LogitArgs j) {
     auto fetch = [&](const void* src, int64_t at, int64_t last, void* dst) {
       __builtin_amdgcn_global_load_lds((VFL_GLOBAL void*)(glb((const float*)src) + min(at, last)), (lds_t*)dst, 4, 0, 0);
     };
-    constexpr int NB = TL::BM / 64, NR = GRAD ? TL::BN / 64 : 0;
+    constexpr int NB = TL::BM / 64, NR = TL::BN / 64, KINDS = GRAD ? 3 : 1;
 #pragma unroll
-    for (int n = 0; n < (NB + 3 * NR + TL::kWaves - 1) / TL::kWaves; ++n) {
+    for (int n = 0; n < (NB + KINDS * NR + TL::kWaves - 1) / TL::kWaves; ++n) {
       const int i = wave + n * TL::kWaves;
       if (i < NB) {
         if (j.bias) fetch(j.bias, c0 + 64 * i + tile.lane, j.classes - 1, e_bias + 64 * i);
-      } else if (i < NB + 3 * NR) {
-        const int k = 64 * ((i - NB) % (NR > 0 ? NR : 1));
+      } else if (i < NB + KINDS * NR) {
+        const int k = 64 * ((i - NB) % NR);
         const int64_t row = r0 + k + tile.lane;
-        if (i < NB + NR) fetch(j.labels, row, j.rows - 1, e_label + k);
-        else if (i < NB + 2 * NR) fetch(j.lse, row, j.rows - 1, e_lse + k);
+        if (i < NB + NR) {
+          if (GRAD || j.label_z) fetch(j.labels, row, j.rows - 1, e_label + k);
+        } else if (i < NB + 2 * NR) fetch(j.lse, row, j.rows - 1, e_lse + k);
         else if (j.dloss) fetch(j.dloss, row, j.rows - 1, e_d + k);
       }
     }
@@ -218,6 +232,10 @@ __global__ __launch_bounds__(TL::kThreads) void k_logits(LogitArgs j) {
       top = quarters_top(top);
       const float from = top == -__builtin_inff() ? 0.f : top;
       const float sum = quarters_sum(sum_of(z, bias, from, 0.f));
+      if (j.label_z) {
+        const int in = tile.col(c / TL::DN) + c % TL::DN;
+        if (r0 + in < j.rows) keep_label(z, bias, (uint32_t)e_label[in] - (uint32_t)mine, j.label_z + r0 + in);
+      }
       if (tile.lane < 16) stat[tile.wm / TL::WM * TL::BN + tile.col(c / TL::DN) + c % TL::DN] = f32x2{top, sum};
     }
     __syncthreads();
@@ -463,40 +481,54 @@ __global__ __launch_bounds__(512) void k_strip(StripArgs j) {
 // ---------------------------------------------------------------------- join
 struct FinishArgs {
   const f32x2* part;
-  Mat x, w;
+  const float* label_z;
+  Operand x, w;                        // after strips, and the biases
   const float* bias;
   const int32_t* labels;
   float *loss, *lse;
   int64_t rows, classes, tiles;
-  int dim;
 };
 
-// A row a group of 16 lanes: the tiles' pairs joined, and the label's logit (whose
-// operands are asked for first: latency bounds this; 3 to 5 us).  The logit is a sum of
-// float32 products of its own, so no tile has to find the row's label among its classes.
-template <typename T, Form F>
+// A row a group of 16 lanes: the tiles' pairs joined, and the loss as the sum of two
+// differences of what the tiles saw, both 0 or more: where the label has the largest
+// logit the first is 0, whatever the logits' own rounding.  After strips (KP panels of
+// 64 columns), whose registers have no room for labels, a wavefront makes the labels'
+// logits of the 16 rows again, by the same instructions in the same order: the same bits.
+// Latency bounds it: 3 to 5 us.
+template <int KP>
 __global__ __launch_bounds__(kThreads) void k_loss(FinishArgs j) {
-  const int lane = threadIdx.x & 15;
-  const int64_t row = (int64_t)blockIdx.x * (kThreads / 16) + (threadIdx.x >> 4);
+  constexpr int kRows = kThreads / 16;
+  const int lane = threadIdx.x & 15, in = threadIdx.x >> 4;
+  const int64_t row = (int64_t)blockIdx.x * kRows + in;
+  __shared__ float logits[kRows];
+  if constexpr (KP > 0) {
+    if (threadIdx.x < 64 && j.loss) {
+      const int64_t r = min((int64_t)blockIdx.x * kRows + lane, j.rows - 1);
+      const int label = j.labels[r];
+      const int64_t c = label >= 0 && label < j.classes ? label : 0;
+      const VFL_GLOBAL char* const x = glb(j.x.p) + r * j.x.ld + 16 * in;
+      const VFL_GLOBAL char* const w = glb(j.w.p) + c * j.w.ld + 16 * in;
+      const float b = j.bias ? j.bias[c] : 0.f;
+      bf16x8 wf[2 * KP], xf[2 * KP];
+#pragma unroll
+      for (int k = 0; k < 2 * KP; ++k) {
+        wf[k] = __builtin_bit_cast(bf16x8, *(const VFL_GLOBAL u32x4*)(w + 64 * k));
+        xf[k] = __builtin_bit_cast(bf16x8, *(const VFL_GLOBAL u32x4*)(x + 64 * k));
+      }
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < 2 * KP; ++k) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[k], xf[k], acc, 0, 0, 0);
+      // a lane has classes 4 in .. 4 in + 3 of row `lane`: its own is among them in one
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        if (lane == 4 * in + t) logits[lane] = b == -__builtin_inff() ? b : fmaf(acc[t], kLog2e, b * kLog2e);
+    }
+    __syncthreads();
+  }
   if (row >= j.rows) return;
   const int label = j.loss ? j.labels[row] : -1;
   const bool has = label >= 0 && label < j.classes;
-  float z = 0.f, b = 0.f;
-  if (has) {
-    const Cols kx(j.dim, j.rows), kw(j.dim, j.classes);
-    const T* const x = row_of<T>(j.x, row);
-    const T* const w = row_of<T>(j.w, label);
-    b = j.bias ? j.bias[label] : 0.f;
-#pragma unroll 2
-    for (int q = lane; q < kx.per; q += 16) {
-      float u[8], v[8];
-      const Raw<T> xr = load_chunk<F>(x, q, kx, row >= kx.edge), wr = load_chunk<F>(w, q, kw, label >= kw.edge);
-      chunk_values<F>(xr, q, kx, row >= kx.edge, u);
-      chunk_values<F>(wr, q, kw, label >= kw.edge, v);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) z = fmaf(u[i], v[i], z);
-    }
-  }
+  const float z = !has ? 0.f : KP > 0 ? logits[in] : j.label_z[row];
   float top = -__builtin_inff(), sum = 0.f;
 #pragma unroll 4
   for (int64_t t = lane; t < j.tiles; t += 16) {
@@ -512,11 +544,10 @@ __global__ __launch_bounds__(kThreads) void k_loss(FinishArgs j) {
   all = fmaxf(all, dpp<0x140>(all));
   const float from = all == -__builtin_inff() ? 0.f : all;
   sum = group_sum<16>(sum * exp2_of(top - from));
-  const float lse = all == -__builtin_inff() ? all : fmaf(all, kUnitHigh, fmaf(all, kUnitLow, __builtin_amdgcn_logf(sum) * kUnitHigh));
-  if (j.lse && lane == 0) j.lse[row] = lse;
-  if (!j.loss) return;
-  z = group_sum<16>(z);
-  if (lane == 0) j.loss[row] = !has ? 0.f : b == -__builtin_inff() ? __builtin_inff() : lse - (z + b);
+  if (lane > 0) return;
+  const float log = __builtin_amdgcn_logf(sum);
+  if (j.lse) j.lse[row] = all == -__builtin_inff() ? all : fmaf(all, kUnitHigh, fmaf(all, kUnitLow, log * kUnitHigh));
+  if (j.loss) j.loss[row] = !has ? 0.f : z == -__builtin_inff() ? __builtin_inff() : (all - z + log) * kUnitHigh;
 }
 
 // the gradients of no rows
@@ -647,9 +678,14 @@ int rows_of(Size s) {
 // pieces of 256 MB, 2.51 of 512, 2.40 of 1 GB, 2.31 where those are of a size).
 constexpr int64_t kPiece = 1 << 30;
 
-// bf16 gradients of at most so many rows take G as the sum of two: what is lost where a
-// row's largest term, its label's, is rounded is the same for the whole row, and only over
-// many rows does it average to what the result's own rounding loses.
+// bf16 gradients of at most so many rows take G as the sum of two terms, the second ones in
+// rows of their own: more rows of dx's sums, a longer sum of dw.  What is lost where a
+// row's largest term is rounded is the same for the whole row, and only over many rows
+// does it average to what the result's own rounding loses: off by 1.7 times the latter
+// (2 rows), 1.4 to 1.5 (100 to 300) and 1.4 (1000) in dw with one term, 1.0 with two.
+// dx takes the label's loss from LabelTerm instead where G has one term (1.5 times
+// without, 1.0 with it; as fast).  One and two terms, us: 64 x 256 rows over 100000
+// classes 97, 111; 256 rows 156, 198; 512 rows 218, 315.
 constexpr int64_t kTwoTerms = 256;
 
 // Where things lie in the workspace, and how the classes are cut up.
@@ -660,7 +696,7 @@ struct Plan {
   int64_t rest;                                      // rows of G to its second terms' (0: none)
   int64_t g_rows;
   int64_t strips, parts;                             // k_strip's strips (0: tiles); the forward's pairs of a row
-  size_t x, w, part, g, bias, dx, dw, label, bytes;
+  size_t x, w, part, label_z, g, bias, dx, dw, label, bytes;
   Pass to_x, to_w;
 };
 
@@ -704,6 +740,7 @@ Plan plan(int64_t rows, int dim, int64_t classes) {
     }
   }
   p.part = take(p.parts * rows, sizeof(f32x2));
+  p.label_z = take(rows, sizeof(float));
   const size_t forward = at;
   at = both;
   p.g = take(p.g_rows * p.piece, sizeof(T));
@@ -801,6 +838,7 @@ hipError_t forward(const LossJob& j, hipStream_t st) {
   hipError_t e = operands<T>(j, p.dim_pad, nullptr, nullptr, 0, j.workspace + p.x, j.workspace + p.w, &a.x, &a.w, st);
   if (e != hipSuccess) return e;
   f32x2* const part = (f32x2*)(j.workspace + p.part);
+  float* const label_z = j.loss ? (float*)(j.workspace + p.label_z) : nullptr;
   if (p.strips) {
     const StripArgs s{a.w, a.x, j.bias, j.rows, j.classes, part, (int)tiles_of(j.classes, kStripClasses), (int)p.strips};
     auto run = [&](auto kernel, int lds) {
@@ -815,12 +853,19 @@ hipError_t forward(const LossJob& j, hipStream_t st) {
     a.rows = j.rows;
     a.classes = j.classes;
     a.part = part;
+    a.labels = j.labels;
+    a.label_z = label_z;
     e = logits<T, false>(a, p, j.classes, st);
   }
   if (e != hipSuccess) return e;
   const int64_t parts = p.strips ? p.parts : a.tm;
-  const FinishArgs f{part, j.x, j.w, j.bias, j.labels, j.loss, j.lse, j.rows, j.classes, parts, j.dim};
-  return enqueue(j.dim % 8 == 0 ? k_loss<T, kExact> : j.dim > 8 ? k_loss<T, kRagged> : k_loss<T, kSmall>,
+  const FinishArgs f{part, label_z, a.x, a.w, j.bias, j.labels, j.loss, j.lse, j.rows, j.classes, parts};
+  const int64_t panels = p.strips ? p.dim_pad / 64 : 0;
+  return enqueue(panels == 0   ? k_loss<0>
+                 : panels == 1 ? k_loss<1>
+                 : panels == 2 ? k_loss<2>
+                 : panels == 3 ? k_loss<3>
+                               : k_loss<4>,
                  dim3((unsigned)tiles_of(j.rows, kThreads / 16)), dim3(kThreads), 0, st, f);
 }
 
