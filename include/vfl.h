@@ -39,7 +39,8 @@
  * Errors.  Every call returns a vfl_status; nothing else crosses the ABI.
  * vfl_last_error() gives a text for the last failure on a context; with a
  * NULL context, the text of the calling thread's last vfl_workspace_size,
- * vfl_create or row operator failure (empty after a success of one of them).
+ * vfl_create or operator failure (of a call that takes no context; empty after a
+ * success of one of them).
  * An earlier HIP error that the calling thread has not asked for yet is not
  * taken for a call's own.
  */
@@ -699,8 +700,8 @@ vfl_status vfl_timing_read(vfl_ctx* c, int32_t kernel_class, double* ms, int64_t
 
 /* Text of the last failure on c (owned by the context, valid until its next
  * call); c == NULL: the calling thread's last vfl_workspace_size, vfl_create
- * or row operator failure (thread-local storage, valid until that thread's
- * next such call). */
+ * or operator failure (of a call that takes no context; thread-local storage,
+ * valid until that thread's next such call). */
 const char* vfl_last_error(const vfl_ctx* c);
 
 /* Synchronise both streams and release the context's events and host state.

@@ -283,7 +283,7 @@ template <typename T>
 T* at(vfl_ctx* c, size_t off) { return (T*)(c->ws + off); }
 
 // Failures of calls that have no context (vfl_workspace_size, vfl_create, the
-// row operators) keep their text per host thread; vfl_last_error(NULL) returns
+// operators) keep their text per host thread; vfl_last_error(NULL) returns
 // it.
 thread_local std::string t_create_err;
 

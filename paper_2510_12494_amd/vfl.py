@@ -221,7 +221,7 @@ _lib = _load()
 def _chk(st: int, where: str, ctx=None):
     if st != VFL_OK:
         # without a context the text is the calling thread's last
-        # vfl_workspace_size / vfl_create / row operator failure
+        # vfl_workspace_size / vfl_create / operator failure
         raw = _lib.vfl_last_error(ctx)
         text = raw.decode() if raw else ""
         raise VflError(st, where, text)
@@ -337,7 +337,7 @@ def vfl_philox(seed: int, step: int, tag: int, row0: int, rows: int, groups: int
                          C.c_void_p(stream or None)), "vfl_philox")
 
 
-# row operators: `a` describes the call (fill it once per layer), stream is a
+# operators: `a` describes the call (fill it once per layer), stream is a
 # raw hipStream_t (0: the null stream)
 def vfl_dropout(a: vfl_dropout_args, stream: int = 0):
     _chk(_lib.vfl_dropout(a, stream), "vfl_dropout")
