@@ -148,9 +148,12 @@ __device__ __forceinline__ void keep_label(const float (&z)[N], const float (&bi
   *to = at;
 }
 
-// LDS of a tile: the copies, then the biases of its classes and three words a row.
+// LDS of a tile: the copies, then the biases of its classes and three words a row, each in
+// whole wavefronts' copies.
 template <class TL>
-constexpr int logits_lds() { return TL::kLds + 4 * TL::BM + 12 * TL::BN; }
+constexpr int row_words() { return TL::BN < 64 ? 64 : TL::BN; }
+template <class TL>
+constexpr int logits_lds() { return TL::kLds + 4 * TL::BM + 12 * row_words<TL>(); }
 
 // A tile of classes x rows: with the classes as the MFMA's rows a lane holds 16
 // consecutive classes (4 DM in general) of each of its batch rows, so a row's
@@ -178,14 +181,15 @@ __global__ __launch_bounds__(TL::kThreads) void k_logits(LogitArgs j) {
   // load it after the products would add two latencies to every tile, to keep it in
   // registers would take workgroups off the CU.
   float* const e_bias = (float*)(smem + TL::kLds);   // [BM]
+  constexpr int WORDS = row_words<TL>();
   int* const e_label = (int*)(e_bias + TL::BM);      // [BN], and lse, dloss
-  float *const e_lse = (float*)(e_label + TL::BN), *const e_d = e_lse + TL::BN;
+  float *const e_lse = (float*)(e_label + WORDS), *const e_d = e_lse + WORDS;
   {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     auto fetch = [&](const void* src, int64_t at, int64_t last, void* dst) {
       __builtin_amdgcn_global_load_lds((VFL_GLOBAL void*)(glb((const float*)src) + min(at, last)), (lds_t*)dst, 4, 0, 0);
     };
-    constexpr int NB = TL::BM / 64, NR = TL::BN / 64, KINDS = GRAD ? 3 : 1;
+    constexpr int NB = TL::BM / 64, NR = WORDS / 64, KINDS = GRAD ? 3 : 1;
 #pragma unroll
     for (int n = 0; n < (NB + KINDS * NR + TL::kWaves - 1) / TL::kWaves; ++n) {
       const int i = wave + n * TL::kWaves;
@@ -294,9 +298,13 @@ __global__ __launch_bounds__(TL::kThreads) void k_logits(LogitArgs j) {
       if (sizeof(T) == 2 && j.rest && row >= j.rest) continue;   // where a second term lies
 #pragma unroll
       for (int t = 0; t < RUN; t += 8) {
+        if constexpr (RUN == 4) {
+          store4(to, g);
+          break;
+        }
         float v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = g[t + i];
+        for (int i = 0; i < 8; ++i) v[i] = g[(t + i) % RUN];
         store8<false>(to + t, v);
         if constexpr (sizeof(T) == 2) {
           if (j.rest) {
@@ -612,8 +620,8 @@ template <> struct Tiles<uint16_t> {
 template <> struct Tiles<float> {
   typedef Tile<kF32, 128, 128, 2, 2, 64, 2, kBlocks> Long;
   typedef Tile<kF32, 128, 128, 2, 2, 64, 2, kBlocks> Short;
-  typedef Tile<kF32, 64, 64, 2, 2, 128, 2, kBlocks> Few;
-  typedef Few Tiny;
+  typedef Tile<kF32, 64, 32, 4, 1, 128, 3, kBlocks> Few;        // few tiles of the next
+  typedef Tile<kF32, 64, 64, 2, 2, 128, 2, kBlocks> Tiny;
   template <bool BOTH> using Large = SumTile<kF32, 128, 128, 2, 2, 64, 2, BOTH>;
   template <bool BOTH> using Small = SumTile<kF32, 64, 64, 2, 2, 128, 2, BOTH>;
   template <bool BOTH> using Least = Small<BOTH>;
@@ -634,10 +642,15 @@ auto with_tile(Kind k, F f) {
 // rule and in the next larger ones, us: 1000 rows x 1000 over 1000 classes 51, 94; 90 x
 // 90 over 450 26, 37).  float32 tiles of 64 x 64 until those of 128 x 128 fill the CUs four
 // times: a last round of these that is not full costs more (1537 rows over 5003 classes:
-// 60 us, 87).
+// 60 us, 87), and of 64 x 32 where not every CU has one of those: a step of a tile is then
+// what a CU takes to make it (64 x 64 and 64 x 32, a step of the loss, us: 200 rows x 1000
+// over 300 classes 71, 58; 4 x 1000 over 500 63, 49; 16 x 32 over 100 20, 23).
 template <typename T>
 Kind kind_of(int64_t rows, int dim, int64_t classes) {
-  if (sizeof(T) == 4) return tiles_of(rows, 128) * tiles_of(classes, 128) < 1024 ? kTiny : kLong;
+  if (sizeof(T) == 4) {
+    if (tiles_of(rows, 64) * tiles_of(classes, 64) <= 256) return kFew;
+    return tiles_of(rows, 128) * tiles_of(classes, 128) < 1024 ? kTiny : kLong;
+  }
   if (rows <= 64) return tiles_of(classes, 256) >= 192 ? kFew : kTiny;
   if (dim > 256 && tiles_of(rows, 256) * tiles_of(classes, 256) >= 192) return kLong;
   return tiles_of(rows, 128) * tiles_of(classes, 256) >= 192 ? kShort : kTiny;
