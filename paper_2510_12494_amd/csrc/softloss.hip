@@ -669,7 +669,7 @@ Pass pass(int64_t m, int64_t n, int64_t depth) {
   auto cut = [&](int bm, int bn, int elements, const StepTime& t) {
     return cut_up(m, n, bm, bn, (int)tiles_of(depth, elements), t);
   };
-  Pass p{cut(L::BM, L::BN, L::kElements, bf16 ? StepTime{2.05, 2.05, 1} : StepTime{1.07, 1.3, 4}), kLargeSum};
+  Pass p{cut(L::BM, L::BN, L::kElements, bf16 ? StepTime{2.05, 2.05, 1} : StepTime{1.07, 1.3, 3}), kLargeSum};
   const Cut s = cut(S::BM, S::BN, S::kElements, bf16 ? StepTime{0.67, 0.8, 2} : StepTime{0.58, 0.8, 4});
   if (s.us < p.us) p = {s, kSmallSum};
   if (bf16) {
