@@ -555,7 +555,9 @@ __global__ __launch_bounds__(kThreads) void k_loss(FinishArgs j) {
   sum = group_sum<16>(sum * exp2_of(top - from));
   if (lane > 0) return;
   const float log = __builtin_amdgcn_logf(sum);
-  if (j.lse) j.lse[row] = all == -__builtin_inff() ? all : fmaf(all, kUnitHigh, fmaf(all, kUnitLow, log * kUnitHigh));
+  // no class at all (a sum that is no number is a row of no numbers)
+  const bool none = all == -__builtin_inff() && sum == 0.f;
+  if (j.lse) j.lse[row] = none ? all : fmaf(all, kUnitHigh, fmaf(all, kUnitLow, log * kUnitHigh));
   if (j.loss) j.loss[row] = !has ? 0.f : z == -__builtin_inff() ? __builtin_inff() : (all - z + log) * kUnitHigh;
 }
 
