@@ -637,8 +637,8 @@ vfl_status vfl_matmul8(const vfl_matmul8_args* a, void* stream);
  * each where it is not NULL (one at least).  dloss: float32 [rows], the gradient
  * of each row's loss (NULL: `scale` for every row).  A class taken out has a
  * gradient of 0.  In bf16 G enters its products as one rounded value, and what its
- * rounding loses at the row's label is added to dx; of up to 256 rows as the sum of
- * two such values.  `scale`, and all sums, are float32.
+ * rounding loses at the row's label is added to dx; in dw of up to 512 rows, and
+ * both of up to 256, as the sum of two such values.  `scale`, and all sums, are float32.
  *   The workspace (16-byte aligned, vfl_softmax_loss_workspace_size() bytes: copies
  * of x and w in the products' layout, and G in pieces of all rows by as many classes as
  * 1 GB holds, 256 at least) means nothing between calls; calls that may run at the

@@ -695,14 +695,15 @@ int rows_of(Size s) {
 constexpr int64_t kPiece = 1 << 30;
 
 // bf16 gradients of at most so many rows take G as the sum of two terms, the second ones in
-// rows of their own: more rows of dx's sums, a longer sum of dw.  What is lost where a
+// rows of their own: a longer sum of dw, more rows of dx's sums.  What is lost where a
 // row's largest term is rounded is the same for the whole row, and only over many rows
-// does it average to what the result's own rounding loses: off by 1.7 times the latter
-// (2 rows), 1.4 to 1.5 (100 to 300) and 1.4 (1000) in dw with one term, 1.0 with two.
-// dx takes the label's loss from LabelTerm instead where G has one term (1.5 times
-// without, 1.0 with it; as fast).  One and two terms, us: 64 x 256 rows over 100000
-// classes 97, 111; 256 rows 156, 198; 512 rows 218, 315.
-constexpr int64_t kTwoTerms = 256;
+// does it average to what the result's own rounding loses.  In the norm, one term: dw is
+// off by 1.7 times the latter (2 rows), 1.4 to 1.5 (100 to 500), 1.2 to 1.44 (more), with
+// two by 1.0; dx is as far off as dw without LabelTerm, and with it, which costs nothing,
+// by 1.0 to 1.35 of more rows than a few.  One term, two for dw, two for both, us: 512 x
+// 256 rows over 100000 classes 222, 291, 315; 256 rows 156, 175, 198; 400 x 1000 over
+// 10000 117, 131; 64 x 256 over 100000 97, 113, 113.
+constexpr int64_t kTwoTerms = 512, kTwoTermsOfX = 256;
 
 // Where things lie in the workspace, and how the classes are cut up.
 struct Plan {
@@ -710,6 +711,7 @@ struct Plan {
   int bm, bn;                                        // of the logits' tile
   int64_t dim_pad, rows_pad, all, piece, pieces;     // all, piece: classes in whole tiles
   int64_t rest;                                      // rows of G to its second terms' (0: none)
+  bool x_terms;                                      // dx takes them too
   int64_t g_rows;
   int64_t strips, parts;                             // k_strip's strips (0: tiles); the forward's pairs of a row
   size_t x, w, part, label_z, g, bias, dx, dw, label, bytes;
@@ -735,13 +737,14 @@ Plan plan(int64_t rows, int dim, int64_t classes) {
   p.all = round_up(classes, p.bm);                   // a step of every product divides a tile's classes
   p.rest = sizeof(T) == 4 || rows > kTwoTerms ? 0 : 2 * rows <= p.rows_pad ? p.rows_pad / 2 : p.rows_pad;
   p.g_rows = std::max(p.rows_pad, 2 * p.rest);
+  p.x_terms = p.rest && rows <= kTwoTermsOfX;
   const int64_t most = kPiece / ((int64_t)sizeof(T) * p.g_rows) / p.bm * p.bm;
   p.piece = std::min<int64_t>(p.all, std::max<int64_t>(p.bm, most));
   p.pieces = (p.all + p.piece - 1) / p.piece;
   p.piece = round_up((p.all + p.pieces - 1) / p.pieces, p.bm);
   p.pieces = (p.all + p.piece - 1) / p.piece;
-  const int64_t terms = p.rest ? p.g_rows : rows;
-  p.to_x = pass<T>(dim, terms, p.piece);
+  const int64_t terms = p.rest ? p.g_rows : rows, x_rows = p.x_terms ? p.g_rows : rows;
+  p.to_x = pass<T>(dim, x_rows, p.piece);
   p.to_w = pass<T>(dim, p.piece, terms);
   p.x = take(terms * p.dim_pad, sizeof(T));
   p.w = take(classes * p.dim_pad, sizeof(T));
@@ -761,9 +764,9 @@ Plan plan(int64_t rows, int dim, int64_t classes) {
   at = both;
   p.g = take(p.g_rows * p.piece, sizeof(T));
   p.bias = take(p.rows_pad / p.bn * p.all, sizeof(float));
-  p.dx = take(p.to_x.parts * terms * part_ld(dim), sizeof(float));
+  p.dx = take(p.to_x.parts * x_rows * part_ld(dim), sizeof(float));
   p.dw = take(p.to_w.parts * p.piece * part_ld(dim), sizeof(float));
-  p.label = take(sizeof(T) == 2 && !p.rest ? rows : 0, sizeof(float));
+  p.label = take(sizeof(T) == 2 && !p.x_terms ? rows : 0, sizeof(float));
   p.bytes = std::max(at, forward);
   return p;
 }
@@ -917,14 +920,14 @@ hipError_t backward(const LossJob& j, hipStream_t st) {
   const bool factor = !j.dloss && std::isfinite(j.scale);
   a.scale = factor ? 1.f : j.scale;
   a.rest = p.rest;
-  if (sizeof(T) == 2 && j.dx.p && !p.rest) a.label_rest = (float*)(ws + p.label);
+  if (sizeof(T) == 2 && j.dx.p && !p.x_terms) a.label_rest = (float*)(ws + p.label);
   a.all_classes = j.classes;
   a.g = ws + p.g;
   a.g_ld = p.piece;
   a.bias_ld = p.all;
   const LabelTerm label{a.label_rest, j.labels, (const uint16_t*)w.p, w.ld / E, j.classes, factor ? j.scale : 1.f};
   // sums that are not the result yet
-  const bool dx_sums = p.pieces > 1 || p.to_x.parts > 1 || p.rest, dw_sums = p.to_w.parts > 1;
+  const bool dx_sums = p.pieces > 1 || p.to_x.parts > 1 || p.x_terms, dw_sums = p.to_w.parts > 1;
   for (int64_t i = 0; e == hipSuccess && i < p.pieces; ++i) {
     const int64_t first = i * p.piece, left = j.classes - first, mine = std::min(left, p.piece);
     const int64_t wide = round_up(mine, p.bm);       // columns of G that are written
@@ -946,7 +949,7 @@ hipError_t backward(const LossJob& j, hipStream_t st) {
       x.ldc = dx_sums ? part_ld(j.dim) : j.dx.ld;
       x.wide = dx_sums;
       x.m = j.dim;
-      x.n = p.rest ? p.g_rows : j.rows;
+      x.n = p.x_terms ? p.g_rows : j.rows;
       x.add = i > 0;
       if (!dx_sums) x.label = label;
       Pass t = p.to_x;
@@ -982,7 +985,7 @@ hipError_t backward(const LossJob& j, hipStream_t st) {
     }
     if (last && j.dx.p && dx_sums) {
       end.x = join_args((const float*)(ws + p.dx), p.to_x.parts, j.rows, j.dim, nullptr, 0, j.dx);
-      if (p.rest) {                                  // the second terms' rows are parts too
+      if (p.x_terms) {                               // the second terms' rows are parts too
         end.x.parts = 2 * p.to_x.parts;
         end.x.m = p.rest;
       }
