@@ -536,7 +536,7 @@ vfl_status vfl_residual_backward(const vfl_residual_args* a, void* stream);
 /* A matrix in 8 bits: e4m3 values (1 sign, 4 exponent and 3 fraction bits,
  * largest value 448, no infinities) with one power of two for each block of
  * VFL_Q8_BLOCK consecutive columns of a row.  Element (r, c) is
- * e4m3(data[r * ld + c]) * 2^(scale[(c / 128) * scale_ld + r] - 127).
+ * e4m3(data[r * ld + c]) * 2^(scale[(c / 128) * scale_ld + r] - 127), bytes of 0 to 254.
  * data: 16-byte aligned; ld: bytes from row to row, a multiple of 128 and at
  * least the columns rounded up to one (0: that).  scale: 16-byte aligned;
  * scale_ld: a multiple of 16, at least the rows (0: the rows rounded up to one).

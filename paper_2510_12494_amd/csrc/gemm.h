@@ -16,8 +16,8 @@
 // products with about 16 bits: results are 1.5e-5 of their norm off whatever the
 // length of the sum (256 and 4096 squared, 128 to 8192 long), 1 / 100 of what
 // rounding them to bf16 adds.  kE4m3Wide makes bf16 of the values, powers and all,
-// which loses nothing, and takes the bf16 instruction at half the rate, whose sums
-// are float32 ones.
+// and takes the bf16 instruction at half the rate, whose sums are float32 ones; what
+// lies past either end of bf16 goes by parts (EndsPart).
 //
 // LDS holds a fragment's rows together, chunk c of its row i at place
 // c ^ swizzle(i): 16 lanes read 256 consecutive bytes in some order, without bank
@@ -69,6 +69,41 @@ __device__ __forceinline__ void widen_e4m3(const u32x4& v, uint32_t s, bf16x8 (&
 #pragma unroll
   for (int t = 0; t < 2; ++t) out[t] = __builtin_bit_cast(bf16x8, w[t]);
 }
+
+// bf16 has every e4m3 value times the power of a byte from 3 (whose smallest magnitude is
+// 2^-9 2^-124) to 246 (448 2^119 the largest).  A block of another power has its values
+// moved by 2^64 towards 1 and those that they meet by as much the other way, one part of
+// the rows and columns after the other, each pair in one part:
+//   rows, columns:  between, between 0;  low, all +64;  high, all -64;  between, low -64;
+//                   between, high +64
+// What then leaves the bytes 0 to 246 is held there: its products are below 2^-149 or past
+// float32 either way.
+constexpr uint32_t kLowByte = 3, kHighByte = 246;
+__device__ __forceinline__ bool at_an_end(uint32_t byte) { return byte - kLowByte > kHighByte - kLowByte; }
+// whether one of four bytes may be such a one: those from 64 to 191, whose two highest
+// bits differ, are not
+__device__ __forceinline__ bool maybe_at_an_end(uint32_t four) {
+  return ((four ^ (four << 1)) & 0x80808080u) != 0x80808080u;
+}
+// bits of sixteen values whose power is such a one; none of kMagnitudes: zeros
+constexpr uint32_t kMagnitudes = 0x7f7f7f7fu;
+__device__ __forceinline__ uint32_t bits_at_an_end(const u32x4& v, uint32_t byte) {
+  return (v[0] | v[1] | v[2] | v[3]) & (at_an_end(byte) ? ~0u : 0u);
+}
+constexpr int kEndsParts = 5;
+struct EndsPart {
+  enum Take { kBetween, kLow, kHigh, kAll };
+  int rows, columns, by;
+  __device__ explicit EndsPart(int i)
+      : rows(i == 1 ? kLow : i == 2 ? kHigh : kBetween),
+        columns(i == 0 ? kBetween : i == 3 ? kLow : i == 4 ? kHigh : kAll),
+        by(i == 0 ? 0 : i == 1 || i == 4 ? 64 : -64) {}
+  __device__ static __forceinline__ void widen(const u32x4& v, uint32_t byte, int take, int by, bf16x8 (&out)[2]) {
+    const int is = byte < kLowByte ? kLow : byte > kHighByte ? kHigh : kBetween;
+    const bool in = take == kAll || take == is;
+    widen_e4m3(in ? v : u32x4{0u, 0u, 0u, 0u}, (uint32_t)min(max((int)byte + by, 0), (int)kHighByte), out);
+  }
+};
 
 // An operand: rows of ld bytes, `last` the last row's index; rows past it are
 // read as that row (their results are not kept).  8-bit operands: the exponent
@@ -157,6 +192,8 @@ struct Tile {
     uint32_t sa[kScales ? MF / 4 : 1], sb[kScales ? NF / 4 : 1], na[kScales ? MF / 4 : 1], nb[kScales ? NF / 4 : 1];
     const VFL_GLOBAL uint8_t *sa0 = nullptr, *sb0 = nullptr;
     uint32_t soa[kScales ? MF / 4 : 1], sob[kScales ? NF / 4 : 1];
+    // the bits of such a dword that are rows' (past the last row lies anything)
+    uint32_t ka[kScales ? MF / 4 : 1], kb[kScales ? NF / 4 : 1];
     if constexpr (is_e4m3(TY)) {
       static_assert(ROWS == kDealt, "a dword of exponents is four consecutive rows");
       sa0 = glb(A.scale);
@@ -167,6 +204,11 @@ struct Tile {
 #pragma unroll
       for (int q = 0; q < NF / 4; ++q)
         sob[q] = (uint32_t)min(n0 + wn + 64 * q + 4 * (lane & 15), B.last & ~(int64_t)3);
+      auto rows = [](int64_t last, uint32_t at) { return 0xffffffffu >> (8 * (3 - (int)min(last - at, (int64_t)3))); };
+#pragma unroll
+      for (int q = 0; q < MF / 4; ++q) ka[q] = rows(A.last, soa[q]);
+#pragma unroll
+      for (int q = 0; q < NF / 4; ++q) kb[q] = rows(B.last, sob[q]);
     }
     auto scales = [&](int s, uint32_t* da, uint32_t* db) {
       const VFL_GLOBAL uint8_t* pa = sa0 + (int64_t)(s0 + s) * A.scale_ld;
@@ -188,6 +230,7 @@ struct Tile {
     for (int s = 0; s < NST - 1; ++s)
       if (s < n) copy(s);
     if constexpr (is_e4m3(TY)) scales(0, na, nb);
+    bool ends = false;
     for (int s = 0; s < n; ++s) {
       // this wavefront's copies of step s have landed, and after the barrier
       // everyone's; everyone has also read step s - 1, whose buffer is next
@@ -197,9 +240,9 @@ struct Tile {
       __builtin_amdgcn_sched_barrier(0);
       if constexpr (is_e4m3(TY)) {
 #pragma unroll
-        for (int q = 0; q < MF / 4; ++q) sa[q] = na[q];
+        for (int q = 0; q < MF / 4; ++q) sa[q] = TY == kE4m3Wide ? rows_alone(na[q], ka[q]) : na[q];
 #pragma unroll
-        for (int q = 0; q < NF / 4; ++q) sb[q] = nb[q];
+        for (int q = 0; q < NF / 4; ++q) sb[q] = TY == kE4m3Wide ? rows_alone(nb[q], kb[q]) : nb[q];
         if (s + 1 < n) scales(s + 1, na, nb);
       }
       if (s + NST - 1 < n) copy(s + NST - 1);
@@ -221,6 +264,7 @@ struct Tile {
           mma8(a, b, sa[f / 4], sb, f & 3, acc[f], std::make_integer_sequence<int, NF>{});
         }
       } else if constexpr (TY == kE4m3Wide) {
+        ends |= powers_at_an_end(SA, SB, place, sa, sb);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           bf16x8 b[NF][2];
@@ -260,6 +304,91 @@ struct Tile {
                                                                    acc[f][c], 0, 0, 0);
             }
           }
+        }
+      }
+    }
+    if constexpr (TY == kE4m3Wide) {
+      // values past an end of bf16 in this tile: the sum again, such steps by parts.  Beside
+      // the other steps' products these took registers that every sum paid for (4096 cubed:
+      // 129 us without parts, 133 so, 246 beside them).
+      __syncthreads();
+      if (threadIdx.x % 64 == 0) ((uint32_t*)lds)[wave] = ends;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) ends |= ((const uint32_t*)lds)[w] != 0;
+      if (!__any(ends)) return;
+#pragma unroll
+      for (int f = 0; f < MF; ++f)
+#pragma unroll
+        for (int c = 0; c < NF; ++c) acc[f][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+      for (int s = 0; s < n; ++s) {
+        __syncthreads();
+        copy(s);
+        scales(s, sa, sb);
+#pragma unroll
+        for (int q = 0; q < MF / 4; ++q) sa[q] = rows_alone(sa[q], ka[q]);
+#pragma unroll
+        for (int q = 0; q < NF / 4; ++q) sb[q] = rows_alone(sb[q], kb[q]);
+        wait_copies<0>();
+        __syncthreads();
+        const char* S = lds + (NST == 2 ? s & 1 : s % NST) * kStage;
+        mma_in_parts(S + wm * KB, S + (BM + wn) * KB, place, sa, sb, acc);
+      }
+    }
+  }
+
+  static constexpr uint32_t kOnes = 127 * 0x01010101u;        // powers of 1
+  __device__ static __forceinline__ uint32_t rows_alone(uint32_t four, uint32_t keep) {
+    return (four & keep) | (kOnes & ~keep);
+  }
+  // kE4m3Wide: whether a step has values whose powers take them past an end of bf16 (blocks
+  // of zeros, whose power is the smallest one, have none); the same in every lane
+  __device__ static __forceinline__ bool powers_at_an_end(const char* SA, const char* SB, const int (&place)[kHalves],
+                                                          const uint32_t* sa, const uint32_t* sb) {
+    bool maybe = false;
+#pragma unroll
+    for (int q = 0; q < MF / 4; ++q) maybe |= maybe_at_an_end(sa[q]);
+#pragma unroll
+    for (int q = 0; q < NF / 4; ++q) maybe |= maybe_at_an_end(sb[q]);
+    if (!__any(maybe)) return false;
+    asm volatile("" ::: "memory");                   // what is read here is not kept for the products
+    uint32_t is = 0;
+    auto look = [&](const char* S, uint32_t byte) {
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) is |= bits_at_an_end(*(const u32x4*)(S + place[h]), byte);
+    };
+#pragma unroll
+    for (int f = 0; f < MF; ++f) look(SA + f * 16 * KB, (sa[f / 4] >> (8 * (f & 3))) & 255u);
+#pragma unroll
+    for (int f = 0; f < NF; ++f) look(SB + f * 16 * KB, (sb[f / 4] >> (8 * (f & 3))) & 255u);
+    asm volatile("" ::: "memory");
+    return __any((is & kMagnitudes) != 0);
+  }
+  __device__ static __forceinline__ void mma_in_parts(const char* SA, const char* SB, const int (&place)[kHalves],
+                                                      const uint32_t* sa, const uint32_t* sb, Acc& acc) {
+    const int parts = powers_at_an_end(SA, SB, place, sa, sb) ? kEndsParts : 1;
+#pragma unroll 1
+    for (int i = 0; i < parts; ++i) {
+      const EndsPart part(i);
+      asm volatile("" ::: "memory");                 // a part reads for itself
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) {
+        bf16x8 b[NF][2];
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+          EndsPart::widen(*(const u32x4*)(SB + f * 16 * KB + place[h]), (sb[f / 4] >> (8 * (f & 3))) & 255u, part.columns,
+                          -part.by, b[f]);
+#pragma unroll
+        for (int f = 0; f < MF; ++f) {
+          bf16x8 a[2];
+          EndsPart::widen(*(const u32x4*)(SA + f * 16 * KB + place[h]), (sa[f / 4] >> (8 * (f & 3))) & 255u, part.rows,
+                          part.by, a);
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int c = 0; c < NF; ++c)
+              acc[f][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[t], b[c][t], acc[f][c], 0, 0, 0);
         }
       }
     }

@@ -52,6 +52,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_rows(RowsArgs j) {
 #pragma unroll
   for (int t = 0; t < MT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
   constexpr int U = MT > 1 ? 2 : 4;     // steps in flight
+  uint32_t ends = 0;                    // bits of values past an end of bf16
   for (int s0 = wave; s0 < j.steps; s0 += U * kRowWaves) {
     u32x4 b[U][2], a[U][MT][2];
     uint32_t eb[U], ea[U][MT];
@@ -84,15 +85,43 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_rows(RowsArgs j) {
         for (int h = 0; h < 2; ++h) {
           bf16x8 wb[2];
           widen_e4m3(b[u][h], eb[u], wb);
+          ends |= bits_at_an_end(b[u][h], eb[u]);
 #pragma unroll
           for (int t = 0; t < MT; ++t) {
             bf16x8 wa[2];
             widen_e4m3(a[u][t][h], ea[u][t], wa);
+            ends |= bits_at_an_end(a[u][t][h], ea[u][t]);
             acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa[0], wb[0], acc[t], 0, 0, 0);
             acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa[1], wb[1], acc[t], 0, 0, 0);
           }
         }
       }
+    }
+  }
+  if constexpr (TY == kE4m3Wide) {
+    if (__any((ends & kMagnitudes) != 0)) {          // the sum again, by parts (gemm.h)
+#pragma unroll
+      for (int t = 0; t < MT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+      for (int64_t s = wave; s < j.steps; s += kRowWaves)
+#pragma unroll 1
+        for (int p = 0; p < kEndsParts; ++p) {
+          const EndsPart part(p);
+#pragma unroll 1
+          for (int h = 0; h < 2; ++h) {
+            bf16x8 wb[2];
+            const u32x4 vb = *(const VFL_GLOBAL u32x4*)(pb + s * 128 + 64 * h);
+            EndsPart::widen(vb, sb[s * j.b.scale_ld], part.columns, -part.by, wb);
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+              bf16x8 wa[2];
+              const u32x4 va = *(const VFL_GLOBAL u32x4*)(pa[t] + s * 128 + 64 * h);
+              EndsPart::widen(va, sa[t][s * j.a.scale_ld], part.rows, part.by, wa);
+              acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa[0], wb[0], acc[t], 0, 0, 0);
+              acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa[1], wb[1], acc[t], 0, 0, 0);
+            }
+          }
+        }
     }
   }
 #pragma unroll
