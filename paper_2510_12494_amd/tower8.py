@@ -249,7 +249,7 @@ class EightTower:
                 self._weight_grad(d, h, f"W2.{l}", st)
                 self._quantize(d, self.dq[self.width], None, st)
                 self._product(self.dq[self.width], self.WT[f"W2.{l}"], rows, self.hidden, self.width, dh, st)
-                dh.mul_(h > 0)
+                dh.masked_fill_(h <= 0, 0.0)       # whatever it holds: a product would leave NaN of an infinity
                 self._column_sums(dh, G[f"b.{l}"], st)
                 self._weight_grad(dh, self.y[l][:rows], f"W1.{l}", st)
                 self._quantize(dh, self.dq[self.hidden], None, st)
