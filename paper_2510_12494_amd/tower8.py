@@ -115,7 +115,8 @@ class EightTower:
         self.ds = [new(width) for _ in range(2)]
         self.xq, self.yq, self.hq = rows8(d_in), rows8(width), rows8(hidden)
         self.dq = {width: rows8(width), hidden: rows8(hidden)}                       # gradients in 8 bits
-        self.turned = {n: (cols8(n), cols8(n)) for n in {d_in, width, hidden}}       # and both operands of a weight's
+        self.turned = {n: (cols8(n), cols8(n)) for n in {width, hidden}}             # and both operands of a weight's
+        self.xt = cols8(d_in)               # a training forward's input, for the gradient of W_in
         self.stats = torch.empty((blocks + 1, max_rows), device=self.dev)
         sizes = [(max_rows, width, d_in), (max_rows, hidden, width), (max_rows, width, hidden), (width, hidden, max_rows),
                  (hidden, width, max_rows), (width, d_in, max_rows)]
@@ -178,12 +179,13 @@ class EightTower:
         self.ws.put(a, V.vfl_norm_workspace_size(rows, self.width))
         V.vfl_rmsnorm_backward(a, st)
 
-    def _weight_grad(self, d: torch.Tensor, x: torch.Tensor, name: str, st: int):
-        """d^T x: both operands' blocks run along the rows."""
+    def _weight_grad(self, d: torch.Tensor, x: torch.Tensor | Eight, name: str, st: int):
+        """d^T x: both operands' blocks run along the rows; x may be there in 8 bits."""
         (n, k), rows = self.grads[name].shape, d.shape[0]
-        a8, b8 = self.turned[n][0], self.turned[k][1]
+        a8, b8 = self.turned[n][0], x if isinstance(x, Eight) else self.turned[k][1]
         self._quantize(d, None, a8, st)
-        self._quantize(x, None, b8, st)
+        if b8 is not x:
+            self._quantize(x, None, b8, st)
         self._product(a8, b8, n, k, rows, self.grads[name], st)
 
     def _column_sums(self, d: torch.Tensor, out: torch.Tensor, st: int):
@@ -210,7 +212,7 @@ class EightTower:
     def forward(self, x: torch.Tensor, train: bool = True) -> torch.Tensor:
         """The embedding of rows ``x`` (bf16), a view of the tower's buffer that the
         next forward overwrites.  Only a training forward can be followed by
-        ``backward``."""
+        ``backward``, which takes nothing more from x: its owner may use it again."""
         if (x.dim() != 2 or not 1 <= x.shape[0] <= self.max_rows or x.shape[1] != self.d_in
                 or x.dtype != torch.bfloat16 or x.device != self.dev or not _rows_apart(x)):
             raise ValueError(f"x must be [1..{self.max_rows} x {self.d_in}] of bfloat16 on {self.dev}, rows apart")
@@ -218,8 +220,7 @@ class EightTower:
         self.trained = 0
         with torch.cuda.device(self.dev):
             st = torch.cuda.current_stream(self.dev).cuda_stream
-            self.x = x
-            self._quantize(x, self.xq, None, st)
+            self._quantize(x, self.xq, self.xt if train else None, st)
             self._product(self.xq, W["W_in"], rows, self.width, self.d_in, self.s[0][:rows], st)
             self._norm(0, rows, self.s[0], None, None, st)
             for l in range(self.blocks):
@@ -256,7 +257,7 @@ class EightTower:
                 self._product(self.dq[self.hidden], self.WT[f"W1.{l}"], rows, self.width, self.hidden, self.dy[:rows], st)
                 self._norm_backward(l, rows, self.dy, ds, other, st)
                 ds, other = other, ds
-            self._weight_grad(ds[:rows], self.x, "W_in", st)
+            self._weight_grad(ds[:rows], self.xt, "W_in", st)
 
     @torch.no_grad()
     def sgd(self, lr: float):

@@ -36,3 +36,18 @@ def test_infinite_gradients_of_masked_units(rows):
         assert not t.h[0][:, 128:].any() and t.h[0][:, :128].any()
     for k, want in found[0].items():
         assert torch.isfinite(found[1][k]).all() and torch.equal(found[1][k], want), k
+
+
+@pytest.mark.parametrize("d_in,width,hidden,rows", [(24, 64, 96, 300), (64, 64, 64, 1), (130, 64, 130, 77)])
+def test_an_input_that_is_used_again_before_the_backward_pass(d_in, width, hidden, rows):
+    from paper_2510_12494_amd.tower8 import EightTower
+    t = EightTower(d_in, width, hidden, 1, rows + 30, seed=2)
+    g = torch.Generator().manual_seed(rows)
+    x = torch.randn(rows, d_in, generator=g).bfloat16().cuda()
+    dz = torch.randn(rows, width, generator=g).bfloat16().cuda()
+    want = gradients(t, x, dz)
+    t.forward(x)
+    x.fill_(float("nan"))
+    t.backward(dz)
+    torch.cuda.synchronize()
+    assert torch.isfinite(want["W_in"]).all() and all(torch.equal(t.grads[k], v) for k, v in want.items())
