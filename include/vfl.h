@@ -639,10 +639,11 @@ vfl_status vfl_matmul8(const vfl_matmul8_args* a, void* stream);
  * gradient of 0.  In bf16 G enters its products as one rounded value, and what its
  * rounding loses at the row's label is added to dx; in dw of up to 512 rows, and
  * both of up to 256, as the sum of two such values.  `scale`, and all sums, are float32.
- *   The workspace (16-byte aligned, vfl_softmax_loss_workspace_size() bytes: copies
- * of x and w in the products' layout, and G in pieces of all rows by as many classes as
- * 1 GB holds, 256 at least) means nothing between calls; calls that may run at the
- * same time need one each.  No element that is written may be one that is read.
+ *   The workspace (16-byte aligned, vfl_softmax_loss_workspace_size() bytes for either
+ * direction: copies of x and w in the products' layout, G in pieces of all rows by as many
+ * classes as 1 GB holds, a tile of 64 to 256 at least, and float32 sums of dbias, of dx,
+ * and of dw where a piece's sum over the rows is cut into parts) means nothing between
+ * calls; calls that may run at the same time need one each.  No element that is written may be one that is read.
  * Fields that a direction does not use are ignored. */
 #define VFL_LOSS_MAX_ROWS 2097152
 #define VFL_LOSS_MAX_CLASSES 2097152

@@ -712,6 +712,7 @@ struct Plan {
   int64_t dim_pad, rows_pad, all, piece, pieces;     // all, piece: classes in whole tiles
   int64_t rest;                                      // rows of G to its second terms' (0: none)
   bool x_terms;                                      // dx takes them too
+  bool dx_sums, dw_sums;                             // float32 sums that are not the result yet
   int64_t g_rows;
   int64_t strips, parts;                             // k_strip's strips (0: tiles); the forward's pairs of a row
   size_t x, w, part, label_z, g, bias, dx, dw, label, bytes;
@@ -764,8 +765,10 @@ Plan plan(int64_t rows, int dim, int64_t classes) {
   at = both;
   p.g = take(p.g_rows * p.piece, sizeof(T));
   p.bias = take(p.rows_pad / p.bn * p.all, sizeof(float));
-  p.dx = take(p.to_x.parts * x_rows * part_ld(dim), sizeof(float));
-  p.dw = take(p.to_w.parts * p.piece * part_ld(dim), sizeof(float));
+  p.dx_sums = p.pieces > 1 || p.to_x.parts > 1 || p.x_terms;
+  p.dw_sums = p.to_w.parts > 1;
+  p.dx = take(p.dx_sums ? p.to_x.parts * x_rows * part_ld(dim) : 0, sizeof(float));
+  p.dw = take(p.dw_sums ? p.to_w.parts * p.piece * part_ld(dim) : 0, sizeof(float));
   p.label = take(sizeof(T) == 2 && !p.x_terms ? rows : 0, sizeof(float));
   p.bytes = std::max(at, forward);
   return p;
@@ -926,8 +929,6 @@ hipError_t backward(const LossJob& j, hipStream_t st) {
   a.g_ld = p.piece;
   a.bias_ld = p.all;
   const LabelTerm label{a.label_rest, j.labels, (const uint16_t*)w.p, w.ld / E, j.classes, factor ? j.scale : 1.f};
-  // sums that are not the result yet
-  const bool dx_sums = p.pieces > 1 || p.to_x.parts > 1 || p.x_terms, dw_sums = p.to_w.parts > 1;
   for (int64_t i = 0; e == hipSuccess && i < p.pieces; ++i) {
     const int64_t first = i * p.piece, left = j.classes - first, mine = std::min(left, p.piece);
     const int64_t wide = round_up(mine, p.bm);       // columns of G that are written
@@ -945,13 +946,13 @@ hipError_t backward(const LossJob& j, hipStream_t st) {
     if (j.dx.p) {
       x.a = terms(a.w, p.dim_pad * E);
       x.b = {ws + p.g, p.piece * E, p.g_rows - 1, nullptr, 0};
-      x.c = dx_sums ? (void*)(ws + p.dx) : j.dx.p;
-      x.ldc = dx_sums ? part_ld(j.dim) : j.dx.ld;
-      x.wide = dx_sums;
+      x.c = p.dx_sums ? (void*)(ws + p.dx) : j.dx.p;
+      x.ldc = p.dx_sums ? part_ld(j.dim) : j.dx.ld;
+      x.wide = p.dx_sums;
       x.m = j.dim;
       x.n = p.x_terms ? p.g_rows : j.rows;
       x.add = i > 0;
-      if (!dx_sums) x.label = label;
+      if (!p.dx_sums) x.label = label;
       Pass t = p.to_x;
       // the last piece may have fewer steps than parts: all parts hold sums by then
       t.steps = (int)(wide / (p.piece / t.steps));
@@ -965,9 +966,9 @@ hipError_t backward(const LossJob& j, hipStream_t st) {
       w.bs = {ws + p.g, p.piece * E, p.g_rows - 1, (int)(p.piece * E / 16)};
       w.m = j.dim;
       w.n = mine;
-      w.c = dw_sums ? (void*)(ws + p.dw) : (T*)j.dw.p + first * j.dw.ld;
-      w.ldc = dw_sums ? part_ld(j.dim) : j.dw.ld;
-      w.wide = dw_sums;
+      w.c = p.dw_sums ? (void*)(ws + p.dw) : (T*)j.dw.p + first * j.dw.ld;
+      w.ldc = p.dw_sums ? part_ld(j.dim) : j.dw.ld;
+      w.wide = p.dw_sums;
       Pass t = p.to_w;
       t.tn = tiles_of(mine, rows_of<T>(t.size));
       cut_as(w, t);
@@ -977,13 +978,13 @@ hipError_t backward(const LossJob& j, hipStream_t st) {
     const bool last = i + 1 == p.pieces;
     EndArgs end{};
     uint32_t nb = 0;
-    if (j.dw.p && dw_sums) {
+    if (j.dw.p && p.dw_sums) {
       const Mat out = {(T*)j.dw.p + first * j.dw.ld, j.dw.ld};
       end.w = join_args((const float*)(ws + p.dw), p.to_w.parts, mine, j.dim, nullptr, 0, out);
       end.nw = (uint32_t)join_blocks(end.w);
       end.w_slices = joins_in_slices(end.w);
     }
-    if (last && j.dx.p && dx_sums) {
+    if (last && j.dx.p && p.dx_sums) {
       end.x = join_args((const float*)(ws + p.dx), p.to_x.parts, j.rows, j.dim, nullptr, 0, j.dx);
       if (p.x_terms) {                               // the second terms' rows are parts too
         end.x.parts = 2 * p.to_x.parts;

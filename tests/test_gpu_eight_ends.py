@@ -134,3 +134,18 @@ def test_products_that_cancel_within_a_block(V, dt, m, n):
     # the pair lies at the same columns of both
     b._bytes()[:, :k] = torch.where((a._bytes()[0, :k] & 0x7F) == 0x7E, 0x7E, b._bytes()[:, :k].clamp(max=0x50))
     check(V, dt, a, b, k)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,dim,classes", [(16, 1024, 5000), (16, 1024, 20_000), (1, 64, 100_000), (40, 300, 3000), (200, 64, 900),
+                                              (300, 1000, 700), (3000, 64, 260), (700, 200, 2000)])
+def test_the_loss_stays_within_its_workspace(V, dt, rows, dim, classes):
+    """Sums of dw in one part and in several, of dx written at once and joined."""
+    from test_gpu_eight import Loss
+    t = Loss(V, dt, rows, dim, classes)
+    size = t.a.workspace_bytes
+    t.ws = torch.full((size + (1 << 16),), 0xFF, dtype=torch.uint8, device="cuda")
+    t.a.workspace = t.ws.data_ptr()
+    t.run()
+    t.check()
+    assert bool((t.ws[size:] == 0xFF).all())
