@@ -51,9 +51,10 @@ class Eight:
 
     def values(self, rows: int, cols: int) -> torch.Tensor:
         """What it stands for, in float64."""
-        e = self.scale[:, :rows].T.double() - 127
+        # 2^e by its bits: a device's pow is not exact
+        power = ((self.scale[:, :rows].T.long() - 127 + 1023) << 52).view(torch.float64)
         v = self.data[:rows].view(torch.float8_e4m3fn).double()
-        return (v * torch.pow(2.0, e).repeat_interleave(V.VFL_Q8_BLOCK, 1))[:, :cols]
+        return (v * power.repeat_interleave(V.VFL_Q8_BLOCK, 1))[:, :cols]
 
 
 def _rows_apart(t: torch.Tensor) -> bool:

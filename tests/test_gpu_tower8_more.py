@@ -51,3 +51,14 @@ def test_an_input_that_is_used_again_before_the_backward_pass(d_in, width, hidde
     t.backward(dz)
     torch.cuda.synchronize()
     assert torch.isfinite(want["W_in"]).all() and all(torch.equal(t.grads[k], v) for k, v in want.items())
+
+
+def test_what_a_matrix_in_8_bits_stands_for():
+    """Every byte of values and of powers, to the last bit."""
+    from paper_2510_12494_amd.tower8 import Eight
+    m = Eight(255, 256, "cuda")
+    m.data.copy_(torch.arange(256, dtype=torch.uint8).expand(255, 256))
+    m.scale[:, :255] = torch.arange(255, dtype=torch.uint8, device="cuda")
+    powers = np.broadcast_to(np.arange(-127, 128), (2, 255))
+    want = E.dequantize(np.broadcast_to(E.e4m3_table(), (255, 256)), powers)
+    assert np.array_equal(m.values(255, 250).cpu().numpy(), want[:, :250], equal_nan=True)
