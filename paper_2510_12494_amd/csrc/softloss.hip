@@ -18,8 +18,9 @@
 //
 // Of 8192 x 256 bf16 rows over 100000 classes (three products of 2 x 8192 x 256 x 100000
 // operations, 0.99 ms at a library product's rate, and the logits once more) a step
-// takes 2.28 ms: copies of the operands 18 us, k_strip 440 to 480, G 2 x 360, both
-// products 2 x 580, what is summed 22.
+// takes 2.27 ms: copies of the operands 18 us, k_strip 442, its pairs joined 5, G 2 x 336,
+// both products 2 x 560, what is summed 22 (a run once the clock has settled; within the
+// first 20 ms of such load they take up to a quarter more).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>

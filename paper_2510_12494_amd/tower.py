@@ -121,7 +121,8 @@ class ResidualTower:
     def forward(self, x: torch.Tensor, row0: int = 0, step: int | None = None, train: bool = True) -> torch.Tensor:
         """The embedding of rows ``x`` (global sample ids from ``row0``), a view of
         the tower's buffer that the next forward overwrites; without ``train``
-        nothing is dropped (scoring).  ``step`` keys the masks: towers that have to
+        nothing is dropped (scoring).  ``backward`` reads ``x`` again, as it is then.
+        ``step`` keys the masks: towers that have to
         make the same ones (replicas, a replay, a batch in parts) name it; without
         it a training forward takes the step after the last one's, from 0."""
         if (x.dim() != 2 or not 1 <= x.shape[0] <= self.max_rows or x.shape[1] != self.d_in or x.dtype != self.tdt
